@@ -302,6 +302,118 @@ vvs_status vvs_draft(vvs_ctx* drafter, vvs_ctx* target, int32_t n_nodes, const i
                      int32_t n_unverified, const int32_t* d_given_tokens, int32_t* d_draft_tokens,
                      float* d_draft_probs, vvs_stream s);
 
+/* ---- Key/value cache in 8 bits -------------------------------------------------------------------------------
+ *
+ * A cache of its own beside the contexts': keys and values of one attention layer (or of all layers of a model), appended to, looked at
+ * and thinned out by the calls below, for programs that keep more in HBM, or read less of it, than bf16 allows.
+ *
+ * What is held.  The slots of one layer, row and key/value head are cut into blocks of VVS_QCACHE_BLOCK; keys and values of a block each have one
+ * power of two 2^E, and their elements are e4m3 numbers (4 exponent bits, 3 of mantissa, largest 448) times 2^E.  E is the smallest one, at least -110, with
+ * |x| <= 448 * 2^E for every finite x that was appended to the block; an append to a block that holds something keeps the larger E, and what was held is
+ * rounded to it (exact, but for elements below 2^-6 * 2^E).  Rounding is to nearest, ties to even; an element that is not finite is held as NaN.
+ *
+ * Lengths are the caller's: d_len int32 [n_rows] says how many slots of each row are filled, and is only read (values outside [0, capacity] are taken as
+ * the nearest inside).  Tokens per row may differ: d_n_tokens int32 [n_rows], in [0, n_tokens] (clamped), or NULL for n_tokens everywhere; of the tokens behind a row's
+ * number nothing is read, and nothing is written for them.
+ *
+ * Tensors are [n_rows, n_tokens, heads, head_size] in the cache's dtype; a stride argument gives the elements from one token to the next where they lie further apart
+ * than heads * head_size (0: they do not), so that q, k and v can be parts of one projection's output.  Rows are n_tokens tokens apart.  Pointers and
+ * strides have to be multiples of 16 bytes.  All tensors live on the device that was current at vvs_qcache_create, which has to be current at every call.
+ * Calls on one cache share its workspace: issue them on one stream, or order them.  All calls can be captured into a graph. */
+#define VVS_QCACHE_BLOCK 32
+typedef struct vvs_qcache vvs_qcache;  /* opaque host object; owns no device memory */
+
+typedef struct {
+  int32_t n_layers, n_rows;
+  int32_t n_heads, n_kv_heads;   /* query heads; key/value heads (each serves n_heads / n_kv_heads query heads in a row) */
+  int32_t head_size;             /* 32, 64 or 128 */
+  int32_t capacity;              /* slots per layer, row and key/value head */
+  int32_t max_tokens;            /* largest n_tokens of an attention call */
+  int32_t dtype;                 /* VVS_FP32 or VVS_BF16: type of q, k, v and outputs */
+} vvs_qcache_config;
+
+/* Sizes in bytes of the two device buffers of a cache. */
+vvs_status vvs_qcache_query_sizes(const vvs_qcache_config* cfg, size_t* cache_bytes, size_t* workspace_bytes);
+/* Creates a cache over caller-allocated device buffers (256-byte aligned).  Synchronous: clears both. */
+vvs_status vvs_qcache_create(const vvs_qcache_config* cfg, void* d_cache, void* d_workspace, vvs_qcache** out);
+void vvs_qcache_destroy(vvs_qcache* c);
+const char* vvs_qcache_last_error(const vvs_qcache* c);   /* c must not be NULL (a failed create or query: vvs_last_error(NULL)) */
+
+/* Rounds keys and values into the slots d_len[r] .. of layers layer .. layer + n_layers - 1.
+ *   d_k, d_v   : [n_layers, n_rows, src_tokens, n_kv_heads, head_size]
+ *   n_tokens   : most tokens taken of a row; src_tokens: tokens per row of d_k and d_v
+ *   d_select   : int32 [n_rows, n_tokens]: the source token of each taken one (an accepted path; one outside [0, src_tokens) is taken as zeros), or
+ *                NULL: the first ones, and n_tokens <= src_tokens
+ * Tokens beyond the capacity are dropped.  Slots below d_len keep their values up to the rounding above. */
+vvs_status vvs_qcache_append(vvs_qcache* c, int32_t layer, int32_t n_layers, const int32_t* d_len, int32_t n_tokens, const int32_t* d_n_tokens,
+                             int32_t src_tokens, const int32_t* d_select, const void* d_k, const void* d_v, int64_t kv_stride, vvs_stream s);
+
+/* Attention of a block of query tokens over the cached slots of their row and over the block's own keys and values, which are not rounded to 8 bits:
+ * out = softmax(scale q K^T) V, every query over slots 0 .. d_len[r] - 1 and the block tokens it may see.
+ *   h_parent, h_tree_mask: the block's topology as for vvs_verify with n_tokens - 1 nodes (token 0 is the root); both NULL: a chain, the only form with
+ *                n_tokens > VVS_MAX_T.  What a masked token holds, NaN and infinities included, does not matter.
+ *   d_k, d_v   : [n_rows, n_tokens, n_kv_heads, head_size]; both NULL: the queries see the cache alone
+ *   scale      : positive and finite
+ *   d_out      : [n_rows, n_tokens, n_heads, head_size], contiguous; a query that sees nothing (no block, nothing cached) gets zeros
+ *   d_lse      : float [n_rows, n_tokens, n_heads] out, log of the sum of exp(scale q k) (-inf for a query that sees nothing); may be NULL
+ *   n_counted  : the softmax weights of tokens 0 .. n_counted - 1 of every row, of all query heads of a key/value head, are added up per key:
+ *   d_mass     : float [n_rows, n_kv_heads, capacity], cached slots: added to (NULL: left out)
+ *   d_block_mass: float [n_rows, n_kv_heads, n_tokens], block tokens: set (NULL: left out)
+ * Sums are in a fixed order: the same call gives the same bits. */
+vvs_status vvs_qcache_attention(vvs_qcache* c, int32_t layer, const int32_t* d_len, int32_t n_tokens, const int32_t* d_n_tokens, const int32_t* h_parent,
+                                const uint8_t* h_tree_mask, const void* d_q, int64_t q_stride, const void* d_k, const void* d_v, int64_t kv_stride,
+                                float scale, void* d_out, float* d_lse, int32_t n_counted, float* d_mass, float* d_block_mass, vvs_stream s);
+
+/* Eviction by accumulated attention weight: every layer, row and key/value head whose length is above `keep` keeps the `keep` slots of largest weight (equal ones: the
+ * lower slot; a NaN counts as the largest); the `recent` newest tokens - those at positions above the row's largest filled one minus `recent` - are kept whatever their weight, as
+ * far as there is room.  Kept slots from `keep` on move, in order, into the slots below that were given up; the others stay where they are.  A block that something moves into
+ * takes the largest E of the blocks that its slots were in.  The new length is min(d_len[r], keep); the caller sets it.
+ *   keep       : a multiple of VVS_QCACHE_BLOCK, at least one block; recent: in [0, keep]
+ *   d_mass     : float [n_layers, n_rows, n_kv_heads, capacity];  d_mass_out: the same, out, weights of what lies in the slots now, 0 behind the new length (may
+ *                be d_mass itself)
+ *   d_pos, d_pos_out: int32, likewise, positions of the tokens in the slots (0 behind the new length); both NULL: a slot's number is its position, as it is before the first eviction */
+vvs_status vvs_qcache_evict(vvs_qcache* c, int32_t layer, int32_t n_layers, const int32_t* d_len, int32_t keep, int32_t recent, const float* d_mass,
+                            float* d_mass_out, const int32_t* d_pos, int32_t* d_pos_out, vvs_stream s);
+
+/* Cached keys and values as numbers: d_k, d_v [n_layers, n_rows, n_slots, n_kv_heads, head_size] out, slots d_first[r] .. (NULL: from 0) of every row; slots that
+ * are not in [0, d_len[r]) read as zeros. */
+vvs_status vvs_qcache_read(vvs_qcache* c, int32_t layer, int32_t n_layers, const int32_t* d_len, const int32_t* d_first, int32_t n_slots, void* d_k,
+                           void* d_v, vvs_stream s);
+
+/* ---- Rotary positions on several axes (frame, row, column of a video; text) ----------------------------------------
+ *
+ * A head's first 2 * (sum of pairs) dims are rotated in pairs by the angle position[axis of the pair] * rate[pair], the others copied.  Pairs belong to the axes in order:
+ * the first pairs[0] to axis 0, and so on.  The contexts' own positions are two axes (row, column) of head_size / 4 pairs each, VVS_ROPE_OWN, VVS_ROPE_ADJACENT. */
+#define VVS_ROPE_MAX_AXES 4
+enum { VVS_ROPE_OWN = 0,       /* rate of pair i of an axis with n pairs: base^(-i / n), every axis a series of its own */
+       VVS_ROPE_SHARED = 1 };  /* rate of pair j of the head: base^(-2 j / head_size), one series cut into axes */
+enum { VVS_ROPE_ADJACENT = 0,  /* pair j: dims 2 j and 2 j + 1 */
+       VVS_ROPE_HALVES = 1 };  /* pair j: dims j and j + (sum of pairs) */
+typedef struct vvs_rope vvs_rope;   /* opaque host object */
+
+typedef struct {
+  int32_t head_size;                  /* a multiple of 8, at most 256 */
+  int32_t n_axes;                     /* 1 .. VVS_ROPE_MAX_AXES */
+  int32_t pairs[VVS_ROPE_MAX_AXES];   /* of axes 0 .. n_axes - 1, at least 1 each; their sum is a multiple of 4
+                                         (VVS_ROPE_HALVES: of 8) and at most head_size / 2 */
+  int32_t series, pairing;
+  int32_t dtype;
+  float base;                         /* > 1 */
+} vvs_rope_config;
+
+vvs_status vvs_rope_create(const vvs_rope_config* cfg, vvs_rope** out);   /* host only */
+void vvs_rope_destroy(vvs_rope* r);
+const char* vvs_rope_last_error(const vvs_rope* r);                       /* r must not be NULL */
+
+/* Rotates queries and keys of n_tokens tokens in one launch; angles are taken in 64 bits, so that far positions are as exact as near ones.
+ *   d_pos      : int32 [n_tokens, n_axes], any sign
+ *   d_q, d_q_out [n_tokens, n_heads, head_size]; d_k, d_k_out [n_tokens, n_kv_heads, head_size] (n_kv_heads 0: NULL); an output may be its input; strides as for
+ *                the cache's tensors, 0: contiguous; pointers and strides multiples of 16 bytes
+ *   inverse    : 1: by the negative angles - takes a rotation back, and is its gradient */
+vvs_status vvs_rope_apply(vvs_rope* r, int32_t n_tokens, const int32_t* d_pos, int32_t n_heads, const void* d_q, int64_t q_stride, void* d_q_out,
+                          int64_t q_out_stride, int32_t n_kv_heads, const void* d_k, int64_t k_stride, void* d_k_out, int64_t k_out_stride,
+                          int32_t inverse, vvs_stream s);
+
 /* 1 if a forward over n_tokens query tokens per row (a verify call with n_tokens - 1 draft nodes, or a
  * prefill chunk) takes the fused layer described at vvs_config.norm_mode, 0 if it runs the separate
  * normalisation kernels.  Host only; ctx must not be NULL. */

@@ -21,6 +21,10 @@ VVS_FP32, VVS_BF16 = 0, 1
 VVS_STRICT, VVS_RELAXED = 0, 1
 VVS_NORM_AUTO, VVS_NORM_SEPARATE = 0, 1
 VVS_MAX_T = 64
+VVS_QCACHE_BLOCK = 32
+VVS_ROPE_MAX_AXES = 4
+VVS_ROPE_OWN, VVS_ROPE_SHARED = 0, 1
+VVS_ROPE_ADJACENT, VVS_ROPE_HALVES = 0, 1
 VVS_K_GEMM, VVS_K_ATTENTION, VVS_K_ACCEPT, VVS_K_ELEMENTWISE, VVS_K_COMMIT = range(5)
 
 
@@ -34,6 +38,15 @@ class VvsConfig(C.Structure):
                 ("norm_mode", C.c_int32)]
 
 
+class VvsQCacheConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_rows", "n_heads", "n_kv_heads", "head_size", "capacity", "max_tokens", "dtype")]
+
+
+class VvsRopeConfig(C.Structure):
+    _fields_ = [("head_size", C.c_int32), ("n_axes", C.c_int32), ("pairs", C.c_int32 * VVS_ROPE_MAX_AXES), ("series", C.c_int32),
+                ("pairing", C.c_int32), ("dtype", C.c_int32), ("base", C.c_float)]
+
+
 class VvsError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"vvs status {status}: {msg}")
@@ -45,7 +58,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} is missing: build it first (python -m paper_2511_13587_amd.build); "
                           "there is no CPU or PyTorch fallback for the verify pass")
     lib = C.CDLL(LIB_PATH)
-    vp, i32, sz = C.c_void_p, C.c_int32, C.c_size_t
+    vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
     sigs = {
         "vvs_query_sizes": (i32, [C.POINTER(VvsConfig), C.POINTER(sz), C.POINTER(sz), C.POINTER(sz)]),
         "vvs_create": (i32, [C.POINTER(VvsConfig), vp, vp, vp, C.POINTER(vp)]),
@@ -78,6 +91,18 @@ def _load():
         "vvs_debug_gemm_scratch_bytes": (sz, [vp, i32, i32, i32]),
         "vvs_debug_gemm": (i32, [vp, i32, i32, i32, vp, vp, vp, vp, vp]),
         "vvs_debug_copy": (i32, [vp, vp, vp, sz, vp]),
+        "vvs_qcache_query_sizes": (i32, [C.POINTER(VvsQCacheConfig), C.POINTER(sz), C.POINTER(sz)]),
+        "vvs_qcache_create": (i32, [C.POINTER(VvsQCacheConfig), vp, vp, C.POINTER(vp)]),
+        "vvs_qcache_destroy": (None, [vp]),
+        "vvs_qcache_last_error": (C.c_char_p, [vp]),
+        "vvs_qcache_append": (i32, [vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, i64, vp]),
+        "vvs_qcache_attention": (i32, [vp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp, i64, C.c_float, vp, vp, i32, vp, vp, vp]),
+        "vvs_qcache_evict": (i32, [vp, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp]),
+        "vvs_qcache_read": (i32, [vp, i32, i32, vp, vp, i32, vp, vp, vp]),
+        "vvs_rope_create": (i32, [C.POINTER(VvsRopeConfig), C.POINTER(vp)]),
+        "vvs_rope_destroy": (None, [vp]),
+        "vvs_rope_last_error": (C.c_char_p, [vp]),
+        "vvs_rope_apply": (i32, [vp, i32, vp, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp]),
         "vvs_debug_wait_limit": (i32, [vp, i32]),
         "vvs_debug_fill_probe": (i32, [vp, vp, sz, sz, i32, i32, i32, i32, vp, vp]),
     }
@@ -361,3 +386,193 @@ class Context:
         self._check(lib.vvs_debug_gemm(self.h, m, n, k, _ptr(a), _ptr(w), _ptr(scratch), _ptr(out), _stream()))
         torch.cuda.synchronize()
         return out
+
+
+# ---------------------------------------------------------------------------------------------- operators beside a context
+def _on(t: Optional[torch.Tensor], device: torch.device, dtype: torch.dtype, shape, what: str):
+    """Pointer of a contiguous tensor of the library's arguments (None stays None)."""
+    if t is None:
+        return None
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what}: wants a contiguous {dtype} tensor {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _per_token(t: Optional[torch.Tensor], device: torch.device, dtype: torch.dtype, shape, what: str):
+    """(pointer, elements from token to token) of a tensor [..., tokens, heads, size] that may be a part of a wider one: heads and dims contiguous, every
+    dimension in front of them in steps of whole tokens."""
+    if t is None:
+        return None, 0
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: wants a {dtype} tensor {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    heads, size = t.shape[-2:]
+    token = t.stride(-3) if t.shape[-3] > 1 else None
+    n = 1                                # tokens below each dimension
+    ok = (t.stride(-1) == 1 or size == 1) and (t.stride(-2) == size or heads == 1)
+    for d in range(t.dim() - 3, -1, -1):
+        if t.shape[d] > 1:
+            token = t.stride(d) // n if token is None else token
+            ok = ok and t.stride(d) == token * n
+        n *= t.shape[d]
+    token = heads * size if token is None else token
+    if not ok or token < heads * size:
+        raise ValueError(f"{what}: strides {t.stride()} of {list(t.shape)} are not those of tokens one after the other")
+    return t.data_ptr(), token
+
+
+_TORCH_DTYPE = {VVS_FP32: torch.float32, VVS_BF16: torch.bfloat16}
+
+
+class QCache:
+    """A key/value cache in 8 bits: owns its two device buffers; methods mirror the C entry points (include/vvs.h).  Lengths, accumulated weights and positions
+    are the caller's tensors; tensors may be bfloat16 or float32, as the cache's dtype says."""
+
+    def __init__(self, n_layers: int, n_rows: int, n_heads: int, n_kv_heads: int, head_size: int, capacity: int, max_tokens: int, dtype: int,
+                 device: str = "cuda:0"):
+        self.cfg = VvsQCacheConfig(n_layers, n_rows, n_heads, n_kv_heads, head_size, capacity, max_tokens, dtype)
+        self.cache_bytes, self.ws_bytes = vvs_qcache_query_sizes(self.cfg)
+        if not torch.cuda.is_available():
+            raise RuntimeError("libvvs needs a HIP device; there is no CPU path")
+        self.device, self.dtype = torch.device(device), _TORCH_DTYPE[dtype]
+        with torch.cuda.device(self.device):
+            self.cache = torch.empty(self.cache_bytes, dtype=torch.uint8, device=self.device)
+            self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+            torch.cuda.synchronize()
+            h = C.c_void_p()
+            st = lib.vvs_qcache_create(C.byref(self.cfg), self.cache.data_ptr(), self.ws.data_ptr(), C.byref(h))
+        if st != VVS_OK:
+            raise VvsError(st, (lib.vvs_last_error(None) or b"").decode())
+        self.h = h
+
+    def close(self):
+        if getattr(self, "h", None):
+            torch.cuda.synchronize(self.device)
+            lib.vvs_qcache_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, st: int):
+        if st != VVS_OK:
+            raise VvsError(st, (lib.vvs_qcache_last_error(self.h) or b"").decode())
+
+    def _rows(self, t, what):
+        return _on(t, self.device, torch.int32, (self.cfg.n_rows,), what)
+
+    def vvs_qcache_append(self, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_tokens: Optional[torch.Tensor] = None,
+                          select: Optional[torch.Tensor] = None, layer: int = 0, n_layers: int = 1):
+        """k, v [n_layers, rows, tokens, kv heads, size]; select int32 [rows, n]: the tokens taken; n_tokens int32 [rows]: how many of them."""
+        g = self.cfg
+        src = k.shape[2] if k.dim() == 5 else 0
+        shape = (n_layers, g.n_rows, src, g.n_kv_heads, g.head_size)
+        kp, ks = _per_token(k, self.device, self.dtype, shape, "k")
+        vp, vs = _per_token(v, self.device, self.dtype, shape, "v")
+        if ks != vs:
+            raise ValueError("k and v have different strides")
+        n = src if select is None else int(select.shape[1])
+        with torch.cuda.device(self.device):
+            self._check(lib.vvs_qcache_append(self.h, layer, n_layers, self._rows(length, "length"), n, self._rows(n_tokens, "n_tokens"), src,
+                                              _on(select, self.device, torch.int32, (g.n_rows, n), "select"), kp, vp, ks, _stream()))
+
+    def vvs_qcache_attention(self, length: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor], v: Optional[torch.Tensor], out: torch.Tensor,
+                             n_tokens: Optional[torch.Tensor] = None, parent=None, tree_mask=None, scale: Optional[float] = None,
+                             lse: Optional[torch.Tensor] = None, n_counted: int = 0, mass: Optional[torch.Tensor] = None,
+                             block_mass: Optional[torch.Tensor] = None, layer: int = 0):
+        """q [rows, tokens, heads, size]; k, v [rows, tokens, kv heads, size] or None; out like q, contiguous.  scale: None = size ** -0.5."""
+        g = self.cfg
+        t = q.shape[1] if q.dim() == 4 else 0
+        qp, qs = _per_token(q, self.device, self.dtype, (g.n_rows, t, g.n_heads, g.head_size), "q")
+        kp, ks = _per_token(k, self.device, self.dtype, (g.n_rows, t, g.n_kv_heads, g.head_size), "k")
+        vp, vs = _per_token(v, self.device, self.dtype, (g.n_rows, t, g.n_kv_heads, g.head_size), "v")
+        if ks != vs:
+            raise ValueError("k and v have different strides, or only one of them is given")
+        p = None if parent is None else np.ascontiguousarray(parent, dtype=np.int32)
+        m = None if tree_mask is None else np.ascontiguousarray(tree_mask, dtype=np.uint8)
+        if (p is not None and p.shape != (t - 1,)) or (m is not None and m.shape != (t, t)):
+            raise ValueError("parent wants [tokens - 1] and tree_mask [tokens, tokens] entries")
+        with torch.cuda.device(self.device):
+            self._check(lib.vvs_qcache_attention(
+                self.h, layer, self._rows(length, "length"), t, self._rows(n_tokens, "n_tokens"), None if p is None else p.ctypes.data,
+                None if m is None else m.ctypes.data, qp, qs, kp, vp, ks, g.head_size ** -0.5 if scale is None else float(scale),
+                _on(out, self.device, self.dtype, (g.n_rows, t, g.n_heads, g.head_size), "out"),
+                _on(lse, self.device, torch.float32, (g.n_rows, t, g.n_heads), "lse"), n_counted,
+                _on(mass, self.device, torch.float32, (g.n_rows, g.n_kv_heads, g.capacity), "mass"),
+                _on(block_mass, self.device, torch.float32, (g.n_rows, g.n_kv_heads, t), "block_mass"), _stream()))
+
+    def vvs_qcache_evict(self, length: torch.Tensor, keep: int, recent: int, mass: torch.Tensor, mass_out: torch.Tensor,
+                         pos: Optional[torch.Tensor] = None, pos_out: Optional[torch.Tensor] = None, layer: int = 0, n_layers: int = 1):
+        """mass, mass_out float32, pos, pos_out int32 [n_layers, rows, kv heads, capacity]; an output may be its input."""
+        g = self.cfg
+        shape = (n_layers, g.n_rows, g.n_kv_heads, g.capacity)
+        with torch.cuda.device(self.device):
+            self._check(lib.vvs_qcache_evict(self.h, layer, n_layers, self._rows(length, "length"), keep, recent,
+                                             _on(mass, self.device, torch.float32, shape, "mass"), _on(mass_out, self.device, torch.float32, shape, "mass_out"),
+                                             _on(pos, self.device, torch.int32, shape, "pos"), _on(pos_out, self.device, torch.int32, shape, "pos_out"),
+                                             _stream()))
+
+    def vvs_qcache_read(self, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: Optional[torch.Tensor] = None, layer: int = 0, n_layers: int = 1):
+        """k, v [n_layers, rows, slots, kv heads, size] out."""
+        g = self.cfg
+        n = k.shape[2] if k.dim() == 5 else 0
+        shape = (n_layers, g.n_rows, n, g.n_kv_heads, g.head_size)
+        with torch.cuda.device(self.device):
+            self._check(lib.vvs_qcache_read(self.h, layer, n_layers, self._rows(length, "length"), self._rows(first, "first"), n,
+                                            _on(k, self.device, self.dtype, shape, "k"), _on(v, self.device, self.dtype, shape, "v"), _stream()))
+
+
+def vvs_qcache_query_sizes(cfg: VvsQCacheConfig):
+    cache, ws = C.c_size_t(), C.c_size_t()
+    st = lib.vvs_qcache_query_sizes(C.byref(cfg), C.byref(cache), C.byref(ws))
+    if st != VVS_OK:
+        raise VvsError(st, (lib.vvs_last_error(None) or b"").decode())
+    return cache.value, ws.value
+
+
+class Rope:
+    """Rotary positions on several axes; pairs: rotated pairs of each axis.  Owns a host object only."""
+
+    def __init__(self, head_size: int, pairs: Sequence[int], base: float, dtype: int, shared: bool = False, halves: bool = False):
+        if not 1 <= len(pairs) <= VVS_ROPE_MAX_AXES:
+            raise VvsError(VVS_ESIZE, "rope config: 1 to VVS_ROPE_MAX_AXES axes")
+        self.cfg = VvsRopeConfig(head_size, len(pairs), (C.c_int32 * VVS_ROPE_MAX_AXES)(*pairs), VVS_ROPE_SHARED if shared else VVS_ROPE_OWN,
+                                 VVS_ROPE_HALVES if halves else VVS_ROPE_ADJACENT, dtype, base)
+        h = C.c_void_p()
+        st = lib.vvs_rope_create(C.byref(self.cfg), C.byref(h))
+        if st != VVS_OK:
+            raise VvsError(st, (lib.vvs_last_error(None) or b"").decode())
+        self.h = h
+
+    def close(self):
+        if getattr(self, "h", None):
+            lib.vvs_rope_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def vvs_rope_apply(self, pos: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor], q_out: torch.Tensor, k_out: Optional[torch.Tensor],
+                       inverse: bool = False):
+        """pos int32 [..., axes]; q, k, q_out, k_out [..., heads, size] with the same leading dimensions; an output may be its input."""
+        device, dtype, lead = q.device, _TORCH_DTYPE[self.cfg.dtype], tuple(q.shape[:-2])
+        if not q.is_cuda or q.dim() < 3:
+            raise ValueError("q: wants a tensor [..., heads, size] on a HIP device")
+        n = 1
+        for d in lead:
+            n *= d
+        qp, qs = _per_token(q, device, dtype, (*lead, q.shape[-2], self.cfg.head_size), "q")
+        op, os_ = _per_token(q_out, device, dtype, q.shape, "q_out")
+        kv = 0 if k is None else k.shape[-2]
+        kp, ks = _per_token(k, device, dtype, (*lead, kv, self.cfg.head_size), "k")
+        kop, kos = _per_token(k_out, device, dtype, (*lead, kv, self.cfg.head_size), "k_out")
+        with torch.cuda.device(device):
+            st = lib.vvs_rope_apply(self.h, n, _on(pos, device, torch.int32, (*lead, self.cfg.n_axes), "pos"), q.shape[-2], qp, qs, op, os_, kv, kp, ks, kop, kos,
+                                    1 if inverse else 0, _stream())
+        if st != VVS_OK:
+            raise VvsError(st, (lib.vvs_rope_last_error(self.h) or b"").decode())

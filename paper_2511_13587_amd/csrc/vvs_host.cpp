@@ -23,6 +23,8 @@ static vvs_status fail(std::string* err, vvs_status st, const std::string& msg) 
   return st;
 }
 
+vvs_status fail_without_context(vvs_status st, const char* msg) { return fail(nullptr, st, msg); }
+
 // Every launch of a projection and every prefetch of its weights takes its tiles from here (or from plan_resid), so that the two
 // cannot disagree about which XCD reads which weight tile.
 //

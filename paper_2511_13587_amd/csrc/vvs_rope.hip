@@ -1,0 +1,91 @@
+// Rotary positions on several axes.
+#include "vvs_device.h"
+#include "vvs_qcache.h"
+
+namespace vvs {
+
+// A workgroup takes kRopeTokens tokens: first the sines and cosines of all their pairs, once for all heads, then the heads, 8 elements a time.
+// The angle is a product in 64 bits, counted in turns, so that taking whole turns off is exact: in 32 bits position 100000 would be off by 0.008 rad.
+constexpr int kRopeTokens = 4;
+
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16_t* p, float (&v)[8]) {
+  const uint4 a = *(const uint4*)p;
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void put8(float* p, const float (&v)[8]) {
+  ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void put8(bf16_t* p, const float (&v)[8]) {
+  *(uint4*)p = make_uint4(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7]));
+}
+
+template <typename T, bool HALVES>
+__global__ __launch_bounds__(256) void k_rope_axes(RopeArgs a) {
+  __shared__ float2 turn[kRopeTokens][128];
+  const int m0 = blockIdx.x * kRopeTokens, nm = min(kRopeTokens, a.M - m0);
+  for (int i = threadIdx.x; i < nm * a.pairs; i += 256) {
+    const int t = i / a.pairs, j = i % a.pairs;
+    const double w = (double)a.pos[(size_t)(m0 + t) * a.axes + a.axis[j]] * a.turns[j];
+    float sn, cs;
+    sincospif((float)(2.0 * (w - rint(w))), &sn, &cs);
+    turn[t][j] = make_float2(cs, a.inverse ? -sn : sn);
+  }
+  __syncthreads();
+  // a unit: 8 elements, or two runs of 8 that rotate against each other (HALVES); then what is copied
+  const int rot = HALVES ? a.pairs / 8 : a.pairs / 4, units = rot + (a.dh - 2 * a.pairs) / 8, all = (a.heads + a.kv_heads) * units;
+  for (int i = threadIdx.x; i < nm * all; i += 256) {
+    const int t = i / all, u = i % all, hd = u / units, e = u % units;
+    const bool is_k = hd >= a.heads;
+    const size_t m = m0 + t, at = (size_t)(is_k ? hd - a.heads : hd) * a.dh;
+    const T* x = (const T*)(is_k ? a.k : a.q) + m * (is_k ? a.k_stride : a.q_stride) + at;
+    T* y = (T*)(is_k ? a.k_out : a.q_out) + m * (is_k ? a.k_out_stride : a.q_out_stride) + at;
+    float v[8];
+    if (e >= rot) {
+      const int d = 2 * a.pairs + (e - rot) * 8;
+      load8(x + d, v);
+      put8(y + d, v);
+    } else if (HALVES) {
+      float b[8], p[8], q[8];
+      load8(x + e * 8, v);
+      load8(x + a.pairs + e * 8, b);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float2 c = turn[t][e * 8 + j];
+        p[j] = v[j] * c.x - b[j] * c.y;
+        q[j] = v[j] * c.y + b[j] * c.x;
+      }
+      put8(y + e * 8, p);
+      put8(y + a.pairs + e * 8, q);
+    } else {
+      load8(x + e * 8, v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 c = turn[t][e * 4 + j];
+        const float p = v[2 * j] * c.x - v[2 * j + 1] * c.y;
+        v[2 * j + 1] = v[2 * j] * c.y + v[2 * j + 1] * c.x;
+        v[2 * j] = p;
+      }
+      put8(y + e * 8, v);
+    }
+  }
+}
+
+void launch_rope_axes(const RopeArgs& a, int dtype, hipStream_t s) {
+  const dim3 grid((a.M + kRopeTokens - 1) / kRopeTokens);
+  if (dtype == VVS_BF16) {
+    if (a.halves) hipLaunchKernelGGL((k_rope_axes<bf16_t, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_rope_axes<bf16_t, false>), grid, dim3(256), 0, s, a);
+  } else {
+    if (a.halves) hipLaunchKernelGGL((k_rope_axes<float, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_rope_axes<float, false>), grid, dim3(256), 0, s, a);
+  }
+}
+
+}  // namespace vvs

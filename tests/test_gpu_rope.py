@@ -1,0 +1,88 @@
+"""Rotary positions on several axes against the formula in 64 bits.  Tolerance: an element is x c - y s in fp32, four roundings of values up to |x| + |y| <= sqrt(2) r
+(r: the pair's length), sine and cosine each off by at most 2^-22 (their own rounding, and the angle's: pi times one of 24 bits below 1), and a last rounding of 2^-8 (bf16) or 2^-24."""
+import numpy as np
+import pytest
+import torch
+
+import qcache_common as qc
+from paper_2511_13587_amd import binding as vb
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"bf16": (vb.VVS_BF16, torch.bfloat16, 2.0 ** -8), "fp32": (vb.VVS_FP32, torch.float32, 2.0 ** -24)}
+
+
+def check(got, x, pos, pairs, base, shared, halves, inverse, half_step):
+    x = x.double().cpu().numpy()
+    lead, (heads, size) = x.shape[:-2], x.shape[-2:]
+    x = x.reshape(-1, heads, size)
+    want = qc.rope(x, pos.cpu().numpy().reshape(len(x), -1), pairs, base, shared, halves, inverse)
+    total = sum(pairs)
+    r = np.zeros_like(x)
+    if halves:
+        r[..., :total] = r[..., total:2 * total] = np.hypot(x[..., :total], x[..., total:2 * total])
+    else:
+        r[..., 0:2 * total:2] = r[..., 1:2 * total:2] = np.hypot(x[..., 0:2 * total:2], x[..., 1:2 * total:2])
+    d = np.abs(got.double().cpu().numpy().reshape(want.shape) - want)
+    assert (d <= 2.0 ** -21 * r + half_step * np.abs(want)).all(), (d - 2.0 ** -21 * r - half_step * np.abs(want)).max()
+    assert (d[..., 2 * total:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size,pairs,shared,halves,heads,kv_heads,tokens", [
+    (64, [16, 16], False, False, 3, 3, 9),            # the contexts' own positions
+    (64, [12, 10, 10], False, False, 4, 2, 27),
+    (128, [16, 24, 24], True, True, 4, 1, 5),
+    (128, [64], True, True, 2, 2, 1),
+    (32, [3, 1, 3, 1], False, True, 1, 1, 130),
+    (96, [7, 5], True, False, 2, 1, 33),              # the rest of the head is copied
+    (256, [40, 40, 40], False, True, 1, 1, 3),
+    (8, [4], False, False, 5, 0, 17),
+])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rope(dtype, size, pairs, shared, halves, heads, kv_heads, tokens, inverse):
+    code, dt, half_step = DTYPES[dtype]
+    g = torch.Generator("cuda").manual_seed(size + tokens)
+    rope = vb.Rope(size, pairs, 10000.0, code, shared=shared, halves=halves)
+    wide = torch.randn((2, tokens, heads + 2 * kv_heads, size), generator=g, device="cuda").to(dt)
+    q, k = wide[:, :, :heads], wide[:, :, heads:heads + kv_heads] if kv_heads else None
+    pos = torch.randint(-40, 5000, (2, tokens, len(pairs)), generator=g, device="cuda", dtype=torch.int32)
+    pos[0, 0], pos[1, tokens - 1] = 0, 2 ** 31 - 1                  # far positions are as exact as near ones
+    pos[1, 0, -1] = -2 ** 31
+    q_out, k_out = torch.empty((2, tokens, heads, size), dtype=dt, device="cuda"), torch.empty((2, tokens, kv_heads, size), dtype=dt, device="cuda") if kv_heads else None
+    kept = wide.clone()
+    rope.vvs_rope_apply(pos, q, k, q_out, k_out, inverse=inverse)
+    check(q_out, q, pos, pairs, 10000.0, shared, halves, inverse, half_step)
+    if kv_heads:
+        check(k_out, k, pos, pairs, 10000.0, shared, halves, inverse, half_step)
+    assert torch.equal(wide, kept)
+    rope.vvs_rope_apply(pos, q, k, q, k, inverse=inverse)           # in place, inside the wider tensor
+    assert torch.equal(q, q_out) and (not kv_heads or torch.equal(k, k_out)) and torch.equal(wide[:, :, heads + kv_heads:], kept[:, :, heads + kv_heads:])
+
+
+def test_inverse_is_the_gradient():
+    """The gradient of sum(w * rope(x)) with respect to x is the inverse rotation of w, and differences of the forward agree with it."""
+    rope = vb.Rope(64, [12, 10, 10], 10000.0, vb.VVS_FP32)
+    g = torch.Generator("cuda").manual_seed(3)
+    x, w, step = (torch.randn((6, 2, 64), generator=g, device="cuda") for _ in range(3))
+    pos = torch.randint(0, 300, (6, 3), generator=g, device="cuda", dtype=torch.int32)
+    y0, y1, grad = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    rope.vvs_rope_apply(pos, w, None, grad, None, inverse=True)
+    rope.vvs_rope_apply(pos, x, None, y0, None)
+    rope.vvs_rope_apply(pos, x + step, None, y1, None)
+    # linear: the difference is exact but for the roundings of 768 products of normal values, each off by 2^-21 of its pair
+    a, b = ((y1 - y0).double() * w.double()).sum(), (grad.double() * step.double()).sum()
+    assert abs(float(a - b)) <= 768 * 16 * 2.0 ** -21
+
+
+def test_two_axes_are_the_contexts_positions():
+    """VVS_ROPE_OWN with two axes of size / 4 pairs rotates as the checker of the forward does."""
+    from oracle import vvs_oracle as vo
+    rope = vb.Rope(64, [16, 16], 10000.0, vb.VVS_FP32)
+    x = torch.randn((5, 3, 64), generator=torch.Generator("cuda").manual_seed(4), device="cuda")
+    pos = torch.tensor([[0, 0], [1, 2], [23, 5], [7, 23], [15, 15]], dtype=torch.int32, device="cuda")
+    y = torch.empty_like(x)
+    rope.vvs_rope_apply(pos, x, None, y, None)
+    for t in range(5):
+        want = vo.rope_2d(x[t].double().cpu().numpy(), int(pos[t, 0]), int(pos[t, 1]), 10000.0)
+        assert np.abs(y[t].double().cpu().numpy() - want).max() <= 2.0 ** -20 * float(x.abs().max()) * 1.5
