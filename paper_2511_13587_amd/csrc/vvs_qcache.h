@@ -7,7 +7,7 @@ namespace vvs {
 constexpr int kQBlock = VVS_QCACHE_BLOCK;   // slots that share a power of two
 constexpr int kQLeast = -110;               // smallest exponent of a block
 constexpr int kQParts = 2048;               // partial results of a split attention call that the workspace has room for, of 16 queries each
-constexpr size_t kQTicket = 64 * 1024;      // bytes of counters at the start of the workspace
+constexpr int kQKept = 8;                   // queries per row and key/value head whose scores are kept for the counted weights
 
 // One cache (all layers).  A region is what one (layer, row, key/value head) holds: blocks of 32 slots, each 32 * head_size bytes of keys and
 // then as many of values; behind all regions, in the same order, two floats per block: 2^E of its keys and of its values.
@@ -46,6 +46,8 @@ struct QAttention {
   int capacity;
   int packed;                       // 1: out in the operand order of the projections
   float* parts;                     // partial results: o, then (m, l)
+  float* scores;                    // workspace: kept scores of one layer, [rows][kv_heads][score_steps][n_kept][32]
+  int score_steps, n_kept;          // (n_kept: the launcher's choice)
   int splits;
   int causal;
   uint64_t anc[VVS_MAX_T];          // !causal: bit j = token sees block token j

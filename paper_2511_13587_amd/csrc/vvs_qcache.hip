@@ -1,4 +1,6 @@
 // Key/value cache in 8 bits: append, attention with counted weights, eviction, read.
+#include <float.h>
+#include <limits.h>
 #include <algorithm>
 
 #include "vvs_mfma.h"
@@ -51,128 +53,252 @@ __device__ __forceinline__ int key_byte(int w, int dim) {
 }
 __device__ __forceinline__ int value_byte(int w, int dim) { return (((dim >> 5) * 64 + (w >> 3) * 16 + (dim & 15)) * 2 + ((dim >> 4) & 1)) * 8 + (w & 7); }
 
-// ------------------------------------------------------------------------------------------------ append
-// One wave per (layer, row, head, block that is written into), first its keys, then its values.  Two passes over the wave's share: the largest new
-// element gives E, then every lane makes the 16 bytes that it stores.  What the block held is rounded to the larger E.
-template <typename T>
-__device__ __forceinline__ float element(const void* p, size_t at) { return ld((const T*)p + at); }
 
-template <typename T>
+// Transposes of 8 x 8 elements between the 8 lanes l % 8 (lane: a row, element: a column), in registers: half of what a lane holds is exchanged with the lane 4 on, 2 on, 1 on.
+// What the cache wants of the values - 8 slots of one dim in a lane - is the transpose of what memory gives - 8 dims of one slot.
+__device__ __forceinline__ uint32_t lane_xor1(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0xB1, 0xF, 0xF, false); }
+__device__ __forceinline__ uint32_t lane_xor2(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x4E, 0xF, 0xF, false); }
+__device__ __forceinline__ uint32_t lane_xor4(uint32_t x) {
+  const int y = __builtin_amdgcn_update_dpp((int)x, (int)x, 0x141, 0xF, 0xF, false);             // row_half_mirror, then quad_perm:[3,2,1,0]
+  return (uint32_t)__builtin_amdgcn_update_dpp(y, y, 0x1B, 0xF, 0xF, false);
+}
+__device__ __forceinline__ void swap_rows(uint32_t& a, uint32_t& b, bool odd, uint32_t (*partner)(uint32_t)) {
+  const uint32_t got = partner(odd ? a : b);
+  a = odd ? got : a;
+  b = odd ? b : got;
+}
+__device__ __forceinline__ uint2 transpose_bytes(uint2 v, int lane) {
+  swap_rows(v.x, v.y, lane & 4, lane_xor4);
+  const uint32_t half = lane & 2 ? 0x03020706u : 0x05040100u, byte = lane & 1 ? 0x03070105u : 0x06020400u;
+  v.x = __builtin_amdgcn_perm(lane_xor2(v.x), v.x, half);
+  v.y = __builtin_amdgcn_perm(lane_xor2(v.y), v.y, half);
+  v.x = __builtin_amdgcn_perm(lane_xor1(v.x), v.x, byte);
+  v.y = __builtin_amdgcn_perm(lane_xor1(v.y), v.y, byte);
+  return v;
+}
+__device__ __forceinline__ uint4 transpose_halves(uint4 v, int lane) {
+  swap_rows(v.x, v.z, lane & 4, lane_xor4);
+  swap_rows(v.y, v.w, lane & 4, lane_xor4);
+  swap_rows(v.x, v.y, lane & 2, lane_xor2);
+  swap_rows(v.z, v.w, lane & 2, lane_xor2);
+  const uint32_t half = lane & 1 ? 0x03020706u : 0x05040100u;
+  v.x = __builtin_amdgcn_perm(lane_xor1(v.x), v.x, half);
+  v.y = __builtin_amdgcn_perm(lane_xor1(v.y), v.y, half);
+  v.z = __builtin_amdgcn_perm(lane_xor1(v.z), v.z, half);
+  v.w = __builtin_amdgcn_perm(lane_xor1(v.w), v.w, half);
+  return v;
+}
+
+__device__ __forceinline__ void read8(const float* p, float (&v)[8]) {
+  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void unpack8(uint4 a, float (&v)[8]) {
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void read8(const bf16_t* p, float (&v)[8]) { unpack8(*(const uint4*)p, v); }
+__device__ __forceinline__ void write8(float* p, const float (&v)[8]) {
+  ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void write8(bf16_t* p, const float (&v)[8]) {
+  *(uint4*)p = make_uint4(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7]));
+}
+
+// slot of tile t's row that lane l % 16 = i supplies (keys), and the one whose dims it takes before the transpose (values)
+__device__ __forceinline__ int slot_of(int t, int i) { return 8 * (i >> 2) + 4 * t + (i & 3); }
+__device__ __forceinline__ int value_slot(int lane) { return 8 * (lane >> 4) + (lane & 7); }
+
+// ------------------------------------------------------------------------------------------------ append
+// One wave per (layer, row, head, block that is written into); heads are next to each other in a workgroup, as their elements are in memory.  A lane loads the 16 bytes
+// (fp32: 32) of 8 dims of the slots that it stores, all at once; their largest gives E; what the block held already is only read where it shares 8 bytes with new slots, or where E grew.
+template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_qcache_append(QAppend a, int max_blocks) {
+  constexpr int KD = DH / 32;
   const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6), r = blockIdx.y, layer = blockIdx.z;
-  const int head = unit / max_blocks, nth = unit % max_blocks;
-  if (head >= a.c.kv_heads) return;
+  const int head = unit % a.c.kv_heads, nth = unit / a.c.kv_heads;
+  if (nth >= max_blocks) return;
   if (a.skip && a.skip[r >> a.len.shift] < 0) return;
   const int len = row_len(a.len, r, a.capacity);
   const int want = a.n_tokens ? min(max(a.n_tokens[r >> a.n_shift] + a.count_plus, 0), a.n) : a.n, n = min(want, a.capacity - len);
   const int block = (len >> 5) + nth, slot0 = block * kQBlock;
   if (n < 1 || slot0 >= len + n) return;
   const int begin = max(len - slot0, 0), end = min(len + n - slot0, kQBlock);   // slots of the block that are written
-  const int dh = a.c.dh, shift = slot0 - len;                                   // slot w takes token w + shift
-  const size_t row0 = (size_t)layer * a.layer_stride + (size_t)r * a.src_tokens * a.stride + (size_t)head * dh;
+  const size_t row0 = (size_t)layer * a.layer_stride + (size_t)r * a.src_tokens * a.stride + (size_t)head * DH;
   const size_t region = a.c.region(a.layer + layer, r, head);
   uint8_t* data = a.c.data + (region * a.c.blocks + block) * a.c.block_bytes();
   float2* scale = a.c.scale + region * a.c.blocks + block;
-  // source token of slot w, < 0: none
+  const float2 was = *scale;
+  // source token of slot w (slot w takes token w + slot0 - len), < 0: zeros
   auto token = [&](int w) {
-    if (w < begin || w >= end) return -1;
-    const int t = w + shift;
-    if (!a.select) return t;
-    const int p = a.select[(size_t)(r >> a.select_shift) * a.select_stride + t];
+    const int t = min(max(w, begin), end - 1) + slot0 - len;
+    const int p = a.select ? a.select[(size_t)(r >> a.select_shift) * a.select_stride + t] : t;
     return p >= 0 && p < a.src_tokens ? p : -1;
   };
+  const int g = lane >> 4, i = lane & 15;
+  const int w_k[2] = {slot_of(0, i), slot_of(1, i)}, w_v = value_slot(lane);
+  const int tok[3] = {token(w_k[0]), token(w_k[1]), token(w_v)};
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    const void* src = half ? a.v : a.k;
+    const T* src = (const T*)(half ? a.v : a.k) + row0;
+    float x[KD][2][8];
     float top = 0.f;
-    for (int i = lane; i < kQBlock * dh; i += 64) {
-      const int t = token(i / dh);
-      if (t < 0) continue;
-      const float x = fabsf(element<T>(src, row0 + (size_t)t * a.stride + i % dh));
-      if (finite(x)) top = fmaxf(top, x);
-    }
-    const int was = exponent_of(half ? scale->y : scale->x);
-    int e = e4m3_exponent(wave_max(top));
-    if (begin > 0) e = max(e, was);
-    uint8_t* out = data + half * kQBlock * dh;
-    const int g = lane >> 4, i = lane & 15;
-    for (int c = 0; c < dh / 32; ++c) {
-      uint2* at = (uint2*)(out + (c * 64 + lane) * 16);
+#pragma unroll
+    for (int c = 0; c < KD; ++c)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        float old[8], v[8];
-        const uint2 held = at[t];
-        from_e4m3x8(held, old);
-        bool any = false;
+        const int from = half ? tok[2] : tok[t], dim = half ? c * 32 + t * 16 + (i & 8) : c * 32 + 8 * g;
+        read8(src + (size_t)max(from, 0) * a.stride + dim, x[c][t]);
+      }
+#pragma unroll
+    for (int c = 0; c < KD; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int w = half ? w_v : w_k[t];
+        const bool is_new = w >= begin && w < end, there = w < end && (half ? tok[2] : tok[t]) >= 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int w = half ? 8 * g + j : 8 * (i >> 2) + 4 * t + (i & 3), dim = half ? c * 32 + t * 16 + i : c * 32 + 8 * g + j;
-          const int tok = token(w);
-          float x = 0.f;
-          if (tok >= 0) x = ldexpf(element<T>(src, row0 + (size_t)tok * a.stride + dim), -e);
-          v[j] = w < begin ? ldexpf(old[j], was - e) : finite(x) ? x : __uint_as_float(0x7FC00000u);
-          any |= w < end;
+          const float v = there ? x[c][t][j] : 0.f;
+          x[c][t][j] = v;
+          const float m = fabsf(v);
+          top = fmaxf(top, is_new && m < INFINITY ? m : 0.f);
         }
-        if (any) at[t] = to_e4m3x8(v);
       }
-    }
+    const int was_e = exponent_of(half ? was.y : was.x);
+    int e = e4m3_exponent(wave_max(top));
+    if (begin > 0) e = max(e, was_e);
+    const bool grew = begin > 0 && e > was_e;
+    uint8_t* out = data + half * kQBlock * DH;
+#pragma unroll
+    for (int c = 0; c < KD; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float y = ldexpf(x[c][t][j], -e);
+          v[j] = finite(y) ? y : __uint_as_float(0x7FC00000u);
+        }
+        uint2 bytes = to_e4m3x8(v);
+        uint2* at = (uint2*)(out + (c * 64 + lane) * 16) + t;
+        // the 8 bytes are one slot's dims (keys), or 8 slots of a dim (values): which of them are old
+        const int first = half ? 8 * g : w_k[t], slots = half ? 8 : 1;
+        if (half) bytes = transpose_bytes(bytes, lane);
+        const bool has_new = first < end && first + slots > begin, has_old = first < begin;
+        if (!has_new && !(grew && has_old)) continue;
+        if (has_old) {
+          uint2 held = *at;
+          if (grew) {
+            float old[8];
+            from_e4m3x8(held, old);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) old[j] = ldexpf(old[j], was_e - e);
+            held = to_e4m3x8(old);
+          }
+          const int keep = begin - first;                    // leading bytes of the 8 that are old (keys: all)
+          const uint64_t mask = !half || keep >= 8 ? ~0ull : (1ull << (8 * keep)) - 1;
+          bytes.x = (held.x & (uint32_t)mask) | (bytes.x & ~(uint32_t)mask);
+          bytes.y = (held.y & (uint32_t)(mask >> 32)) | (bytes.y & ~(uint32_t)(mask >> 32));
+        }
+        *at = bytes;
+      }
     if (lane == 0) (half ? scale->y : scale->x) = ldexpf(1.f, e);
   }
 }
 
-void launch_qcache_append(const QAppend& a, int dtype, hipStream_t s) {
+template <typename T>
+static void append_t(const QAppend& a, hipStream_t s) {
   const int max_blocks = (int)std::min<int64_t>(((int64_t)a.n + 2 * kQBlock - 2) / kQBlock, a.c.blocks);
   const dim3 grid(((int64_t)a.c.kv_heads * max_blocks + 3) / 4, a.c.rows, a.n_layers);
-  if (dtype == VVS_BF16) hipLaunchKernelGGL(k_qcache_append<bf16_t>, grid, dim3(256), 0, s, a, max_blocks);
-  else hipLaunchKernelGGL(k_qcache_append<float>, grid, dim3(256), 0, s, a, max_blocks);
+  if (a.c.dh == 32) hipLaunchKernelGGL((k_qcache_append<T, 32>), grid, dim3(256), 0, s, a, max_blocks);
+  else if (a.c.dh == 64) hipLaunchKernelGGL((k_qcache_append<T, 64>), grid, dim3(256), 0, s, a, max_blocks);
+  else hipLaunchKernelGGL((k_qcache_append<T, 128>), grid, dim3(256), 0, s, a, max_blocks);
+}
+
+void launch_qcache_append(const QAppend& a, int dtype, hipStream_t s) {
+  if (dtype == VVS_BF16) append_t<bf16_t>(a, s);
+  else append_t<float>(a, s);
 }
 
 // ------------------------------------------------------------------------------------------------ read
-template <typename T>
-__global__ __launch_bounds__(256) void k_qcache_read(QRead a) {
-  const int dh = a.c.dh, r = blockIdx.y, layer = blockIdx.z, per = a.c.kv_heads * (dh / 8);
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)a.n * per) return;
-  const int j = (int)(i / per), head = (int)(i % per) / (dh / 8), dim = (int)(i % per) % (dh / 8) * 8;
+// One wave per (layer, row, head, block that the window touches): whole 16-byte pieces of the block, the values turned in registers.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_qcache_read(QRead a, int max_blocks) {
+  constexpr int KD = DH / 32;
+  const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6), r = blockIdx.y, layer = blockIdx.z;
+  const int head = unit % a.c.kv_heads, nth = unit / a.c.kv_heads;
+  if (nth >= max_blocks) return;
   const int len = row_len(a.len, r, a.capacity);
-  const int64_t slot = (int64_t)(a.first ? a.first[r] : 0) + j;
-  float k[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (slot >= 0 && slot < len) {
-    const size_t block = a.c.region(a.layer + layer, r, head) * a.c.blocks + (slot >> 5);
-    const uint8_t* data = a.c.data + block * a.c.block_bytes();
-    const float2 sc = a.c.scale[block];
-    const int w = (int)(slot & 31);
-    from_e4m3x8(*(const uint2*)(data + key_byte(w, dim)), k);
-    const uint8_t* vb = data + kQBlock * dh + value_byte(w, dim);
+  const int64_t first = a.first ? a.first[r] : 0, block = (first >> 5) + nth, slot0 = block * kQBlock;
+  if (slot0 >= first + a.n) return;
+  const bool held = block >= 0 && slot0 < len;
+  const size_t at = a.c.region(a.layer + layer, r, head) * a.c.blocks + (held ? (size_t)block : 0);
+  const uint8_t* data = a.c.data + at * a.c.block_bytes();
+  const float2 sc = a.c.scale[at];
+  const size_t out0 = ((size_t)layer * a.c.rows + r) * a.n;
+  const int g = lane >> 4, i = lane & 15;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      k[e] *= sc.x;
-      v[e] = e4m3_at<0>(vb[e * 16]) * sc.y;
-    }
-  }
-  const size_t at = (((size_t)layer * a.c.rows + r) * a.n + j) * a.c.kv_heads * dh + (size_t)head * dh + dim;
-  if constexpr (sizeof(T) == 4) {
-    ((float4*)((T*)a.k + at))[0] = make_float4(k[0], k[1], k[2], k[3]);
-    ((float4*)((T*)a.k + at))[1] = make_float4(k[4], k[5], k[6], k[7]);
-    ((float4*)((T*)a.v + at))[0] = make_float4(v[0], v[1], v[2], v[3]);
-    ((float4*)((T*)a.v + at))[1] = make_float4(v[4], v[5], v[6], v[7]);
-  } else {
-    *(uint4*)((T*)a.k + at) = make_uint4(pack2bf(k[0], k[1]), pack2bf(k[2], k[3]), pack2bf(k[4], k[5]), pack2bf(k[6], k[7]));
-    *(uint4*)((T*)a.v + at) = make_uint4(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7]));
+  for (int half = 0; half < 2; ++half) {
+    const float unit_of = half ? sc.y : sc.x;
+    uint4 b[KD];
+#pragma unroll
+    for (int c = 0; c < KD; ++c) b[c] = held ? *(const uint4*)(data + half * kQBlock * DH + (c * 64 + lane) * 16) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int c = 0; c < KD; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        uint2 v8 = t ? make_uint2(b[c].z, b[c].w) : make_uint2(b[c].x, b[c].y);
+        if (half) v8 = transpose_bytes(v8, lane);
+        const int w = half ? value_slot(lane) : slot_of(t, i), dim = half ? c * 32 + t * 16 + (i & 8) : c * 32 + 8 * g;
+        const int64_t slot = slot0 + w;
+        float v[8];
+        from_e4m3x8(v8, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = held && slot < len ? v[j] * unit_of : 0.f;
+        if (slot >= first && slot < first + a.n)
+          write8((T*)(half ? a.v : a.k) + ((out0 + (size_t)(slot - first)) * a.c.kv_heads + head) * DH + dim, v);
+      }
   }
 }
 
+template <typename T>
+static void read_t(const QRead& a, hipStream_t s) {
+  const int max_blocks = (int)(((int64_t)a.n + 2 * kQBlock - 2) / kQBlock);
+  const dim3 grid(((int64_t)a.c.kv_heads * max_blocks + 3) / 4, a.c.rows, a.n_layers);
+  if (a.c.dh == 32) hipLaunchKernelGGL((k_qcache_read<T, 32>), grid, dim3(256), 0, s, a, max_blocks);
+  else if (a.c.dh == 64) hipLaunchKernelGGL((k_qcache_read<T, 64>), grid, dim3(256), 0, s, a, max_blocks);
+  else hipLaunchKernelGGL((k_qcache_read<T, 128>), grid, dim3(256), 0, s, a, max_blocks);
+}
+
 void launch_qcache_read(const QRead& a, int dtype, hipStream_t s) {
-  const int64_t items = (int64_t)a.n * a.c.kv_heads * (a.c.dh / 8);
-  const dim3 grid((items + 255) / 256, a.c.rows, a.n_layers);
-  if (dtype == VVS_BF16) hipLaunchKernelGGL(k_qcache_read<bf16_t>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(k_qcache_read<float>, grid, dim3(256), 0, s, a);
+  if (dtype == VVS_BF16) read_t<bf16_t>(a, s);
+  else read_t<float>(a, s);
 }
 
 // ------------------------------------------------------------------------------------------------ attention
 // One wave takes 32 keys a step (a cached block, or 32 block tokens) against 16 NQB queries; a query is (block token, query head of the key/value head).
-// The online softmax keeps the running maximum in units of log2: m = max(score * c), weights 2^(score c - m).  Cached elements are exact in bf16, so scores
-// are bf16 products summed in fp32; fp32 queries (and block keys, values and weights) go in as sums of NS bf16 values, which hold all 24 bits.
+//
+// Scores S^T = K Q^T: e4m3 numbers are exact in bf16, the block's power of two is multiplied into the softmax's constant.  Weights are 2^(score c + E - M) with E the exponent of the
+// block's values, so that O^T += V^T P^T takes the e4m3 numbers themselves, as fp16; M is at most 2^6 below the largest such exponent so far, so that
+// weights fit fp16 (rounded to 2^-11, an eighth of the output's own rounding) and the accumulators are rescaled only when a maximum grows by more than that.  The normaliser sums the
+// fp32 weights, divided by 2^E, per lane; lanes, waves and splits are joined at the end, in a fixed order.
+// fp32 calls (queries, block keys and values, weights as sums of NS = 3 bf16 values, which hold all 24 bits), block tokens (values are bf16: weights as two bf16
+// values, to 2^-17) and blocks whose E is beyond +-40 (where fp16 weights could vanish beside others) take values in bf16, times 2^E.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// Eight e4m3 numbers as fp16 (exact)
+__device__ __forceinline__ f16x8 e4m3_to_f16(uint2 b) {
+  uint4 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.x, 1.f, false));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.x, 1.f, true));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.y, 1.f, false));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.y, 1.f, true));
+  return __builtin_bit_cast(f16x8, r);
+}
+__device__ __forceinline__ uint32_t pack2half(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2_t{a, b}, f16x2)); }
 
 // x as a sum of NS bf16 values
 template <int NS>
@@ -192,80 +318,107 @@ __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[NS]) {
     out[n] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
   }
 }
-__device__ __forceinline__ void read8(const float* p, float (&v)[8]) {
-  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
 template <int NS>
-__device__ __forceinline__ void load_operand(const float* p, bool there, bf16x8 (&out)[NS]) {
-  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (there) read8(p, v);
+__device__ __forceinline__ void load_operand(const float* p, bf16x8 (&out)[NS]) {
+  float v[8];
+  read8(p, v);
   split8<NS>(v, out);
 }
 template <int NS>
-__device__ __forceinline__ void load_operand(const bf16_t* p, bool there, bf16x8 (&out)[NS]) {
+__device__ __forceinline__ void load_operand(const bf16_t* p, bf16x8 (&out)[NS]) {
   static_assert(NS == 1, "");
-  out[0] = as_bf16x8(there ? *(const uint4*)p : make_uint4(0, 0, 0, 0));
+  out[0] = as_bf16x8(*(const uint4*)p);
 }
 
 template <typename T, int DH>
 struct QShape {
+  static constexpr bool F16 = sizeof(T) == 2;           // weights and cached values in fp16
   static constexpr int NS = sizeof(T) == 4 ? 3 : 1;     // bf16 values that make up an operand of the caller's type
-  static constexpr int NP = sizeof(T) == 4 ? 3 : 2;     // ... and a softmax weight (of bf16 calls: to 2^-17)
+  static constexpr int NP = sizeof(T) == 4 ? 3 : 2;     // ... and a softmax weight beside values in bf16
   static constexpr int KD = DH / 32, DT = DH / 16;
 };
 
-// Keys of a step in the operand registers: kf[tile][dims][part]
-template <typename T, int DH, int NK>
-__device__ __forceinline__ void keys_of_block(const uint8_t* data, float scale, int lane, bf16x8 (&kf)[2][DH / 32][NK]) {
-#pragma unroll
-  for (int kd = 0; kd < DH / 32; ++kd) {
-    const uint4 b = *(const uint4*)(data + (kd * 64 + lane) * 16);
-    kf[0][kd][0] = e4m3_to_bf16(make_uint2(b.x, b.y), scale);
-    kf[1][kd][0] = e4m3_to_bf16(make_uint2(b.z, b.w), scale);
-  }
-}
-// Values; slots from `valid` on of the block (of the wave's 32) are zeros: what lies behind the length may be anything
-template <int DH>
-__device__ __forceinline__ void values_of_block(const uint8_t* data, float scale, int lane, int valid, bf16x8 (&vf)[DH / 16][1]) {
-  const int mine = valid - 8 * (lane >> 4);       // of this lane's 8 slots
-  const uint64_t keep = mine >= 8 ? ~0ull : mine <= 0 ? 0ull : (1ull << (8 * mine)) - 1;
-#pragma unroll
-  for (int c = 0; c < DH / 32; ++c) {
-    uint4 b = *(const uint4*)(data + kQBlock * DH + (c * 64 + lane) * 16);
-    b.x &= (uint32_t)keep; b.y &= (uint32_t)(keep >> 32); b.z &= (uint32_t)keep; b.w &= (uint32_t)(keep >> 32);
-    vf[2 * c][0] = e4m3_to_bf16(make_uint2(b.x, b.y), scale);
-    vf[2 * c + 1][0] = e4m3_to_bf16(make_uint2(b.z, b.w), scale);
-  }
-}
-// slot of tile t's row that lane l % 16 = i supplies
-__device__ __forceinline__ int slot_of(int t, int i) { return 8 * (i >> 2) + 4 * t + (i & 3); }
+constexpr float kQSmall = 0x1p-110f;      // 2^kQLeast
 
+// A cached block in registers, as it lies in memory
+template <int DH>
+struct QRaw {
+  uint4 k[DH / 32], v[DH / 32];
+  float2 scale;
+  __device__ __forceinline__ void load(const uint8_t* data, const float2* sc, int lane) {
+#pragma unroll
+    for (int c = 0; c < DH / 32; ++c) k[c] = *(const uint4*)(data + (c * 64 + lane) * 16);
+#pragma unroll
+    for (int c = 0; c < DH / 32; ++c) v[c] = *(const uint4*)(data + kQBlock * DH + (c * 64 + lane) * 16);
+    scale = make_float2(fmaxf(sc->x, kQSmall), fmaxf(sc->y, kQSmall));     // (a block never written holds 0)
+  }
+  // slots from `valid` on are zeros among the values: what lies behind the length may be anything, NaN included
+  __device__ __forceinline__ void mask_values(int lane, int valid) {
+    const int mine = valid - 8 * (lane >> 4);       // of this lane's 8 slots
+    const uint64_t keep = mine >= 8 ? ~0ull : mine <= 0 ? 0ull : (1ull << (8 * mine)) - 1;
+#pragma unroll
+    for (int c = 0; c < DH / 32; ++c) {
+      v[c].x &= (uint32_t)keep; v[c].y &= (uint32_t)(keep >> 32); v[c].z &= (uint32_t)keep; v[c].w &= (uint32_t)(keep >> 32);
+    }
+  }
+};
+
+// Keys of a step of block tokens.  Tokens from n on are the last one again: their scores are masked.
 template <typename T, int DH, int NS>
 __device__ __forceinline__ void keys_of_tokens(const T* k, size_t stride, int tok0, int n, int lane, bf16x8 (&kf)[2][DH / 32][NS]) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int tok = tok0 + slot_of(t, lane & 15);
+    const T* p = k + (size_t)min(tok0 + slot_of(t, lane & 15), n - 1) * stride + (lane >> 4) * 8;
 #pragma unroll
-    for (int kd = 0; kd < DH / 32; ++kd) load_operand<NS>(k + (size_t)min(tok, n - 1) * stride + kd * 32 + (lane >> 4) * 8, tok < n, kf[t][kd]);
+    for (int kd = 0; kd < DH / 32; ++kd) load_operand<NS>(p + kd * 32, kf[t][kd]);
   }
 }
-// ... with zeros for elements that are not finite; returns whether this lane met any
-template <typename T, int DH, int NS>
-__device__ __forceinline__ bool values_of_tokens(const T* v, size_t stride, int tok0, int n, int lane, bf16x8 (&vf)[DH / 16][NS]) {
+// Values: 8 dims of one slot are loaded, and turned.  Zeros in the place of tokens from n on, and of elements that are not finite; returns whether this lane met any of those.
+template <int DH, int NS>
+__device__ __forceinline__ bool values_of_tokens(const float* v, size_t stride, int tok0, int n, int lane, bf16x8 (&vf)[DH / 16][NS]) {
+  const int tok = tok0 + value_slot(lane);
+  const float* p = v + (size_t)min(tok, n - 1) * stride + (lane & 8);
   bool odd = false;
 #pragma unroll
   for (int dt = 0; dt < DH / 16; ++dt) {
     float x[8];
+    read8(p + dt * 16, x);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int tok = tok0 + (lane >> 4) * 8 + j;
-      x[j] = tok < n ? ld(v + (size_t)min(tok, n - 1) * stride + dt * 16 + (lane & 15)) : 0.f;
-      if (!finite(x[j])) { odd = true; x[j] = 0.f; }
+      const bool fin = finite(x[j]);
+      odd |= !fin && tok < n;
+      x[j] = fin && tok < n ? x[j] : 0.f;
     }
-    split8<NS>(x, vf[dt]);
+    bf16x8 part[NS];
+    split8<NS>(x, part);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) vf[dt][s] = as_bf16x8(transpose_halves(__builtin_bit_cast(uint4, part[s]), lane));
   }
   return odd;
+}
+
+template <int DH, int NS>
+__device__ __forceinline__ bool values_of_tokens(const bf16_t* v, size_t stride, int tok0, int n, int lane, bf16x8 (&vf)[DH / 16][NS]) {
+  static_assert(NS == 1, "");
+  const int tok = tok0 + value_slot(lane);
+  const bf16_t* p = v + (size_t)min(tok, n - 1) * stride + (lane & 8);
+  const uint32_t there = tok < n ? 0xFFFFFFFFu : 0u;
+  uint32_t odd = 0;
+#pragma unroll
+  for (int dt = 0; dt < DH / 16; ++dt) {
+    const uint4 b = *(const uint4*)(p + dt * 16);
+    uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w[j] &= there;
+      // exponents of all ones: the carry of one more into the sign, half by half
+      const uint32_t bad = ((w[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+      odd |= bad;
+      w[j] &= ~((bad >> 15) * 0xFFFFu);
+    }
+    vf[dt][0] = as_bf16x8(transpose_halves(make_uint4(w[0], w[1], w[2], w[3]), lane));
+  }
+  return odd != 0;
 }
 
 // scores of the step's 32 keys for 16 queries: lane (g, query) gets those of keys 8 g .. 8 g + 7
@@ -287,41 +440,60 @@ __device__ __forceinline__ void step_scores(const bf16x8 (&kf)[2][KD][NK], const
   }
 }
 
-// Online softmax of 8 scores per lane and O^T += V^T P^T; e: the weights, as they went in
-template <int DT, int NK, int NP>
-__device__ __forceinline__ void step_softmax(const float (&sv)[8], const bf16x8 (&vf)[DT][NK], float c_exp, float& m_run, float& l_run, floatx4 (&o)[DT], float (&e)[8]) {
-  float mx = sv[0];
+// What a wave carries along for 16 queries (column col of a lane): reference exponent (the same in all four lanes of a query), this lane's part of the normaliser, O^T
+template <int DT>
+struct QRun {
+  float m, l;
+  floatx4 o[DT];
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = 0.f;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) mx = fmaxf(mx, sv[i]);
-  const float m_new = fmaxf(m_run, rows_max(mx) * c_exp);
-  const float m_safe = m_new == -INFINITY ? 0.f : m_new;
-  const float alpha = __builtin_amdgcn_exp2f(m_run - m_safe);
-  float rs = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    e[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], c_exp, -m_safe));
-    rs += e[i];
+    for (int dt = 0; dt < DT; ++dt) o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  l_run = l_run * alpha + rows_sum(rs);
-  m_run = m_new;
-  bf16x8 pf[NP];
-  split8<NP>(e, pf);
-  if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {
+  // weights of 8 keys, e[i] = 2^(sv[i] c + ev - m)
+  __device__ __forceinline__ void weights(const float (&sv)[8], float c, float ev, float per_unit, float (&e)[8]) {
+    float mx = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
+    const float cand = fmaf(rows_max(mx), c, ev);
+    if (__builtin_amdgcn_ballot_w64(cand > m + 6.f)) {
+      const float to = fmaxf(m, cand), alpha = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[dt][j] *= alpha;
+    }
+    const float off = ev - (m == -INFINITY ? 0.f : m);
+    float rs = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      e[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], c, off));
+      rs += e[i];
+    }
+    l = fmaf(rs, per_unit, l);
+  }
+  template <int NK, int NP>
+  __device__ __forceinline__ void add_bf16(const float (&e)[8], const bf16x8 (&vf)[DT][NK]) {
+    bf16x8 pf[NP];
+    split8<NP>(e, pf);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[dt][j] *= alpha;
+      for (int sum = (NK > 1 ? NP - 1 : NP + NK - 2); sum >= 0; --sum)
+#pragma unroll
+        for (int p = 0; p < NK; ++p) {
+          if (sum - p < 0 || sum - p >= NP) continue;
+          o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dt][p], pf[sum - p], o[dt], 0, 0, 0);
+        }
   }
+  __device__ __forceinline__ void add_f16(const float (&e)[8], const f16x8 (&vf)[DT]) {
+    const uint4 w = make_uint4(pack2half(e[0], e[1]), pack2half(e[2], e[3]), pack2half(e[4], e[5]), pack2half(e[6], e[7]));
+    const f16x8 pf = __builtin_bit_cast(f16x8, w);
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int sum = (NK > 1 ? NP - 1 : NP + NK - 2); sum >= 0; --sum)
-#pragma unroll
-      for (int p = 0; p < NK; ++p) {
-        if (sum - p < 0 || sum - p >= NP) continue;
-        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dt][p], pf[sum - p], o[dt], 0, 0, 0);
-      }
-}
+    for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[dt], pf, o[dt], 0, 0, 0);
+  }
+};
 
 // What of the row a wave sees
 struct QRow {
@@ -334,6 +506,11 @@ __device__ __forceinline__ QRow row_of(const QAttention& a, int r) {
   w.n = a.n_tokens ? min(max(a.n_tokens[r], 0), a.T) : a.T;
   w.blocks = (w.len + kQBlock - 1) / kQBlock;
   return w;
+}
+
+// Block tokens that the queries in front of query `end` can see: with a chain none behind the last query
+__device__ __forceinline__ int seen_by(const QAttention& a, const QRow& w, int end) {
+  return !a.k || end < 1 ? 0 : a.causal ? min(w.n, (end - 1) / a.group + 1) : w.n;
 }
 
 // Bit i: query token t sees block token tok + i (below `seen`)
@@ -363,20 +540,42 @@ __device__ __forceinline__ void store4(const QAttention& a, size_t at, int dim, 
   }
 }
 
-// log-sum-exp for the caller, maximum and 1 / sum for the counted weights (from the log alone they would lose what its size takes of 24 bits)
+// log-sum-exp for the caller, reference exponent and 1 / sum for the counted weights (from the log alone they would lose what its size takes of 24 bits)
 __device__ __forceinline__ void tell_norm(const QAttention& a, size_t at, float m, float l) {
-  const bool none = m == -INFINITY;
+  const bool none = l == 0.f;            // a query that sees nothing
   if (a.lse) a.lse[at] = none ? -INFINITY : (m + log2f(l)) * kLn2;
   if (a.norm) a.norm[at] = make_float2(none ? 0.f : m, none ? 0.f : 1.f / l);
 }
 
+// Scores (times c: units of log2) that the main kernel leaves for the counted weights: [rows][kv heads][steps][counted queries][32 keys]
+__device__ __forceinline__ float* kept_scores(const QAttention& a, int r, int hk, int step) {
+  return a.scores + (((size_t)r * a.c.kv_heads + hk) * a.score_steps + step) * a.n_kept * kQBlock;
+}
+
+// Adds up the weights of slots / block tokens first, first + by .. of one (row, key/value head) from the kept scores; norm: [n_kept] (reference exponent, 1 / sum); seen: block tokens that the
+// counted queries' tile looked at (the others have weight 0)
+__device__ __forceinline__ void mass_of_kept(const QAttention& a, const QRow& w, int r, int hk, const float2* norm, int n_queries, int seen, int first, int by) {
+  const int steps = w.blocks + (a.block_mass ? (w.n + 31) / 32 : 0);
+  for (int i = first + (a.mass ? 0 : w.blocks * kQBlock); i < steps * kQBlock; i += by) {
+    const int step = i / kQBlock, at = i % kQBlock, slot = i, tok = i - w.blocks * kQBlock;
+    const bool cached = step < w.blocks;
+    if (cached ? slot >= w.len : tok >= w.n) continue;
+    const float* x = kept_scores(a, r, hk, step) + at;
+    float sum = 0.f;
+    for (int q = 0; q < n_queries && (cached || tok < seen); ++q) sum += __builtin_amdgcn_exp2f(x[q * kQBlock] - norm[q].x) * norm[q].y;
+    if (cached) a.mass[((size_t)r * a.c.kv_heads + hk) * a.capacity + slot] += sum;
+    else a.block_mass[((size_t)r * a.c.kv_heads + hk) * a.T + tok] = sum;
+  }
+}
+
 // grid (kv_heads * query tiles, splits, rows), 4 waves.  The steps of a split go to its waves in turn; the waves' results are joined through LDS.
 template <typename T, int DH, int NQB>
-__global__ __launch_bounds__(256) void k_qcache_attention(QAttention a, int q_tiles) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qcache_attention(QAttention a, int q_tiles) {
   using S = QShape<T, DH>;
   constexpr int KD = S::KD, DT = S::DT, NS = S::NS, NP = S::NP, NQ = 16 * NQB;
   __shared__ float s_o[2][NQ][DH + 4];
   __shared__ float s_m[4][NQ], s_l[4][NQ];
+  __shared__ float2 s_norm[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
   const int hk = blockIdx.x / q_tiles, q0 = (blockIdx.x % q_tiles) * NQ, r = blockIdx.z, split = blockIdx.y;
   const QRow w = row_of(a, r);
@@ -394,79 +593,127 @@ __global__ __launch_bounds__(256) void k_qcache_attention(QAttention a, int q_ti
     qt[qb] = qi / a.group;
 #pragma unroll
     for (int kd = 0; kd < KD; ++kd)
-      load_operand<NS>(q + (size_t)qt[qb] * a.q_stride + (size_t)(qi % a.group) * DH + kd * 32 + g * 8, true, qf[qb][kd]);
+      load_operand<NS>(q + (size_t)qt[qb] * a.q_stride + (size_t)(qi % a.group) * DH + kd * 32 + g * 8, qf[qb][kd]);
   }
-  float m_run[NQB], l_run[NQB];
-  floatx4 o[NQB][DT];
+  QRun<DT> run[NQB];
 #pragma unroll
-  for (int qb = 0; qb < NQB; ++qb) {
-    m_run[qb] = -INFINITY;
-    l_run[qb] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[qb][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
-  // block tokens that the tile's queries can see: with a chain none behind the last query
-  const int seen = !a.k ? 0 : a.causal ? min(w.n, (min(q0 + NQ, nq) - 1) / a.group + 1) : w.n;
+  for (int qb = 0; qb < NQB; ++qb) run[qb].clear();
+  // scores of the counted queries, the first ones, are kept by the tile that has them
+  const int n_kept = a.n_kept && q0 == 0 ? min(a.n_kept, nq) : 0;
+  auto keep_scores = [&](int step, const float (&sv)[8], float c) {
+    if (col < n_kept) {
+      float* p = kept_scores(a, r, hk, step) + col * kQBlock + 8 * g;
+      ((float4*)p)[0] = make_float4(sv[0] * c, sv[1] * c, sv[2] * c, sv[3] * c);
+      ((float4*)p)[1] = make_float4(sv[4] * c, sv[5] * c, sv[6] * c, sv[7] * c);
+    }
+  };
+  const int seen = seen_by(a, w, min(q0 + NQ, nq));
   const int steps = w.blocks + (seen + 31) / 32;
   const int s0 = (int)((int64_t)steps * split / a.splits), s1 = (int)((int64_t)steps * (split + 1) / a.splits);
-  for (int step = s0 + wave; step < s1; step += 4) {
-    float e[8];
-    if (step < w.blocks) {
-      const uint8_t* data = a.c.data + (region + step) * a.c.block_bytes();
-      const float2 sc = a.c.scale[region + step];
-      const int valid = w.len - step * kQBlock;
-      bf16x8 kf[2][KD][1], vf[DT][1];
-      keys_of_block<T, DH, 1>(data, sc.x, lane, kf);
-      values_of_block<DH>(data, sc.y, lane, valid, vf);
+  const int cached_end = min(s1, w.blocks);
+  const uint8_t* data = a.c.data + region * a.c.block_bytes();
+  QRaw<DH> raw;
+  int step = s0 + wave;
+  if (step < cached_end) raw.load(data + (size_t)step * a.c.block_bytes(), a.c.scale + region + step, lane);
+  for (; step < cached_end; step += 4) {
+    const int valid = w.len - step * kQBlock;
+    if (valid < kQBlock) raw.mask_values(lane, valid);
+    const float2 sc = raw.scale;
+    bf16x8 kf[2][KD][1];
+#pragma unroll
+    for (int c = 0; c < KD; ++c) {
+      kf[0][c][0] = e4m3_to_bf16(make_uint2(raw.k[c].x, raw.k[c].y), 1.f);
+      kf[1][c][0] = e4m3_to_bf16(make_uint2(raw.k[c].z, raw.k[c].w), 1.f);
+    }
+    const float c_exp = fmaxf(a.c_exp * sc.x, FLT_MIN);     // above 0: masked scores are -inf
+    const int ev = exponent_of(sc.y);
+    uint4 vraw[KD];
+#pragma unroll
+    for (int c = 0; c < KD; ++c) vraw[c] = raw.v[c];
+    // the wave's next block is on its way meanwhile
+    if (step + 4 < cached_end) raw.load(data + (size_t)(step + 4) * a.c.block_bytes(), a.c.scale + region + step + 4, lane);
+    auto masked = [&](float (&sv)[8]) {
+      if (valid < kQBlock) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sv[i] = 8 * g + i < valid ? sv[i] : -INFINITY;
+      }
+    };
+    if (S::F16 && ev <= 40 && ev >= -40) {
+      f16x8 vf[DT];
+#pragma unroll
+      for (int c = 0; c < KD; ++c) {
+        vf[2 * c] = e4m3_to_f16(make_uint2(vraw[c].x, vraw[c].y));
+        vf[2 * c + 1] = e4m3_to_f16(make_uint2(vraw[c].z, vraw[c].w));
+      }
+      const float per_unit = 1.f / sc.y;
 #pragma unroll
       for (int qb = 0; qb < NQB; ++qb) {
-        float sv[8];
+        float sv[8], e[8];
         step_scores<KD, 1, NS>(kf, qf[qb], sv);
-        if (valid < kQBlock) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) sv[i] = 8 * g + i < valid ? sv[i] : -INFINITY;
-        }
-        step_softmax<DT, 1, NP>(sv, vf, a.c_exp, m_run[qb], l_run[qb], o[qb], e);
+        masked(sv);
+        if (qb == 0 && n_kept) keep_scores(step, sv, c_exp);
+        run[qb].weights(sv, c_exp, (float)ev, per_unit, e);
+        run[qb].add_f16(e, vf);
       }
     } else {
-      const int tok0 = (step - w.blocks) * 32;
-      bf16x8 kf[2][KD][NS], vf[DT][NS];
-      keys_of_tokens<T, DH, NS>(k, a.kv_stride, tok0, seen, lane, kf);
-      const bool odd = __builtin_amdgcn_ballot_w64(values_of_tokens<T, DH, NS>(v, a.kv_stride, tok0, seen, lane, vf)) != 0;
+      bf16x8 vf[DT][1];
+#pragma unroll
+      for (int c = 0; c < KD; ++c) {
+        vf[2 * c][0] = e4m3_to_bf16(make_uint2(vraw[c].x, vraw[c].y), sc.y);
+        vf[2 * c + 1][0] = e4m3_to_bf16(make_uint2(vraw[c].z, vraw[c].w), sc.y);
+      }
 #pragma unroll
       for (int qb = 0; qb < NQB; ++qb) {
-        float sv[8];
-        step_scores<KD, NS, NS>(kf, qf[qb], sv);
-        const uint32_t vis = sees8(a, qt[qb], tok0 + 8 * g, seen);
+        float sv[8], e[8];
+        step_scores<KD, 1, NS>(kf, qf[qb], sv);
+        masked(sv);
+        if (qb == 0 && n_kept) keep_scores(step, sv, c_exp);
+        run[qb].weights(sv, c_exp, 0.f, 1.f, e);
+        run[qb].template add_bf16<1, NP>(e, vf);
+      }
+    }
+  }
+  for (; step < s1; step += 4) {
+    const int tok0 = (step - w.blocks) * 32;
+    bf16x8 kf[2][KD][NS], vf[DT][NS];
+    keys_of_tokens<T, DH, NS>(k, a.kv_stride, tok0, seen, lane, kf);
+    const bool odd = __builtin_amdgcn_ballot_w64(values_of_tokens<DH, NS>(v, a.kv_stride, tok0, seen, lane, vf)) != 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sv[i] = (vis >> i) & 1 ? sv[i] : -INFINITY;
-        step_softmax<DT, NS, NP>(sv, vf, a.c_exp, m_run[qb], l_run[qb], o[qb], e);
-        if (odd) {                            // values that are not finite: only for the queries that see them
-          for (int j = 0; j < 32 && tok0 + j < seen; ++j) {
-            float p = 0.f;
+    for (int qb = 0; qb < NQB; ++qb) {
+      float sv[8], e[8];
+      step_scores<KD, NS, NS>(kf, qf[qb], sv);
+      const uint32_t vis = sees8(a, qt[qb], tok0 + 8 * g, seen);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float x = __shfl(e[i], (j >> 3) * 16 + col, 64);
-              if ((j & 7) == i) p = x;
-            }
-            if (sees8(a, qt[qb], tok0 + j, seen) & 1) {
+      for (int i = 0; i < 8; ++i) sv[i] = (vis >> i) & 1 ? sv[i] : -INFINITY;
+      if (qb == 0 && n_kept) keep_scores(step, sv, a.c_exp);
+      run[qb].weights(sv, a.c_exp, 0.f, 1.f, e);
+      run[qb].template add_bf16<NS, NP>(e, vf);
+      if (odd) {                              // values that are not finite: only for the queries that see them
+        for (int j = 0; j < 32 && tok0 + j < seen; ++j) {
+          float p = 0.f;
 #pragma unroll
-              for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const float x = ld(v + (size_t)(tok0 + j) * a.kv_stride + dt * 16 + 4 * g + i);
-                  if (!finite(x)) o[qb][dt][i] += p * x;
-                }
-            }
+          for (int i = 0; i < 8; ++i) {
+            const float x = __shfl(e[i], (j >> 3) * 16 + col, 64);
+            p = (j & 7) == i ? x : p;
           }
+          const bool vis1 = sees8(a, qt[qb], tok0 + j, seen) & 1;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float x = ld(v + (size_t)(tok0 + j) * a.kv_stride + dt * 16 + 4 * g + i);
+              run[qb].o[dt][i] += vis1 && !finite(x) ? p * x : 0.f;
+            }
         }
       }
     }
   }
-  // join the four waves: common maximum, then sums in the order (0 + 2) + (1 + 3)
+  // join the four waves: common reference, then sums in the order (0 + 2) + (1 + 3)
 #pragma unroll
-  for (int qb = 0; qb < NQB; ++qb)
-    if (g == 0) { s_m[wave][qb * 16 + col] = m_run[qb]; s_l[wave][qb * 16 + col] = l_run[qb]; }
+  for (int qb = 0; qb < NQB; ++qb) {
+    run[qb].l = rows_sum(run[qb].l);
+    if (g == 0) { s_m[wave][qb * 16 + col] = run[qb].m; s_l[wave][qb * 16 + col] = run[qb].l; }
+  }
   __syncthreads();
   float l_all[NQB], m_all[NQB];
 #pragma unroll
@@ -477,12 +724,15 @@ __global__ __launch_bounds__(256) void k_qcache_attention(QAttention a, int q_ti
     if (m == -INFINITY) m = 0.f;
     l_all[qb] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) l_all[qb] += s_l[i][qi] * __builtin_amdgcn_exp2f(s_m[i][qi] - m);
-    const float f = __builtin_amdgcn_exp2f(m_run[qb] - m);
+    for (int i = 0; i < 4; ++i) {
+      const float f = s_m[i][qi] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_m[i][qi] - m);      // (without a maximum: nothing, or NaN)
+      l_all[qb] += s_l[i][qi] * f;
+    }
+    const float f = run[qb].m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run[qb].m - m);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[qb][dt][i] *= f;
+      for (int i = 0; i < 4; ++i) run[qb].o[dt][i] *= f;
   }
 #pragma unroll
   for (int round = 0; round < 2; ++round) {
@@ -492,81 +742,104 @@ __global__ __launch_bounds__(256) void k_qcache_attention(QAttention a, int q_ti
 #pragma unroll
       for (int qb = 0; qb < NQB; ++qb)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) *(floatx4*)&s_o[wave & 1][qb * 16 + col][dt * 16 + 4 * g] = o[qb][dt];
+        for (int dt = 0; dt < DT; ++dt) *(floatx4*)&s_o[wave & 1][qb * 16 + col][dt * 16 + 4 * g] = run[qb].o[dt];
     }
     __syncthreads();
     if (takes) {
 #pragma unroll
       for (int qb = 0; qb < NQB; ++qb)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[qb][dt] += *(const floatx4*)&s_o[round ? 1 : wave][qb * 16 + col][dt * 16 + 4 * g];
+        for (int dt = 0; dt < DT; ++dt) run[qb].o[dt] += *(const floatx4*)&s_o[round ? 1 : wave][qb * 16 + col][dt * 16 + 4 * g];
     }
   }
-  if (wave) return;
+  if (wave == 0) {
 #pragma unroll
-  for (int qb = 0; qb < NQB; ++qb) {
-    const int qi = q0 + qb * 16 + col;
-    if (qi >= nq) continue;
-    if (a.splits > 1) {
-      float* part = a.parts + ((((size_t)r * gridDim.x + blockIdx.x) * a.splits + split) * NQ + qb * 16 + col) * (DH + 2);
+    for (int qb = 0; qb < NQB; ++qb) {
+      const int qi = q0 + qb * 16 + col;
+      if (qi >= nq) continue;
+      if (a.splits > 1) {
+        float* part = a.parts + ((((size_t)r * gridDim.x + blockIdx.x) * a.splits + split) * NQ + qb * 16 + col) * (DH + 2);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int i = 0; i < 4; i += 2) *(float2*)(part + dt * 16 + 4 * g + i) = make_float2(o[qb][dt][i], o[qb][dt][i + 1]);
-      if (g == 0) *(float2*)(part + DH) = make_float2(m_all[qb], l_all[qb]);
-      continue;
+          for (int i = 0; i < 4; i += 2) *(float2*)(part + dt * 16 + 4 * g + i) = make_float2(run[qb].o[dt][i], run[qb].o[dt][i + 1]);
+        if (g == 0) *(float2*)(part + DH) = make_float2(m_all[qb], l_all[qb]);
+        continue;
+      }
+      const size_t at = query_at(a, r, hk, qi);
+      const float inv = l_all[qb] == 0.f ? 0.f : 1.f / l_all[qb];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = run[qb].o[dt][i] * inv;
+        store4<T, DH>(a, at, dt * 16 + 4 * g, x);
+      }
+      if (g == 0) {
+        tell_norm(a, at, m_all[qb], l_all[qb]);
+        if (qb == 0) s_norm[col] = make_float2(m_all[qb] == -INFINITY ? 0.f : m_all[qb], inv);
+      }
     }
-    const size_t at = query_at(a, r, hk, qi);
-    const bool none = m_all[qb] == -INFINITY;
-    const float inv = none ? 0.f : 1.f / l_all[qb];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      float x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = o[qb][dt][i] * inv;
-      store4<T, DH>(a, at, dt * 16 + 4 * g, x);
-    }
-    if (g == 0) tell_norm(a, at, m_all[qb], l_all[qb]);
   }
+  if (a.splits > 1 || !a.n_kept || q0) return;
+  // the only split: the counted weights are added up here
+  __syncthreads();
+  mass_of_kept(a, w, r, hk, s_norm, n_kept, seen, threadIdx.x, 256);
 }
 
-// Joins the splits: one group of DH / 4 lanes per query
+// Joins the splits: one group of DH / 4 lanes per query.  Workgroups of blockIdx.y >= joins add up the counted weights instead.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, int nq_tile) {
+__global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, int nq_tile, int joins) {
   constexpr int LQ = DH / 4;
-  const int hk = blockIdx.x / q_tiles, tile = blockIdx.x % q_tiles, r = blockIdx.z;
-  const int in_tile = blockIdx.y * (256 / LQ) + threadIdx.x / LQ, dim = threadIdx.x % LQ * 4;
+  const int r = blockIdx.z;
   const QRow w = row_of(a, r);
+  const size_t step = (size_t)nq_tile * (DH + 2);
+  if ((int)blockIdx.y >= joins) {
+    const int hk = blockIdx.x / q_tiles;
+    if (blockIdx.x % q_tiles) return;
+    __shared__ float2 s_norm[16];
+    const int n_kept = min(a.n_kept, w.n * a.group);
+    if ((int)threadIdx.x < n_kept) {
+      const float* part = a.parts + (((size_t)r * gridDim.x + blockIdx.x) * a.splits * nq_tile + threadIdx.x) * (DH + 2) + DH;
+      float m = -INFINITY, l = 0.f;
+      for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * step]);
+      for (int s = 0; s < a.splits; ++s) l += part[s * step + 1] * (part[s * step] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(part[s * step] - m));
+      s_norm[threadIdx.x] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
+    }
+    __syncthreads();
+    mass_of_kept(a, w, r, hk, s_norm, n_kept, seen_by(a, w, min(nq_tile, w.n * a.group)), (blockIdx.y - joins) * 256 + threadIdx.x, (gridDim.y - joins) * 256);
+    return;
+  }
+  const int hk = blockIdx.x / q_tiles, tile = blockIdx.x % q_tiles;
+  const int in_tile = blockIdx.y * (256 / LQ) + threadIdx.x / LQ, dim = threadIdx.x % LQ * 4;
   const int qi = tile * nq_tile + in_tile;
   if (in_tile >= nq_tile || qi >= w.n * a.group) return;
   const float* part = a.parts + (((size_t)r * gridDim.x + blockIdx.x) * a.splits * nq_tile + in_tile) * (DH + 2);
-  const size_t step = (size_t)nq_tile * (DH + 2);
   float m = -INFINITY;
   for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * step + DH]);
-  const bool none = m == -INFINITY;
   float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits && !none; ++s) {
-    const float f = __builtin_amdgcn_exp2f(part[s * step + DH] - m);
+  for (int s = 0; s < a.splits; ++s) {
+    const float ms = part[s * step + DH], f = ms == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ms - m);
     l += part[s * step + DH + 1] * f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] += part[s * step + dim + i] * f;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = none ? 0.f : x[i] / l;
+  for (int i = 0; i < 4; ++i) x[i] = l == 0.f ? 0.f : x[i] / l;
   const size_t at = query_at(a, r, hk, qi);
   store4<T, DH>(a, at, dim, x);
   if (dim == 0) tell_norm(a, at, m, l);
 }
 
-// Counted weights: the scores are made again, now with the normaliser known.  One wave per 32 keys, over all counted queries in order.
+// Counted weights of many queries: the scores are made again, now with the normaliser known.  One wave per 32 keys, over all counted queries in order.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_qcache_mass(QAttention a) {
+__global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
   using S = QShape<T, DH>;
   constexpr int KD = S::KD, NS = S::NS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
   const int hk = blockIdx.y, r = blockIdx.z;
   const QRow w = row_of(a, r);
-  const int seen = a.k ? w.n : 0, steps = w.blocks + (a.block_mass ? (a.T + 31) / 32 : 0), nq = min(a.n_counted, w.n) * a.group;
+  const int seen = a.k ? w.n : 0, steps = w.blocks + (a.block_mass ? (w.n + 31) / 32 : 0), nq = min(a.n_counted, w.n) * a.group;
   const T* q = (const T*)a.q + (size_t)r * a.T * a.q_stride + (size_t)hk * a.group * DH;
   const T* k = (const T*)a.k + (size_t)r * a.T * a.kv_stride + (size_t)hk * DH;
   const size_t region = a.c.region(a.layer, r, hk) * a.c.blocks;
@@ -576,25 +849,25 @@ __global__ __launch_bounds__(256) void k_qcache_mass(QAttention a) {
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     bf16x8 kf[2][KD][NS];
     if (cached) {
-      bf16x8 one[2][KD][1];
-      keys_of_block<T, DH, 1>(a.c.data + (region + step) * a.c.block_bytes(), a.c.scale[region + step].x, lane, one);
+      const uint8_t* data = a.c.data + (region + step) * a.c.block_bytes();
+      const float unit_of = a.c.scale[region + step].x;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int kd = 0; kd < KD; ++kd) {
+        const uint4 b = *(const uint4*)(data + (kd * 64 + lane) * 16);
+        kf[0][kd][0] = e4m3_to_bf16(make_uint2(b.x, b.y), unit_of);
+        kf[1][kd][0] = e4m3_to_bf16(make_uint2(b.z, b.w), unit_of);
 #pragma unroll
-        for (int kd = 0; kd < KD; ++kd) {
-          kf[t][kd][0] = one[t][kd][0];
-#pragma unroll
-          for (int p = 1; p < NS; ++p) kf[t][kd][p] = as_bf16x8(make_uint4(0, 0, 0, 0));
-        }
-    } else if (valid > 0) {
+        for (int p = 1; p < NS; ++p) kf[0][kd][p] = kf[1][kd][p] = as_bf16x8(make_uint4(0, 0, 0, 0));
+      }
+    } else {
       keys_of_tokens<T, DH, NS>(k, a.kv_stride, tok0, seen, lane, kf);
     }
     // (of a chain only the queries from the step's first token on see anything)
-    for (int q0 = !cached && a.causal ? tok0 * a.group / 16 * 16 : 0; q0 < nq && valid > 0; q0 += 16) {
+    for (int q0 = !cached && a.causal ? tok0 * a.group / 16 * 16 : 0; q0 < nq; q0 += 16) {
       const int qi = min(q0 + col, nq - 1), t = qi / a.group;
       bf16x8 qf[KD][NS];
 #pragma unroll
-      for (int kd = 0; kd < KD; ++kd) load_operand<NS>(q + (size_t)t * a.q_stride + (size_t)(qi % a.group) * DH + kd * 32 + g * 8, true, qf[kd]);
+      for (int kd = 0; kd < KD; ++kd) load_operand<NS>(q + (size_t)t * a.q_stride + (size_t)(qi % a.group) * DH + kd * 32 + g * 8, qf[kd]);
       const float2 norm = a.norm[query_at(a, r, hk, qi)];
       float sv[8];
       step_scores<KD, NS, NS>(kf, qf, sv);
@@ -633,16 +906,21 @@ template <typename T, int DH, int NQB>
 static void attention_t(QAttention a, hipStream_t s) {
   const int q_tiles = (a.T * a.group + 16 * NQB - 1) / (16 * NQB);
   const int64_t tiles = (int64_t)a.c.rows * a.c.kv_heads * q_tiles;
-  // As many splits as give each CU about four workgroups, with at least four steps each where the cache is full; the partial results have room for kQParts
+  // As many splits as give each CU about four workgroups, but at least four steps to each of a split's waves where the cache is full; the partial results have room for kQParts
   const int64_t most = (int64_t)kQParts / (tiles * NQB);
-  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / tiles, most, (a.c.blocks + 3) / 4}));
+  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / tiles, most, a.c.blocks / 16}));
+  // Few counted queries: their scores are kept, 4 bytes per query and slot written and read, where reading the keys again is DH bytes per slot (and many times the work)
+  const int counted = a.n_counted * a.group;
+  a.n_kept = (counted || a.block_mass) && counted <= std::min(kQKept, DH / 16) ? counted : 0;
+  if (a.n_kept) a.norm = nullptr;
   const dim3 grid(a.c.kv_heads * q_tiles, a.splits, a.c.rows);
   hipLaunchKernelGGL((k_qcache_attention<T, DH, NQB>), grid, dim3(256), 0, s, a, q_tiles);
   if (a.splits > 1) {
-    const int per = 256 / (DH / 4);
-    hipLaunchKernelGGL((k_qcache_join<T, DH>), dim3(grid.x, (16 * NQB + per - 1) / per, grid.z), dim3(256), 0, s, a, q_tiles, 16 * NQB);
+    const int per = 256 / (DH / 4), joins = (16 * NQB + per - 1) / per;
+    const int masses = a.n_kept ? std::max(1, std::min(a.c.blocks / 32, 64)) : 0;
+    hipLaunchKernelGGL((k_qcache_join<T, DH>), dim3(grid.x, joins + masses, grid.z), dim3(256), 0, s, a, q_tiles, 16 * NQB, joins);
   }
-  if (a.n_counted > 0 || a.block_mass) {
+  if (!a.n_kept && (a.n_counted > 0 || a.block_mass)) {
     const int steps = a.c.blocks + (a.T + 31) / 32;
     hipLaunchKernelGGL((k_qcache_mass<T, DH>), dim3(std::min((steps + 3) / 4, 1024), a.c.kv_heads, a.c.rows), dim3(256), 0, s, a);
   }
@@ -674,8 +952,8 @@ void launch_qcache_attention(const QAttention& a, int dtype, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------------------------------------ eviction
-// Which slots stay: one workgroup per (layer, row, head) finds the keep-th largest weight by its bits, 8 at a time, then deals the kept slots behind `keep` to the
-// holes in front of it, in order.  Order-preserving bits: a weight's sign bit is flipped, or all its bits when it is set; -0 counts as 0, NaN as the largest.
+// Which slots stay: per (layer, row, head) the keep-th largest weight is found by its bits, then the kept slots behind `keep` are dealt to the holes in front of it, in order.
+// Order-preserving bits: a weight's sign bit is flipped, or all its bits when it is set; -0 counts as 0, NaN as the largest number, the newest tokens lie above all.
 constexpr int kQSelect = 1024;
 
 __device__ __forceinline__ uint32_t mass_bits(float m) {
@@ -684,7 +962,148 @@ __device__ __forceinline__ uint32_t mass_bits(float m) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// exclusive prefix over the workgroup; *total: the sum.  red: kQSelect / 64 + 1 ints
+struct QSelect {           // one (layer, row, head)
+  int len, left;
+  const float* mass;
+  float* mass_out;
+  const int32_t* pos;
+  int32_t *pos_out, *origin;
+};
+__device__ __forceinline__ QSelect select_of(const QEvict& a, int head, int r, int layer) {
+  const size_t base = (((size_t)layer * a.c.rows + r) * a.c.kv_heads + head) * a.capacity;
+  const int len = row_len(a.len, r, a.capacity);
+  return QSelect{len, min(len, a.keep), a.mass + base, a.mass_out + base, a.pos ? a.pos + base : nullptr, a.pos ? a.pos_out + base : nullptr, a.origin + base};
+}
+// Slot i of the new row comes from slot `from`
+__device__ __forceinline__ void settle(const QSelect& h, int i, int from) {
+  h.origin[i] = from;
+  h.mass_out[i] = h.mass[from];
+  if (h.pos) h.pos_out[i] = h.pos[from];
+}
+__device__ __forceinline__ void clear_behind(const QSelect& h, int capacity, int tid, int threads) {
+  for (int i = h.left + tid; i < capacity; i += threads) {
+    h.mass_out[i] = 0.f;
+    if (h.pos) h.pos_out[i] = 0;
+  }
+}
+
+// Rows of up to 64 * WAVES * KPT slots: every lane holds the keys of KPT slots (a wave's slots lie together), 32 rounds of counting find the threshold.
+// A workgroup of one wave needs no barrier.  Bound by the rounds (KPT comparisons each), not by the 8 bytes per slot: 36 x 16 x 20 rows of 696 slots take 57 us,
+// 16 x 8 rows of 32768 88.  (Digits of 8 bits counted in LDS: 1521 and 208 us - most weights share a few exponents, so that the counters collide.)
+template <int WAVES, int KPT>
+__global__ __launch_bounds__(64 * WAVES) void k_qcache_select(QEvict a) {
+  constexpr int THREADS = 64 * WAVES;
+  __shared__ uint16_t s_list[THREADS * KPT / 2];
+  __shared__ int s_count[2][WAVES], s_equal[WAVES], s_hole[WAVES], s_source[WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const QSelect h = select_of(a, blockIdx.x, blockIdx.y, blockIdx.z);
+  if (h.len <= a.keep) {
+    for (int i = tid; i < h.left; i += THREADS) settle(h, i, i);
+    clear_behind(h, a.capacity, tid, THREADS);
+    return;
+  }
+  const int slot0 = wave * 64 * KPT + lane;
+  uint32_t key[KPT];
+  int newest = h.pos ? INT_MIN : h.len - 1;
+  if (h.pos) {
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+      const int i = slot0 + j * 64;
+      key[j] = i < h.len ? (uint32_t)h.pos[i] : 0x80000000u;
+      newest = max(newest, (int)key[j]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) newest = max(newest, __shfl_xor(newest, o, 64));
+    if (WAVES > 1) {
+      if (lane == 0) s_equal[wave] = newest;
+      __syncthreads();
+      for (int w = 0; w < WAVES; ++w) newest = max(newest, s_equal[w]);
+      __syncthreads();
+    }
+  }
+  const int64_t above = (int64_t)newest - a.recent;
+#pragma unroll
+  for (int j = 0; j < KPT; ++j) {
+    const int i = slot0 + j * 64;
+    const bool recent = (h.pos ? (int)key[j] : i) > above;
+    key[j] = i >= h.len ? 0u : recent ? 0xFFFFFFFFu : mass_bits(h.mass[i]);       // (a slot that is filled has a key above 0: no float is all ones but a NaN)
+  }
+  // largest bound that `keep` keys reach
+  uint32_t bound = 0;
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t cand = bound | 1u << b;
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) n += __popcll(__builtin_amdgcn_ballot_w64(key[j] >= cand));
+    if (WAVES > 1) {
+      if (lane == 0) s_count[b & 1][wave] = n;
+      __syncthreads();
+      n = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) n += s_count[b & 1][w];
+    }
+    if (n >= a.keep) bound = cand;
+    if (n == a.keep) break;
+  }
+  // kept: keys above the bound, and as many equal ones, from the lowest slot on, as there is room for
+  int n_above = 0, n_equal = 0;
+#pragma unroll
+  for (int j = 0; j < KPT; ++j) {
+    n_above += __popcll(__builtin_amdgcn_ballot_w64(key[j] > bound));
+    n_equal += __popcll(__builtin_amdgcn_ballot_w64(key[j] == bound && slot0 + j * 64 < h.len));
+  }
+  int equal_before = 0;
+  if (WAVES > 1) {
+    if (lane == 0) { s_equal[wave] = n_equal; s_hole[wave] = n_above; }
+    __syncthreads();
+    n_above = 0;
+    for (int w = 0; w < WAVES; ++w) { n_above += s_hole[w]; equal_before += w < wave ? s_equal[w] : 0; }
+    __syncthreads();
+  }
+  const int room = a.keep - n_above;
+  const uint64_t below = (1ull << lane) - 1;
+  uint32_t kept = 0;
+  int n_hole = 0, n_source = 0;
+#pragma unroll
+  for (int j = 0; j < KPT; ++j) {
+    const int i = slot0 + j * 64;
+    const bool equal = key[j] == bound && i < h.len;
+    const uint64_t eq = __builtin_amdgcn_ballot_w64(equal);
+    const bool k = key[j] > bound || (equal && equal_before + __popcll(eq & below) < room);
+    equal_before += __popcll(eq);
+    kept |= (uint32_t)k << j;
+    n_hole += __popcll(__builtin_amdgcn_ballot_w64(!k && i < a.keep));
+    n_source += __popcll(__builtin_amdgcn_ballot_w64(k && i >= a.keep));
+  }
+  int hole = 0, source = 0;
+  if (WAVES > 1) {
+    if (lane == 0) { s_hole[wave] = n_hole; s_source[wave] = n_source; }
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) { hole += s_hole[w]; source += s_source[w]; }
+  }
+#pragma unroll
+  for (int j = 0; j < KPT; ++j) {                // the sources, in order
+    const int i = slot0 + j * 64;
+    const bool s = (kept >> j & 1) && i >= a.keep;
+    const uint64_t b = __builtin_amdgcn_ballot_w64(s);
+    if (s) s_list[source + __popcll(b & below)] = (uint16_t)i;
+    source += __popcll(b);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < KPT; ++j) {                // the n-th hole takes the n-th source
+    const int i = slot0 + j * 64;
+    const bool o = !(kept >> j & 1) && i < a.keep;
+    const uint64_t b = __builtin_amdgcn_ballot_w64(o);
+    if (i < a.keep) settle(h, i, o ? s_list[hole + __popcll(b & below)] : i);
+    hole += __popcll(b);
+  }
+  __syncthreads();                               // the sources' weights have been read
+  clear_behind(h, a.capacity, tid, THREADS);
+}
+
+// Longer rows: the keys are read again for each digit of 8 bits, counted in LDS, and for the dealing.
+// exclusive prefix over the workgroup; *total: the sum.  red: kQSelect / 64 ints
 __device__ __forceinline__ int block_rank(bool mine, int* red, int* total) {
   const uint64_t b = __builtin_amdgcn_ballot_w64(mine);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -701,139 +1120,142 @@ __device__ __forceinline__ int block_rank(bool mine, int* red, int* total) {
   return before + __popcll(b & ((1ull << lane) - 1));
 }
 
-__global__ __launch_bounds__(kQSelect) void k_qcache_select(QEvict a) {
-  __shared__ int s_hist[256], s_red[kQSelect / 64 + 1], s_pick[2];
-  const int head = blockIdx.x, r = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x;
-  const size_t region = ((size_t)layer * a.c.rows + r) * a.c.kv_heads + head, base = region * a.capacity;
-  const int len = row_len(a.len, r, a.capacity), left = min(len, a.keep);
-  const float* mass = a.mass + base;
-  float* mass_out = a.mass_out + base;
-  const int32_t* pos = a.pos ? a.pos + base : nullptr;
-  int32_t* pos_out = a.pos ? a.pos_out + base : nullptr;
-  int32_t* origin = a.origin + base;
-  if (len <= a.keep) {
-    for (int i = tid; i < a.capacity; i += kQSelect) {
-      if (i < left) origin[i] = i;
-      mass_out[i] = i < left ? mass[i] : 0.f;
-      if (pos) pos_out[i] = i < left ? pos[i] : 0;
-    }
+__global__ __launch_bounds__(kQSelect) void k_qcache_select_long(QEvict a) {
+  __shared__ int s_hist[256], s_red[kQSelect / 64], s_pick[2];
+  const int tid = threadIdx.x;
+  const QSelect h = select_of(a, blockIdx.x, blockIdx.y, blockIdx.z);
+  if (h.len <= a.keep) {
+    for (int i = tid; i < h.left; i += kQSelect) settle(h, i, i);
+    clear_behind(h, a.capacity, tid, kQSelect);
     return;
   }
-  int newest = len - 1;
-  if (pos) {
-    newest = pos[0];
-    for (int i = tid; i < len; i += kQSelect) newest = max(newest, pos[i]);
+  int newest = h.len - 1;
+  if (h.pos) {
+    newest = INT_MIN;
+    for (int i = tid; i < h.len; i += kQSelect) newest = max(newest, h.pos[i]);
     newest = block_max_int(newest, s_red);
   }
   auto key = [&](int i) {
-    const int64_t p = pos ? pos[i] : i;
-    return p > (int64_t)newest - a.recent ? 0xFFFFFFFFu : mass_bits(mass[i]);
+    const int64_t p = h.pos ? h.pos[i] : i;
+    return p > (int64_t)newest - a.recent ? 0xFFFFFFFFu : mass_bits(h.mass[i]);
   };
   uint32_t prefix = 0;
-  int need = a.keep;                       // of the keys that share the prefix, how many are kept
+  int room = a.keep;                       // of the keys that share the prefix, how many are kept
   for (int shift = 24; shift >= 0; shift -= 8) {
     __syncthreads();
     if (tid < 256) s_hist[tid] = 0;
     __syncthreads();
-    for (int i = tid; i < len; i += kQSelect) {
+    for (int i = tid; i < h.len; i += kQSelect) {
       const uint32_t k = key(i);
       if (shift == 24 || k >> (shift + 8) == prefix) atomicAdd(&s_hist[(k >> shift) & 255], 1);   // whole numbers: in any order the same
     }
     __syncthreads();
     if (tid == 0) {
       int b = 255, above = 0;
-      while (above + s_hist[b] < need) above += s_hist[b--];
+      while (above + s_hist[b] < room) above += s_hist[b--];
       s_pick[0] = b;
-      s_pick[1] = need - above;
+      s_pick[1] = room - above;
     }
     __syncthreads();
     prefix = prefix << 8 | (uint32_t)s_pick[0];
-    need = s_pick[1];
+    room = s_pick[1];
   }
-  // kept: keys above the prefix, and the first `need` equal to it
   int equal = 0, holes = 0, sources = 0;
-  for (int i0 = 0; i0 < len; i0 += kQSelect) {
+  for (int i0 = 0; i0 < h.len; i0 += kQSelect) {
     const int i = i0 + tid;
-    const uint32_t k = i < len ? key(i) : 0;
+    const uint32_t k = i < h.len ? key(i) : 0;
     int total;
-    const bool eq = i < len && k == prefix;
+    const bool eq = i < h.len && k == prefix;
     const int rank = equal + block_rank(eq, s_red, &total);
     equal += total;
-    const bool kept = i < len && (k > prefix || (eq && rank < need));
+    const bool kept = i < h.len && (k > prefix || (eq && rank < room));
     const bool hole = i < a.keep && !kept, source = i >= a.keep && kept;
-    const int h = holes + block_rank(hole, s_red, &total);
+    const int o = holes + block_rank(hole, s_red, &total);
     holes += total;
     const int q = sources + block_rank(source, s_red, &total);
     sources += total;
     // a hole notes its number; the sources, as many as there are holes, are listed behind `keep`
-    if (i < a.keep) origin[i] = kept ? i : -1 - h;
-    if (source) origin[a.keep + q] = i;
+    if (i < a.keep) h.origin[i] = kept ? i : -1 - o;
+    if (source) h.origin[a.keep + q] = i;
   }
   __syncthreads();
   for (int i = tid; i < a.keep; i += kQSelect) {
-    const int o = origin[i];
-    const int from = o >= 0 ? i : origin[a.keep + (-1 - o)];
-    origin[i] = from;
-    const float m = mass[from];
-    mass_out[i] = m;
-    if (pos) pos_out[i] = pos[from];
+    const int o = h.origin[i];
+    settle(h, i, o >= 0 ? i : h.origin[a.keep + (-1 - o)]);
   }
   __syncthreads();
-  for (int i = a.keep + tid; i < a.capacity; i += kQSelect) {
-    mass_out[i] = 0.f;
-    if (pos) pos_out[i] = 0;
-  }
+  clear_behind(h, a.capacity, tid, kQSelect);
 }
 
-// Moves the elements: one wave per (layer, row, head, block below keep)
+// Moves the elements: one wave per (layer, row, head, block below keep).  A slot's dims are 8 bytes in a row among the keys, and single bytes 16 apart among the values
+// (there the 8 bytes in a row are 8 slots of a dim): gathered by the lane that holds the slot, turned, stored as 16 bytes.
+template <int DH>
 __global__ __launch_bounds__(256) void k_qcache_move(QEvict a) {
   const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6), r = blockIdx.y, layer = blockIdx.z;
   const int blocks = a.keep / kQBlock, head = unit / blocks, block = unit % blocks;
   if (head >= a.c.kv_heads) return;
   if (row_len(a.len, r, a.capacity) <= a.keep) return;
-  const int dh = a.c.dh;
   const size_t base = (((size_t)layer * a.c.rows + r) * a.c.kv_heads + head) * a.capacity, region = a.c.region(a.layer + layer, r, head) * a.c.blocks;
-  const int from = a.origin[base + block * kQBlock + (lane & 31)];
-  if (!__builtin_amdgcn_ballot_w64(from != block * kQBlock + (lane & 31))) return;
-  const float2 sc = a.c.scale[region + (from >> 5)];
-  const int ek = exponent_of(sc.x), ev = exponent_of(sc.y);
-  int tk = ek, tv = ev;
+  const int g = lane >> 4, i = lane & 15, slot0 = block * kQBlock;
+  const int w[3] = {slot_of(0, i), slot_of(1, i), value_slot(lane)};        // this lane's slots: keys of both tiles, values
+  int from[3];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { tk = max(tk, __shfl_xor(tk, o, 64)); tv = max(tv, __shfl_xor(tv, o, 64)); }
-  uint8_t* data = a.c.data + (region + block) * a.c.block_bytes();
-  const int g = lane >> 4, i = lane & 15;
+  for (int n = 0; n < 3; ++n) from[n] = a.origin[base + slot0 + w[n]];
+  if (!__builtin_amdgcn_ballot_w64(from[2] != slot0 + w[2])) return;        // (value slots cover the block)
+  const float least = ldexpf(1.f, kQLeast);
+  float unit_of[3];
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    uint8_t* out = data + half * kQBlock * dh;
-    for (int c = 0; c < dh / 32; ++c) {
-      uint2* at = (uint2*)(out + (c * 64 + lane) * 16);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        float v[8];
-        if (half == 0) {
-          const int w = slot_of(t, i), src = __shfl(from, w, 64), e = __shfl(ek, w, 64);
-          from_e4m3x8(*(const uint2*)(a.c.data + (region + (src >> 5)) * a.c.block_bytes() + key_byte(src & 31, c * 32 + 8 * g)), v);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = ldexpf(v[j], e - tk);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int w = 8 * g + j, src = __shfl(from, w, 64), e = __shfl(ev, w, 64);
-            const uint8_t b = a.c.data[(region + (src >> 5)) * a.c.block_bytes() + kQBlock * dh + value_byte(src & 31, c * 32 + t * 16 + i)];
-            v[j] = ldexpf(e4m3_at<0>(b), e - tv);
-          }
-        }
-        at[t] = to_e4m3x8(v);
-      }
-    }
+  for (int n = 0; n < 3; ++n) {
+    const float2 sc = a.c.scale[region + (from[n] >> 5)];
+    unit_of[n] = fmaxf(n < 2 ? sc.x : sc.y, least);
   }
-  if (lane == 0) a.c.scale[region + block] = make_float2(ldexpf(1.f, tk), ldexpf(1.f, tv));
+  const float tk = wave_max(fmaxf(unit_of[0], unit_of[1])), tv = wave_max(unit_of[2]);
+  const bool again[2] = {__builtin_amdgcn_ballot_w64(unit_of[0] != tk || unit_of[1] != tk) != 0, __builtin_amdgcn_ballot_w64(unit_of[2] != tv) != 0};
+  uint8_t* data = a.c.data + (region + block) * a.c.block_bytes();
+  const uint8_t* src[3];
+#pragma unroll
+  for (int n = 0; n < 3; ++n) src[n] = a.c.data + (region + (from[n] >> 5)) * a.c.block_bytes();
+  auto rounded = [&](uint2 b, float ratio) {      // to the block's larger power of two
+    float v[8];
+    from_e4m3x8(b, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= ratio;
+    return to_e4m3x8(v);
+  };
+#pragma unroll
+  for (int c = 0; c < DH / 32; ++c) {
+    uint4 k;
+    const uint2 k0 = *(const uint2*)(src[0] + key_byte(from[0] & 31, c * 32 + 8 * g)), k1 = *(const uint2*)(src[1] + key_byte(from[1] & 31, c * 32 + 8 * g));
+    const uint2 r0 = again[0] ? rounded(k0, unit_of[0] / tk) : k0, r1 = again[0] ? rounded(k1, unit_of[1] / tk) : k1;
+    k = make_uint4(r0.x, r0.y, r1.x, r1.y);
+    uint2 v[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint8_t* b = src[2] + kQBlock * DH + value_byte(from[2] & 31, c * 32 + t * 16 + (i & 8));
+      uint32_t e[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[j] = b[j * 16];
+      v[t] = make_uint2(e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24, e[4] | e[5] << 8 | e[6] << 16 | e[7] << 24);
+      if (again[1]) v[t] = rounded(v[t], unit_of[2] / tv);
+      v[t] = transpose_bytes(v[t], lane);
+    }
+    *(uint4*)(data + (c * 64 + lane) * 16) = k;
+    *(uint4*)(data + kQBlock * DH + (c * 64 + lane) * 16) = make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+  }
+  if (lane == 0) a.c.scale[region + block] = make_float2(tk, tv);
 }
 
 void launch_qcache_evict(const QEvict& a, hipStream_t s) {
-  hipLaunchKernelGGL(k_qcache_select, dim3(a.c.kv_heads, a.c.rows, a.n_layers), dim3(kQSelect), 0, s, a);
+  const dim3 heads(a.c.kv_heads, a.c.rows, a.n_layers);
+  if (a.capacity <= 1024) hipLaunchKernelGGL((k_qcache_select<1, 16>), heads, dim3(64), 0, s, a);
+  else if (a.capacity <= 8192) hipLaunchKernelGGL((k_qcache_select<4, 32>), heads, dim3(256), 0, s, a);
+  else if (a.capacity <= 32768) hipLaunchKernelGGL((k_qcache_select<16, 32>), heads, dim3(1024), 0, s, a);
+  else hipLaunchKernelGGL(k_qcache_select_long, heads, dim3(kQSelect), 0, s, a);
   if (a.keep >= a.capacity) return;
-  hipLaunchKernelGGL(k_qcache_move, dim3(((int64_t)a.c.kv_heads * (a.keep / kQBlock) + 3) / 4, a.c.rows, a.n_layers), dim3(256), 0, s, a);
+  const dim3 grid(((int64_t)a.c.kv_heads * (a.keep / kQBlock) + 3) / 4, a.c.rows, a.n_layers);
+  if (a.c.dh == 32) hipLaunchKernelGGL(k_qcache_move<32>, grid, dim3(256), 0, s, a);
+  else if (a.c.dh == 64) hipLaunchKernelGGL(k_qcache_move<64>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_qcache_move<128>, grid, dim3(256), 0, s, a);
 }
 
 }  // namespace vvs

@@ -1,6 +1,7 @@
 // Host side of the 8-bit key/value cache and of the rotary operator: argument checks, buffer sizes, entry points.
 #include "vvs_qcache.h"
 
+#include <float.h>
 #include <math.h>
 #include <string.h>
 #include <algorithm>
@@ -11,7 +12,8 @@ namespace vvs {
 struct QCache {
   vvs_qcache_config cfg;
   QLayout lay;
-  size_t cache_bytes, ws_bytes, parts_off, norm_off, origin_off;
+  size_t cache_bytes, ws_bytes, parts_off, norm_off, origin_off, scores_off;
+  int score_steps;
   int dev, cus;
   char* ws;
   std::string err;
@@ -48,13 +50,16 @@ static vvs_status plan_qcache(const vvs_qcache_config* cfg, QCache* c) {
   const size_t regions = (size_t)g.n_layers * g.n_rows * g.n_kv_heads, blocks = regions * c->lay.blocks;
   if (blocks > ((size_t)1 << 31) - 1) return no(nullptr, VVS_ESIZE, "qcache config: 2^31 blocks or more");
   c->cache_bytes = align_up(blocks * c->lay.block_bytes(), 256) + align_up(blocks * sizeof(float2), 256);
-  size_t off = kQTicket;
+  size_t off = 0;
   c->parts_off = off;
   off = align_up(off + (size_t)kQParts * 16 * (g.head_size + 2) * sizeof(float), 256);
   c->norm_off = off;
   off = align_up(off + (size_t)g.n_rows * g.max_tokens * g.n_heads * sizeof(float2), 256);
   c->origin_off = off;
   off = align_up(off + regions * g.capacity * sizeof(int32_t), 256);
+  c->scores_off = off;
+  c->score_steps = c->lay.blocks + (g.max_tokens + kQBlock - 1) / kQBlock;
+  off = align_up(off + (size_t)g.n_rows * g.n_kv_heads * c->score_steps * kQKept * kQBlock * sizeof(float), 256);
   c->ws_bytes = off;
   return VVS_OK;
 }
@@ -197,7 +202,7 @@ vvs_status vvs_qcache_attention(vvs_qcache* qc, int32_t layer, const int32_t* d_
   a.layer = layer; a.T = n_tokens; a.group = g.n_heads / g.n_kv_heads;
   a.n_tokens = d_n_tokens;
   a.q = d_q; a.k = d_k; a.v = d_v; a.q_stride = (size_t)qs; a.kv_stride = (size_t)ks;
-  a.c_exp = (float)((double)scale * 1.4426950408889634);
+  a.c_exp = std::max((float)((double)scale * 1.4426950408889634), FLT_MIN);   // above 0: masked scores are -inf
   a.out = d_out;
   a.n_counted = n_counted;
   a.mass = d_mass; a.block_mass = d_block_mass;
@@ -205,6 +210,8 @@ vvs_status vvs_qcache_attention(vvs_qcache* qc, int32_t layer, const int32_t* d_
   a.lse = d_lse;
   a.norm = n_counted || d_block_mass ? (float2*)(c->ws + c->norm_off) : nullptr;
   a.parts = (float*)(c->ws + c->parts_off);
+  a.scores = (float*)(c->ws + c->scores_off);
+  a.score_steps = c->score_steps;
   launch_qcache_attention(a, g.dtype, (hipStream_t)s);
   return launched(c, "qcache attention");
 }
