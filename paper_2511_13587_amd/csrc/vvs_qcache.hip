@@ -9,6 +9,7 @@
 namespace vvs {
 
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kQSmall = 0x1p-110f;   // 2^kQLeast
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -223,11 +224,13 @@ void launch_qcache_append(const QAppend& a, int dtype, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------------------------------------ read
-// One wave per (layer, row, head, block that the window touches): whole 16-byte pieces of the block, the values turned in registers.
+// One wave per (layer, row, head, block that the window touches): whole 16-byte pieces of the block, the values turned in registers.  The numbers go through LDS (32 slots at a
+// time, a wave's own), so that a slot's dims are written side by side: straight from the registers a store covers 32 bytes of each of 32 slots.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_qcache_read(QRead a, int max_blocks) {
-  constexpr int KD = DH / 32;
-  const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6), r = blockIdx.y, layer = blockIdx.z;
+  constexpr int KD = DH / 32, PAD = 16 / sizeof(T), LANES = DH * sizeof(T) / 16;      // LANES: pieces of 16 bytes that make up a slot
+  __shared__ __align__(16) T s_out[4][kQBlock][DH + PAD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, unit = blockIdx.x * 4 + wave, r = blockIdx.y, layer = blockIdx.z;
   const int head = unit % a.c.kv_heads, nth = unit / a.c.kv_heads;
   if (nth >= max_blocks) return;
   const int len = row_len(a.len, r, a.capacity);
@@ -239,27 +242,37 @@ __global__ __launch_bounds__(256) void k_qcache_read(QRead a, int max_blocks) {
   const float2 sc = a.c.scale[at];
   const size_t out0 = ((size_t)layer * a.c.rows + r) * a.n;
   const int g = lane >> 4, i = lane & 15;
+  uint4 b[2][KD];
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int c = 0; c < KD; ++c) b[half][c] = held ? *(const uint4*)(data + half * kQBlock * DH + (c * 64 + lane) * 16) : make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const float unit_of = half ? sc.y : sc.x;
-    uint4 b[KD];
-#pragma unroll
-    for (int c = 0; c < KD; ++c) b[c] = held ? *(const uint4*)(data + half * kQBlock * DH + (c * 64 + lane) * 16) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int c = 0; c < KD; ++c)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        uint2 v8 = t ? make_uint2(b[c].z, b[c].w) : make_uint2(b[c].x, b[c].y);
+        uint2 v8 = t ? make_uint2(b[half][c].z, b[half][c].w) : make_uint2(b[half][c].x, b[half][c].y);
         if (half) v8 = transpose_bytes(v8, lane);
         const int w = half ? value_slot(lane) : slot_of(t, i), dim = half ? c * 32 + t * 16 + (i & 8) : c * 32 + 8 * g;
-        const int64_t slot = slot0 + w;
         float v[8];
         from_e4m3x8(v8, v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = held && slot < len ? v[j] * unit_of : 0.f;
-        if (slot >= first && slot < first + a.n)
-          write8((T*)(half ? a.v : a.k) + ((out0 + (size_t)(slot - first)) * a.c.kv_heads + head) * DH + dim, v);
+        for (int j = 0; j < 8; ++j) v[j] = held && slot0 + w < len ? v[j] * unit_of : 0.f;
+        write8(&s_out[wave][w][dim], v);
       }
+    __builtin_amdgcn_wave_barrier();
+    T* out = (T*)(half ? a.v : a.k);
+#pragma unroll
+    for (int j = 0; j < kQBlock * LANES / 64; ++j) {
+      const int w = (j * 64 + lane) / LANES, dim = lane % LANES * PAD;
+      const uint4 x = *(const uint4*)&s_out[wave][w][dim];
+      const int64_t slot = slot0 + w;
+      if (slot >= first && slot < first + a.n) *(uint4*)(out + ((out0 + (size_t)(slot - first)) * a.c.kv_heads + head) * DH + dim) = x;
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -337,8 +350,6 @@ struct QShape {
   static constexpr int NP = sizeof(T) == 4 ? 3 : 2;     // ... and a softmax weight beside values in bf16
   static constexpr int KD = DH / 32, DT = DH / 16;
 };
-
-constexpr float kQSmall = 0x1p-110f;      // 2^kQLeast
 
 // A cached block in registers, as it lies in memory
 template <int DH>
@@ -552,19 +563,31 @@ __device__ __forceinline__ float* kept_scores(const QAttention& a, int r, int hk
   return a.scores + (((size_t)r * a.c.kv_heads + hk) * a.score_steps + step) * a.n_kept * kQBlock;
 }
 
-// Adds up the weights of slots / block tokens first, first + by .. of one (row, key/value head) from the kept scores; norm: [n_kept] (reference exponent, 1 / sum); seen: block tokens that the
+// Adds up the weights of one (row, key/value head) from the kept scores, 4 keys at a time: thread `first` of `by`.  norm: [n_queries] (reference exponent, 1 / sum); seen: block tokens that the
 // counted queries' tile looked at (the others have weight 0)
 __device__ __forceinline__ void mass_of_kept(const QAttention& a, const QRow& w, int r, int hk, const float2* norm, int n_queries, int seen, int first, int by) {
   const int steps = w.blocks + (a.block_mass ? (w.n + 31) / 32 : 0);
-  for (int i = first + (a.mass ? 0 : w.blocks * kQBlock); i < steps * kQBlock; i += by) {
-    const int step = i / kQBlock, at = i % kQBlock, slot = i, tok = i - w.blocks * kQBlock;
+  float* mass = a.mass + ((size_t)r * a.c.kv_heads + hk) * a.capacity;
+  float* block_mass = a.block_mass + ((size_t)r * a.c.kv_heads + hk) * a.T;
+  for (int i = first + (a.mass ? 0 : w.blocks * 8); i < steps * 8; i += by) {
+    const int step = i >> 3, at = (i & 7) * 4;
     const bool cached = step < w.blocks;
-    if (cached ? slot >= w.len : tok >= w.n) continue;
+    const int key = cached ? i * 4 : (i - w.blocks * 8) * 4, end = cached ? w.len : w.n, there = cached ? w.len : seen;
     const float* x = kept_scores(a, r, hk, step) + at;
-    float sum = 0.f;
-    for (int q = 0; q < n_queries && (cached || tok < seen); ++q) sum += __builtin_amdgcn_exp2f(x[q * kQBlock] - norm[q].x) * norm[q].y;
-    if (cached) a.mass[((size_t)r * a.c.kv_heads + hk) * a.capacity + slot] += sum;
-    else a.block_mass[((size_t)r * a.c.kv_heads + hk) * a.T + tok] = sum;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (key < there)
+      for (int q = 0; q < n_queries; ++q) {
+        const float4 s = *(const float4*)(x + q * kQBlock);
+        const float2 n = norm[q];
+        sum[0] += __builtin_amdgcn_exp2f(s.x - n.x) * n.y;
+        sum[1] += __builtin_amdgcn_exp2f(s.y - n.x) * n.y;
+        sum[2] += __builtin_amdgcn_exp2f(s.z - n.x) * n.y;
+        sum[3] += __builtin_amdgcn_exp2f(s.w - n.x) * n.y;
+      }
+    float* out = cached ? mass : block_mass;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (key + j < end) out[key + j] = (cached ? out[key + j] : 0.f) + (key + j < there ? sum[j] : 0.f);
   }
 }
 
@@ -802,7 +825,9 @@ __global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, 
     if ((int)threadIdx.x < n_kept) {
       const float* part = a.parts + (((size_t)r * gridDim.x + blockIdx.x) * a.splits * nq_tile + threadIdx.x) * (DH + 2) + DH;
       float m = -INFINITY, l = 0.f;
+#pragma unroll 8
       for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * step]);
+#pragma unroll 8
       for (int s = 0; s < a.splits; ++s) l += part[s * step + 1] * (part[s * step] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(part[s * step] - m));
       s_norm[threadIdx.x] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
     }
@@ -917,7 +942,8 @@ static void attention_t(QAttention a, hipStream_t s) {
   hipLaunchKernelGGL((k_qcache_attention<T, DH, NQB>), grid, dim3(256), 0, s, a, q_tiles);
   if (a.splits > 1) {
     const int per = 256 / (DH / 4), joins = (16 * NQB + per - 1) / per;
-    const int masses = a.n_kept ? std::max(1, std::min(a.c.blocks / 32, 64)) : 0;
+    // (a workgroup first finds the norms: a few workgroups with much to add rather than many with little)
+    const int masses = a.n_kept ? (int)std::max<int64_t>(1, std::min<int64_t>(a.c.blocks / 32, 2048 / ((int64_t)a.c.rows * a.c.kv_heads))) : 0;
     hipLaunchKernelGGL((k_qcache_join<T, DH>), dim3(grid.x, joins + masses, grid.z), dim3(256), 0, s, a, q_tiles, 16 * NQB, joins);
   }
   if (!a.n_kept && (a.n_counted > 0 || a.block_mass)) {
@@ -1187,8 +1213,10 @@ __global__ __launch_bounds__(kQSelect) void k_qcache_select_long(QEvict a) {
   clear_behind(h, a.capacity, tid, kQSelect);
 }
 
-// Moves the elements: one wave per (layer, row, head, block below keep).  A slot's dims are 8 bytes in a row among the keys, and single bytes 16 apart among the values
-// (there the 8 bytes in a row are 8 slots of a dim): gathered by the lane that holds the slot, turned, stored as 16 bytes.
+// Moves the elements: one wave per (layer, row, head, block below keep).  Of the keys a lane gathers 8 dims of its two slots, 8 bytes in a row.  Of the values it gathers its dims of 8 slots: the 16
+// lanes of a group read the 256 bytes in which a source's dims lie beside those of the 7 slots around it, and each picks its byte.  (Single bytes by the lane that holds the slot: every lane
+// touches a segment of its own, 370 us instead
+// of 276 for 36 x 16 x 20 rows of 696 slots cut to 256.)  Bound by HBM: a slot's values share their cache lines with 7 others, so that nearly all of them are read, 1.08 GB with keys and stores: 3.9 TB/s.
 template <int DH>
 __global__ __launch_bounds__(256) void k_qcache_move(QEvict a) {
   const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6), r = blockIdx.y, layer = blockIdx.z;
@@ -1197,50 +1225,66 @@ __global__ __launch_bounds__(256) void k_qcache_move(QEvict a) {
   if (row_len(a.len, r, a.capacity) <= a.keep) return;
   const size_t base = (((size_t)layer * a.c.rows + r) * a.c.kv_heads + head) * a.capacity, region = a.c.region(a.layer + layer, r, head) * a.c.blocks;
   const int g = lane >> 4, i = lane & 15, slot0 = block * kQBlock;
-  const int w[3] = {slot_of(0, i), slot_of(1, i), value_slot(lane)};        // this lane's slots: keys of both tiles, values
-  int from[3];
+  const int32_t* origin = a.origin + base + slot0;
+  const int from_k[2] = {origin[slot_of(0, i)], origin[slot_of(1, i)]};        // this lane's slots: keys of both tiles
+  const int4 o0 = *(const int4*)(origin + 8 * g), o1 = *(const int4*)(origin + 8 * g + 4);
+  const int from_v[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};      // ... and values
+  if (!__builtin_amdgcn_ballot_w64(from_k[0] != slot0 + slot_of(0, i) || from_k[1] != slot0 + slot_of(1, i))) return;
+  float unit_k[2], unit_v[8], tk = 0.f, tv = 0.f;
 #pragma unroll
-  for (int n = 0; n < 3; ++n) from[n] = a.origin[base + slot0 + w[n]];
-  if (!__builtin_amdgcn_ballot_w64(from[2] != slot0 + w[2])) return;        // (value slots cover the block)
-  const float least = ldexpf(1.f, kQLeast);
-  float unit_of[3];
+  for (int t = 0; t < 2; ++t) { unit_k[t] = fmaxf(a.c.scale[region + (from_k[t] >> 5)].x, kQSmall); tk = fmaxf(tk, unit_k[t]); }
 #pragma unroll
-  for (int n = 0; n < 3; ++n) {
-    const float2 sc = a.c.scale[region + (from[n] >> 5)];
-    unit_of[n] = fmaxf(n < 2 ? sc.x : sc.y, least);
-  }
-  const float tk = wave_max(fmaxf(unit_of[0], unit_of[1])), tv = wave_max(unit_of[2]);
-  const bool again[2] = {__builtin_amdgcn_ballot_w64(unit_of[0] != tk || unit_of[1] != tk) != 0, __builtin_amdgcn_ballot_w64(unit_of[2] != tv) != 0};
-  uint8_t* data = a.c.data + (region + block) * a.c.block_bytes();
-  const uint8_t* src[3];
+  for (int j = 0; j < 8; ++j) { unit_v[j] = fmaxf(a.c.scale[region + (from_v[j] >> 5)].y, kQSmall); tv = fmaxf(tv, unit_v[j]); }
+  tk = wave_max(tk);
+  tv = wave_max(tv);
+  bool other_v = false;
 #pragma unroll
-  for (int n = 0; n < 3; ++n) src[n] = a.c.data + (region + (from[n] >> 5)) * a.c.block_bytes();
-  auto rounded = [&](uint2 b, float ratio) {      // to the block's larger power of two
-    float v[8];
-    from_e4m3x8(b, v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= ratio;
-    return to_e4m3x8(v);
-  };
+  for (int j = 0; j < 8; ++j) other_v |= unit_v[j] != tv;
+  const bool again_k = __builtin_amdgcn_ballot_w64(unit_k[0] != tk || unit_k[1] != tk) != 0, again_v = __builtin_amdgcn_ballot_w64(other_v) != 0;
+  uint8_t* data = a.c.data + region * a.c.block_bytes();
+  uint8_t* out = data + (size_t)block * a.c.block_bytes();
 #pragma unroll
   for (int c = 0; c < DH / 32; ++c) {
-    uint4 k;
-    const uint2 k0 = *(const uint2*)(src[0] + key_byte(from[0] & 31, c * 32 + 8 * g)), k1 = *(const uint2*)(src[1] + key_byte(from[1] & 31, c * 32 + 8 * g));
-    const uint2 r0 = again[0] ? rounded(k0, unit_of[0] / tk) : k0, r1 = again[0] ? rounded(k1, unit_of[1] / tk) : k1;
-    k = make_uint4(r0.x, r0.y, r1.x, r1.y);
-    uint2 v[2];
+    uint2 k[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint8_t* b = src[2] + kQBlock * DH + value_byte(from[2] & 31, c * 32 + t * 16 + (i & 8));
-      uint32_t e[8];
+    for (int t = 0; t < 2; ++t) k[t] = *(const uint2*)(data + (size_t)(from_k[t] >> 5) * a.c.block_bytes() + key_byte(from_k[t] & 31, c * 32 + 8 * g));
+    u32x4 b[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = b[j * 16];
-      v[t] = make_uint2(e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24, e[4] | e[5] << 8 | e[6] << 16 | e[7] << 24);
-      if (again[1]) v[t] = rounded(v[t], unit_of[2] / tv);
-      v[t] = transpose_bytes(v[t], lane);
+    for (int j = 0; j < 8; ++j)
+      b[j] = *(const u32x4*)(data + (size_t)(from_v[j] >> 5) * a.c.block_bytes() + kQBlock * DH + (c * 64 + (from_v[j] >> 3 & 3) * 16 + i) * 16);
+    uint32_t v0[2] = {0, 0}, v1[2] = {0, 0};      // slots 0 .. 3 and 4 .. 7 of both dims
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int at = from_v[j] & 7;
+      const u32x4 x = b[j];
+      const uint32_t w0 = at & 4 ? x[1] : x[0], w1 = at & 4 ? x[3] : x[2];
+      const uint32_t x0 = (w0 >> (at & 3) * 8) & 255u, x1 = (w1 >> (at & 3) * 8) & 255u;
+      v0[j >> 2] |= x0 << (j & 3) * 8;
+      v1[j >> 2] |= x1 << (j & 3) * 8;
     }
-    *(uint4*)(data + (c * 64 + lane) * 16) = k;
-    *(uint4*)(data + kQBlock * DH + (c * 64 + lane) * 16) = make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+    uint2 v[2] = {make_uint2(v0[0], v0[1]), make_uint2(v1[0], v1[1])};
+    if (again_k) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float x[8];
+        from_e4m3x8(k[t], x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= unit_k[t] / tk;
+        k[t] = to_e4m3x8(x);
+      }
+    }
+    if (again_v) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float x[8];
+        from_e4m3x8(v[t], x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= unit_v[j] / tv;
+        v[t] = to_e4m3x8(x);
+      }
+    }
+    *(uint4*)(out + (c * 64 + lane) * 16) = make_uint4(k[0].x, k[0].y, k[1].x, k[1].y);
+    *(uint4*)(out + kQBlock * DH + (c * 64 + lane) * 16) = make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
   }
   if (lane == 0) a.c.scale[region + block] = make_float2(tk, tv);
 }
