@@ -40,7 +40,7 @@ struct QAttention {
   float c_exp;                      // scale * log2(e)
   void* out;
   float* lse;                       // [rows][T][heads] or nullptr
-  float2* norm;                     // workspace, likewise: maximum (in units of log2) and 1 / sum, or nullptr: nothing is counted
+  float* norm;                      // workspace, likewise, in units of log2, or nullptr: nothing is counted
   int n_counted;
   float *mass, *block_mass;         // [rows][kv_heads][capacity], [rows][kv_heads][T]
   int capacity;

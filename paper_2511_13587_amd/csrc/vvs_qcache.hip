@@ -408,27 +408,27 @@ __device__ __forceinline__ bool values_of_tokens(const float* v, size_t stride, 
   return odd;
 }
 
+// (bf16: one piece of 16 bytes; there: all ones, or 0 behind the last token; odd: not 0 if anything was not finite)
+__device__ __forceinline__ uint4 turned_values(uint4 b, uint32_t there, int lane, uint32_t& odd) {
+  uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    w[j] &= there;
+    // exponents of all ones: the carry of one more into the sign, half by half
+    const uint32_t bad = ((w[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+    odd |= bad;
+    w[j] &= ~((bad >> 15) * 0xFFFFu);
+  }
+  return transpose_halves(make_uint4(w[0], w[1], w[2], w[3]), lane);
+}
 template <int DH, int NS>
 __device__ __forceinline__ bool values_of_tokens(const bf16_t* v, size_t stride, int tok0, int n, int lane, bf16x8 (&vf)[DH / 16][NS]) {
   static_assert(NS == 1, "");
   const int tok = tok0 + value_slot(lane);
   const bf16_t* p = v + (size_t)min(tok, n - 1) * stride + (lane & 8);
-  const uint32_t there = tok < n ? 0xFFFFFFFFu : 0u;
   uint32_t odd = 0;
 #pragma unroll
-  for (int dt = 0; dt < DH / 16; ++dt) {
-    const uint4 b = *(const uint4*)(p + dt * 16);
-    uint32_t w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      w[j] &= there;
-      // exponents of all ones: the carry of one more into the sign, half by half
-      const uint32_t bad = ((w[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-      odd |= bad;
-      w[j] &= ~((bad >> 15) * 0xFFFFu);
-    }
-    vf[dt][0] = as_bf16x8(transpose_halves(make_uint4(w[0], w[1], w[2], w[3]), lane));
-  }
+  for (int dt = 0; dt < DH / 16; ++dt) vf[dt][0] = as_bf16x8(turned_values(*(const uint4*)(p + dt * 16), tok < n ? 0xFFFFFFFFu : 0u, lane, odd));
   return odd != 0;
 }
 
@@ -462,10 +462,12 @@ struct QRun {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  // weights of 8 keys, e[i] = 2^(sv[i] c + ev - m)
-  __device__ __forceinline__ void weights(const float (&sv)[8], float c, float ev, float per_unit, float (&e)[8]) {
-    float mx = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
-    const float cand = fmaf(rows_max(mx), c, ev);
+  static __device__ __forceinline__ float top(const float (&sv)[8]) {
+    return fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
+  }
+  // the reference follows where the largest exponent to come, `cand` in this lane, is more than 2^6 above it
+  __device__ __forceinline__ void follow(float cand) {
+    cand = rows_max(cand);
     if (__builtin_amdgcn_ballot_w64(cand > m + 6.f)) {
       const float to = fmaxf(m, cand), alpha = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
       m = to;
@@ -475,14 +477,17 @@ struct QRun {
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[dt][j] *= alpha;
     }
+  }
+  // weights of 8 keys, e[i] = 2^(sv[i] c + ev - m); their sum times 2^-ev = per_unit goes into the normaliser
+  __device__ __forceinline__ void exponentials(const float (&sv)[8], float c, float ev, float per_unit, float (&e)[8]) {
     const float off = ev - (m == -INFINITY ? 0.f : m);
-    float rs = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      e[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], c, off));
-      rs += e[i];
-    }
-    l = fmaf(rs, per_unit, l);
+    for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], c, off));
+    l = fmaf(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])), per_unit, l);
+  }
+  __device__ __forceinline__ void weights(const float (&sv)[8], float c, float ev, float per_unit, float (&e)[8]) {
+    follow(fmaf(top(sv), c, ev));
+    exponentials(sv, c, ev, per_unit, e);
   }
   template <int NK, int NP>
   __device__ __forceinline__ void add_bf16(const float (&e)[8], const bf16x8 (&vf)[DT][NK]) {
@@ -551,11 +556,11 @@ __device__ __forceinline__ void store4(const QAttention& a, size_t at, int dim, 
   }
 }
 
-// log-sum-exp for the caller, reference exponent and 1 / sum for the counted weights (from the log alone they would lose what its size takes of 24 bits)
+// log-sum-exp for the caller, and in units of log2 for the counted weights of many queries (its size takes some of the 24 bits: weights to 2^-20 of themselves)
 __device__ __forceinline__ void tell_norm(const QAttention& a, size_t at, float m, float l) {
   const bool none = l == 0.f;            // a query that sees nothing
   if (a.lse) a.lse[at] = none ? -INFINITY : (m + log2f(l)) * kLn2;
-  if (a.norm) a.norm[at] = make_float2(none ? 0.f : m, none ? 0.f : 1.f / l);
+  if (a.norm) a.norm[at] = none ? INFINITY : m + log2f(l);
 }
 
 // Scores (times c: units of log2) that the main kernel leaves for the counted weights: [rows][kv heads][steps][counted queries][32 keys]
@@ -588,6 +593,27 @@ __device__ __forceinline__ void mass_of_kept(const QAttention& a, const QRow& w,
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (key + j < end) out[key + j] = (cached ? out[key + j] : 0.f) + (key + j < there ? sum[j] : 0.f);
+  }
+}
+
+// Values of block tokens that are not finite (their places in the product held zeros): only for the queries that see them.  e: the step's weights
+template <int DT, typename T>
+__device__ __forceinline__ void add_odd_values(const QAttention& a, const T* v, const float (&e)[8], int t, int tok0, int seen, int lane, floatx4 (&o)[DT]) {
+  for (int j = 0; j < 32 && tok0 + j < seen; ++j) {
+    float p = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = __shfl(e[i], (j >> 3) * 16 + (lane & 15), 64);
+      p = (j & 7) == i ? x : p;
+    }
+    const bool vis = sees8(a, t, tok0 + j, seen) & 1;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = ld(v + (size_t)(tok0 + j) * a.kv_stride + dt * 16 + 4 * (lane >> 4) + i);
+        o[dt][i] += vis && !finite(x) ? p * x : 0.f;
+      }
   }
 }
 
@@ -711,24 +737,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
       if (qb == 0 && n_kept) keep_scores(step, sv, a.c_exp);
       run[qb].weights(sv, a.c_exp, 0.f, 1.f, e);
       run[qb].template add_bf16<NS, NP>(e, vf);
-      if (odd) {                              // values that are not finite: only for the queries that see them
-        for (int j = 0; j < 32 && tok0 + j < seen; ++j) {
-          float p = 0.f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float x = __shfl(e[i], (j >> 3) * 16 + col, 64);
-            p = (j & 7) == i ? x : p;
-          }
-          const bool vis1 = sees8(a, qt[qb], tok0 + j, seen) & 1;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float x = ld(v + (size_t)(tok0 + j) * a.kv_stride + dt * 16 + 4 * g + i);
-              run[qb].o[dt][i] += vis1 && !finite(x) ? p * x : 0.f;
-            }
-        }
-      }
+      if (odd) add_odd_values<DT>(a, v, e, qt[qb], tok0, seen, lane, run[qb].o);
     }
   }
   // join the four waves: common reference, then sums in the order (0 + 2) + (1 + 3)
@@ -810,9 +819,297 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
   mass_of_kept(a, w, r, hk, s_norm, n_kept, seen, threadIdx.x, 256);
 }
 
-// Joins the splits: one group of DH / 4 lanes per query.  Workgroups of blockIdx.y >= joins add up the counted weights instead.
+// Many queries: a workgroup takes 128 of them, 32 per wave, and all its waves go through the same keys, so that what is done once per key - load, conversion, turning - is
+// shared: the waves bring the operands of 64 keys to LDS while those before are at work, from registers that were loaded another 64 keys earlier.  bf16 calls; grid as above.
+// 8 rows x 32 query heads on 8 x 512 tokens over 4096 slots, head size 128: 434 us, 670 TFLOP/s (16 queries per wave 646: every operand read from LDS for half as many); 4 rows over 2048
+// slots 151 us.  Bound by vector instructions and the waits between them and the matrix cores, of two waves per SIMD.
+// Blocks whose values do not go as fp16 (rare) are left for the end, each wave on its own, so that the registers of that path are not taken in the others.
+template <int DH>
+__global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, int q_tiles) {
+  constexpr int KD = DH / 32, DT = DH / 16, NQB = 2, NQ = 64 * NQB;
+  __shared__ uint4 s_k[2][2][2 * KD][64], s_v[2][2][DT][64];      // [buffer][block of 32 keys]
+  __shared__ int s_odd[2][2];                 // block tokens: whether any values are not finite
+  __shared__ float2 s_norm[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
+  const int hk = blockIdx.x / q_tiles, q0 = (blockIdx.x % q_tiles) * NQ, r = blockIdx.z, split = blockIdx.y;
+  const QRow w = row_of(a, r);
+  const int nq = w.n * a.group;
+  if (q0 >= nq) return;
+  const bf16_t* k = (const bf16_t*)a.k + (size_t)r * a.T * a.kv_stride + (size_t)hk * DH;
+  const bf16_t* v = (const bf16_t*)a.v + (size_t)r * a.T * a.kv_stride + (size_t)hk * DH;
+  const size_t region = a.c.region(a.layer, r, hk) * a.c.blocks;
+  const int qw = q0 + wave * 16 * NQB;        // this wave's first query
+  bf16x8 qf[NQB][KD][1];
+  int qt[NQB];
+#pragma unroll
+  for (int qb = 0; qb < NQB; ++qb) {
+    const int qi = min(qw + qb * 16 + col, nq - 1);
+    qt[qb] = qi / a.group;
+    const bf16_t* q = (const bf16_t*)a.q + ((size_t)r * a.T + qt[qb]) * a.q_stride + ((size_t)hk * a.group + qi % a.group) * DH + g * 8;
+#pragma unroll
+    for (int kd = 0; kd < KD; ++kd) load_operand<1>(q + kd * 32, qf[qb][kd]);
+  }
+  const int t_first = min(qw, nq - 1) / a.group, t_last = min(qw + 16 * NQB - 1, nq - 1) / a.group;      // tokens of the wave's queries
+  QRun<DT> run[NQB];
+#pragma unroll
+  for (int qb = 0; qb < NQB; ++qb) run[qb].clear();
+  const int n_kept = a.n_kept && qw == 0 ? min(a.n_kept, nq) : 0;
+  auto keep_scores = [&](int step, const float (&sv)[8], float c) {
+    if (col < n_kept) {
+      float* p = kept_scores(a, r, hk, step) + col * kQBlock + 8 * g;
+      ((float4*)p)[0] = make_float4(sv[0] * c, sv[1] * c, sv[2] * c, sv[3] * c);
+      ((float4*)p)[1] = make_float4(sv[4] * c, sv[5] * c, sv[6] * c, sv[7] * c);
+    }
+  };
+  const int seen = seen_by(a, w, min(q0 + NQ, nq));
+  const int steps = w.blocks + (seen + 31) / 32;
+  const int s0 = (int)((int64_t)steps * split / a.splits), s1 = (int)((int64_t)steps * (split + 1) / a.splits);
+  const int cached_end = min(s1, w.blocks);
+  const uint8_t* data = a.c.data + region * a.c.block_bytes();
+  const float2* scales = a.c.scale + region;
+  auto scale_of = [&](int step) { const float2 sc = scales[step]; return make_float2(fmaxf(sc.x, kQSmall), fmaxf(sc.y, kQSmall)); };
+  auto half_values = [](float unit_of) { return unit_of <= 0x1p40f && unit_of >= 0x1p-40f; };
+  auto tail = [&](int step, float (&sv)[8]) {   // slots behind the length
+    const int mine = w.len - step * kQBlock - 8 * g;
+    const uint32_t vis = mine >= 8 ? 255u : mine <= 0 ? 0u : (1u << mine) - 1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sv[i] = (vis >> i) & 1 ? sv[i] : -INFINITY;
+  };
+  bool left_out = false;                      // some cached block waits for the end
+
+  // ---- cached blocks, two at a time: a wave brings KD of the 4 KD pieces of 1 KiB
+  if (s0 < cached_end) {
+    uint4 raw[KD];
+    auto load_raw = [&](int step) {
+#pragma unroll
+      for (int n = 0; n < KD; ++n) {
+        const int piece = wave * KD + n, b = piece / (2 * KD);
+        raw[n] = *(const uint4*)(data + (size_t)min(step + b, cached_end - 1) * a.c.block_bytes() + (piece % (2 * KD) * 64 + lane) * 16);
+      }
+    };
+    auto bring = [&](int step, int buf) {
+#pragma unroll
+      for (int n = 0; n < KD; ++n) {
+        const int piece = (wave * KD + n) % (2 * KD), b = (wave * KD + n) / (2 * KD);
+        uint2 lo = make_uint2(raw[n].x, raw[n].y), hi = make_uint2(raw[n].z, raw[n].w);
+        if (piece < KD) {
+          s_k[buf][b][piece][lane] = __builtin_bit_cast(uint4, e4m3_to_bf16(lo, 1.f));
+          s_k[buf][b][KD + piece][lane] = __builtin_bit_cast(uint4, e4m3_to_bf16(hi, 1.f));
+        } else {
+          if (step + b >= cached_end || w.len - (step + b) * kQBlock < kQBlock) {                 // (a second block that is not there: zeros)
+            const int mine = step + b < cached_end ? w.len - (step + b) * kQBlock - 8 * g : 0;
+            const uint64_t keep = mine >= 8 ? ~0ull : mine <= 0 ? 0ull : (1ull << (8 * mine)) - 1;
+            lo.x &= (uint32_t)keep; lo.y &= (uint32_t)(keep >> 32); hi.x &= (uint32_t)keep; hi.y &= (uint32_t)(keep >> 32);
+          }
+          s_v[buf][b][2 * (piece - KD)][lane] = __builtin_bit_cast(uint4, e4m3_to_f16(lo));
+          s_v[buf][b][2 * (piece - KD) + 1][lane] = __builtin_bit_cast(uint4, e4m3_to_f16(hi));
+        }
+      }
+    };
+    load_raw(s0);
+    bring(s0, 0);
+    if (s0 + 2 < cached_end) load_raw(s0 + 2);
+    __syncthreads();
+    for (int step0 = s0, buf = 0; step0 < cached_end; step0 += 2, buf ^= 1) {
+      if (step0 + 2 < cached_end) bring(step0 + 2, buf ^ 1);
+      if (step0 + 4 < cached_end) load_raw(step0 + 4);
+      // both blocks at once: twice the independent work between the waits for the matrix cores and for the maxima.  One that is not there or goes as bf16 gets weights of 0
+      float c_exp[2], ev[2], per_unit[2];
+      bool gone[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const float2 scale = scale_of(min(step0 + b, cached_end - 1));
+        const bool there = step0 + b < cached_end, half = half_values(scale.y);
+        left_out |= there && !half;
+        gone[b] = !there || !half;
+        c_exp[b] = fmaxf(a.c_exp * scale.x, FLT_MIN);
+        ev[b] = half ? (float)exponent_of(scale.y) : 0.f;
+        per_unit[b] = half ? 1.f / scale.y : 1.f;
+      }
+      float sv[2][NQB][8];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        bf16x8 kf[2][KD][1];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int kd = 0; kd < KD; ++kd) kf[t][kd][0] = as_bf16x8(s_k[buf][b][t * KD + kd][lane]);
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+          step_scores<KD, 1, 1>(kf, qf[qb], sv[b][qb]);
+          // (in units of log2 from here on: what comes out of a product needs no quieting of NaN in front of a maximum, which costs as much)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sv[b][qb][i] *= c_exp[b];
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if (w.len - (step0 + b) * kQBlock < kQBlock) {
+#pragma unroll
+          for (int qb = 0; qb < NQB; ++qb) tail(step0 + b, sv[b][qb]);
+        }
+        if (n_kept && !gone[b]) keep_scores(step0 + b, sv[b][0], 1.f);
+        if (gone[b]) {
+#pragma unroll
+          for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sv[b][qb][i] = -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int qb = 0; qb < NQB; ++qb)
+        run[qb].follow(fmaxf(QRun<DT>::top(sv[0][qb]) + ev[0], QRun<DT>::top(sv[1][qb]) + ev[1]));
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        f16x8 vf[DT];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vf[dt] = __builtin_bit_cast(f16x8, s_v[buf][b][dt][lane]);
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+          float e[8];
+          run[qb].exponentials(sv[b][qb], 1.f, ev[b], per_unit[b], e);
+          run[qb].add_f16(e, vf);
+        }
+      }
+      __syncthreads();
+    }
+  }
+
+  // ---- block tokens, 32 at a time: waves 0 and 1 bring the keys of both tiles, waves 2 and 3 half of the values each
+  {
+    const int f0 = max(s0, w.blocks);
+    uint4 raw[KD];
+    auto load_raw = [&](int step) {
+      const int tok0 = (step - w.blocks) * 32, tok = min(tok0 + (wave < 2 ? slot_of(wave, col) : value_slot(lane)), seen - 1);
+      const bf16_t* p = (wave < 2 ? k : v) + (size_t)tok * a.kv_stride + (wave < 2 ? g * 8 : (wave - 2) * (DH / 2) + (lane & 8));
+      const int next = wave < 2 ? 32 : 16;
+#pragma unroll
+      for (int n = 0; n < KD; ++n) raw[n] = *(const uint4*)(p + n * next);
+    };
+    auto bring = [&](int step, int buf) {
+      if (wave < 2) {
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd) s_k[buf][0][wave * KD + kd][lane] = raw[kd];
+      } else {
+        uint32_t odd = 0;
+        const uint32_t there = (step - w.blocks) * 32 + value_slot(lane) < seen ? 0xFFFFFFFFu : 0u;
+#pragma unroll
+        for (int n = 0; n < KD; ++n) s_v[buf][0][(wave - 2) * KD + n][lane] = turned_values(raw[n], there, lane, odd);
+        const bool any = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+        if (lane == 0) s_odd[buf][wave - 2] = any;
+      }
+    };
+    if (f0 < s1) {
+      load_raw(f0);
+      bring(f0, 0);
+      if (f0 + 1 < s1) load_raw(f0 + 1);
+    }
+    __syncthreads();
+    for (int step = f0, buf = 0; step < s1; ++step, buf ^= 1) {
+      if (step + 1 < s1) bring(step + 1, buf ^ 1);
+      if (step + 2 < s1) load_raw(step + 2);
+      const int tok0 = (step - w.blocks) * 32;
+      if (!a.causal || tok0 <= t_last) {
+        float sv[NQB][8];
+        {
+          bf16x8 kf[2][KD][1];
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int kd = 0; kd < KD; ++kd) kf[t][kd][0] = as_bf16x8(s_k[buf][0][t * KD + kd][lane]);
+#pragma unroll
+          for (int qb = 0; qb < NQB; ++qb) step_scores<KD, 1, 1>(kf, qf[qb], sv[qb]);
+        }
+        if (!a.causal || tok0 + 31 > t_first || tok0 + 31 >= seen) {
+#pragma unroll
+          for (int qb = 0; qb < NQB; ++qb) {
+            const uint32_t vis = sees8(a, qt[qb], tok0 + 8 * g, seen);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sv[qb][i] = (vis >> i) & 1 ? sv[qb][i] : -INFINITY;
+          }
+        }
+        if (n_kept) keep_scores(step, sv[0], a.c_exp);
+        bf16x8 vf[DT][1];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vf[dt][0] = as_bf16x8(s_v[buf][0][dt][lane]);
+        const bool odd = s_odd[buf][0] | s_odd[buf][1];
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+          float e[8];
+          run[qb].weights(sv[qb], a.c_exp, 0.f, 1.f, e);
+          run[qb].template add_bf16<1, 2>(e, vf);
+          if (odd) add_odd_values<DT>(a, v, e, qt[qb], tok0, seen, lane, run[qb].o);
+        }
+      }
+      __syncthreads();
+    }
+  }
+
+  // ---- cached blocks whose values go as bf16
+  for (int step = s0; left_out && step < cached_end; ++step) {
+    const float2 scale = scale_of(step);
+    if (half_values(scale.y)) continue;
+    QRaw<DH> block;
+    block.load(data + (size_t)step * a.c.block_bytes(), scales + step, lane);
+    block.mask_values(lane, w.len - step * kQBlock);
+    bf16x8 kf[2][KD][1], vf[DT][1];
+#pragma unroll
+    for (int c = 0; c < KD; ++c) {
+      kf[0][c][0] = e4m3_to_bf16(make_uint2(block.k[c].x, block.k[c].y), 1.f);
+      kf[1][c][0] = e4m3_to_bf16(make_uint2(block.k[c].z, block.k[c].w), 1.f);
+      vf[2 * c][0] = e4m3_to_bf16(make_uint2(block.v[c].x, block.v[c].y), scale.y);
+      vf[2 * c + 1][0] = e4m3_to_bf16(make_uint2(block.v[c].z, block.v[c].w), scale.y);
+    }
+    const float c_exp = fmaxf(a.c_exp * scale.x, FLT_MIN);
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      float sv[8], e[8];
+      step_scores<KD, 1, 1>(kf, qf[qb], sv);
+      tail(step, sv);
+      if (qb == 0 && n_kept) keep_scores(step, sv, c_exp);
+      run[qb].weights(sv, c_exp, 0.f, 1.f, e);
+      run[qb].template add_bf16<1, 2>(e, vf);
+    }
+  }
+
+#pragma unroll
+  for (int qb = 0; qb < NQB; ++qb) {
+    const int qi = qw + qb * 16 + col;
+    const float l = rows_sum(run[qb].l), m = run[qb].m;
+    if (qi < nq) {
+      if (a.splits > 1) {
+        float* part = a.parts + ((((size_t)r * gridDim.x + blockIdx.x) * a.splits + split) * NQ + (qi - q0)) * (DH + 2);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) *(float2*)(part + dt * 16 + 4 * g + i) = make_float2(run[qb].o[dt][i], run[qb].o[dt][i + 1]);
+        if (g == 0) *(float2*)(part + DH) = make_float2(m, l);
+      } else {
+        const size_t at = query_at(a, r, hk, qi);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          float x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = run[qb].o[dt][i] * inv;
+          store4<bf16_t, DH>(a, at, dt * 16 + 4 * g, x);
+        }
+        if (g == 0) {
+          tell_norm(a, at, m, l);
+          if (qw == 0 && qb == 0) s_norm[col] = make_float2(m == -INFINITY ? 0.f : m, inv);
+        }
+      }
+    }
+  }
+  if (a.splits > 1 || !a.n_kept || q0) return;
+  __syncthreads();
+  mass_of_kept(a, w, r, hk, s_norm, min(a.n_kept, nq), seen_by(a, w, min(16 * NQB, nq)), threadIdx.x, 256);
+}
+
+// Joins the splits: one group of DH / 4 lanes per query.  Workgroups of blockIdx.y >= joins add up the counted weights instead (kept_tile: queries that went
+// through the keys with the counted ones).
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, int nq_tile, int joins) {
+__global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, int nq_tile, int joins, int kept_tile) {
   constexpr int LQ = DH / 4;
   const int r = blockIdx.z;
   const QRow w = row_of(a, r);
@@ -832,7 +1129,7 @@ __global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, 
       s_norm[threadIdx.x] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
     }
     __syncthreads();
-    mass_of_kept(a, w, r, hk, s_norm, n_kept, seen_by(a, w, min(nq_tile, w.n * a.group)), (blockIdx.y - joins) * 256 + threadIdx.x, (gridDim.y - joins) * 256);
+    mass_of_kept(a, w, r, hk, s_norm, n_kept, seen_by(a, w, min(kept_tile, w.n * a.group)), (blockIdx.y - joins) * 256 + threadIdx.x, (gridDim.y - joins) * 256);
     return;
   }
   const int hk = blockIdx.x / q_tiles, tile = blockIdx.x % q_tiles;
@@ -856,99 +1153,156 @@ __global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, 
   if (dim == 0) tell_norm(a, at, m, l);
 }
 
-// Counted weights of many queries: the scores are made again, now with the normaliser known.  One wave per 32 keys, over all counted queries in order.
+// Counted weights of many queries: the scores are made again, now with the normaliser known.  A wave holds the keys of STEPS steps of 32 in registers, the queries pass by, 64 at a
+// time, through LDS, shared by the four waves; their order is fixed.  Bound by exponentials: per score a product share, an fma, an exponential and an addition.
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
   using S = QShape<T, DH>;
-  constexpr int KD = S::KD, NS = S::NS;
+  constexpr int KD = S::KD, NS = S::NS, STEPS = 1;
+  __shared__ uint4 s_q[2][4][KD * NS][64];
+  __shared__ float s_norm[2][4][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
   const int hk = blockIdx.y, r = blockIdx.z;
   const QRow w = row_of(a, r);
   const int seen = a.k ? w.n : 0, steps = w.blocks + (a.block_mass ? (w.n + 31) / 32 : 0), nq = min(a.n_counted, w.n) * a.group;
+  const int first = a.mass ? 0 : w.blocks;
   const T* q = (const T*)a.q + (size_t)r * a.T * a.q_stride + (size_t)hk * a.group * DH;
   const T* k = (const T*)a.k + (size_t)r * a.T * a.kv_stride + (size_t)hk * DH;
   const size_t region = a.c.region(a.layer, r, hk) * a.c.blocks;
-  for (int step = (a.mass ? 0 : w.blocks) + blockIdx.x * 4 + wave; step < steps; step += gridDim.x * 4) {
-    const bool cached = step < w.blocks;
-    const int tok0 = (step - w.blocks) * 32, valid = cached ? w.len - step * kQBlock : seen - tok0;
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    bf16x8 kf[2][KD][NS];
-    if (cached) {
-      const uint8_t* data = a.c.data + (region + step) * a.c.block_bytes();
-      const float unit_of = a.c.scale[region + step].x;
+  for (int step0 = first + blockIdx.x * 4 * STEPS; step0 < steps; step0 += gridDim.x * 4 * STEPS) {
+    bf16x8 kf[STEPS][2][KD][NS];
+    float sum[STEPS][8], c_exp[STEPS];
+    int valid[STEPS], tok0[STEPS];               // keys there; first block token (cached: -1)
 #pragma unroll
-      for (int kd = 0; kd < KD; ++kd) {
-        const uint4 b = *(const uint4*)(data + (kd * 64 + lane) * 16);
-        kf[0][kd][0] = e4m3_to_bf16(make_uint2(b.x, b.y), unit_of);
-        kf[1][kd][0] = e4m3_to_bf16(make_uint2(b.z, b.w), unit_of);
+    for (int n = 0; n < STEPS; ++n) {
+      const int step = min(step0 + wave * STEPS + n, steps - 1);
+      const bool there = step0 + wave * STEPS + n < steps, cached = step < w.blocks;
+      tok0[n] = cached ? -1 : (step - w.blocks) * 32;
+      valid[n] = !there ? 0 : cached ? min(w.len - step * kQBlock, 32) : min(seen - tok0[n], 32);
+      c_exp[n] = a.c_exp;
 #pragma unroll
-        for (int p = 1; p < NS; ++p) kf[0][kd][p] = kf[1][kd][p] = as_bf16x8(make_uint4(0, 0, 0, 0));
-      }
-    } else {
-      keys_of_tokens<T, DH, NS>(k, a.kv_stride, tok0, seen, lane, kf);
-    }
-    // (of a chain only the queries from the step's first token on see anything)
-    for (int q0 = !cached && a.causal ? tok0 * a.group / 16 * 16 : 0; q0 < nq; q0 += 16) {
-      const int qi = min(q0 + col, nq - 1), t = qi / a.group;
-      bf16x8 qf[KD][NS];
-#pragma unroll
-      for (int kd = 0; kd < KD; ++kd) load_operand<NS>(q + (size_t)t * a.q_stride + (size_t)(qi % a.group) * DH + kd * 32 + g * 8, qf[kd]);
-      const float2 norm = a.norm[query_at(a, r, hk, qi)];
-      float sv[8];
-      step_scores<KD, NS, NS>(kf, qf, sv);
-      const int there = valid - 8 * g;
-      const uint32_t vis = q0 + col >= nq ? 0u : cached ? (there >= 8 ? 255u : there <= 0 ? 0u : (1u << there) - 1) : sees8(a, t, tok0 + 8 * g, seen);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(sv[i], a.c_exp, -norm.x)) * norm.y;
-        sum[i] += (vis >> i) & 1 ? p : 0.f;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {                 // over the 16 queries of the lane's row
-      float x = sum[i];
-      x += dpp_move<0x128>(x);
-      x += dpp_move<0x141>(x);
-      x += dpp_move<0x4E>(x);
-      x += dpp_move<0xB1>(x);
-      sum[i] = x;
-    }
-    if (col < 8) {
-      float x = sum[0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) x = col == i ? sum[i] : x;
-      const int at = 8 * g + col;
+      for (int i = 0; i < 8; ++i) sum[n][i] = 0.f;
       if (cached) {
-        if (at < valid) a.mass[((size_t)r * a.c.kv_heads + hk) * a.capacity + (size_t)step * kQBlock + at] += x;
-      } else if (tok0 + at < w.n) {
-        a.block_mass[((size_t)r * a.c.kv_heads + hk) * a.T + tok0 + at] = x;
+        const uint8_t* data = a.c.data + (region + step) * a.c.block_bytes();
+        c_exp[n] = fmaxf(a.c_exp * a.c.scale[region + step].x, FLT_MIN);
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd) {
+          const uint4 b = *(const uint4*)(data + (kd * 64 + lane) * 16);
+          kf[n][0][kd][0] = e4m3_to_bf16(make_uint2(b.x, b.y), 1.f);
+          kf[n][1][kd][0] = e4m3_to_bf16(make_uint2(b.z, b.w), 1.f);
+#pragma unroll
+          for (int p = 1; p < NS; ++p) kf[n][0][kd][p] = kf[n][1][kd][p] = as_bf16x8(make_uint4(0, 0, 0, 0));
+        }
+      } else {
+        keys_of_tokens<T, DH, NS>(k, a.kv_stride, tok0[n], seen, lane, kf[n]);
+      }
+    }
+    // (of a chain only the queries from the workgroup's first block token on see anything of block tokens)
+    const int q_first = step0 >= w.blocks && a.causal ? (step0 - w.blocks) * 32 * a.group / 64 * 64 : 0;
+    // a wave brings 16 of the 64 queries that pass by together: into registers while the ones before are at work, then to LDS; +inf as the norm of what is no query
+    bf16x8 next[KD][NS];
+    float next_norm = 0.f;
+    auto load_queries = [&](int q0) {
+      const int at = q0 + wave * 16 + col, qi = min(at, nq - 1), t = qi / a.group;
+#pragma unroll
+      for (int kd = 0; kd < KD; ++kd) load_operand<NS>(q + (size_t)t * a.q_stride + (size_t)(qi % a.group) * DH + kd * 32 + g * 8, next[kd]);
+      const float norm = a.norm[query_at(a, r, hk, qi)];
+      next_norm = at < nq ? norm : INFINITY;
+    };
+    auto put_queries = [&](int buf) {
+#pragma unroll
+      for (int kd = 0; kd < KD; ++kd)
+#pragma unroll
+        for (int p = 0; p < NS; ++p) s_q[buf][wave][kd * NS + p][lane] = __builtin_bit_cast(uint4, next[kd][p]);
+      if (g == 0) s_norm[buf][wave][col] = next_norm;
+    };
+    if (q_first < nq) load_queries(q_first);
+    __syncthreads();
+    if (q_first < nq) put_queries(0);
+    if (q_first + 64 < nq) load_queries(q_first + 64);
+    __syncthreads();
+    int buf = 0;
+    for (int q0 = q_first; q0 < nq; q0 += 64, buf ^= 1) {
+      if (q0 + 64 < nq) put_queries(buf ^ 1);
+      if (q0 + 128 < nq) load_queries(q0 + 128);
+#pragma unroll 2
+      for (int b = 0; b < 4; ++b) {
+        bf16x8 qf[KD][NS];
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd)
+#pragma unroll
+          for (int p = 0; p < NS; ++p) qf[kd][p] = as_bf16x8(s_q[buf][b][kd * NS + p][lane]);
+        const float norm = s_norm[buf][b][col];
+        const int t = min(q0 + b * 16 + col, nq - 1) / a.group, t0 = (q0 + b * 16) / a.group;
+        float sv[STEPS][8];
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n) step_scores<KD, NS, NS>(kf[n], qf, sv[n]);
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n) {
+          if (tok0[n] < 0 || (a.causal && tok0[n] + 31 <= t0)) {       // all queries see all keys that there are (the others' sums are left out below)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[n][i] += __builtin_amdgcn_exp2f(fmaf(sv[n][i], c_exp[n], -norm));
+          } else {
+            const uint32_t vis = sees8(a, t, tok0[n] + 8 * g, seen);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float p = __builtin_amdgcn_exp2f(fmaf(sv[n][i], c_exp[n], -norm));
+              sum[n][i] += (vis >> i) & 1 ? p : 0.f;
+            }
+          }
+        }
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < STEPS; ++n) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {               // over the 16 queries of the lane's row
+        float x = sum[n][i];
+        x += dpp_move<0x128>(x);
+        x += dpp_move<0x141>(x);
+        x += dpp_move<0x4E>(x);
+        x += dpp_move<0xB1>(x);
+        sum[n][i] = x;
+      }
+      if (col < 8) {
+        float x = sum[n][0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) x = col == i ? sum[n][i] : x;
+        const int at = 8 * g + col, step = step0 + wave * STEPS + n;
+        if (at < valid[n]) {
+          if (tok0[n] < 0) a.mass[((size_t)r * a.c.kv_heads + hk) * a.capacity + (size_t)step * kQBlock + at] += x;
+          else a.block_mass[((size_t)r * a.c.kv_heads + hk) * a.T + tok0[n] + at] = x;
+        }
       }
     }
   }
 }
 
-template <typename T, int DH, int NQB>
+template <typename T, int DH, int NQB, bool MANY = false>
 static void attention_t(QAttention a, hipStream_t s) {
-  const int q_tiles = (a.T * a.group + 16 * NQB - 1) / (16 * NQB);
+  constexpr int BLOCKS = MANY ? 4 * NQB : NQB;      // of 16 queries per workgroup
+  const int q_tiles = (a.T * a.group + 16 * BLOCKS - 1) / (16 * BLOCKS);
   const int64_t tiles = (int64_t)a.c.rows * a.c.kv_heads * q_tiles;
   // As many splits as give each CU about four workgroups, but at least four steps to each of a split's waves where the cache is full; the partial results have room for kQParts
-  const int64_t most = (int64_t)kQParts / (tiles * NQB);
+  const int64_t most = (int64_t)kQParts / (tiles * BLOCKS);
   a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / tiles, most, a.c.blocks / 16}));
   // Few counted queries: their scores are kept, 4 bytes per query and slot written and read, where reading the keys again is DH bytes per slot (and many times the work)
   const int counted = a.n_counted * a.group;
-  a.n_kept = (counted || a.block_mass) && counted <= std::min(kQKept, DH / 16) ? counted : 0;
+  a.n_kept = counted <= std::min(kQKept, DH / 16) ? counted : 0;
   if (a.n_kept) a.norm = nullptr;
   const dim3 grid(a.c.kv_heads * q_tiles, a.splits, a.c.rows);
-  hipLaunchKernelGGL((k_qcache_attention<T, DH, NQB>), grid, dim3(256), 0, s, a, q_tiles);
+  if constexpr (MANY) hipLaunchKernelGGL((k_qcache_attention_many<DH>), grid, dim3(256), 0, s, a, q_tiles);
+  else hipLaunchKernelGGL((k_qcache_attention<T, DH, NQB>), grid, dim3(256), 0, s, a, q_tiles);
   if (a.splits > 1) {
-    const int per = 256 / (DH / 4), joins = (16 * NQB + per - 1) / per;
+    const int per = 256 / (DH / 4), joins = (16 * BLOCKS + per - 1) / per;
     // (a workgroup first finds the norms: a few workgroups with much to add rather than many with little)
     const int masses = a.n_kept ? (int)std::max<int64_t>(1, std::min<int64_t>(a.c.blocks / 32, 2048 / ((int64_t)a.c.rows * a.c.kv_heads))) : 0;
-    hipLaunchKernelGGL((k_qcache_join<T, DH>), dim3(grid.x, joins + masses, grid.z), dim3(256), 0, s, a, q_tiles, 16 * NQB, joins);
+    hipLaunchKernelGGL((k_qcache_join<T, DH>), dim3(grid.x, joins + masses, grid.z), dim3(256), 0, s, a, q_tiles, 16 * BLOCKS, joins, 16 * NQB);
   }
   if (!a.n_kept && (a.n_counted > 0 || a.block_mass)) {
-    const int steps = a.c.blocks + (a.T + 31) / 32;
-    hipLaunchKernelGGL((k_qcache_mass<T, DH>), dim3(std::min((steps + 3) / 4, 1024), a.c.kv_heads, a.c.rows), dim3(256), 0, s, a);
+    const int steps = a.c.blocks + (a.T + 31) / 32, per = 4;
+    hipLaunchKernelGGL((k_qcache_mass<T, DH>), dim3(std::min((steps + per - 1) / per, 1024), a.c.kv_heads, a.c.rows), dim3(256), 0, s, a);
   }
 }
 
@@ -960,8 +1314,9 @@ static void attention_d(const QAttention& a, hipStream_t s) {
     attention_t<T, DH, 1>(a, s);
   } else {
     if (nq <= 16) attention_t<T, DH, 1>(a, s);
-    else if (nq <= 32 || DH == 128) attention_t<T, DH, 2>(a, s);
-    else if constexpr (DH < 128) attention_t<T, DH, 4>(a, s);
+    else if (nq <= 32) attention_t<T, DH, 2>(a, s);
+    else if (nq <= 64 && DH < 128) attention_t<T, DH < 128 ? DH : 64, 4>(a, s);
+    else attention_t<T, DH, 2, true>(a, s);
   }
 }
 

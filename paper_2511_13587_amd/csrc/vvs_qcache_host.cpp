@@ -54,7 +54,7 @@ static vvs_status plan_qcache(const vvs_qcache_config* cfg, QCache* c) {
   c->parts_off = off;
   off = align_up(off + (size_t)kQParts * 16 * (g.head_size + 2) * sizeof(float), 256);
   c->norm_off = off;
-  off = align_up(off + (size_t)g.n_rows * g.max_tokens * g.n_heads * sizeof(float2), 256);
+  off = align_up(off + (size_t)g.n_rows * g.max_tokens * g.n_heads * sizeof(float), 256);
   c->origin_off = off;
   off = align_up(off + regions * g.capacity * sizeof(int32_t), 256);
   c->scores_off = off;
@@ -208,7 +208,7 @@ vvs_status vvs_qcache_attention(vvs_qcache* qc, int32_t layer, const int32_t* d_
   a.mass = d_mass; a.block_mass = d_block_mass;
   a.capacity = g.capacity;
   a.lse = d_lse;
-  a.norm = n_counted || d_block_mass ? (float2*)(c->ws + c->norm_off) : nullptr;
+  a.norm = n_counted || d_block_mass ? (float*)(c->ws + c->norm_off) : nullptr;
   a.parts = (float*)(c->ws + c->parts_off);
   a.scores = (float*)(c->ws + c->scores_off);
   a.score_steps = c->score_steps;

@@ -14,7 +14,7 @@ static RopeArgs g_rope_args;
 void launch_qcache_attention(const QAttention& a, int, hipStream_t) {
   if (a.T < 1 || a.c.heads % a.c.kv_heads || !a.q || !a.out || !(a.c_exp > 0.f) || !a.k != !a.v || a.n_counted > a.T || a.c.blocks * kQBlock < a.capacity) abort();
   if (a.q_stride < (size_t)a.c.heads * a.c.dh || a.kv_stride < (size_t)a.c.kv_heads * a.c.dh || (!a.causal && a.T > VVS_MAX_T)) abort();
-  if (a.norm) memset(a.norm, 0, sizeof(float2) * a.c.rows * a.T * a.c.heads);      // inside the workspace
+  if (a.norm) memset(a.norm, 0, sizeof(float) * a.c.rows * a.T * a.c.heads);      // inside the workspace
   if (a.parts) memset(a.parts, 0, sizeof(float) * kQParts * 16 * (a.c.dh + 2));
   g_attn_args = a;
   ++g_attention;
