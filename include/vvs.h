@@ -97,8 +97,15 @@ typedef struct {
                                     VVS_NORM_SEPARATE: always separate normalisation kernels, which
                                       round bf16(x * rsqrt(mean x^2 + eps) * g), the definition's own
                                       rounding point (more launches per layer) */
+  int32_t cache_kind;            /* VVS_CACHE_SAME: cached keys and values have the context's dtype;
+                                    VVS_CACHE_E4M3: they are held in 8 bits (see vvs_qcache below: what is held, and by which rounding), in
+                                      half of the bytes of bf16, for contexts whose cache is what fills HBM.  Keys and values of the tokens of
+                                      a call are taken as they are (a verify call: of all its nodes; a prefill: of a chunk of up to 512 tokens, fp32
+                                      64), and rounded when they are cached.  Layers run as separate launches (no drafter contexts; head size 32,
+                                      64 or 128, as the dtype allows), so that calls of few rows take longer than with VVS_CACHE_SAME */
 } vvs_config;
 enum { VVS_NORM_AUTO = 0, VVS_NORM_SEPARATE = 1 };
+enum { VVS_CACHE_SAME = 0, VVS_CACHE_E4M3 = 1 };
 #define VVS_MAX_FEATURE_SLOTS 8
 
 /* Sizes in bytes of the three device buffers a context needs.  VVS_ESIZE if the shape is not
@@ -223,6 +230,13 @@ vvs_status vvs_accept_from_logits_noalloc(vvs_ctx* ctx, int32_t n_nodes, const i
  * into consecutive cache slots S_b .. S_b + a_b, advances S_b and n_emitted_b by a_b + 1 and makes
  * next_token the pending token.  Exactly one commit per verify. */
 vvs_status vvs_kv_commit(vvs_ctx* ctx, vvs_stream s);
+
+/* Contexts with VVS_CACHE_E4M3: shortens the cache of every prompt whose length is above `keep` to `keep` slots per layer, row and head, as
+ * vvs_qcache_evict does: the slots with the largest accumulated attention weight stay, and the `recent` newest tokens.  Weights are accumulated by the library: of all
+ * tokens of a prefill, and of those tokens of a verify call that are certain to be kept (the pending token and the post-verified ones), over cached slots.
+ * Positions of later tokens do not change; S_b does.  Not between a verify and its commit (VVS_ESTATE).
+ *   keep: a multiple of VVS_QCACHE_BLOCK, at least one block; recent: in [0, keep] */
+vvs_status vvs_kv_evict(vvs_ctx* ctx, int32_t keep, int32_t recent, vvs_stream s);
 
 /* Token-level feature cache (Section 4.3; Algorithm 2, "UpdateCache").  vvs_prefill stores the feature
  * of the last prefilled position of every row, vvs_kv_commit appends the features of the tokens it
@@ -449,7 +463,7 @@ vvs_status vvs_debug_logits(vvs_ctx* ctx, float* d_raw_logits, float* d_mixed_lo
                             vvs_stream s);
 
 /* Cached K and V of one (layer, row) as float [n_slots, d_model] (head-major inside a row), slots
- * 0 .. n_slots - 1. */
+ * 0 .. n_slots - 1 (after vvs_kv_evict a slot holds another token for every head). */
 vvs_status vvs_debug_kv(vvs_ctx* ctx, int32_t layer, int32_t row, int32_t n_slots, float* d_k, float* d_v,
                         vvs_stream s);
 

@@ -20,6 +20,7 @@ VVS_OK, VVS_EINVAL, VVS_ESTATE, VVS_ESIZE, VVS_EHIP = 0, -1, -2, -3, -4
 VVS_FP32, VVS_BF16 = 0, 1
 VVS_STRICT, VVS_RELAXED = 0, 1
 VVS_NORM_AUTO, VVS_NORM_SEPARATE = 0, 1
+VVS_CACHE_SAME, VVS_CACHE_E4M3 = 0, 1
 VVS_MAX_T = 64
 VVS_QCACHE_BLOCK = 32
 VVS_ROPE_MAX_AXES = 4
@@ -35,7 +36,7 @@ class VvsConfig(C.Structure):
                [("cfg_scale", C.c_float), ("rms_eps", C.c_float), ("rope_base", C.c_float),
                 ("relax_k", C.c_int32), ("relax_delta", C.c_float),
                 ("feature_slots", C.c_int32), ("feature_pre_norm", C.c_int32), ("draft_input", C.c_int32),
-                ("norm_mode", C.c_int32)]
+                ("norm_mode", C.c_int32), ("cache_kind", C.c_int32)]
 
 
 class VvsQCacheConfig(C.Structure):
@@ -82,6 +83,7 @@ def _load():
         "vvs_accept_from_logits": (i32, [vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]),
         "vvs_accept_from_logits_noalloc": (i32, [vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]),
         "vvs_kv_commit": (i32, [vp, vp]),
+        "vvs_kv_evict": (i32, [vp, i32, i32, vp]),
         "vvs_read_state": (i32, [vp, vp, vp]),
         "vvs_set_state": (i32, [vp, vp, vp]),
         "vvs_timing_enable": (i32, [vp, i32]),
@@ -116,13 +118,13 @@ lib, EXPORTS = _load()
 
 
 def make_config(shape, max_nodes: Optional[int] = None, feature_slots: int = 5, feature_pre_norm: int = 0,
-                draft_input: int = 0, norm_mode: int = 0) -> VvsConfig:
+                draft_input: int = 0, norm_mode: int = 0, cache_kind: int = 0) -> VvsConfig:
     """vvs_config from a synth.Shape-like object."""
     return VvsConfig(shape.n_layers, shape.d_model, shape.n_heads, shape.d_ff, shape.vocab, shape.logit_lo,
                      shape.logit_hi, shape.grid_h, shape.grid_w, shape.prefix_len, shape.prefix_kind,
                      shape.n_classes, shape.n_prompts, shape.n_nodes if max_nodes is None else max_nodes,
                      shape.dtype, shape.cfg_scale, shape.rms_eps, shape.rope_base, shape.relax_k, shape.relax_delta,
-                     feature_slots, feature_pre_norm, draft_input, norm_mode)
+                     feature_slots, feature_pre_norm, draft_input, norm_mode, cache_kind)
 
 
 def vvs_query_sizes(cfg: VvsConfig):
@@ -324,6 +326,9 @@ class Context:
     def vvs_kv_commit(self):
         self._check(lib.vvs_kv_commit(self.h, _stream()))
 
+    def vvs_kv_evict(self, keep: int, recent: int):
+        self._check(lib.vvs_kv_evict(self.h, keep, recent, _stream()))
+
     # -- inspection ----------------------------------------------------------------------------
     def vvs_plan_is_fused(self, n_tokens: int) -> bool:
         return bool(lib.vvs_plan_is_fused(self.h, n_tokens))
@@ -389,35 +394,65 @@ class Context:
 
 
 # ---------------------------------------------------------------------------------------------- operators beside a context
-def _on(t: Optional[torch.Tensor], device: torch.device, dtype: torch.dtype, shape, what: str):
-    """Pointer of a contiguous tensor of the library's arguments (None stays None)."""
+def _wrong(what: str, t: torch.Tensor, device: int, dtype: torch.dtype, shape):
+    raise ValueError(f"{what}: wants a {dtype} tensor {list(shape)} on device {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+
+
+def _on(t: Optional[torch.Tensor], device: int, dtype: torch.dtype, shape, what: str):
+    """Pointer of a contiguous tensor of the library's arguments (None stays None); device: its index, -1 for the host."""
     if t is None:
         return None
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{what}: wants a contiguous {dtype} tensor {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    if t.get_device() != device or t.dtype != dtype or t.shape != shape:
+        _wrong(what, t, device, dtype, shape)
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: wants a contiguous tensor, got strides {t.stride()}")
     return t.data_ptr()
 
 
-def _per_token(t: Optional[torch.Tensor], device: torch.device, dtype: torch.dtype, shape, what: str):
+def _per_token(t: Optional[torch.Tensor], device: int, dtype: torch.dtype, shape, what: str):
     """(pointer, elements from token to token) of a tensor [..., tokens, heads, size] that may be a part of a wider one: heads and dims contiguous, every
     dimension in front of them in steps of whole tokens."""
     if t is None:
         return None, 0
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: wants a {dtype} tensor {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
-    heads, size = t.shape[-2:]
-    token = t.stride(-3) if t.shape[-3] > 1 else None
-    n = 1                                # tokens below each dimension
-    ok = (t.stride(-1) == 1 or size == 1) and (t.stride(-2) == size or heads == 1)
-    for d in range(t.dim() - 3, -1, -1):
-        if t.shape[d] > 1:
-            token = t.stride(d) // n if token is None else token
-            ok = ok and t.stride(d) == token * n
-        n *= t.shape[d]
+    if t.get_device() != device or t.dtype != dtype or t.shape != shape:
+        _wrong(what, t, device, dtype, shape)
+    heads, size = shape[-2], shape[-1]
+    if t.is_contiguous():
+        return t.data_ptr(), heads * size
+    strides = t.stride()
+    token, n = None, 1                   # n: tokens below each dimension
+    ok = (strides[-1] == 1 or size == 1) and (strides[-2] == size or heads == 1)
+    for d in range(len(shape) - 3, -1, -1):
+        if shape[d] > 1:
+            if token is None:
+                token = strides[d] // n
+            ok = ok and strides[d] == token * n
+        n *= shape[d]
     token = heads * size if token is None else token
     if not ok or token < heads * size:
-        raise ValueError(f"{what}: strides {t.stride()} of {list(t.shape)} are not those of tokens one after the other")
+        raise ValueError(f"{what}: strides {strides} of {list(shape)} are not those of tokens one after the other")
     return t.data_ptr(), token
+
+
+_raw_stream = torch._C._cuda_getCurrentRawStream     # (current_stream() makes a stream object each time: 1.5 us of a 5 us call)
+
+
+class _Current:
+    """Makes a device current for a call, where it is not already (torch.cuda.device does it always: 2 us)."""
+
+    def __init__(self, index: int):
+        self.index, self.was = index, []
+
+    def __enter__(self):
+        now = torch.cuda.current_device()
+        self.was.append(now)
+        if now != self.index:
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        was = self.was.pop()
+        if was != self.index:
+            torch.cuda.set_device(was)
 
 
 _TORCH_DTYPE = {VVS_FP32: torch.float32, VVS_BF16: torch.bfloat16}
@@ -434,7 +469,8 @@ class QCache:
         if not torch.cuda.is_available():
             raise RuntimeError("libvvs needs a HIP device; there is no CPU path")
         self.device, self.dtype = torch.device(device), _TORCH_DTYPE[dtype]
-        with torch.cuda.device(self.device):
+        self.index = torch.cuda.current_device() if self.device.index is None else self.device.index
+        with torch.cuda.device(self.index):
             self.cache = torch.empty(self.cache_bytes, dtype=torch.uint8, device=self.device)
             self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
             torch.cuda.synchronize()
@@ -443,10 +479,11 @@ class QCache:
         if st != VVS_OK:
             raise VvsError(st, (lib.vvs_last_error(None) or b"").decode())
         self.h = h
+        self.shape = (n_rows, n_heads, n_kv_heads, head_size, capacity)      # (a field of the ctypes structure is 0.1 us to read)
 
     def close(self):
         if getattr(self, "h", None):
-            torch.cuda.synchronize(self.device)
+            torch.cuda.synchronize(self.index)
             lib.vvs_qcache_destroy(self.h)
             self.h = None
 
@@ -461,67 +498,67 @@ class QCache:
             raise VvsError(st, (lib.vvs_qcache_last_error(self.h) or b"").decode())
 
     def _rows(self, t, what):
-        return _on(t, self.device, torch.int32, (self.cfg.n_rows,), what)
+        return _on(t, self.index, torch.int32, self.shape[:1], what)
 
     def vvs_qcache_append(self, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_tokens: Optional[torch.Tensor] = None,
                           select: Optional[torch.Tensor] = None, layer: int = 0, n_layers: int = 1):
         """k, v [n_layers, rows, tokens, kv heads, size]; select int32 [rows, n]: the tokens taken; n_tokens int32 [rows]: how many of them."""
-        g = self.cfg
+        rows, heads, kv, size, capacity = self.shape
         src = k.shape[2] if k.dim() == 5 else 0
-        shape = (n_layers, g.n_rows, src, g.n_kv_heads, g.head_size)
-        kp, ks = _per_token(k, self.device, self.dtype, shape, "k")
-        vp, vs = _per_token(v, self.device, self.dtype, shape, "v")
+        shape = (n_layers, rows, src, kv, size)
+        kp, ks = _per_token(k, self.index, self.dtype, shape, "k")
+        vp, vs = _per_token(v, self.index, self.dtype, shape, "v")
         if ks != vs:
             raise ValueError("k and v have different strides")
         n = src if select is None else int(select.shape[1])
-        with torch.cuda.device(self.device):
+        with _Current(self.index):
             self._check(lib.vvs_qcache_append(self.h, layer, n_layers, self._rows(length, "length"), n, self._rows(n_tokens, "n_tokens"), src,
-                                              _on(select, self.device, torch.int32, (g.n_rows, n), "select"), kp, vp, ks, _stream()))
+                                              _on(select, self.index, torch.int32, (rows, n), "select"), kp, vp, ks, _raw_stream(self.index)))
 
     def vvs_qcache_attention(self, length: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor], v: Optional[torch.Tensor], out: torch.Tensor,
                              n_tokens: Optional[torch.Tensor] = None, parent=None, tree_mask=None, scale: Optional[float] = None,
                              lse: Optional[torch.Tensor] = None, n_counted: int = 0, mass: Optional[torch.Tensor] = None,
                              block_mass: Optional[torch.Tensor] = None, layer: int = 0):
         """q [rows, tokens, heads, size]; k, v [rows, tokens, kv heads, size] or None; out like q, contiguous.  scale: None = size ** -0.5."""
-        g = self.cfg
+        rows, heads, kv, size, capacity = self.shape
         t = q.shape[1] if q.dim() == 4 else 0
-        qp, qs = _per_token(q, self.device, self.dtype, (g.n_rows, t, g.n_heads, g.head_size), "q")
-        kp, ks = _per_token(k, self.device, self.dtype, (g.n_rows, t, g.n_kv_heads, g.head_size), "k")
-        vp, vs = _per_token(v, self.device, self.dtype, (g.n_rows, t, g.n_kv_heads, g.head_size), "v")
+        qp, qs = _per_token(q, self.index, self.dtype, (rows, t, heads, size), "q")
+        kp, ks = _per_token(k, self.index, self.dtype, (rows, t, kv, size), "k")
+        vp, vs = _per_token(v, self.index, self.dtype, (rows, t, kv, size), "v")
         if ks != vs:
             raise ValueError("k and v have different strides, or only one of them is given")
         p = None if parent is None else np.ascontiguousarray(parent, dtype=np.int32)
         m = None if tree_mask is None else np.ascontiguousarray(tree_mask, dtype=np.uint8)
         if (p is not None and p.shape != (t - 1,)) or (m is not None and m.shape != (t, t)):
             raise ValueError("parent wants [tokens - 1] and tree_mask [tokens, tokens] entries")
-        with torch.cuda.device(self.device):
+        with _Current(self.index):
             self._check(lib.vvs_qcache_attention(
                 self.h, layer, self._rows(length, "length"), t, self._rows(n_tokens, "n_tokens"), None if p is None else p.ctypes.data,
-                None if m is None else m.ctypes.data, qp, qs, kp, vp, ks, g.head_size ** -0.5 if scale is None else float(scale),
-                _on(out, self.device, self.dtype, (g.n_rows, t, g.n_heads, g.head_size), "out"),
-                _on(lse, self.device, torch.float32, (g.n_rows, t, g.n_heads), "lse"), n_counted,
-                _on(mass, self.device, torch.float32, (g.n_rows, g.n_kv_heads, g.capacity), "mass"),
-                _on(block_mass, self.device, torch.float32, (g.n_rows, g.n_kv_heads, t), "block_mass"), _stream()))
+                None if m is None else m.ctypes.data, qp, qs, kp, vp, ks, size ** -0.5 if scale is None else float(scale),
+                _on(out, self.index, self.dtype, (rows, t, heads, size), "out"),
+                _on(lse, self.index, torch.float32, (rows, t, heads), "lse"), n_counted,
+                _on(mass, self.index, torch.float32, (rows, kv, capacity), "mass"),
+                _on(block_mass, self.index, torch.float32, (rows, kv, t), "block_mass"), _raw_stream(self.index)))
 
     def vvs_qcache_evict(self, length: torch.Tensor, keep: int, recent: int, mass: torch.Tensor, mass_out: torch.Tensor,
                          pos: Optional[torch.Tensor] = None, pos_out: Optional[torch.Tensor] = None, layer: int = 0, n_layers: int = 1):
         """mass, mass_out float32, pos, pos_out int32 [n_layers, rows, kv heads, capacity]; an output may be its input."""
-        g = self.cfg
-        shape = (n_layers, g.n_rows, g.n_kv_heads, g.capacity)
-        with torch.cuda.device(self.device):
+        rows, heads, kv, size, capacity = self.shape
+        shape = (n_layers, rows, kv, capacity)
+        with _Current(self.index):
             self._check(lib.vvs_qcache_evict(self.h, layer, n_layers, self._rows(length, "length"), keep, recent,
-                                             _on(mass, self.device, torch.float32, shape, "mass"), _on(mass_out, self.device, torch.float32, shape, "mass_out"),
-                                             _on(pos, self.device, torch.int32, shape, "pos"), _on(pos_out, self.device, torch.int32, shape, "pos_out"),
-                                             _stream()))
+                                             _on(mass, self.index, torch.float32, shape, "mass"), _on(mass_out, self.index, torch.float32, shape, "mass_out"),
+                                             _on(pos, self.index, torch.int32, shape, "pos"), _on(pos_out, self.index, torch.int32, shape, "pos_out"),
+                                             _raw_stream(self.index)))
 
     def vvs_qcache_read(self, length: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: Optional[torch.Tensor] = None, layer: int = 0, n_layers: int = 1):
         """k, v [n_layers, rows, slots, kv heads, size] out."""
-        g = self.cfg
+        rows, heads, kv, size, capacity = self.shape
         n = k.shape[2] if k.dim() == 5 else 0
-        shape = (n_layers, g.n_rows, n, g.n_kv_heads, g.head_size)
-        with torch.cuda.device(self.device):
+        shape = (n_layers, rows, n, kv, size)
+        with _Current(self.index):
             self._check(lib.vvs_qcache_read(self.h, layer, n_layers, self._rows(length, "length"), self._rows(first, "first"), n,
-                                            _on(k, self.device, self.dtype, shape, "k"), _on(v, self.device, self.dtype, shape, "v"), _stream()))
+                                            _on(k, self.index, self.dtype, shape, "k"), _on(v, self.index, self.dtype, shape, "v"), _raw_stream(self.index)))
 
 
 def vvs_qcache_query_sizes(cfg: VvsQCacheConfig):
@@ -544,7 +581,7 @@ class Rope:
         st = lib.vvs_rope_create(C.byref(self.cfg), C.byref(h))
         if st != VVS_OK:
             raise VvsError(st, (lib.vvs_last_error(None) or b"").decode())
-        self.h = h
+        self.h, self.size, self.axes, self.dtype = h, head_size, len(pairs), _TORCH_DTYPE[dtype]
 
     def close(self):
         if getattr(self, "h", None):
@@ -560,19 +597,20 @@ class Rope:
     def vvs_rope_apply(self, pos: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor], q_out: torch.Tensor, k_out: Optional[torch.Tensor],
                        inverse: bool = False):
         """pos int32 [..., axes]; q, k, q_out, k_out [..., heads, size] with the same leading dimensions; an output may be its input."""
-        device, dtype, lead = q.device, _TORCH_DTYPE[self.cfg.dtype], tuple(q.shape[:-2])
-        if not q.is_cuda or q.dim() < 3:
+        device, dtype, size = q.get_device(), self.dtype, self.size
+        *lead, heads, _ = shape = tuple(q.shape)
+        if device < 0 or not lead:
             raise ValueError("q: wants a tensor [..., heads, size] on a HIP device")
         n = 1
         for d in lead:
             n *= d
-        qp, qs = _per_token(q, device, dtype, (*lead, q.shape[-2], self.cfg.head_size), "q")
-        op, os_ = _per_token(q_out, device, dtype, q.shape, "q_out")
+        qp, qs = _per_token(q, device, dtype, (*lead, heads, size), "q")
+        op, os_ = _per_token(q_out, device, dtype, shape, "q_out")
         kv = 0 if k is None else k.shape[-2]
-        kp, ks = _per_token(k, device, dtype, (*lead, kv, self.cfg.head_size), "k")
-        kop, kos = _per_token(k_out, device, dtype, (*lead, kv, self.cfg.head_size), "k_out")
-        with torch.cuda.device(device):
-            st = lib.vvs_rope_apply(self.h, n, _on(pos, device, torch.int32, (*lead, self.cfg.n_axes), "pos"), q.shape[-2], qp, qs, op, os_, kv, kp, ks, kop, kos,
-                                    1 if inverse else 0, _stream())
+        kp, ks = _per_token(k, device, dtype, (*lead, kv, size), "k")
+        kop, kos = _per_token(k_out, device, dtype, (*lead, kv, size), "k_out")
+        with _Current(device):
+            st = lib.vvs_rope_apply(self.h, n, _on(pos, device, torch.int32, (*lead, self.axes), "pos"), heads, qp, qs, op, os_, kv, kp, ks, kop, kos,
+                                    1 if inverse else 0, _raw_stream(device))
         if st != VVS_OK:
             raise VvsError(st, (lib.vvs_rope_last_error(self.h) or b"").decode())

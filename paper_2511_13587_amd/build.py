@@ -7,7 +7,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libvvs.so")
 SOURCES = ["vvs_host.cpp", "vvs_kernels.hip", "vvs_accept.hip", "vvs_mfma.hip", "vvs_few.hip", "vvs_schedule.hip", "vvs_draft.hip",
-           "vvs_qcache_host.cpp", "vvs_qcache.hip", "vvs_rope.hip"]
+           "vvs_qcache_host.cpp", "vvs_qcache.hip", "vvs_qcache_ctx.hip",
+           "vvs_rope.hip"]
 
 
 def build(verbose: bool = True) -> str:

@@ -1,6 +1,7 @@
 // Host side of libvvs: argument validation, buffer planning, tree tables and the C ABI entry
 // points.  Everything here runs before any launch, so bad input never reaches a kernel.
 #include "vvs_internal.h"
+#include "vvs_qcache.h"
 
 #include <math.h>
 #include <stdio.h>
@@ -179,6 +180,7 @@ GemmPlan plan_resid(const Ctx* c, int M) {
 // the layer is (measured without any kernel: 2 x the noise floor of a correct bf16 evaluation at d = 1280,
 // 3 x at d = 4096).
 bool plan_fused(const Ctx* c, int M) {
+  if (c->cfg.cache_kind) return false;      // the fused layer writes a cache of the context's dtype
   (void)M;
   if (c->cfg.dtype != VVS_BF16 || c->cfg.norm_mode == VVS_NORM_SEPARATE) return false;
   const size_t layer_weight_bytes = c->esz * ((size_t)4 * c->d * c->d + (size_t)3 * c->d * c->F);
@@ -221,7 +223,7 @@ int few_rows(const Ctx* c) {
 //     (13440) 356 / 398, 768 (6144) 570 / 543, (7680) 589 / 634, 896 (8960) 541 / 570, 1024 (8192) 1.14, (10240) 484 / 494, 1280 (10240) 1.02 (O and down share
 //     their operands through LDS where d is a multiple of 128)
 int few_wide_rows(const Ctx* c) {
-  if (plan_fused(c, c->R) || c->cfg.dtype != VVS_BF16 || c->cfg.draft_input || c->d > 4096) return 0;
+  if (plan_fused(c, c->R) || c->cfg.dtype != VVS_BF16 || c->cfg.draft_input || c->d > 4096 || c->cfg.cache_kind) return 0;
   const size_t layer_weight_bytes = c->esz * ((size_t)4 * c->d * c->d + (size_t)3 * c->d * c->F);
   const int d = c->d, F = c->F;
   if (layer_weight_bytes > (size_t)440 << 20 || (d >= 3584 && F > 12288)) return 0;
@@ -262,7 +264,10 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   if (g.feature_pre_norm != 0 && g.feature_pre_norm != 1) return fail(err, VVS_EINVAL, "config: feature_pre_norm must be 0 or 1");
   if (g.draft_input != 0 && g.draft_input != 1) return fail(err, VVS_EINVAL, "config: draft_input must be 0 or 1");
   if (g.norm_mode != VVS_NORM_AUTO && g.norm_mode != VVS_NORM_SEPARATE) return fail(err, VVS_EINVAL, "config: unknown norm_mode");
+  if (g.cache_kind != VVS_CACHE_SAME && g.cache_kind != VVS_CACHE_E4M3) return fail(err, VVS_EINVAL, "config: unknown cache_kind");
+  if (g.cache_kind && g.draft_input) return fail(err, VVS_EINVAL, "config: a drafter context keeps no cache (cache_kind must be VVS_CACHE_SAME)");
   int dh = g.d_model / g.n_heads;
+  if (g.cache_kind && dh != 32 && dh != 64 && dh != 128) return fail(err, VVS_ESIZE, "config: VVS_CACHE_E4M3 needs head size 32, 64 or 128");
   if (dh % 4) return fail(err, VVS_ESIZE, "config: head size must be a multiple of 4 (2D rotary pairs)");
   if (g.d_model % 8 || g.d_ff % 8) return fail(err, VVS_ESIZE, "config: d_model and d_ff must be multiples of 8");
   if (g.d_model > 16384) return fail(err, VVS_ESIZE, "config: d_model above 16384 is not supported");
@@ -298,6 +303,16 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   c->kv_row_stride = c->kv_head_stride * c->H;
   c->kv_layer_stride = c->kv_row_stride * c->R;
   c->kv_v_off = c->kv_layer_stride * c->L;
+  c->kv_bytes = 2 * c->kv_v_off * c->esz;
+  if (g.cache_kind) {          // blocks of keys and values, their powers of two, weights and positions of the slots
+    const size_t slots = (size_t)c->L * c->R * c->H * c->S_cap, blocks = slots / kQBlock;
+    if (blocks > ((size_t)1 << 31) - 1) return fail(err, VVS_ESIZE, "config: 2^31 cache blocks or more");
+    c->q_scale = align_up(2 * slots * dh, 256);
+    c->q_mass = c->q_scale + align_up(blocks * sizeof(float2), 256);
+    c->q_slot_pos = c->q_mass + align_up(slots * sizeof(float), 256);
+    c->kv_bytes = c->q_slot_pos + align_up(slots * sizeof(int32_t), 256);
+    for (int j = 0; j < dh / 2; ++j) c->rope_turns[j] = pow((double)g.rope_base, -2.0 * (j % (dh / 4)) / (dh / 2)) / (2.0 * M_PI);
+  }
   // GEMM partial-sum buffer: worst case over every M this context can be asked for, projection by projection, each with the plan that its
   // launch takes (run_gemm; told apart by their sizes, two with the same columns or contraction would get one plan).  Sums that come whole
   // are written by the projection's own epilogue where it has one.  All limits of a plan lie on multiples of 32 rows, so the largest M of
@@ -309,6 +324,7 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
       if ((size_t)std::min(8, K / 32 / 15 + 1) * M * N > go) go = std::max(go, (size_t)plan_partial(c, M, N, K).splits * M * N);
     };
     const bool bf16 = g.dtype == VVS_BF16;
+    if (g.cache_kind) sums(3 * d, d);
     if (!bf16 || (!takes_shared(M, 3 * d, d) && plan_qkv(c, M).splits > 1)) sums(3 * d, d);   // (the shared-operand tiles of the two: whole sums)
     if (!bf16 || !takes_shared(M, 2 * F, d) || gate_up_own(c, M)) {
       const int shares = plan_gate_up(c, M).splits;
@@ -350,6 +366,15 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   w.ss2 = take(sizeof(float) * (size_t)c->Mlog * n_slabs(d));
   w.ring = take(c->esz * (size_t)c->R * std::max(g.feature_slots, 1) * d);
   w.din = take(g.draft_input ? c->esz * (size_t)c->Mmax * 2 * d : 0);                // drafter: [embedding ; feature] rows
+  const int widest = std::max(c->Tmax, c->chunk), one_layer = g.cache_kind ? std::max(c->L * c->Tmax, c->chunk) : 0;
+  const size_t heads = g.cache_kind ? (size_t)c->R * c->H : 0;
+  c->stage_v = (size_t)c->R * one_layer * d;                                         // a verify call's keys and values wait for the commit, a prefill chunk's for their layer's append
+  w.q_stage = take(c->esz * 2 * c->stage_v);
+  w.q_pos = take(g.cache_kind ? sizeof(int32_t) * 2 * c->Mmax : 0);
+  w.q_parts = take(g.cache_kind ? qcache_parts_bytes(dh) : 0);
+  w.q_norm = take(sizeof(float) * heads * widest);
+  w.q_origin = take(sizeof(int32_t) * heads * c->S_cap * c->L);
+  w.q_scores = take(sizeof(float) * heads * qcache_score_steps(c->S_cap / kQBlock, widest) * kQKept * kQBlock);
   w.total = off;
   // packed weights
   PackedLayout& p = c->p;
@@ -475,7 +500,7 @@ vvs_status vvs_query_sizes(const vvs_config* cfg, size_t* kv_bytes, size_t* work
   Ctx c{};
   vvs_status st = plan_sizes(cfg, &c, nullptr);
   if (st != VVS_OK) return st;
-  if (kv_bytes) *kv_bytes = 2 * c.kv_v_off * c.esz;
+  if (kv_bytes) *kv_bytes = c.kv_bytes;
   if (workspace_bytes) *workspace_bytes = c.w.total;
   if (packed_weight_bytes) *packed_weight_bytes = c.p.total;
   return VVS_OK;
@@ -524,7 +549,7 @@ vvs_status vvs_create(const vvs_config* cfg, void* d_kv, void* d_workspace, void
   c->code_dim = 0;
   c->wait_polls = kFewPolls;
   // zero the KV cache (padded slots are read, multiplied by zero weights) and the state block
-  launch_fill_zero(c->kv, 2 * c->kv_v_off * c->esz, nullptr);
+  launch_fill_zero(c->kv, c->kv_bytes, nullptr);
   launch_fill_zero(c->ws, c->w.x, nullptr);
   // rotary table in double -> float: [pos][pair] (cos, sin); theta_i = base^(-2i / (dh/2))
   int np = c->dh / 4;

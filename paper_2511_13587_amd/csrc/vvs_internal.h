@@ -39,7 +39,7 @@ struct GemmPlan { int bm, bn, splits; bool row_owner = false, shared = false; };
 
 // Byte offsets into the caller's workspace.
 struct Workspace {
-  size_t state, outcome, node_result, tokens, rope_tab, x, h, gemm_out, q, attn, act, hf, logits, probs,
+  size_t state, outcome, node_result, tokens, rope_tab, x, h, gemm_out, q, attn, act, hf, logits, probs, q_stage, q_pos, q_parts, q_norm, q_origin, q_scores,
       pq_work, ss, ss2, ring, ring_state, din, few_sync, few_buf, few_gave_up, walk_sync, total;
 };
 
@@ -59,6 +59,10 @@ struct Ctx {
   size_t esz;                            // bytes per model element
   char* kv; char* ws; char* pw;
   size_t kv_layer_stride, kv_row_stride, kv_head_stride, kv_v_off;  // in elements; V half starts at kv_v_off
+  size_t kv_bytes;                       // of the caller's buffer
+  size_t q_scale, q_mass, q_slot_pos;    // VVS_CACHE_E4M3: byte offsets into it - powers of two, accumulated weights and positions of the slots
+  size_t stage_v;                        // ... elements from staged keys to staged values
+  double rope_turns[128];                // ... turns per position of each rotated pair of a head
   Workspace w;
   PackedLayout p;
   size_t gemm_out_elems;
@@ -126,6 +130,7 @@ vvs_status launch_accept_noalloc(Ctx* c, const TreeDesc& tree, int T, const floa
                                  hipStream_t s, std::string* err);
 void launch_prefill_finish(Ctx* c, int n_forced, int32_t* d_first, hipStream_t s);
 void launch_commit(Ctx* c, hipStream_t s);
+void launch_evict(Ctx* c, int keep, int recent, hipStream_t s);
 void launch_push_prefill_feature(Ctx* c, int T_last_chunk, hipStream_t s);
 void launch_read_features(Ctx* c, float* d_features, int32_t* d_count, hipStream_t s);
 void launch_path_similarity(Ctx* c, const TreeDesc& tree, int n_nodes, const int32_t* d_draft_tokens, float alpha, int stride,

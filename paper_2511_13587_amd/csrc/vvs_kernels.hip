@@ -3,6 +3,7 @@
 // The bf16 GEMM and attention kernels (MFMA) live in vvs_mfma.hip; the acceptance stage in
 // vvs_accept.hip.
 #include "vvs_device.h"
+#include "vvs_qcache.h"
 
 #include <stdlib.h>
 #include <algorithm>
@@ -824,7 +825,8 @@ static void forward_t(Ctx* c, const TreeDesc& tree, const PosDesc& pos, int Tq, 
   // The limits are where the parity tests of the small layer end, not where it stops paying.  Step of 3 layers, plain / small, us: at the limits
   // d 1024, d_ff 4096, 128 rows 1014 / 824; beyond each, 256 rows (d 1024, d_ff 2752) 1405 / 1222, d 1280 (128 rows) 1205 / 1008, d_ff 5504
   // (128 rows) 1297 / 1029; well inside, d 128 with 10 rows 138 / 91.
-  if (sizeof(T) == 4 && M <= 128 && d <= 1024 && F <= 4096) {
+  const bool held8 = c->cfg.cache_kind == VVS_CACHE_E4M3;
+  if (sizeof(T) == 4 && M <= 128 && d <= 1024 && F <= 4096 && !held8) {
     forward_small(c, tree, pos, Tq, d_tokens_bt, pc, pu, chunk_start, forced, n_forced, logits_mode, s, from_din);
     return;
   }
@@ -848,6 +850,7 @@ static void forward_t(Ctx* c, const TreeDesc& tree, const PosDesc& pos, int Tq, 
     hipLaunchKernelGGL(k_embed<T>, dim3(M), dim3(256), 0, s, x, (const T*)(c->pw + c->p.embed),
                        (const T*)(c->pw + c->p.prefix_embed), ea);
   }
+  if (held8) { Timed timed(c, VVS_K_ELEMENTWISE, s); launch_context_positions(c, tree, pos, Tq, s); }
   const bool wide = layers_in_one_launch(c, Tq);
   if (wide) {
     Timed timed(c, VVS_K_GEMM, s);
@@ -867,7 +870,11 @@ static void forward_t(Ctx* c, const TreeDesc& tree, const PosDesc& pos, int Tq, 
     // with 160+ tiles an unsplit projection streams its weights as fast as a split one, and its epilogue
     // does the rotary embedding and the cache write: one kernel less
     if (pq.splits > 1 && ((M + pq.bm - 1) / pq.bm) * (3 * d / pq.bn) >= 160) pq.splits = 1;
-    if (c->cfg.dtype == VVS_BF16 && pq.splits == 1) {
+    if (held8) {
+      sp = run_gemm(c, h, lw + c->p.wqkv, go, M, 3 * d, d, plan_partial(c, M, 3 * d, d), s);
+      Timed timed(c, VVS_K_ELEMENTWISE, s);
+      launch_context_rope(c, l, M, go, sp, s);
+    } else if (c->cfg.dtype == VVS_BF16 && pq.splits == 1) {
       Timed timed(c, VVS_K_GEMM, s);           // projection + rotary + cache write in one kernel
       mfma_gemm_qkv(c, l, (const bf16_t*)h, (const bf16_t*)(lw + c->p.wqkv), nullptr, tree, pos, Tq, pq, s);
     } else {
@@ -876,7 +883,10 @@ static void forward_t(Ctx* c, const TreeDesc& tree, const PosDesc& pos, int Tq, 
       hipLaunchKernelGGL(k_rope_kv<T>, dim3(M, ((d >> 1) + 255) / 256), dim3(256), 0, s, go, sp, (size_t)M * 3 * d, q, kc, vc, rope, tree, pos, Tq, d, c->dh,
                          c->kv_row_stride, c->kv_head_stride, c->S_cap, c->rope_pos);
     }
-    if constexpr (sizeof(T) == 2) {
+    if (held8) {
+      Timed timed(c, VVS_K_ATTENTION, s);
+      launch_context_attention(c, l, tree, pos, Tq, s);
+    } else if constexpr (sizeof(T) == 2) {
       Timed timed(c, VVS_K_ATTENTION, s);
       mfma_attention(c, l, tree, pos, Tq, s);
     } else {
@@ -1081,6 +1091,17 @@ void launch_commit(Ctx* c, hipStream_t s) {
   const PushArgs push = push_args(c, path, c->last_T, -1);
   const CommitState cs{(int32_t*)(c->ws + c->w.state), (int32_t*)(c->ws + c->w.ring_state), oc + kOutcomeSnap * c->B, c->cfg.feature_slots, c->B};
   dim3 grid(c->R, c->L + (slots > 0), std::max((items + 255) / 256, slots));
+  if (c->cfg.cache_kind == VVS_CACHE_E4M3) {     // the accepted tokens are rounded into the cache; state and features as ever (a layer of no heads has nothing to move)
+    launch_context_append(c, s);
+    grid = dim3(c->R, 1 + (slots > 0), std::max(1, slots));
+    if (c->cfg.dtype == VVS_BF16)
+      hipLaunchKernelGGL((k_commit_kv<bf16_t, bf16_t>), grid, dim3(256), 0, s, (bf16_t*)c->kv, (bf16_t*)c->kv, cs, accept_len, next_token, path, 0, c->dh, (size_t)0, (size_t)0,
+                         (size_t)0, c->S_cap, 1, push);
+    else
+      hipLaunchKernelGGL((k_commit_kv<float, float>), grid, dim3(256), 0, s, (float*)c->kv, (float*)c->kv, cs, accept_len, next_token, path, 0, c->dh, (size_t)0, (size_t)0,
+                         (size_t)0, c->S_cap, 1, push);
+    return;
+  }
   if (c->cfg.dtype == VVS_BF16 && vec)
     hipLaunchKernelGGL((k_commit_kv<bf16_t, uint4>), grid, dim3(256), 0, s, (bf16_t*)c->kv, (bf16_t*)c->kv + c->kv_v_off, cs, accept_len,
                        next_token, path, c->H, c->dh, c->kv_layer_stride, c->kv_row_stride, c->kv_head_stride, c->S_cap, c->L, push);
@@ -1172,6 +1193,7 @@ __global__ void k_debug_kv(const T* __restrict__ kh, const T* __restrict__ vh, f
 void launch_debug_kv(Ctx* c, int layer, int row, int n_slots, float* dk, float* dv, hipStream_t s) {
   size_t n = (size_t)n_slots * c->d;
   if (!n) return;
+  if (c->cfg.cache_kind == VVS_CACHE_E4M3) { launch_context_read(c, layer, row, n_slots, dk, dv, s); return; }
   size_t off = c->kv_layer_stride * layer + c->kv_row_stride * row;
   unsigned blocks = (unsigned)((n + 255) / 256);
   if (c->cfg.dtype == VVS_BF16)

@@ -24,11 +24,13 @@ struct QLayout {
   __host__ __device__ size_t block_bytes() const { return (size_t)2 * kQBlock * dh; }
 };
 
-// Cached length of row r: len[r >> len_shift] (a context keeps one per prompt, for two rows)
+// Cached length of row r: len[r >> shift] (a context keeps one per prompt, for two rows), or `fixed` for every row where len is nullptr
 struct QLen {
   const int32_t* len;
-  int shift;
+  int shift, fixed;
 };
+constexpr size_t qcache_parts_bytes(int dh) { return (size_t)kQParts * 16 * (dh + 2) * sizeof(float); }
+constexpr int qcache_score_steps(int blocks, int max_tokens) { return blocks + (max_tokens + kQBlock - 1) / kQBlock; }
 
 struct QAttention {
   QLayout c;
@@ -42,7 +44,8 @@ struct QAttention {
   float* lse;                       // [rows][T][heads] or nullptr
   float* norm;                      // workspace, likewise, in units of log2, or nullptr: nothing is counted
   int n_counted;
-  float *mass, *block_mass;         // [rows][kv_heads][capacity], [rows][kv_heads][T]
+  float *mass, *block_mass;         // [rows][kv_heads][capacity], [rows][kv_heads][block_stride]
+  int block_stride;
   int capacity;
   int packed;                       // 1: out in the operand order of the projections
   float* parts;                     // partial results: o, then (m, l)
@@ -66,6 +69,10 @@ struct QAppend {
   const void *k, *v;
   size_t stride, layer_stride;           // elements between tokens, between layers
   int capacity;
+  float* mass;                           // contexts, or nullptr: weights of the new slots begin at 0 ...
+  int32_t* pos;                          // ... and their positions at pos_base[r >> len.shift] + pos_add (pos_base nullptr: a slot's number); [layers][rows][kv_heads][capacity]
+  const int32_t* pos_base;
+  int pos_add;
 };
 
 struct QEvict {
@@ -88,6 +95,10 @@ struct QRead {
 };
 
 struct RopeArgs {
+  const float* sums;                // contexts: queries, keys and values as `splits` partial sums of a projection, rows of (heads + 2 kv_heads) * dh, instead of q and k ...
+  int splits;
+  size_t split_stride;
+  void* v_out;                      // ... and where the values go (nullptr: no sums)
   const int32_t* pos;
   const void *q, *k;
   void *q_out, *k_out;
@@ -102,5 +113,12 @@ void launch_qcache_append(const QAppend& a, int dtype, hipStream_t s);
 void launch_qcache_evict(const QEvict& a, hipStream_t s);
 void launch_qcache_read(const QRead& a, int dtype, hipStream_t s);
 void launch_rope_axes(const RopeArgs& a, int dtype, hipStream_t s);
+
+// Contexts with VVS_CACHE_E4M3 (vvs_qcache_ctx.hip)
+void launch_context_positions(Ctx* c, const TreeDesc& tree, const PosDesc& pos, int T, hipStream_t s);
+void launch_context_rope(Ctx* c, int layer, int M, const float* sums, int splits, hipStream_t s);
+void launch_context_attention(Ctx* c, int layer, const TreeDesc& tree, const PosDesc& pos, int T, hipStream_t s);
+void launch_context_append(Ctx* c, hipStream_t s);
+void launch_context_read(Ctx* c, int layer, int row, int n_slots, float* dk, float* dv, hipStream_t s);
 
 }  // namespace vvs

@@ -13,7 +13,7 @@ constexpr float kQSmall = 0x1p-110f;   // 2^kQLeast
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ int row_len(const QLen& len, int r, int capacity) { return min(max(len.len[r >> len.shift], 0), capacity); }
+__device__ __forceinline__ int row_len(const QLen& len, int r, int capacity) { return min(max(len.len ? len.len[r >> len.shift] : len.fixed, 0), capacity); }
 
 // Eight e4m3 numbers times a power of two as bf16 (exact)
 __device__ __forceinline__ bf16x8 e4m3_to_bf16(uint2 b, float scale) {
@@ -132,6 +132,11 @@ __global__ __launch_bounds__(256) void k_qcache_append(QAppend a, int max_blocks
   uint8_t* data = a.c.data + (region * a.c.blocks + block) * a.c.block_bytes();
   float2* scale = a.c.scale + region * a.c.blocks + block;
   const float2 was = *scale;
+  if (a.pos && lane >= begin && lane < end) {
+    const size_t at = region * a.capacity + slot0 + lane;
+    if (a.mass) a.mass[at] = 0.f;
+    a.pos[at] = a.pos_base ? a.pos_base[r >> a.len.shift] + a.pos_add + slot0 + lane - len : slot0 + lane;
+  }
   // source token of slot w (slot w takes token w + slot0 - len), < 0: zeros
   auto token = [&](int w) {
     const int t = min(max(w, begin), end - 1) + slot0 - len;
@@ -573,7 +578,7 @@ __device__ __forceinline__ float* kept_scores(const QAttention& a, int r, int hk
 __device__ __forceinline__ void mass_of_kept(const QAttention& a, const QRow& w, int r, int hk, const float2* norm, int n_queries, int seen, int first, int by) {
   const int steps = w.blocks + (a.block_mass ? (w.n + 31) / 32 : 0);
   float* mass = a.mass + ((size_t)r * a.c.kv_heads + hk) * a.capacity;
-  float* block_mass = a.block_mass + ((size_t)r * a.c.kv_heads + hk) * a.T;
+  float* block_mass = a.block_mass + ((size_t)r * a.c.kv_heads + hk) * a.block_stride;
   for (int i = first + (a.mass ? 0 : w.blocks * 8); i < steps * 8; i += by) {
     const int step = i >> 3, at = (i & 7) * 4;
     const bool cached = step < w.blocks;
@@ -1272,7 +1277,7 @@ __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
         const int at = 8 * g + col, step = step0 + wave * STEPS + n;
         if (at < valid[n]) {
           if (tok0[n] < 0) a.mass[((size_t)r * a.c.kv_heads + hk) * a.capacity + (size_t)step * kQBlock + at] += x;
-          else a.block_mass[((size_t)r * a.c.kv_heads + hk) * a.T + tok0[n] + at] = x;
+          else a.block_mass[((size_t)r * a.c.kv_heads + hk) * a.block_stride + tok0[n] + at] = x;
         }
       }
     }

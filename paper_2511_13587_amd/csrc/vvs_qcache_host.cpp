@@ -52,13 +52,13 @@ static vvs_status plan_qcache(const vvs_qcache_config* cfg, QCache* c) {
   c->cache_bytes = align_up(blocks * c->lay.block_bytes(), 256) + align_up(blocks * sizeof(float2), 256);
   size_t off = 0;
   c->parts_off = off;
-  off = align_up(off + (size_t)kQParts * 16 * (g.head_size + 2) * sizeof(float), 256);
+  off = align_up(off + qcache_parts_bytes(g.head_size), 256);
   c->norm_off = off;
   off = align_up(off + (size_t)g.n_rows * g.max_tokens * g.n_heads * sizeof(float), 256);
   c->origin_off = off;
   off = align_up(off + regions * g.capacity * sizeof(int32_t), 256);
   c->scores_off = off;
-  c->score_steps = c->lay.blocks + (g.max_tokens + kQBlock - 1) / kQBlock;
+  c->score_steps = qcache_score_steps(c->lay.blocks, g.max_tokens);
   off = align_up(off + (size_t)g.n_rows * g.n_kv_heads * c->score_steps * kQKept * kQBlock * sizeof(float), 256);
   c->ws_bytes = off;
   return VVS_OK;
@@ -206,6 +206,7 @@ vvs_status vvs_qcache_attention(vvs_qcache* qc, int32_t layer, const int32_t* d_
   a.out = d_out;
   a.n_counted = n_counted;
   a.mass = d_mass; a.block_mass = d_block_mass;
+  a.block_stride = n_tokens;
   a.capacity = g.capacity;
   a.lse = d_lse;
   a.norm = n_counted || d_block_mass ? (float*)(c->ws + c->norm_off) : nullptr;
@@ -255,6 +256,21 @@ vvs_status vvs_qcache_read(vvs_qcache* qc, int32_t layer, int32_t n_layers, cons
   a.first = d_first; a.k = d_k; a.v = d_v;
   launch_qcache_read(a, c->cfg.dtype, (hipStream_t)s);
   return launched(c, "qcache read");
+}
+
+vvs_status vvs_kv_evict(vvs_ctx* ctx, int32_t keep, int32_t recent, vvs_stream s) {
+  Ctx* c = reinterpret_cast<Ctx*>(ctx);
+  if (!c) return VVS_EINVAL;
+  if (c->cfg.cache_kind != VVS_CACHE_E4M3) return no(&c->err, VVS_ESTATE, "kv_evict: the context was created with VVS_CACHE_SAME");
+  if (!c->prefilled) return no(&c->err, VVS_ESTATE, "kv_evict: call vvs_prefill first");
+  if (c->verify_pending) return no(&c->err, VVS_ESTATE, "kv_evict: the previous verify was not committed");
+  if (keep < kQBlock || keep % kQBlock) return no(&c->err, VVS_EINVAL, "kv_evict: keep must be a positive multiple of VVS_QCACHE_BLOCK");
+  if (recent < 0 || recent > keep) return no(&c->err, VVS_EINVAL, "kv_evict: recent must be in [0, keep]");
+  launch_evict(c, keep, recent, (hipStream_t)s);
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return VVS_OK;
+  c->err = std::string("kv_evict: ") + hipGetErrorString(e);
+  return VVS_EHIP;
 }
 
 vvs_status vvs_rope_create(const vvs_rope_config* cfg, vvs_rope** out) {

@@ -36,6 +36,7 @@ void launch_qcache_read(const QRead& a, int, hipStream_t) {
   if (a.n < 1 || !a.k || !a.v) abort();
   ++g_read;
 }
+void launch_evict(Ctx*, int, int, hipStream_t) { ++g_evict; }
 void launch_rope_axes(const RopeArgs& a, int, hipStream_t) {
   if (a.M < 1 || a.heads < 1 || a.pairs < 1 || 2 * a.pairs > a.dh || a.pairs > 128) abort();
   for (int j = 0; j < a.pairs; ++j)

@@ -54,7 +54,7 @@ def test_per_token_strides():
     import torch
     from paper_2511_13587_amd import binding as vb
     wide = torch.zeros((2, 3, 8, 64), dtype=torch.bfloat16)
-    cpu = wide.device
+    cpu = wide.get_device()
     ok = [(wide[:, :, 2:4], (2, 3, 2, 64), 512), (wide, (2, 3, 8, 64), 512), (wide[:, :1, :2], (2, 1, 2, 64), 1536), (wide[:1, :1, :2], (1, 1, 2, 64), 128),
           (wide[:, :, :1], (2, 3, 1, 64), 512)]
     for t, shape, stride in ok:
@@ -62,3 +62,20 @@ def test_per_token_strides():
     for t in (wide[:, :, ::2], wide[:, ::2], wide[:, :, :, ::2], wide.transpose(1, 2), wide[:, :2], wide[:, :1].expand(2, 3, 8, 64)):
         with pytest.raises(ValueError):
             vb._per_token(t, cpu, torch.bfloat16, tuple(t.shape), "x")
+
+
+def test_context_with_the_cache_in_8_bits_takes_half_of_it():
+    from paper_2511_13587_amd import binding as vb
+    from paper_2511_13587_amd import synth
+    same, _, _ = vb.vvs_query_sizes(vb.make_config(synth.SEVEN_B))
+    held8, _, _ = vb.vvs_query_sizes(vb.make_config(synth.SEVEN_B, cache_kind=vb.VVS_CACHE_E4M3))
+    assert 0.5 * same <= held8 <= 0.54 * same                 # weights and positions are 8 bytes per slot of 256
+    for shape, kw, status in ((synth.XL_TREE, dict(cache_kind=-1), vb.VVS_EINVAL), (synth.XL_TREE, dict(cache_kind=1, draft_input=1), vb.VVS_EINVAL),
+                              (synth.TINY.replace(n_heads=8), dict(cache_kind=1), vb.VVS_ESIZE), (synth.TINY.replace(n_heads=8), dict(), vb.VVS_OK)):
+        cfg = vb.make_config(shape, **kw)
+        try:
+            vb.vvs_query_sizes(cfg)
+            got = vb.VVS_OK
+        except vb.VvsError as e:
+            got = e.status
+        assert got == status
