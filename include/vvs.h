@@ -360,7 +360,8 @@ const char* vvs_qcache_last_error(const vvs_qcache* c);   /* c must not be NULL 
  *                NULL: the first ones, and n_tokens <= src_tokens
  * Tokens beyond the capacity are dropped.  Slots below d_len keep their values up to the rounding above. */
 vvs_status vvs_qcache_append(vvs_qcache* c, int32_t layer, int32_t n_layers, const int32_t* d_len, int32_t n_tokens, const int32_t* d_n_tokens,
-                             int32_t src_tokens, const int32_t* d_select, const void* d_k, const void* d_v, int64_t kv_stride, vvs_stream s);
+                             int32_t src_tokens, const int32_t* d_select, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+                             vvs_stream s);
 
 /* Attention of a block of query tokens over the cached slots of their row and over the block's own keys and values, which are not rounded to 8 bits:
  * out = softmax(scale q K^T) V, every query over slots 0 .. d_len[r] - 1 and the block tokens it may see.
@@ -375,8 +376,8 @@ vvs_status vvs_qcache_append(vvs_qcache* c, int32_t layer, int32_t n_layers, con
  *   d_block_mass: float [n_rows, n_kv_heads, n_tokens], block tokens: set (NULL: left out)
  * Sums are in a fixed order: the same call gives the same bits. */
 vvs_status vvs_qcache_attention(vvs_qcache* c, int32_t layer, const int32_t* d_len, int32_t n_tokens, const int32_t* d_n_tokens, const int32_t* h_parent,
-                                const uint8_t* h_tree_mask, const void* d_q, int64_t q_stride, const void* d_k, const void* d_v, int64_t kv_stride,
-                                float scale, void* d_out, float* d_lse, int32_t n_counted, float* d_mass, float* d_block_mass, vvs_stream s);
+                                const uint8_t* h_tree_mask, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v,
+                                int64_t v_stride, float scale, void* d_out, float* d_lse, int32_t n_counted, float* d_mass, float* d_block_mass, vvs_stream s);
 
 /* Eviction by accumulated attention weight: every layer, row and key/value head whose length is above `keep` keeps the `keep` slots of largest weight (equal ones: the
  * lower slot; a NaN counts as the largest); the `recent` newest tokens - those at positions above the row's largest filled one minus `recent` - are kept whatever their weight, as

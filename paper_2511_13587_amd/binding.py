@@ -97,8 +97,8 @@ def _load():
         "vvs_qcache_create": (i32, [C.POINTER(VvsQCacheConfig), vp, vp, C.POINTER(vp)]),
         "vvs_qcache_destroy": (None, [vp]),
         "vvs_qcache_last_error": (C.c_char_p, [vp]),
-        "vvs_qcache_append": (i32, [vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, i64, vp]),
-        "vvs_qcache_attention": (i32, [vp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp, i64, C.c_float, vp, vp, i32, vp, vp, vp]),
+        "vvs_qcache_append": (i32, [vp, i32, i32, vp, i32, vp, i32, vp, vp, i64, vp, i64, vp]),
+        "vvs_qcache_attention": (i32, [vp, i32, vp, i32, vp, vp, vp, vp, i64, vp, i64, vp, i64, C.c_float, vp, vp, i32, vp, vp, vp]),
         "vvs_qcache_evict": (i32, [vp, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp]),
         "vvs_qcache_read": (i32, [vp, i32, i32, vp, vp, i32, vp, vp, vp]),
         "vvs_rope_create": (i32, [C.POINTER(VvsRopeConfig), C.POINTER(vp)]),
@@ -508,12 +508,10 @@ class QCache:
         shape = (n_layers, rows, src, kv, size)
         kp, ks = _per_token(k, self.index, self.dtype, shape, "k")
         vp, vs = _per_token(v, self.index, self.dtype, shape, "v")
-        if ks != vs:
-            raise ValueError("k and v have different strides")
         n = src if select is None else int(select.shape[1])
         with _Current(self.index):
             self._check(lib.vvs_qcache_append(self.h, layer, n_layers, self._rows(length, "length"), n, self._rows(n_tokens, "n_tokens"), src,
-                                              _on(select, self.index, torch.int32, (rows, n), "select"), kp, vp, ks, _raw_stream(self.index)))
+                                              _on(select, self.index, torch.int32, (rows, n), "select"), kp, ks, vp, vs, _raw_stream(self.index)))
 
     def vvs_qcache_attention(self, length: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor], v: Optional[torch.Tensor], out: torch.Tensor,
                              n_tokens: Optional[torch.Tensor] = None, parent=None, tree_mask=None, scale: Optional[float] = None,
@@ -525,8 +523,6 @@ class QCache:
         qp, qs = _per_token(q, self.index, self.dtype, (rows, t, heads, size), "q")
         kp, ks = _per_token(k, self.index, self.dtype, (rows, t, kv, size), "k")
         vp, vs = _per_token(v, self.index, self.dtype, (rows, t, kv, size), "v")
-        if ks != vs:
-            raise ValueError("k and v have different strides, or only one of them is given")
         p = None if parent is None else np.ascontiguousarray(parent, dtype=np.int32)
         m = None if tree_mask is None else np.ascontiguousarray(tree_mask, dtype=np.uint8)
         if (p is not None and p.shape != (t - 1,)) or (m is not None and m.shape != (t, t)):
@@ -534,7 +530,7 @@ class QCache:
         with _Current(self.index):
             self._check(lib.vvs_qcache_attention(
                 self.h, layer, self._rows(length, "length"), t, self._rows(n_tokens, "n_tokens"), None if p is None else p.ctypes.data,
-                None if m is None else m.ctypes.data, qp, qs, kp, vp, ks, size ** -0.5 if scale is None else float(scale),
+                None if m is None else m.ctypes.data, qp, qs, kp, ks, vp, vs, size ** -0.5 if scale is None else float(scale),
                 _on(out, self.index, self.dtype, (rows, t, heads, size), "out"),
                 _on(lse, self.index, torch.float32, (rows, t, heads), "lse"), n_counted,
                 _on(mass, self.index, torch.float32, (rows, kv, capacity), "mass"),

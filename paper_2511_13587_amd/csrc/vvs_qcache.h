@@ -38,7 +38,7 @@ struct QAttention {
   int layer, T, group;              // T: block tokens per row; group: query heads per key/value head
   const int32_t* n_tokens;          // [rows] or nullptr
   const void *q, *k, *v;            // k, v: nullptr = the queries see the cache alone
-  size_t q_stride, kv_stride;       // elements between tokens; rows are T tokens apart
+  size_t q_stride, k_stride, v_stride;      // elements between tokens; rows are T tokens apart
   float c_exp;                      // scale * log2(e)
   void* out;
   float* lse;                       // [rows][T][heads] or nullptr
@@ -67,7 +67,7 @@ struct QAppend {
   int count_plus;                        // n_tokens[r >> shift] + count_plus tokens are taken
   int n_shift;
   const void *k, *v;
-  size_t stride, layer_stride;           // elements between tokens, between layers
+  size_t stride[2], layer_stride[2];     // elements between tokens, between layers: of k, of v
   int capacity;
   float* mass;                           // contexts, or nullptr: weights of the new slots begin at 0 ...
   int32_t* pos;                          // ... and their positions at pos_base[r >> len.shift] + pos_add (pos_base nullptr: a slot's number); [layers][rows][kv_heads][capacity]

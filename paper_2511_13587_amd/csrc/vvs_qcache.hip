@@ -127,7 +127,6 @@ __global__ __launch_bounds__(256) void k_qcache_append(QAppend a, int max_blocks
   const int block = (len >> 5) + nth, slot0 = block * kQBlock;
   if (n < 1 || slot0 >= len + n) return;
   const int begin = max(len - slot0, 0), end = min(len + n - slot0, kQBlock);   // slots of the block that are written
-  const size_t row0 = (size_t)layer * a.layer_stride + (size_t)r * a.src_tokens * a.stride + (size_t)head * DH;
   const size_t region = a.c.region(a.layer + layer, r, head);
   uint8_t* data = a.c.data + (region * a.c.blocks + block) * a.c.block_bytes();
   float2* scale = a.c.scale + region * a.c.blocks + block;
@@ -148,7 +147,7 @@ __global__ __launch_bounds__(256) void k_qcache_append(QAppend a, int max_blocks
   const int tok[3] = {token(w_k[0]), token(w_k[1]), token(w_v)};
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    const T* src = (const T*)(half ? a.v : a.k) + row0;
+    const T* src = (const T*)(half ? a.v : a.k) + (size_t)layer * a.layer_stride[half] + (size_t)r * a.src_tokens * a.stride[half] + (size_t)head * DH;
     float x[KD][2][8];
     float top = 0.f;
 #pragma unroll
@@ -156,7 +155,7 @@ __global__ __launch_bounds__(256) void k_qcache_append(QAppend a, int max_blocks
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int from = half ? tok[2] : tok[t], dim = half ? c * 32 + t * 16 + (i & 8) : c * 32 + 8 * g;
-        read8(src + (size_t)max(from, 0) * a.stride + dim, x[c][t]);
+        read8(src + (size_t)max(from, 0) * a.stride[half] + dim, x[c][t]);
       }
 #pragma unroll
     for (int c = 0; c < KD; ++c)
@@ -616,7 +615,7 @@ __device__ __forceinline__ void add_odd_values(const QAttention& a, const T* v, 
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = ld(v + (size_t)(tok0 + j) * a.kv_stride + dt * 16 + 4 * (lane >> 4) + i);
+        const float x = ld(v + (size_t)(tok0 + j) * a.v_stride + dt * 16 + 4 * (lane >> 4) + i);
         o[dt][i] += vis && !finite(x) ? p * x : 0.f;
       }
   }
@@ -636,8 +635,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
   const int nq = w.n * a.group;
   if (q0 >= nq) return;                       // only tokens behind the row's number
   const T* q = (const T*)a.q + (size_t)r * a.T * a.q_stride + (size_t)hk * a.group * DH;
-  const T* k = (const T*)a.k + (size_t)r * a.T * a.kv_stride + (size_t)hk * DH;
-  const T* v = (const T*)a.v + (size_t)r * a.T * a.kv_stride + (size_t)hk * DH;
+  const T* k = (const T*)a.k + (size_t)r * a.T * a.k_stride + (size_t)hk * DH;
+  const T* v = (const T*)a.v + (size_t)r * a.T * a.v_stride + (size_t)hk * DH;
   const size_t region = a.c.region(a.layer, r, hk) * a.c.blocks;
   bf16x8 qf[NQB][KD][NS];
   int qt[NQB];                                // block token of this lane's query
@@ -730,8 +729,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
   for (; step < s1; step += 4) {
     const int tok0 = (step - w.blocks) * 32;
     bf16x8 kf[2][KD][NS], vf[DT][NS];
-    keys_of_tokens<T, DH, NS>(k, a.kv_stride, tok0, seen, lane, kf);
-    const bool odd = __builtin_amdgcn_ballot_w64(values_of_tokens<DH, NS>(v, a.kv_stride, tok0, seen, lane, vf)) != 0;
+    keys_of_tokens<T, DH, NS>(k, a.k_stride, tok0, seen, lane, kf);
+    const bool odd = __builtin_amdgcn_ballot_w64(values_of_tokens<DH, NS>(v, a.v_stride, tok0, seen, lane, vf)) != 0;
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
       float sv[8], e[8];
@@ -840,8 +839,8 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, 
   const QRow w = row_of(a, r);
   const int nq = w.n * a.group;
   if (q0 >= nq) return;
-  const bf16_t* k = (const bf16_t*)a.k + (size_t)r * a.T * a.kv_stride + (size_t)hk * DH;
-  const bf16_t* v = (const bf16_t*)a.v + (size_t)r * a.T * a.kv_stride + (size_t)hk * DH;
+  const bf16_t* k = (const bf16_t*)a.k + (size_t)r * a.T * a.k_stride + (size_t)hk * DH;
+  const bf16_t* v = (const bf16_t*)a.v + (size_t)r * a.T * a.v_stride + (size_t)hk * DH;
   const size_t region = a.c.region(a.layer, r, hk) * a.c.blocks;
   const int qw = q0 + wave * 16 * NQB;        // this wave's first query
   bf16x8 qf[NQB][KD][1];
@@ -986,7 +985,7 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, 
     uint4 raw[KD];
     auto load_raw = [&](int step) {
       const int tok0 = (step - w.blocks) * 32, tok = min(tok0 + (wave < 2 ? slot_of(wave, col) : value_slot(lane)), seen - 1);
-      const bf16_t* p = (wave < 2 ? k : v) + (size_t)tok * a.kv_stride + (wave < 2 ? g * 8 : (wave - 2) * (DH / 2) + (lane & 8));
+      const bf16_t* p = (wave < 2 ? k : v) + (size_t)tok * (wave < 2 ? a.k_stride : a.v_stride) + (wave < 2 ? g * 8 : (wave - 2) * (DH / 2) + (lane & 8));
       const int next = wave < 2 ? 32 : 16;
 #pragma unroll
       for (int n = 0; n < KD; ++n) raw[n] = *(const uint4*)(p + n * next);
@@ -1172,7 +1171,7 @@ __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
   const int seen = a.k ? w.n : 0, steps = w.blocks + (a.block_mass ? (w.n + 31) / 32 : 0), nq = min(a.n_counted, w.n) * a.group;
   const int first = a.mass ? 0 : w.blocks;
   const T* q = (const T*)a.q + (size_t)r * a.T * a.q_stride + (size_t)hk * a.group * DH;
-  const T* k = (const T*)a.k + (size_t)r * a.T * a.kv_stride + (size_t)hk * DH;
+  const T* k = (const T*)a.k + (size_t)r * a.T * a.k_stride + (size_t)hk * DH;
   const size_t region = a.c.region(a.layer, r, hk) * a.c.blocks;
   for (int step0 = first + blockIdx.x * 4 * STEPS; step0 < steps; step0 += gridDim.x * 4 * STEPS) {
     bf16x8 kf[STEPS][2][KD][NS];
@@ -1199,7 +1198,7 @@ __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
           for (int p = 1; p < NS; ++p) kf[n][0][kd][p] = kf[n][1][kd][p] = as_bf16x8(make_uint4(0, 0, 0, 0));
         }
       } else {
-        keys_of_tokens<T, DH, NS>(k, a.kv_stride, tok0[n], seen, lane, kf[n]);
+        keys_of_tokens<T, DH, NS>(k, a.k_stride, tok0[n], seen, lane, kf[n]);
       }
     }
     // (of a chain only the queries from the workgroup's first block token on see anything of block tokens)

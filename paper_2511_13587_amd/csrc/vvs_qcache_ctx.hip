@@ -48,7 +48,7 @@ void launch_context_attention(Ctx* c, int layer, const TreeDesc& tree, const Pos
   a.len = QLen{pos.kv_len, 1, pos.kv_base};
   a.layer = layer; a.T = T; a.group = 1;
   a.q = c->ws + c->w.q; a.k = k; a.v = k + c->esz * c->stage_v;
-  a.q_stride = a.kv_stride = (size_t)c->d;
+  a.q_stride = a.k_stride = a.v_stride = (size_t)c->d;
   a.c_exp = (float)(1.4426950408889634 / sqrt((double)c->dh));
   a.out = c->ws + c->w.attn;
   a.packed = c->cfg.dtype == VVS_BF16;
@@ -70,7 +70,7 @@ void launch_context_attention(Ctx* c, int layer, const TreeDesc& tree, const Pos
   p.c = a.c;
   p.len = a.len;
   p.layer = layer; p.n_layers = 1; p.n = T; p.src_tokens = T;
-  p.k = a.k; p.v = a.v; p.stride = (size_t)c->d;
+  p.k = a.k; p.v = a.v; p.stride[0] = p.stride[1] = (size_t)c->d;
   p.capacity = c->S_cap;
   p.pos = (int32_t*)(c->kv + c->q_slot_pos);
   launch_qcache_append(p, c->cfg.dtype, s);
@@ -88,7 +88,7 @@ void launch_context_append(Ctx* c, hipStream_t s) {
   p.select = oc + 2 * c->B; p.select_stride = VVS_MAX_T; p.select_shift = 1;
   p.skip = oc + c->B;
   p.k = c->ws + c->w.q_stage; p.v = c->ws + c->w.q_stage + c->esz * c->stage_v;
-  p.stride = (size_t)c->d; p.layer_stride = (size_t)c->R * T * c->d;
+  p.stride[0] = p.stride[1] = (size_t)c->d; p.layer_stride[0] = p.layer_stride[1] = (size_t)c->R * T * c->d;
   p.capacity = c->S_cap;
   p.mass = (float*)(c->kv + c->q_mass);
   p.pos = (int32_t*)(c->kv + c->q_slot_pos);

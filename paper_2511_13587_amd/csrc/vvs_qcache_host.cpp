@@ -142,7 +142,7 @@ void vvs_qcache_destroy(vvs_qcache* c) { delete of(c); }
 const char* vvs_qcache_last_error(const vvs_qcache* c) { return c ? reinterpret_cast<const QCache*>(c)->err.c_str() : ""; }
 
 vvs_status vvs_qcache_append(vvs_qcache* qc, int32_t layer, int32_t n_layers, const int32_t* d_len, int32_t n_tokens, const int32_t* d_n_tokens,
-                             int32_t src_tokens, const int32_t* d_select, const void* d_k, const void* d_v, int64_t kv_stride, vvs_stream s) {
+                             int32_t src_tokens, const int32_t* d_select, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride, vvs_stream s) {
   QCache* c = of(qc);
   if (!c) return VVS_EINVAL;
   vvs_status st = check_layers(c, layer, n_layers);
@@ -150,8 +150,8 @@ vvs_status vvs_qcache_append(vvs_qcache* qc, int32_t layer, int32_t n_layers, co
   if (!d_len || !d_k || !d_v) return no(&c->err, VVS_EINVAL, "qcache append: NULL argument");
   if (n_tokens < 1 || src_tokens < 1 || n_tokens > (1 << 30) || src_tokens > (1 << 30)) return no(&c->err, VVS_EINVAL, "qcache append: numbers of tokens must be positive");
   if (!d_select && n_tokens > src_tokens) return no(&c->err, VVS_EINVAL, "qcache append: more tokens than d_k and d_v hold");
-  const int64_t stride = stride_of(kv_stride, (int64_t)c->cfg.n_kv_heads * c->cfg.head_size, c->cfg.dtype);
-  if (stride < 0 || unaligned(d_k) || unaligned(d_v)) return no(&c->err, VVS_EINVAL, "qcache append: pointers and strides must be multiples of 16 bytes, strides cover a token");
+  const int64_t per = (int64_t)c->cfg.n_kv_heads * c->cfg.head_size, ks = stride_of(k_stride, per, c->cfg.dtype), vs = stride_of(v_stride, per, c->cfg.dtype);
+  if (ks < 0 || vs < 0 || unaligned(d_k) || unaligned(d_v)) return no(&c->err, VVS_EINVAL, "qcache append: pointers and strides must be multiples of 16 bytes, strides cover a token");
   if ((st = check_device(c)) != VVS_OK) return st;
   QAppend a{};
   a.c = c->lay;
@@ -159,14 +159,15 @@ vvs_status vvs_qcache_append(vvs_qcache* qc, int32_t layer, int32_t n_layers, co
   a.layer = layer; a.n_layers = n_layers; a.n = n_tokens; a.src_tokens = src_tokens;
   a.n_tokens = d_n_tokens;
   a.select = d_select; a.select_stride = n_tokens;
-  a.k = d_k; a.v = d_v; a.stride = (size_t)stride; a.layer_stride = (size_t)stride * src_tokens * c->cfg.n_rows;
+  a.k = d_k; a.v = d_v; a.stride[0] = (size_t)ks; a.stride[1] = (size_t)vs;
+  a.layer_stride[0] = (size_t)ks * src_tokens * c->cfg.n_rows; a.layer_stride[1] = (size_t)vs * src_tokens * c->cfg.n_rows;
   a.capacity = c->cfg.capacity;
   launch_qcache_append(a, c->cfg.dtype, (hipStream_t)s);
   return launched(c, "qcache append");
 }
 
 vvs_status vvs_qcache_attention(vvs_qcache* qc, int32_t layer, const int32_t* d_len, int32_t n_tokens, const int32_t* d_n_tokens, const int32_t* h_parent,
-                                const uint8_t* h_tree_mask, const void* d_q, int64_t q_stride, const void* d_k, const void* d_v, int64_t kv_stride, float scale,
+                                const uint8_t* h_tree_mask, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride, float scale,
                                 void* d_out, float* d_lse, int32_t n_counted, float* d_mass, float* d_block_mass, vvs_stream s) {
   QCache* c = of(qc);
   if (!c) return VVS_EINVAL;
@@ -192,8 +193,9 @@ vvs_status vvs_qcache_attention(vvs_qcache* qc, int32_t layer, const int32_t* d_
     a.causal = tree.causal;
     memcpy(a.anc, tree.anc, sizeof(a.anc));
   }
-  const int64_t qs = stride_of(q_stride, (int64_t)g.n_heads * g.head_size, g.dtype), ks = stride_of(kv_stride, (int64_t)g.n_kv_heads * g.head_size, g.dtype);
-  if (qs < 0 || ks < 0 || unaligned(d_q) || unaligned(d_k) || unaligned(d_v) || unaligned(d_out))
+  const int64_t qs = stride_of(q_stride, (int64_t)g.n_heads * g.head_size, g.dtype), per = (int64_t)g.n_kv_heads * g.head_size;
+  const int64_t ks = stride_of(k_stride, per, g.dtype), vs = stride_of(v_stride, per, g.dtype);
+  if (qs < 0 || ks < 0 || vs < 0 || unaligned(d_q) || unaligned(d_k) || unaligned(d_v) || unaligned(d_out))
     return no(&c->err, VVS_EINVAL, "qcache attention: pointers and strides must be multiples of 16 bytes, strides cover a token");
   if (((uintptr_t)d_mass | (uintptr_t)d_block_mass | (uintptr_t)d_lse) & 3) return no(&c->err, VVS_EINVAL, "qcache attention: unaligned weights");
   if ((st = check_device(c)) != VVS_OK) return st;
@@ -201,7 +203,7 @@ vvs_status vvs_qcache_attention(vvs_qcache* qc, int32_t layer, const int32_t* d_
   a.len = QLen{d_len, 0};
   a.layer = layer; a.T = n_tokens; a.group = g.n_heads / g.n_kv_heads;
   a.n_tokens = d_n_tokens;
-  a.q = d_q; a.k = d_k; a.v = d_v; a.q_stride = (size_t)qs; a.kv_stride = (size_t)ks;
+  a.q = d_q; a.k = d_k; a.v = d_v; a.q_stride = (size_t)qs; a.k_stride = (size_t)ks; a.v_stride = (size_t)vs;
   a.c_exp = std::max((float)((double)scale * 1.4426950408889634), FLT_MIN);   // above 0: masked scores are -inf
   a.out = d_out;
   a.n_counted = n_counted;

@@ -13,14 +13,14 @@ static QAttention g_attn_args;
 static RopeArgs g_rope_args;
 void launch_qcache_attention(const QAttention& a, int, hipStream_t) {
   if (a.T < 1 || a.c.heads % a.c.kv_heads || !a.q || !a.out || !(a.c_exp > 0.f) || !a.k != !a.v || a.n_counted > a.T || a.c.blocks * kQBlock < a.capacity) abort();
-  if (a.q_stride < (size_t)a.c.heads * a.c.dh || a.kv_stride < (size_t)a.c.kv_heads * a.c.dh || (!a.causal && a.T > VVS_MAX_T)) abort();
+  if (a.q_stride < (size_t)a.c.heads * a.c.dh || a.k_stride < (size_t)a.c.kv_heads * a.c.dh || a.v_stride < (size_t)a.c.kv_heads * a.c.dh || (!a.causal && a.T > VVS_MAX_T)) abort();
   if (a.norm) memset(a.norm, 0, sizeof(float) * a.c.rows * a.T * a.c.heads);      // inside the workspace
   if (a.parts) memset(a.parts, 0, sizeof(float) * kQParts * 16 * (a.c.dh + 2));
   g_attn_args = a;
   ++g_attention;
 }
 void launch_qcache_append(const QAppend& a, int, hipStream_t) {
-  if (a.n < 1 || a.layer < 0 || a.n_layers < 1 || (!a.select && a.n > a.src_tokens) || a.stride < (size_t)a.c.kv_heads * a.c.dh) abort();
+  if (a.n < 1 || a.layer < 0 || a.n_layers < 1 || (!a.select && a.n > a.src_tokens) || a.stride[0] < (size_t)a.c.kv_heads * a.c.dh || a.stride[1] < (size_t)a.c.kv_heads * a.c.dh) abort();
   // the last block of the last region
   const size_t last = a.c.region(a.layer + a.n_layers - 1, a.c.rows - 1, a.c.kv_heads - 1) * a.c.blocks + a.c.blocks - 1;
   memset(a.c.data + last * a.c.block_bytes(), 0, a.c.block_bytes());
@@ -86,24 +86,25 @@ int main() {
   float* f32 = (float*)buf;
   void* p = buf;
   // append
-  WANT(vvs_qcache_append(nullptr, 0, 1, i32, 5, nullptr, 5, nullptr, p, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, -1, 1, i32, 5, nullptr, 5, nullptr, p, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 1, 2, i32, 5, nullptr, 5, nullptr, p, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 2147483647, 2147483647, i32, 5, nullptr, 5, nullptr, p, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 0, i32, 5, nullptr, 5, nullptr, p, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 1, nullptr, 5, nullptr, 5, nullptr, p, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, nullptr, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 1, i32, 0, nullptr, 5, nullptr, p, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 1, i32, 6, nullptr, 5, nullptr, p, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, p, p, 127, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, p, p, 132, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, p, p, -128, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, buf + 8, p, 0, nullptr), VVS_EINVAL);
-  WANT(vvs_qcache_append(c, 0, 2, i32, 5, nullptr, 5, nullptr, p, p, 136, nullptr), VVS_OK);
-  WANT(vvs_qcache_append(c, 1, 1, i32, 6, i32, 5, i32, p, p, 0, nullptr), VVS_OK);
+  WANT(vvs_qcache_append(nullptr, 0, 1, i32, 5, nullptr, 5, nullptr, p, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, -1, 1, i32, 5, nullptr, 5, nullptr, p, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 1, 2, i32, 5, nullptr, 5, nullptr, p, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 2147483647, 2147483647, i32, 5, nullptr, 5, nullptr, p, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 0, i32, 5, nullptr, 5, nullptr, p, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 1, nullptr, 5, nullptr, 5, nullptr, p, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, nullptr, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 1, i32, 0, nullptr, 5, nullptr, p, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 1, i32, 6, nullptr, 5, nullptr, p, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, p, 127, p, 127, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, p, 132, p, 132, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, p, -128, p, -128, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, buf + 8, 0, p, 0, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 1, i32, 5, nullptr, 5, nullptr, p, 0, p, 132, nullptr), VVS_EINVAL);
+  WANT(vvs_qcache_append(c, 0, 2, i32, 5, nullptr, 5, nullptr, p, 136, p, 136, nullptr), VVS_OK);
+  WANT(vvs_qcache_append(c, 1, 1, i32, 6, i32, 5, i32, p, 0, p, 0, nullptr), VVS_OK);
   // attention
   auto attend = [&](int layer, int T, const int32_t* parent, const uint8_t* mask, void* k, void* v, float scale, int counted, float* mass, float* block, int64_t qs = 0,
-                    void* out = nullptr) { return (int)vvs_qcache_attention(c, layer, i32, T, nullptr, parent, mask, p, qs, k, v, 0, scale, out ? out : p, nullptr, counted, mass, block, nullptr); };
+                    void* out = nullptr) { return (int)vvs_qcache_attention(c, layer, i32, T, nullptr, parent, mask, p, qs, k, 0, v, 0, scale, out ? out : p, nullptr, counted, mass, block, nullptr); };
   const int32_t chain[3] = {0, 1, 2}, fork[3] = {0, 0, 1}, broken[3] = {0, 2, 1};
   uint8_t full[16];
   memset(full, 1, sizeof(full));
