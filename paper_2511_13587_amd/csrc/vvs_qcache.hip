@@ -1110,45 +1110,67 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, 
   mass_of_kept(a, w, r, hk, s_norm, min(a.n_kept, nq), seen_by(a, w, min(16 * NQB, nq)), threadIdx.x, 256);
 }
 
-// Joins the splits: one group of DH / 4 lanes per query.  Workgroups of blockIdx.y >= joins add up the counted weights instead (kept_tile: queries that went
-// through the keys with the counted ones).
-template <typename T, int DH>
+// Joins the splits.  Few of them (up to kQFewSplits): one group of DH / 4 lanes per query goes through them; many (WIDE): a workgroup per query, whose groups take every so-manieth split.
+// Workgroups of blockIdx.y >= joins add up the counted weights instead (kept_tile: queries that went through the keys with the counted ones).  us per call of attention, by groups /
+// by workgroups: one row of 32768 slots, 8 key/value heads in 64 splits 46 / 21, of 131072 slots and one head 124 / 20; 16 rows of 4000 in 8 splits 36.1 / 37.0.
+constexpr int kQFewSplits = 8;
+
+template <typename T, int DH, bool WIDE>
 __global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, int nq_tile, int joins, int kept_tile) {
-  constexpr int LQ = DH / 4;
-  const int r = blockIdx.z;
+  constexpr int LQ = DH / 4, GROUPS = 256 / LQ;
+  __shared__ float2 s_norm[kQKept];
+  __shared__ float s_red[16];
+  __shared__ float s_x[WIDE ? GROUPS : 1][DH];
+  const int r = blockIdx.z, tid = threadIdx.x;
   const QRow w = row_of(a, r);
   const size_t step = (size_t)nq_tile * (DH + 2);
+  const float* tile_parts = a.parts + ((size_t)r * gridDim.x + blockIdx.x) * a.splits * step;
+  auto scaled = [](float ms, float m) { return ms == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ms - m); };      // (without a maximum: nothing, or NaN)
   if ((int)blockIdx.y >= joins) {
     const int hk = blockIdx.x / q_tiles;
     if (blockIdx.x % q_tiles) return;
-    __shared__ float2 s_norm[16];
-    const int n_kept = min(a.n_kept, w.n * a.group);
-    if ((int)threadIdx.x < n_kept) {
-      const float* part = a.parts + (((size_t)r * gridDim.x + blockIdx.x) * a.splits * nq_tile + threadIdx.x) * (DH + 2) + DH;
+    const int n_kept = min(a.n_kept, w.n * a.group), q = tid >> 5;      // 32 threads per kept query
+    if (q < n_kept) {
+      const float* part = tile_parts + (size_t)q * (DH + 2) + DH;
       float m = -INFINITY, l = 0.f;
-#pragma unroll 8
-      for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * step]);
-#pragma unroll 8
-      for (int s = 0; s < a.splits; ++s) l += part[s * step + 1] * (part[s * step] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(part[s * step] - m));
-      s_norm[threadIdx.x] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
+      for (int s = tid & 31; s < a.splits; s += 32) m = fmaxf(m, part[s * step]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 32));
+      for (int s = tid & 31; s < a.splits; s += 32) l += part[s * step + 1] * scaled(part[s * step], m);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor(l, o, 32);
+      if ((tid & 31) == 0) s_norm[q] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
     }
     __syncthreads();
-    mass_of_kept(a, w, r, hk, s_norm, n_kept, seen_by(a, w, min(kept_tile, w.n * a.group)), (blockIdx.y - joins) * 256 + threadIdx.x, (gridDim.y - joins) * 256);
+    mass_of_kept(a, w, r, hk, s_norm, n_kept, seen_by(a, w, min(kept_tile, w.n * a.group)), (blockIdx.y - joins) * 256 + tid, (gridDim.y - joins) * 256);
     return;
   }
-  const int hk = blockIdx.x / q_tiles, tile = blockIdx.x % q_tiles;
-  const int in_tile = blockIdx.y * (256 / LQ) + threadIdx.x / LQ, dim = threadIdx.x % LQ * 4;
-  const int qi = tile * nq_tile + in_tile;
+  const int hk = blockIdx.x / q_tiles, tile = blockIdx.x % q_tiles, group = tid / LQ, dim = tid % LQ * 4;
+  const int in_tile = WIDE ? blockIdx.y : blockIdx.y * GROUPS + group, qi = tile * nq_tile + in_tile;
   if (in_tile >= nq_tile || qi >= w.n * a.group) return;
-  const float* part = a.parts + (((size_t)r * gridDim.x + blockIdx.x) * a.splits * nq_tile + in_tile) * (DH + 2);
-  float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * step + DH]);
-  float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float ms = part[s * step + DH], f = ms == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ms - m);
-    l += part[s * step + DH + 1] * f;
+  const float* part = tile_parts + (size_t)in_tile * (DH + 2);
+  float m = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = WIDE ? tid : 0; s < a.splits; s += WIDE ? 256 : 1) m = fmaxf(m, part[s * step + DH]);
+  if (WIDE) m = block_max(m, s_red);
+  for (int s = WIDE ? tid : 0; s < a.splits; s += WIDE ? 256 : 1) l += part[s * step + DH + 1] * scaled(part[s * step + DH], m);
+  if (WIDE) l = block_sum(l, s_red);
+#pragma unroll 4
+  for (int s = WIDE ? group : 0; s < a.splits; s += WIDE ? GROUPS : 1) {
+    const float f = scaled(part[s * step + DH], m);
+    const float2 p0 = *(const float2*)(part + s * step + dim), p1 = *(const float2*)(part + s * step + dim + 2);
+    x[0] += p0.x * f;
+    x[1] += p0.y * f;
+    x[2] += p1.x * f;
+    x[3] += p1.y * f;
+  }
+  if (WIDE) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] += part[s * step + dim + i] * f;
+    for (int i = 0; i < 4; ++i) s_x[group][dim + i] = x[i];
+    __syncthreads();
+    if (group) return;
+    for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] += s_x[g][dim + i];
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = l == 0.f ? 0.f : x[i] / l;
@@ -1299,10 +1321,12 @@ static void attention_t(QAttention a, hipStream_t s) {
   if constexpr (MANY) hipLaunchKernelGGL((k_qcache_attention_many<DH>), grid, dim3(256), 0, s, a, q_tiles);
   else hipLaunchKernelGGL((k_qcache_attention<T, DH, NQB>), grid, dim3(256), 0, s, a, q_tiles);
   if (a.splits > 1) {
-    const int per = 256 / (DH / 4), joins = (16 * BLOCKS + per - 1) / per;
+    const int per = a.splits > kQFewSplits ? 1 : 256 / (DH / 4), joins = (16 * BLOCKS + per - 1) / per;
     // (a workgroup first finds the norms: a few workgroups with much to add rather than many with little)
     const int masses = a.n_kept ? (int)std::max<int64_t>(1, std::min<int64_t>(a.c.blocks / 32, 2048 / ((int64_t)a.c.rows * a.c.kv_heads))) : 0;
-    hipLaunchKernelGGL((k_qcache_join<T, DH>), dim3(grid.x, joins + masses, grid.z), dim3(256), 0, s, a, q_tiles, 16 * BLOCKS, joins, 16 * NQB);
+    const dim3 join_grid(grid.x, joins + masses, grid.z);
+    if (a.splits > kQFewSplits) hipLaunchKernelGGL((k_qcache_join<T, DH, true>), join_grid, dim3(256), 0, s, a, q_tiles, 16 * BLOCKS, joins, 16 * NQB);
+    else hipLaunchKernelGGL((k_qcache_join<T, DH, false>), join_grid, dim3(256), 0, s, a, q_tiles, 16 * BLOCKS, joins, 16 * NQB);
   }
   if (!a.n_kept && (a.n_counted > 0 || a.block_mass)) {
     const int steps = a.c.blocks + (a.T + 31) / 32, per = 4;
