@@ -83,7 +83,7 @@ struct QEvict {
   float* mass_out;
   const int32_t* pos;
   int32_t* pos_out;
-  int32_t* origin;                  // workspace: [layers of the call][rows][kv_heads][capacity]
+  int32_t* origin;                  // workspace: [layers of the call][rows][kv_heads][blocks * 32]
 };
 
 struct QRead {

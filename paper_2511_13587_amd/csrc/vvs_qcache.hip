@@ -1379,9 +1379,9 @@ struct QSelect {           // one (layer, row, head)
   int32_t *pos_out, *origin;
 };
 __device__ __forceinline__ QSelect select_of(const QEvict& a, int head, int r, int layer) {
-  const size_t base = (((size_t)layer * a.c.rows + r) * a.c.kv_heads + head) * a.capacity;
+  const size_t region = a.c.region(layer, r, head), base = region * a.capacity;
   const int len = row_len(a.len, r, a.capacity);
-  return QSelect{len, min(len, a.keep), a.mass + base, a.mass_out + base, a.pos ? a.pos + base : nullptr, a.pos ? a.pos_out + base : nullptr, a.origin + base};
+  return QSelect{len, min(len, a.keep), a.mass + base, a.mass_out + base, a.pos ? a.pos + base : nullptr, a.pos ? a.pos_out + base : nullptr, a.origin + region * a.c.blocks * kQBlock};
 }
 // Slot i of the new row comes from slot `from`
 __device__ __forceinline__ void settle(const QSelect& h, int i, int from) {
@@ -1606,9 +1606,9 @@ __global__ __launch_bounds__(256) void k_qcache_move(QEvict a) {
   const int blocks = a.keep / kQBlock, head = unit / blocks, block = unit % blocks;
   if (head >= a.c.kv_heads) return;
   if (row_len(a.len, r, a.capacity) <= a.keep) return;
-  const size_t base = (((size_t)layer * a.c.rows + r) * a.c.kv_heads + head) * a.capacity, region = a.c.region(a.layer + layer, r, head) * a.c.blocks;
+  const size_t region = a.c.region(a.layer + layer, r, head) * a.c.blocks;
   const int g = lane >> 4, i = lane & 15, slot0 = block * kQBlock;
-  const int32_t* origin = a.origin + base + slot0;
+  const int32_t* origin = a.origin + a.c.region(layer, r, head) * a.c.blocks * kQBlock + slot0;
   const int from_k[2] = {origin[slot_of(0, i)], origin[slot_of(1, i)]};        // this lane's slots: keys of both tiles
   const int4 o0 = *(const int4*)(origin + 8 * g), o1 = *(const int4*)(origin + 8 * g + 4);
   const int from_v[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};      // ... and values

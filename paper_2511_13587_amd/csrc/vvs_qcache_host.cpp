@@ -56,7 +56,7 @@ static vvs_status plan_qcache(const vvs_qcache_config* cfg, QCache* c) {
   c->norm_off = off;
   off = align_up(off + (size_t)g.n_rows * g.max_tokens * g.n_heads * sizeof(float), 256);
   c->origin_off = off;
-  off = align_up(off + regions * g.capacity * sizeof(int32_t), 256);
+  off = align_up(off + blocks * kQBlock * sizeof(int32_t), 256);
   c->scores_off = off;
   c->score_steps = qcache_score_steps(c->lay.blocks, g.max_tokens);
   off = align_up(off + (size_t)g.n_rows * g.n_kv_heads * c->score_steps * kQKept * kQBlock * sizeof(float), 256);
@@ -249,6 +249,7 @@ vvs_status vvs_qcache_read(vvs_qcache* qc, int32_t layer, int32_t n_layers, cons
   if (st != VVS_OK) return st;
   if (!d_len || !d_k || !d_v) return no(&c->err, VVS_EINVAL, "qcache read: NULL argument");
   if (n_slots < 1 || n_slots > (1 << 30)) return no(&c->err, VVS_EINVAL, "qcache read: n_slots must be positive");
+  if ((int64_t)c->cfg.n_kv_heads * (n_slots / kQBlock + 2) > INT32_MAX) return no(&c->err, VVS_ESIZE, "qcache read: too many slots");
   if (unaligned(d_k) || unaligned(d_v)) return no(&c->err, VVS_EINVAL, "qcache read: pointers must be multiples of 16 bytes");
   if ((st = check_device(c)) != VVS_OK) return st;
   QRead a{};

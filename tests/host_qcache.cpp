@@ -142,12 +142,66 @@ int main() {
   WANT(vvs_qcache_read(c, 0, 1, i32, nullptr, 0, p, p, nullptr), VVS_EINVAL);
   WANT(vvs_qcache_read(c, 0, 1, nullptr, nullptr, 4, p, p, nullptr), VVS_EINVAL);
   WANT(vvs_qcache_read(c, 0, 1, i32, nullptr, 4, p, buf + 8, nullptr), VVS_EINVAL);
+  { vvs_qcache_config h = g; h.n_heads = h.n_kv_heads = 4096; h.n_layers = h.n_rows = h.max_tokens = 1; h.capacity = 32; h.head_size = 32;
+    size_t hb = 0, hw = 0;
+    WANT(vvs_qcache_query_sizes(&h, &hb, &hw), VVS_OK);
+    char *hc = (char*)aligned_alloc(256, hb), *hws = (char*)aligned_alloc(256, hw);
+    vvs_qcache* wide = nullptr;
+    WANT(vvs_qcache_create(&h, hc, hws, &wide), VVS_OK);
+    WANT(vvs_qcache_read(wide, 0, 1, i32, nullptr, 1 << 30, p, p, nullptr), VVS_ESIZE);
+    vvs_qcache_destroy(wide); free(hc); free(hws); }
   WANT(vvs_qcache_read(c, 0, 2, i32, i32, 4, p, p, nullptr), VVS_OK);
   if (std::string(vvs_qcache_last_error(c)).empty() || g_append != 2 || g_attention != 3 || g_evict != 2 || g_read != 1) g_bad = 1;
   vvs_qcache_destroy(c);
   vvs_qcache_destroy(nullptr);
   free(cache);
   free(ws);
+  // a context with its cache in 8 bits
+  {
+    vvs_config cc{};
+    cc.n_layers = 2; cc.d_model = 128; cc.n_heads = 4; cc.d_ff = 64; cc.vocab = 64; cc.logit_hi = 64; cc.grid_h = cc.grid_w = 4; cc.prefix_len = 1;
+    cc.prefix_kind = VVS_PREFIX_CLASS; cc.n_classes = 3; cc.n_prompts = 2; cc.max_nodes = 5; cc.dtype = VVS_FP32; cc.cfg_scale = 2.f; cc.rms_eps = 1e-5f; cc.rope_base = 10000.f;
+    cc.feature_slots = 2;
+    size_t kv = 0, w = 0, pw = 0, kv_same = 0;
+    WANT(vvs_query_sizes(&cc, &kv_same, &w, &pw), VVS_OK);
+    cc.cache_kind = 2;
+    WANT(vvs_query_sizes(&cc, &kv, &w, &pw), VVS_EINVAL);
+    cc.cache_kind = VVS_CACHE_E4M3; cc.draft_input = 1;
+    WANT(vvs_query_sizes(&cc, &kv, &w, &pw), VVS_EINVAL);
+    cc.draft_input = 0; cc.n_heads = 8;
+    WANT(vvs_query_sizes(&cc, &kv, &w, &pw), VVS_ESIZE);
+    cc.n_heads = 4;
+    WANT(vvs_query_sizes(&cc, &kv, &w, &pw), VVS_OK);
+    if (kv >= kv_same / 2) g_bad = 1;                    // a quarter of fp32, and 8 bytes per slot
+    char *dkv = (char*)aligned_alloc(256, kv), *dws = (char*)aligned_alloc(256, w), *dpw = (char*)aligned_alloc(256, pw);
+    vvs_ctx* x = nullptr;
+    WANT(vvs_create(&cc, dkv, dws, dpw, &x), VVS_OK);
+    std::vector<const void*> weights(vvs_num_weight_tensors(&cc), buf);
+    std::vector<float> probs(2 * 6 * 64), u(2 * 6 * 2);
+    std::vector<int32_t> toks(10), acc(2), path(2 * VVS_MAX_T), next(2);
+    WANT(vvs_load_weights(x, weights.data(), (int32_t)weights.size(), nullptr), VVS_OK);
+    WANT(vvs_kv_evict(nullptr, 32, 0, nullptr), VVS_EINVAL);
+    WANT(vvs_kv_evict(x, 32, 0, nullptr), VVS_ESTATE);
+    WANT(vvs_prefill(x, toks.data(), nullptr, 3, toks.data(), u.data(), next.data(), nullptr), VVS_OK);
+    const int evictions = g_evict;
+    for (int keep : {0, 31, -32}) WANT(vvs_kv_evict(x, keep, 0, nullptr), VVS_EINVAL);
+    for (int recent : {-1, 33}) WANT(vvs_kv_evict(x, 32, recent, nullptr), VVS_EINVAL);
+    WANT(vvs_kv_evict(x, 32, 32, nullptr), VVS_OK);
+    WANT(vvs_verify(x, 5, nullptr, nullptr, toks.data(), probs.data(), u.data(), VVS_STRICT, acc.data(), path.data(), next.data(), nullptr), VVS_OK);
+    WANT(vvs_kv_evict(x, 32, 0, nullptr), VVS_ESTATE);
+    WANT(vvs_kv_commit(x, nullptr), VVS_OK);
+    WANT(vvs_kv_evict(x, 64, 0, nullptr), VVS_OK);
+    if (g_evict != evictions + 2 || vvs_plan_is_fused(x, 6)) g_bad = 1;
+    vvs_destroy(x);
+    cc.cache_kind = VVS_CACHE_SAME;
+    WANT(vvs_query_sizes(&cc, &kv, &w, &pw), VVS_OK);
+    free(dkv); free(dws); free(dpw);
+    dkv = (char*)aligned_alloc(256, kv); dws = (char*)aligned_alloc(256, w); dpw = (char*)aligned_alloc(256, pw);
+    WANT(vvs_create(&cc, dkv, dws, dpw, &x), VVS_OK);
+    WANT(vvs_kv_evict(x, 32, 0, nullptr), VVS_ESTATE);
+    vvs_destroy(x);
+    free(dkv); free(dws); free(dpw);
+  }
   // rotary operator
   vvs_rope* r = nullptr;
   const vvs_rope_config rc{64, 3, {12, 10, 10, 0}, VVS_ROPE_OWN, VVS_ROPE_ADJACENT, VVS_BF16, 10000.f};

@@ -141,6 +141,9 @@ FORMS = [
     ("bf16", 4, 2, 64, 20, True, [1536, 1], [20, 20], 1),                 # splits of two query blocks
     ("fp32", 2, 1, 64, 30, True, [1030, 5], None, 2),
     ("fp32", 2, 1, 32, 7, False, [1030, 700], None, 7),
+    ("fp32", 2, 1, 128, 20, True, [70, 0], None, 20),                     # fp32, many counted
+    ("fp32", 4, 1, 64, 70, False, [40, 33], [70, 5], 60),
+    ("bf16", 2, 2, 64, 5, False, [40, 33], None, 0),
 ]
 
 
