@@ -1383,11 +1383,36 @@ __device__ __forceinline__ QSelect select_of(const QEvict& a, int head, int r, i
   const int len = row_len(a.len, r, a.capacity);
   return QSelect{len, min(len, a.keep), a.mass + base, a.mass_out + base, a.pos ? a.pos + base : nullptr, a.pos ? a.pos_out + base : nullptr, a.origin + region * a.c.blocks * kQBlock};
 }
-// Slot i of the new row comes from slot `from`
-__device__ __forceinline__ void settle(const QSelect& h, int i, int from) {
-  h.origin[i] = from;
-  h.mass_out[i] = h.mass[from];
-  if (h.pos) h.pos_out[i] = h.pos[from];
+// Weights and positions of the slots in front of `left`, from where `origin` says (a slot itself, or one behind all of them, so that the outputs may be the inputs).  Eight at a
+// time: outputs that may be inputs keep the loads of a next slot behind the stores of this one (one at a time, 16 x 8 rows of 32768 took 87 us, now 73)
+__device__ __forceinline__ void settle(const QSelect& h, int left, int tid, int threads) {
+  for (int i0 = tid; i0 < left; i0 += 8 * threads) {
+    int from[8], p[8];
+    float m[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) from[j] = h.origin[min(i0 + j * threads, left - 1)];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m[j] = h.mass[from[j]];
+      p[j] = h.pos ? h.pos[from[j]] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = i0 + j * threads;
+      if (i < left) {
+        h.mass_out[i] = m[j];
+        if (h.pos) h.pos_out[i] = p[j];
+      }
+    }
+  }
+}
+// A row that is not shortened
+__device__ __forceinline__ void stay(const QSelect& h, int tid, int threads) {
+  if (h.mass == h.mass_out && (!h.pos || h.pos == h.pos_out)) return;
+  for (int i = tid; i < h.left; i += threads) {
+    h.mass_out[i] = h.mass[i];
+    if (h.pos) h.pos_out[i] = h.pos[i];
+  }
 }
 __device__ __forceinline__ void clear_behind(const QSelect& h, int capacity, int tid, int threads) {
   for (int i = h.left + tid; i < capacity; i += threads) {
@@ -1397,8 +1422,8 @@ __device__ __forceinline__ void clear_behind(const QSelect& h, int capacity, int
 }
 
 // Rows of up to 64 * WAVES * KPT slots: every lane holds the keys of KPT slots (a wave's slots lie together), 32 rounds of counting find the threshold.
-// A workgroup of one wave needs no barrier.  Bound by the rounds (KPT comparisons each), not by the 8 bytes per slot: 36 x 16 x 20 rows of 696 slots take 57 us,
-// 16 x 8 rows of 32768 88.  (Digits of 8 bits counted in LDS: 1521 and 208 us - most weights share a few exponents, so that the counters collide.)
+// A workgroup of one wave needs no barrier.  Bound by the rounds (KPT comparisons each), not by the 8 bytes per slot: 36 x 16 x 20 rows of 696 slots take 59 us,
+// 16 x 8 rows of 32768 73.  (Digits of 8 bits counted in LDS: 1521 and 208 us - most weights share a few exponents, so that the counters collide.)
 template <int WAVES, int KPT>
 __global__ __launch_bounds__(64 * WAVES) void k_qcache_select(QEvict a) {
   constexpr int THREADS = 64 * WAVES;
@@ -1407,7 +1432,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_qcache_select(QEvict a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const QSelect h = select_of(a, blockIdx.x, blockIdx.y, blockIdx.z);
   if (h.len <= a.keep) {
-    for (int i = tid; i < h.left; i += THREADS) settle(h, i, i);
+    stay(h, tid, THREADS);
     clear_behind(h, a.capacity, tid, THREADS);
     return;
   }
@@ -1504,9 +1529,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_qcache_select(QEvict a) {
     const int i = slot0 + j * 64;
     const bool o = !(kept >> j & 1) && i < a.keep;
     const uint64_t b = __builtin_amdgcn_ballot_w64(o);
-    if (i < a.keep) settle(h, i, o ? s_list[hole + __popcll(b & below)] : i);
+    if (i < a.keep) h.origin[i] = o ? s_list[hole + __popcll(b & below)] : i;
     hole += __popcll(b);
   }
+  __syncthreads();
+  settle(h, a.keep, tid, THREADS);
   __syncthreads();                               // the sources' weights have been read
   clear_behind(h, a.capacity, tid, THREADS);
 }
@@ -1534,7 +1561,7 @@ __global__ __launch_bounds__(kQSelect) void k_qcache_select_long(QEvict a) {
   const int tid = threadIdx.x;
   const QSelect h = select_of(a, blockIdx.x, blockIdx.y, blockIdx.z);
   if (h.len <= a.keep) {
-    for (int i = tid; i < h.left; i += kQSelect) settle(h, i, i);
+    stay(h, tid, kQSelect);
     clear_behind(h, a.capacity, tid, kQSelect);
     return;
   }
@@ -1590,8 +1617,10 @@ __global__ __launch_bounds__(kQSelect) void k_qcache_select_long(QEvict a) {
   __syncthreads();
   for (int i = tid; i < a.keep; i += kQSelect) {
     const int o = h.origin[i];
-    settle(h, i, o >= 0 ? i : h.origin[a.keep + (-1 - o)]);
+    h.origin[i] = o >= 0 ? i : h.origin[a.keep + (-1 - o)];
   }
+  __syncthreads();
+  settle(h, a.keep, tid, kQSelect);
   __syncthreads();
   clear_behind(h, a.capacity, tid, kQSelect);
 }
