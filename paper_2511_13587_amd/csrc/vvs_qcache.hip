@@ -826,7 +826,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
 // Many queries: a workgroup takes 128 of them, 32 per wave, and all its waves go through the same keys, so that what is done once per key - load, conversion, turning - is
 // shared: the waves bring the operands of 64 keys to LDS while those before are at work, from registers that were loaded another 64 keys earlier.  bf16 calls; grid as above.
 // 8 rows x 32 query heads on 8 x 512 tokens over 4096 slots, head size 128: 434 us, 670 TFLOP/s (16 queries per wave 646: every operand read from LDS for half as many); 4 rows over 2048
-// slots 151 us.  Bound by vector instructions and the waits between them and the matrix cores, of two waves per SIMD.
+// slots 138 us.  Bound by vector instructions and the waits between them and the matrix cores, of two waves per SIMD.
 // Blocks whose values do not go as fp16 (rare) are left for the end, each wave on its own, so that the registers of that path are not taken in the others.
 template <int DH>
 __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, int q_tiles) {
@@ -1629,7 +1629,7 @@ __global__ __launch_bounds__(kQSelect) void k_qcache_select_long(QEvict a) {
 // Moves the elements: one wave per (layer, row, head, block below keep).  Of the keys a lane gathers 8 dims of its two slots, 8 bytes in a row.  Of the values it gathers its dims of 8 slots: the 16
 // lanes of a group read the 256 bytes in which a source's dims lie beside those of the 7 slots around it, and each picks its byte.  (Single bytes by the lane that holds the slot: every lane
 // touches a segment of its own, 370 us instead
-// of 276 for 36 x 16 x 20 rows of 696 slots cut to 256.)  Bound by HBM: a slot's values share their cache lines with 7 others, so that nearly all of them are read, 1.08 GB with keys and stores: 3.9 TB/s.
+// of 276 for 36 x 16 x 20 rows of 696 slots cut to 256.)  Bound by HBM: a slot's values share their cache lines with 7 others, so that nearly all of them are read: about 1 GB with keys and stores, by arithmetic.
 template <int DH>
 __global__ __launch_bounds__(256) void k_qcache_move(QEvict a) {
   const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6), r = blockIdx.y, layer = blockIdx.z;
