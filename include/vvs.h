@@ -234,6 +234,7 @@ vvs_status vvs_kv_commit(vvs_ctx* ctx, vvs_stream s);
 /* Contexts with VVS_CACHE_E4M3: shortens the cache of every prompt whose length is above `keep` to `keep` slots per layer, row and head, as
  * vvs_qcache_evict does: the slots with the largest accumulated attention weight stay, and the `recent` newest tokens.  Weights are accumulated by the library: of all
  * tokens of a prefill, and of those tokens of a verify call that are certain to be kept (the pending token and the post-verified ones), over cached slots.
+ * vvs_set_state does not take weights back: a verify call that is replayed counts again.
  * Positions of later tokens do not change; S_b does.  Not between a verify and its commit (VVS_ESTATE).
  *   keep: a multiple of VVS_QCACHE_BLOCK, at least one block; recent: in [0, keep] */
 vvs_status vvs_kv_evict(vvs_ctx* ctx, int32_t keep, int32_t recent, vvs_stream s);

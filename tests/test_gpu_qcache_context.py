@@ -1,6 +1,6 @@
-"""Contexts that hold their cache in 8 bits (VVS_CACHE_E4M3) in lockstep with the checker.  After every call that caches tokens, what the context holds is compared with the checker's
-own keys and values rounded as the cache does - a value may lie one e4m3 step off where fp32 and 64 bits fall on two sides of a border - and then becomes the checker's cache, so
-that the next forward is compared on the same cache: fp32 logits to 1e-4 and decisions equal, bf16 logits to the bound of the parity tests (3e-2, or three times what the checker itself moves
+"""Contexts that hold their cache in 8 bits (VVS_CACHE_E4M3) in lockstep with the oracle.  After every call that caches tokens, what the context holds is compared with the oracle's
+own keys and values rounded as the cache does - a value may lie one e4m3 step off where fp32 and 64 bits fall on two sides of a border - and then becomes the oracle's cache, so
+that the next forward is compared on the same cache: fp32 logits to 1e-4 and decisions equal, bf16 logits to the bound of the parity tests (3e-2, or three times what the oracle itself moves
 by under a 1e-7 perturbation in front of its rounding points)."""
 import dataclasses
 
@@ -36,7 +36,7 @@ class Run:
         return [x.double().cpu().numpy().reshape(n, self.ora.H, self.ora.dh) for x in (k, v)]
 
     def take_cache(self, before):
-        """Compares what was cached since the lengths `before` and hands the context's cache to the checker."""
+        """Compares what was cached since the lengths `before` and hands the context's cache to the oracle."""
         o = self.ora
         for row in range(o.R):
             n, m = o.kv_len(row // 2), before[row // 2]
@@ -80,12 +80,14 @@ class Run:
         assert (self.out[2].cpu().numpy() == self.ora.pending).all()
         self.take_cache([0] * s.n_prompts)
 
-    def step(self, seed, tree=True, n_post=0, mode=0):
+    def step(self, seed, tree=True, n_post=0, mode=0, uneven=False):
         s, n = self.shape, self.shape.n_nodes
         parent = np.asarray([min(j, n_post) if j <= n_post else max(n_post, j - 2) for j in range(n)], dtype=np.int32) if tree else None
         q, toks = synth.make_draft(s, parent if parent is not None else synth.tree_parents(None, n), seed)
         u = synth.make_uniforms(s, n, seed)
         u[:, 1 + seed % 3, 0] = 0.0                                # some tokens are accepted
+        if uneven:                                                 # the first prompt takes what it can, the others next to nothing
+            u[0, :, 0], u[1:, :, 0] = 0.0, 0.999999
         before = [self.ora.kv_len(b) for b in range(s.n_prompts)]
         args = (torch.from_numpy(toks).cuda(), torch.from_numpy(q).cuda(), torch.from_numpy(u).cuda(), mode, *self.out)
         if n_post:
@@ -101,7 +103,7 @@ class Run:
         a, p, t = (x.cpu().numpy() for x in self.out)
         if s.dtype == synth.DTYPE_FP32:
             assert (a == acc).all() and (t == nxt).all() and all((p[b, :acc[b] + 1] == paths[b]).all() for b in range(s.n_prompts))
-        else:                                                      # the checker follows the library's decisions: a draw within the noise may fall either way
+        else:                                                      # the oracle follows the library's decisions: a draw within the noise may fall either way
             for x in (self.ora, self.shadow):
                 x.last["paths"] = [[int(v) for v in p[b, :a[b] + 1]] for b in range(s.n_prompts)]
                 x.last["accept_len"], x.last["next_token"] = a.copy(), t.copy()
@@ -115,7 +117,7 @@ class Run:
         return a
 
     def evict(self, keep, recent):
-        """Evicts on the GPU, checks that every head keeps `keep` of its slots and the newest, and hands the cache to the checker."""
+        """Evicts on the GPU, checks that every head keeps `keep` of its slots and the newest, and hands the cache to the oracle."""
         o = self.ora
         lens = [o.kv_len(b) for b in range(o.B)]
         was = {(l, r): self.held(l, r, lens[r // 2]) for l in range(o.L) for r in range(o.R)}
@@ -141,7 +143,7 @@ class Run:
 
 @pytest.mark.parametrize("shape,forced", [(FP32, 5), (FP32.replace(d_model=256, n_heads=4, d_ff=512), 20), (BF16, 5),
                                           (BF16.replace(d_model=512, n_heads=4, d_ff=1024, n_layers=1), 30)], ids=["fp32_32", "fp32_64", "bf16_64", "bf16_128"])
-def test_steps_and_eviction_in_lockstep_with_the_checker(shape, forced):
+def test_steps_and_eviction_in_lockstep_with_the_oracle(shape, forced):
     run = Run(shape)
     run.prefill(forced)
     for i, kw in enumerate((dict(), dict(tree=False), dict(n_post=2), dict())):
@@ -180,6 +182,30 @@ def test_prefill_in_chunks_sees_what_was_cached():
                     assert (np.abs(have[c:] - want) <= np.abs(want) * 2.0 ** -3 + 2e-5).all()
                 o.kc[row][l], o.vc[row][l] = got
         assert np.abs(raw.cpu().numpy()[row, 0] - logits[-1]).max() <= 1e-4
+    run.ctx.close()
+
+
+def test_prompts_that_finish_at_different_steps():
+    """A finished prompt answers -1 and what it holds stays as it is, bit for bit, while the other goes on; an eviction shortens both."""
+    run = Run(FP32)
+    total = FP32.grid_h * FP32.grid_w
+    run.prefill(total - 12)
+    uneven = False
+    for i in range(14):
+        emitted = run.ora.n_emitted.copy()
+        done = [b for b in range(FP32.n_prompts) if emitted[b] >= total]
+        was = {(l, r): run.held(l, r, run.ora.kv_len(r // 2)) for l in range(run.ora.L) for r in range(run.ora.R) if r // 2 in done}
+        uneven |= len(done) == 1
+        a = run.step(i, uneven=True)
+        nxt = run.out[2].cpu().numpy()
+        assert all(nxt[b] == -1 and a[b] == 0 and run.ora.n_emitted[b] == emitted[b] for b in done)
+        for (l, r), held in was.items():
+            now = run.held(l, r, len(held[0]))
+            assert all((x == y).all() for x, y in zip(now, held))
+        if len(done) == FP32.n_prompts:
+            break
+    assert len(done) == FP32.n_prompts and uneven
+    run.evict(32, 6)
     run.ctx.close()
 
 

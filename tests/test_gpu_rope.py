@@ -76,7 +76,7 @@ def test_inverse_is_the_gradient():
 
 
 def test_two_axes_are_the_contexts_positions():
-    """VVS_ROPE_OWN with two axes of size / 4 pairs rotates as the checker of the forward does."""
+    """VVS_ROPE_OWN with two axes of size / 4 pairs rotates as the oracle of the forward does."""
     from oracle import vvs_oracle as vo
     rope = vb.Rope(64, [16, 16], 10000.0, vb.VVS_FP32)
     x = torch.randn((5, 3, 64), generator=torch.Generator("cuda").manual_seed(4), device="cuda")
