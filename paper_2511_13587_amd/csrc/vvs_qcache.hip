@@ -826,7 +826,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
 // Many queries: a workgroup takes 128 of them, 32 per wave, and all its waves go through the same keys, so that what is done once per key - load, conversion, turning - is
 // shared: the waves bring the operands of 64 keys to LDS while those before are at work, from registers that were loaded another 64 keys earlier.  bf16 calls; grid as above.
 // 8 rows x 32 query heads on 8 x 512 tokens over 4096 slots, head size 128: 434 us, 670 TFLOP/s (16 queries per wave 646: every operand read from LDS for half as many); 4 rows over 2048
-// slots 138 us.  Bound by vector instructions and the waits between them and the matrix cores, of two waves per SIMD.
+// slots 138 to 150 us.  Bound by vector instructions and the waits between them and the matrix cores, of two waves per SIMD.
 // Blocks whose values do not go as fp16 (rare) are left for the end, each wave on its own, so that the registers of that path are not taken in the others.
 template <int DH>
 __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, int q_tiles) {
@@ -1181,7 +1181,9 @@ __global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, 
 }
 
 // Counted weights of many queries: the scores are made again, now with the normaliser known.  A wave holds the keys of STEPS steps of 32 in registers, the queries pass by, 64 at a
-// time, through LDS, shared by the four waves; their order is fixed.  Bound by exponentials: per score a product share, an fma, an exponential and an addition.
+// time, through LDS, shared by the four waves; their order is fixed.  Nothing in the loop may wait for the queries that were requested last: with the norms looked at as soon as they were
+// requested, and keys on their way when the loop began, 4 rows of 512, 384, 256 and 128 tokens over 2048 slots each, 8 x 4 heads of 128, took 78 us, now 60.  Products and exponentials would be
+// some 18 us each: bound by the chain LDS - product - exponential of few waves, the longest row's workgroups last.
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
   using S = QShape<T, DH>;
@@ -1199,12 +1201,13 @@ __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
   for (int step0 = first + blockIdx.x * 4 * STEPS; step0 < steps; step0 += gridDim.x * 4 * STEPS) {
     bf16x8 kf[STEPS][2][KD][NS];
     float sum[STEPS][8], c_exp[STEPS];
-    int valid[STEPS], tok0[STEPS];               // keys there; first block token (cached: -1)
+    int valid[STEPS], tok0[STEPS], q_all[STEPS];  // keys there; first block token (cached: -1); first query from which on all see all keys
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
       const int step = min(step0 + wave * STEPS + n, steps - 1);
       const bool there = step0 + wave * STEPS + n < steps, cached = step < w.blocks;
       tok0[n] = cached ? -1 : (step - w.blocks) * 32;
+      q_all[n] = cached ? 0 : a.causal ? (tok0[n] + 31) * a.group : INT_MAX;
       valid[n] = !there ? 0 : cached ? min(w.len - step * kQBlock, 32) : min(seen - tok0[n], 32);
       c_exp[n] = a.c_exp;
 #pragma unroll
@@ -1225,23 +1228,26 @@ __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
       }
     }
     // (of a chain only the queries from the workgroup's first block token on see anything of block tokens)
+    // Keys that are still on their way here would have every pass of the loop wait for whatever was requested last
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0)
     const int q_first = step0 >= w.blocks && a.causal ? (step0 - w.blocks) * 32 * a.group / 64 * 64 : 0;
     // a wave brings 16 of the 64 queries that pass by together: into registers while the ones before are at work, then to LDS; +inf as the norm of what is no query
     bf16x8 next[KD][NS];
     float next_norm = 0.f;
+    bool next_there = false;                     // (looked at when the norm is stored: here it would wait for the load)
     auto load_queries = [&](int q0) {
       const int at = q0 + wave * 16 + col, qi = min(at, nq - 1), t = qi / a.group;
 #pragma unroll
       for (int kd = 0; kd < KD; ++kd) load_operand<NS>(q + (size_t)t * a.q_stride + (size_t)(qi % a.group) * DH + kd * 32 + g * 8, next[kd]);
-      const float norm = a.norm[query_at(a, r, hk, qi)];
-      next_norm = at < nq ? norm : INFINITY;
+      next_norm = a.norm[query_at(a, r, hk, qi)];
+      next_there = at < nq;
     };
     auto put_queries = [&](int buf) {
 #pragma unroll
       for (int kd = 0; kd < KD; ++kd)
 #pragma unroll
         for (int p = 0; p < NS; ++p) s_q[buf][wave][kd * NS + p][lane] = __builtin_bit_cast(uint4, next[kd][p]);
-      if (g == 0) s_norm[buf][wave][col] = next_norm;
+      if (g == 0) s_norm[buf][wave][col] = next_there ? next_norm : INFINITY;
     };
     if (q_first < nq) load_queries(q_first);
     __syncthreads();
@@ -1260,17 +1266,16 @@ __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
 #pragma unroll
           for (int p = 0; p < NS; ++p) qf[kd][p] = as_bf16x8(s_q[buf][b][kd * NS + p][lane]);
         const float norm = s_norm[buf][b][col];
-        const int t = min(q0 + b * 16 + col, nq - 1) / a.group, t0 = (q0 + b * 16) / a.group;
         float sv[STEPS][8];
 #pragma unroll
         for (int n = 0; n < STEPS; ++n) step_scores<KD, NS, NS>(kf[n], qf, sv[n]);
 #pragma unroll
         for (int n = 0; n < STEPS; ++n) {
-          if (tok0[n] < 0 || (a.causal && tok0[n] + 31 <= t0)) {       // all queries see all keys that there are (the others' sums are left out below)
+          if (q0 + b * 16 >= q_all[n]) {       // all queries see all keys that there are (the others' sums are left out below)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[n][i] += __builtin_amdgcn_exp2f(fmaf(sv[n][i], c_exp[n], -norm));
           } else {
-            const uint32_t vis = sees8(a, t, tok0[n] + 8 * g, seen);
+            const uint32_t vis = sees8(a, min(q0 + b * 16 + col, nq - 1) / a.group, tok0[n] + 8 * g, seen);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const float p = __builtin_amdgcn_exp2f(fmaf(sv[n][i], c_exp[n], -norm));
