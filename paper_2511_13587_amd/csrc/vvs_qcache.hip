@@ -297,25 +297,13 @@ void launch_qcache_read(const QRead& a, int dtype, hipStream_t s) {
 // ------------------------------------------------------------------------------------------------ attention
 // One wave takes 32 keys a step (a cached block, or 32 block tokens) against 16 NQB queries; a query is (block token, query head of the key/value head).
 //
-// Scores S^T = K Q^T: e4m3 numbers are exact in bf16, the block's power of two is multiplied into the softmax's constant.  Weights are 2^(score c + E - M) with E the exponent of the
-// block's values, so that O^T += V^T P^T takes the e4m3 numbers themselves, as fp16; M is at most 2^6 below the largest such exponent so far, so that
-// weights fit fp16 (rounded to 2^-11, an eighth of the output's own rounding) and the accumulators are rescaled only when a maximum grows by more than that.  The normaliser sums the
-// fp32 weights, divided by 2^E, per lane; lanes, waves and splits are joined at the end, in a fixed order.
-// fp32 calls (queries, block keys and values, weights as sums of NS = 3 bf16 values, which hold all 24 bits), block tokens (values are bf16: weights as two bf16
-// values, to 2^-17) and blocks whose E is beyond +-40 (where fp16 weights could vanish beside others) take values in bf16, times 2^E.
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-
-// Eight e4m3 numbers as fp16 (exact)
-__device__ __forceinline__ f16x8 e4m3_to_f16(uint2 b) {
-  uint4 r;
-  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.x, 1.f, false));
-  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.x, 1.f, true));
-  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.y, 1.f, false));
-  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b.y, 1.f, true));
-  return __builtin_bit_cast(f16x8, r);
-}
-__device__ __forceinline__ uint32_t pack2half(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2_t{a, b}, f16x2)); }
+// Scores S^T = K Q^T: e4m3 numbers are exact in bf16, the block's power of two is multiplied into the softmax's constant.  Values go into O^T += V^T P^T as bf16 too, times their
+// block's power of two (exact).  Weights are 2^(score c - M), M at most 2^6 below the largest exponent so far, so that the accumulators are rescaled only when a maximum grows by more
+// than that; beside bf16 values they go as sums of two bf16 values (to 2^-17 of themselves, as in the contexts' attention), in fp32 calls as three, as queries, block keys and block values do,
+// which hold all 24 bits.  The exponents of bf16 are those of fp32: a weight keeps its bits however far it lies below others, and a block's power of two has no say in M.  (Single fp16 weights,
+// times their block's power of two, took half of the products, but what lay 2^14 below the largest of them lost bits, and 2^25 below it vanished, beside a normaliser that had
+// it: whole outputs behind a first token without value, small values behind a block of zeros.)  The normaliser sums the fp32 weights per lane; lanes, waves and splits are joined at the end,
+// in a fixed order.
 
 // x as a sum of NS bf16 values
 template <int NS>
@@ -349,9 +337,8 @@ __device__ __forceinline__ void load_operand(const bf16_t* p, bf16x8 (&out)[NS])
 
 template <typename T, int DH>
 struct QShape {
-  static constexpr bool F16 = sizeof(T) == 2;           // weights and cached values in fp16
   static constexpr int NS = sizeof(T) == 4 ? 3 : 1;     // bf16 values that make up an operand of the caller's type
-  static constexpr int NP = sizeof(T) == 4 ? 3 : 2;     // ... and a softmax weight beside values in bf16
+  static constexpr int NP = sizeof(T) == 4 ? 3 : 2;     // ... and a softmax weight
   static constexpr int KD = DH / 32, DT = DH / 16;
 };
 
@@ -482,19 +469,19 @@ struct QRun {
         for (int j = 0; j < 4; ++j) o[dt][j] *= alpha;
     }
   }
-  // weights of 8 keys, e[i] = 2^(sv[i] c + ev - m); their sum times 2^-ev = per_unit goes into the normaliser
-  __device__ __forceinline__ void exponentials(const float (&sv)[8], float c, float ev, float per_unit, float (&e)[8]) {
-    const float off = ev - (m == -INFINITY ? 0.f : m);
+  // weights of 8 keys, e[i] = 2^(sv[i] c - m), and their sum into the normaliser
+  __device__ __forceinline__ void exponentials(const float (&sv)[8], float c, float (&e)[8]) {
+    const float off = m == -INFINITY ? 0.f : -m;
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], c, off));
-    l = fmaf(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])), per_unit, l);
+    l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
   }
-  __device__ __forceinline__ void weights(const float (&sv)[8], float c, float ev, float per_unit, float (&e)[8]) {
-    follow(fmaf(top(sv), c, ev));
-    exponentials(sv, c, ev, per_unit, e);
+  __device__ __forceinline__ void weights(const float (&sv)[8], float c, float (&e)[8]) {
+    follow(top(sv) * c);
+    exponentials(sv, c, e);
   }
   template <int NK, int NP>
-  __device__ __forceinline__ void add_bf16(const float (&e)[8], const bf16x8 (&vf)[DT][NK]) {
+  __device__ __forceinline__ void add(const float (&e)[8], const bf16x8 (&vf)[DT][NK]) {
     bf16x8 pf[NP];
     split8<NP>(e, pf);
 #pragma unroll
@@ -506,12 +493,6 @@ struct QRun {
           if (sum - p < 0 || sum - p >= NP) continue;
           o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dt][p], pf[sum - p], o[dt], 0, 0, 0);
         }
-  }
-  __device__ __forceinline__ void add_f16(const float (&e)[8], const f16x8 (&vf)[DT]) {
-    const uint4 w = make_uint4(pack2half(e[0], e[1]), pack2half(e[2], e[3]), pack2half(e[4], e[5]), pack2half(e[6], e[7]));
-    const f16x8 pf = __builtin_bit_cast(f16x8, w);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[dt], pf, o[dt], 0, 0, 0);
   }
 };
 
@@ -679,51 +660,28 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
       kf[1][c][0] = e4m3_to_bf16(make_uint2(raw.k[c].z, raw.k[c].w), 1.f);
     }
     const float c_exp = fmaxf(a.c_exp * sc.x, FLT_MIN);     // above 0: masked scores are -inf
-    const int ev = exponent_of(sc.y);
     uint4 vraw[KD];
 #pragma unroll
     for (int c = 0; c < KD; ++c) vraw[c] = raw.v[c];
     // the wave's next block is on its way meanwhile
     if (step + 4 < cached_end) raw.load(data + (size_t)(step + 4) * a.c.block_bytes(), a.c.scale + region + step + 4, lane);
-    auto masked = [&](float (&sv)[8]) {
+    bf16x8 vf[DT][1];
+#pragma unroll
+    for (int c = 0; c < KD; ++c) {
+      vf[2 * c][0] = e4m3_to_bf16(make_uint2(vraw[c].x, vraw[c].y), sc.y);
+      vf[2 * c + 1][0] = e4m3_to_bf16(make_uint2(vraw[c].z, vraw[c].w), sc.y);
+    }
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      float sv[8], e[8];
+      step_scores<KD, 1, NS>(kf, qf[qb], sv);
       if (valid < kQBlock) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) sv[i] = 8 * g + i < valid ? sv[i] : -INFINITY;
       }
-    };
-    if (S::F16 && ev <= 40 && ev >= -40) {
-      f16x8 vf[DT];
-#pragma unroll
-      for (int c = 0; c < KD; ++c) {
-        vf[2 * c] = e4m3_to_f16(make_uint2(vraw[c].x, vraw[c].y));
-        vf[2 * c + 1] = e4m3_to_f16(make_uint2(vraw[c].z, vraw[c].w));
-      }
-      const float per_unit = 1.f / sc.y;
-#pragma unroll
-      for (int qb = 0; qb < NQB; ++qb) {
-        float sv[8], e[8];
-        step_scores<KD, 1, NS>(kf, qf[qb], sv);
-        masked(sv);
-        if (qb == 0 && n_kept) keep_scores(step, sv, c_exp);
-        run[qb].weights(sv, c_exp, (float)ev, per_unit, e);
-        run[qb].add_f16(e, vf);
-      }
-    } else {
-      bf16x8 vf[DT][1];
-#pragma unroll
-      for (int c = 0; c < KD; ++c) {
-        vf[2 * c][0] = e4m3_to_bf16(make_uint2(vraw[c].x, vraw[c].y), sc.y);
-        vf[2 * c + 1][0] = e4m3_to_bf16(make_uint2(vraw[c].z, vraw[c].w), sc.y);
-      }
-#pragma unroll
-      for (int qb = 0; qb < NQB; ++qb) {
-        float sv[8], e[8];
-        step_scores<KD, 1, NS>(kf, qf[qb], sv);
-        masked(sv);
-        if (qb == 0 && n_kept) keep_scores(step, sv, c_exp);
-        run[qb].weights(sv, c_exp, 0.f, 1.f, e);
-        run[qb].template add_bf16<1, NP>(e, vf);
-      }
+      if (qb == 0 && n_kept) keep_scores(step, sv, c_exp);
+      run[qb].weights(sv, c_exp, e);
+      run[qb].template add<1, NP>(e, vf);
     }
   }
   for (; step < s1; step += 4) {
@@ -739,8 +697,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
 #pragma unroll
       for (int i = 0; i < 8; ++i) sv[i] = (vis >> i) & 1 ? sv[i] : -INFINITY;
       if (qb == 0 && n_kept) keep_scores(step, sv, a.c_exp);
-      run[qb].weights(sv, a.c_exp, 0.f, 1.f, e);
-      run[qb].template add_bf16<NS, NP>(e, vf);
+      run[qb].weights(sv, a.c_exp, e);
+      run[qb].template add<NS, NP>(e, vf);
       if (odd) add_odd_values<DT>(a, v, e, qt[qb], tok0, seen, lane, run[qb].o);
     }
   }
@@ -827,7 +785,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
 // shared: the waves bring the operands of 64 keys to LDS while those before are at work, from registers that were loaded another 64 keys earlier.  bf16 calls; grid as above.
 // 8 rows x 32 query heads on 8 x 512 tokens over 4096 slots, head size 128: 434 us, 670 TFLOP/s (16 queries per wave 646: every operand read from LDS for half as many); 4 rows over 2048
 // slots 138 to 150 us.  Bound by vector instructions and the waits between them and the matrix cores, of two waves per SIMD.
-// Blocks whose values do not go as fp16 (rare) are left for the end, each wave on its own, so that the registers of that path are not taken in the others.
 template <int DH>
 __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, int q_tiles) {
   constexpr int KD = DH / 32, DT = DH / 16, NQB = 2, NQ = 64 * NQB;
@@ -871,42 +828,40 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, 
   const int cached_end = min(s1, w.blocks);
   const uint8_t* data = a.c.data + region * a.c.block_bytes();
   const float2* scales = a.c.scale + region;
-  auto scale_of = [&](int step) { const float2 sc = scales[step]; return make_float2(fmaxf(sc.x, kQSmall), fmaxf(sc.y, kQSmall)); };
-  auto half_values = [](float unit_of) { return unit_of <= 0x1p40f && unit_of >= 0x1p-40f; };
   auto tail = [&](int step, float (&sv)[8]) {   // slots behind the length
     const int mine = w.len - step * kQBlock - 8 * g;
     const uint32_t vis = mine >= 8 ? 255u : mine <= 0 ? 0u : (1u << mine) - 1;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sv[i] = (vis >> i) & 1 ? sv[i] : -INFINITY;
   };
-  bool left_out = false;                      // some cached block waits for the end
 
-  // ---- cached blocks, two at a time: a wave brings KD of the 4 KD pieces of 1 KiB
+  // ---- cached blocks, two at a time: a wave brings KD of the 4 KD pieces of 1 KiB, the keys or the values of one block
   if (s0 < cached_end) {
     uint4 raw[KD];
+    float unit_of = 0.f;                       // power of two of the values on their way
+    const int b = wave >> 1;
     auto load_raw = [&](int step) {
+      const int at = min(step + b, cached_end - 1);
+      unit_of = scales[at].y;
 #pragma unroll
-      for (int n = 0; n < KD; ++n) {
-        const int piece = wave * KD + n, b = piece / (2 * KD);
-        raw[n] = *(const uint4*)(data + (size_t)min(step + b, cached_end - 1) * a.c.block_bytes() + (piece % (2 * KD) * 64 + lane) * 16);
-      }
+      for (int n = 0; n < KD; ++n) raw[n] = *(const uint4*)(data + (size_t)at * a.c.block_bytes() + (((wave & 1) * KD + n) * 64 + lane) * 16);
     };
     auto bring = [&](int step, int buf) {
+      const float unit = fmaxf(unit_of, kQSmall);
 #pragma unroll
       for (int n = 0; n < KD; ++n) {
-        const int piece = (wave * KD + n) % (2 * KD), b = (wave * KD + n) / (2 * KD);
         uint2 lo = make_uint2(raw[n].x, raw[n].y), hi = make_uint2(raw[n].z, raw[n].w);
-        if (piece < KD) {
-          s_k[buf][b][piece][lane] = __builtin_bit_cast(uint4, e4m3_to_bf16(lo, 1.f));
-          s_k[buf][b][KD + piece][lane] = __builtin_bit_cast(uint4, e4m3_to_bf16(hi, 1.f));
+        if (!(wave & 1)) {
+          s_k[buf][b][n][lane] = __builtin_bit_cast(uint4, e4m3_to_bf16(lo, 1.f));
+          s_k[buf][b][KD + n][lane] = __builtin_bit_cast(uint4, e4m3_to_bf16(hi, 1.f));
         } else {
           if (step + b >= cached_end || w.len - (step + b) * kQBlock < kQBlock) {                 // (a second block that is not there: zeros)
             const int mine = step + b < cached_end ? w.len - (step + b) * kQBlock - 8 * g : 0;
             const uint64_t keep = mine >= 8 ? ~0ull : mine <= 0 ? 0ull : (1ull << (8 * mine)) - 1;
             lo.x &= (uint32_t)keep; lo.y &= (uint32_t)(keep >> 32); hi.x &= (uint32_t)keep; hi.y &= (uint32_t)(keep >> 32);
           }
-          s_v[buf][b][2 * (piece - KD)][lane] = __builtin_bit_cast(uint4, e4m3_to_f16(lo));
-          s_v[buf][b][2 * (piece - KD) + 1][lane] = __builtin_bit_cast(uint4, e4m3_to_f16(hi));
+          s_v[buf][b][2 * n][lane] = __builtin_bit_cast(uint4, e4m3_to_bf16(lo, unit));
+          s_v[buf][b][2 * n + 1][lane] = __builtin_bit_cast(uint4, e4m3_to_bf16(hi, unit));
         }
       }
     };
@@ -915,19 +870,10 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, 
     if (s0 + 2 < cached_end) load_raw(s0 + 2);
     __syncthreads();
     for (int step0 = s0, buf = 0; step0 < cached_end; step0 += 2, buf ^= 1) {
-      // both blocks at once: twice the independent work between the waits for the matrix cores and for the maxima.  One that is not there or goes as bf16 gets weights of 0
-      float c_exp[2], ev[2], per_unit[2];
-      bool gone[2];
+      // both blocks at once: twice the independent work between the waits for the matrix cores and for the maxima.  One that is not there gets weights of 0
+      float c_exp[2];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const float2 scale = scale_of(min(step0 + b, cached_end - 1));
-        const bool there = step0 + b < cached_end, half = half_values(scale.y);
-        left_out |= there && !half;
-        gone[b] = !there || !half;
-        c_exp[b] = fmaxf(a.c_exp * scale.x, FLT_MIN);
-        ev[b] = half ? (float)exponent_of(scale.y) : 0.f;
-        per_unit[b] = half ? 1.f / scale.y : 1.f;
-      }
+      for (int b = 0; b < 2; ++b) c_exp[b] = fmaxf(a.c_exp * fmaxf(scales[min(step0 + b, cached_end - 1)].x, kQSmall), FLT_MIN);
       float sv[2][NQB][8];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -953,27 +899,27 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, 
 #pragma unroll
           for (int qb = 0; qb < NQB; ++qb) tail(step0 + b, sv[b][qb]);
         }
-        if (n_kept && !gone[b]) keep_scores(step0 + b, sv[b][0], 1.f);
-        if (gone[b]) {
+        if (step0 + b >= cached_end) {
 #pragma unroll
           for (int qb = 0; qb < NQB; ++qb)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sv[b][qb][i] = -INFINITY;
+        } else if (n_kept) {
+          keep_scores(step0 + b, sv[b][0], 1.f);
         }
       }
 #pragma unroll
-      for (int qb = 0; qb < NQB; ++qb)
-        run[qb].follow(fmaxf(QRun<DT>::top(sv[0][qb]) + ev[0], QRun<DT>::top(sv[1][qb]) + ev[1]));
+      for (int qb = 0; qb < NQB; ++qb) run[qb].follow(fmaxf(QRun<DT>::top(sv[0][qb]), QRun<DT>::top(sv[1][qb])));
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        f16x8 vf[DT];
+        bf16x8 vf[DT][1];
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) vf[dt] = __builtin_bit_cast(f16x8, s_v[buf][b][dt][lane]);
+        for (int dt = 0; dt < DT; ++dt) vf[dt][0] = as_bf16x8(s_v[buf][b][dt][lane]);
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb) {
           float e[8];
-          run[qb].exponentials(sv[b][qb], 1.f, ev[b], per_unit[b], e);
-          run[qb].add_f16(e, vf);
+          run[qb].exponentials(sv[b][qb], 1.f, e);
+          run[qb].template add<1, 2>(e, vf);
         }
       }
       __syncthreads();
@@ -1041,39 +987,12 @@ __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, 
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb) {
           float e[8];
-          run[qb].weights(sv[qb], a.c_exp, 0.f, 1.f, e);
-          run[qb].template add_bf16<1, 2>(e, vf);
+          run[qb].weights(sv[qb], a.c_exp, e);
+          run[qb].template add<1, 2>(e, vf);
           if (odd) add_odd_values<DT>(a, v, e, qt[qb], tok0, seen, lane, run[qb].o);
         }
       }
       __syncthreads();
-    }
-  }
-
-  // ---- cached blocks whose values go as bf16
-  for (int step = s0; left_out && step < cached_end; ++step) {
-    const float2 scale = scale_of(step);
-    if (half_values(scale.y)) continue;
-    QRaw<DH> block;
-    block.load(data + (size_t)step * a.c.block_bytes(), scales + step, lane);
-    block.mask_values(lane, w.len - step * kQBlock);
-    bf16x8 kf[2][KD][1], vf[DT][1];
-#pragma unroll
-    for (int c = 0; c < KD; ++c) {
-      kf[0][c][0] = e4m3_to_bf16(make_uint2(block.k[c].x, block.k[c].y), 1.f);
-      kf[1][c][0] = e4m3_to_bf16(make_uint2(block.k[c].z, block.k[c].w), 1.f);
-      vf[2 * c][0] = e4m3_to_bf16(make_uint2(block.v[c].x, block.v[c].y), scale.y);
-      vf[2 * c + 1][0] = e4m3_to_bf16(make_uint2(block.v[c].z, block.v[c].w), scale.y);
-    }
-    const float c_exp = fmaxf(a.c_exp * scale.x, FLT_MIN);
-#pragma unroll
-    for (int qb = 0; qb < NQB; ++qb) {
-      float sv[8], e[8];
-      step_scores<KD, 1, 1>(kf, qf[qb], sv);
-      tail(step, sv);
-      if (qb == 0 && n_kept) keep_scores(step, sv, c_exp);
-      run[qb].weights(sv, c_exp, 0.f, 1.f, e);
-      run[qb].template add_bf16<1, 2>(e, vf);
     }
   }
 
