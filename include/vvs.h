@@ -370,7 +370,8 @@ vvs_status vvs_qcache_append(vvs_qcache* c, int32_t layer, int32_t n_layers, con
  *                n_tokens > VVS_MAX_T.  What a masked token holds, NaN and infinities included, does not matter.
  *   d_k, d_v   : [n_rows, n_tokens, n_kv_heads, head_size]; both NULL: the queries see the cache alone
  *   scale      : positive and finite
- *   d_out      : [n_rows, n_tokens, n_heads, head_size], contiguous; a query that sees nothing (no block, nothing cached) gets zeros
+ *   d_out      : [n_rows, n_tokens, n_heads, head_size], contiguous; a query that sees nothing (no block, nothing cached) gets zeros.  Apart from d_k and d_v, and from d_q,
+ *                whose queries are read again behind the outputs where weights are counted; without d_mass and d_block_mass it may be a contiguous d_q itself
  *   d_lse      : float [n_rows, n_tokens, n_heads] out, log of the sum of exp(scale q k) (-inf for a query that sees nothing); may be NULL
  *   n_counted  : the softmax weights of tokens 0 .. n_counted - 1 of every row, of all query heads of a key/value head, are added up per key:
  *   d_mass     : float [n_rows, n_kv_heads, capacity], cached slots: added to (NULL: left out)

@@ -434,6 +434,13 @@ def _per_token(t: Optional[torch.Tensor], device: int, dtype: torch.dtype, shape
     return t.data_ptr(), token
 
 
+def _apart(out: int, n_out: int, tensors, tokens: int, width: int):
+    """Refuses an output at address `out`, of n_out elements of `width` bytes, that shares memory with one of tensors: (address or None, elements from token to token, elements of a token)."""
+    for p, stride, per in tensors:
+        if p is not None and p < out + n_out * width and out < p + ((tokens - 1) * stride + per) * width:
+            raise ValueError("out: shares memory with q, k or v")
+
+
 _raw_stream = torch._C._cuda_getCurrentRawStream     # (current_stream() makes a stream object each time: 1.5 us of a 5 us call)
 
 
@@ -469,6 +476,7 @@ class QCache:
         if not torch.cuda.is_available():
             raise RuntimeError("libvvs needs a HIP device; there is no CPU path")
         self.device, self.dtype = torch.device(device), _TORCH_DTYPE[dtype]
+        self.width = self.dtype.itemsize
         self.index = torch.cuda.current_device() if self.device.index is None else self.device.index
         with torch.cuda.device(self.index):
             self.cache = torch.empty(self.cache_bytes, dtype=torch.uint8, device=self.device)
@@ -517,7 +525,8 @@ class QCache:
                              n_tokens: Optional[torch.Tensor] = None, parent=None, tree_mask=None, scale: Optional[float] = None,
                              lse: Optional[torch.Tensor] = None, n_counted: int = 0, mass: Optional[torch.Tensor] = None,
                              block_mass: Optional[torch.Tensor] = None, layer: int = 0):
-        """q [rows, tokens, heads, size]; k, v [rows, tokens, kv heads, size] or None; out like q, contiguous.  scale: None = size ** -0.5."""
+        """q [rows, tokens, heads, size]; k, v [rows, tokens, kv heads, size] or None; out like q, contiguous, in memory of its own (or q itself, contiguous,
+        where no weights are counted).  scale: None = size ** -0.5."""
         rows, heads, kv, size, capacity = self.shape
         t = q.shape[1] if q.dim() == 4 else 0
         qp, qs = _per_token(q, self.index, self.dtype, (rows, t, heads, size), "q")
@@ -525,14 +534,19 @@ class QCache:
         vp, vs = _per_token(v, self.index, self.dtype, (rows, t, kv, size), "v")
         p = None if parent is None else np.ascontiguousarray(parent, dtype=np.int32)
         m = None if tree_mask is None else np.ascontiguousarray(tree_mask, dtype=np.uint8)
+        op = _on(out, self.index, self.dtype, (rows, t, heads, size), "out")
+        token = self.width * rows * t                        # bytes per element of a token
+        end = op + token * heads * size
+        if (qp < end and op < qp + token * qs) or (kp is not None and kp < end and op < kp + token * ks) or (vp is not None and vp < end and op < vp + token * vs):
+            in_place = op == qp and qs == heads * size and n_counted == 0 and block_mass is None
+            _apart(op, rows * t * heads * size, ((None if in_place else qp, qs, heads * size), (kp, ks, kv * size), (vp, vs, kv * size)), rows * t, self.width)
         if (p is not None and p.shape != (t - 1,)) or (m is not None and m.shape != (t, t)):
             raise ValueError("parent wants [tokens - 1] and tree_mask [tokens, tokens] entries")
         with _Current(self.index):
             self._check(lib.vvs_qcache_attention(
                 self.h, layer, self._rows(length, "length"), t, self._rows(n_tokens, "n_tokens"), None if p is None else p.ctypes.data,
                 None if m is None else m.ctypes.data, qp, qs, kp, ks, vp, vs, size ** -0.5 if scale is None else float(scale),
-                _on(out, self.index, self.dtype, (rows, t, heads, size), "out"),
-                _on(lse, self.index, torch.float32, (rows, t, heads), "lse"), n_counted,
+                op, _on(lse, self.index, torch.float32, (rows, t, heads), "lse"), n_counted,
                 _on(mass, self.index, torch.float32, (rows, kv, capacity), "mass"),
                 _on(block_mass, self.index, torch.float32, (rows, kv, t), "block_mass"), _raw_stream(self.index)))
 
