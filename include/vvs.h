@@ -359,7 +359,8 @@ const char* vvs_qcache_last_error(const vvs_qcache* c);   /* c must not be NULL 
  *   n_tokens   : most tokens taken of a row; src_tokens: tokens per row of d_k and d_v
  *   d_select   : int32 [n_rows, n_tokens]: the source token of each taken one (an accepted path; one outside [0, src_tokens) is taken as zeros), or
  *                NULL: the first ones, and n_tokens <= src_tokens
- * Tokens beyond the capacity are dropped.  Slots below d_len keep their values up to the rounding above. */
+ * Tokens beyond the capacity are dropped.  Slots below d_len keep their values up to the rounding above.  Weights and positions of the slots (vvs_qcache_evict) are the caller's: whoever
+ * evicts more than once writes the positions of the appended tokens into their slots. */
 vvs_status vvs_qcache_append(vvs_qcache* c, int32_t layer, int32_t n_layers, const int32_t* d_len, int32_t n_tokens, const int32_t* d_n_tokens,
                              int32_t src_tokens, const int32_t* d_select, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
                              vvs_stream s);
@@ -388,7 +389,8 @@ vvs_status vvs_qcache_attention(vvs_qcache* c, int32_t layer, const int32_t* d_l
  *   keep       : a multiple of VVS_QCACHE_BLOCK, at least one block; recent: in [0, keep]
  *   d_mass     : float [n_layers, n_rows, n_kv_heads, capacity];  d_mass_out: the same, out, weights of what lies in the slots now, 0 behind the new length (may
  *                be d_mass itself)
- *   d_pos, d_pos_out: int32, likewise, positions of the tokens in the slots (0 behind the new length); both NULL: a slot's number is its position, as it is before the first eviction */
+ *   d_pos, d_pos_out: int32, likewise, positions of the tokens in the slots (0 behind the new length); both NULL: a slot's number is its position, as it is before the first
+ *                eviction.  Behind one, slots that are appended to hold 0 until the caller says which tokens they hold: left at that, they are the oldest, not the newest */
 vvs_status vvs_qcache_evict(vvs_qcache* c, int32_t layer, int32_t n_layers, const int32_t* d_len, int32_t keep, int32_t recent, const float* d_mass,
                             float* d_mass_out, const int32_t* d_pos, int32_t* d_pos_out, vvs_stream s);
 
