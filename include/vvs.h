@@ -101,7 +101,7 @@ typedef struct {
                                     VVS_CACHE_E4M3: they are held in 8 bits (see vvs_qcache below: what is held, and by which rounding), in
                                       half of the bytes of bf16, for contexts whose cache is what fills HBM.  Keys and values of the tokens of
                                       a call are taken as they are (a verify call: of all its nodes; a prefill: of a chunk of up to 512 tokens, fp32
-                                      64), and rounded when they are cached.  Layers run as separate launches (no drafter contexts; head size 32,
+                                      64), and rounded when they are cached (see vvs_set_state for roll-backs).  Layers run as separate launches (no drafter contexts; head size 32,
                                       64 or 128, as the dtype allows), so that calls of few rows take longer than with VVS_CACHE_SAME */
 } vvs_config;
 enum { VVS_NORM_AUTO = 0, VVS_NORM_SEPARATE = 1 };
@@ -444,7 +444,10 @@ vvs_status vvs_read_state(vvs_ctx* ctx, int32_t* d_state, vvs_stream s);
 /* Overwrites the per-prompt state with int32 [3, B] (same layout as vvs_read_state): rolls the context
  * back (or forward) to a cached length whose K/V are still in the cache, e.g. to replay one verify
  * call.  Cached slots below the given length must hold valid K/V; that is the caller's business.
- * Clears a pending (uncommitted) verify. */
+ * Clears a pending (uncommitted) verify.
+ * With VVS_CACHE_E4M3 a roll-back into a block of VVS_QCACHE_BLOCK slots does not undo what the tokens committed since did to it: where they were larger than the block's, it keeps their power
+ * of two, and its slots the rounding to it (elements below 2^-6 of it lose bits).  A replay of a verify call may therefore differ from the call; replays among each other have the same bits.
+ * Nor does it undo an eviction: a state from before one is not restored. */
 vvs_status vvs_set_state(vvs_ctx* ctx, const int32_t* d_state, vvs_stream s);
 
 /* Kernel-class timing for benchmarks.  While enabled, every kernel launch of prefill / verify /
