@@ -334,7 +334,8 @@ vvs_status vvs_draft(vvs_ctx* drafter, vvs_ctx* target, int32_t n_nodes, const i
  * Tensors are [n_rows, n_tokens, heads, head_size] in the cache's dtype; a stride argument gives the elements from one token to the next where they lie further apart
  * than heads * head_size (0: they do not), so that q, k and v can be parts of one projection's output.  Rows are n_tokens tokens apart.  Pointers and
  * strides have to be multiples of 16 bytes.  All tensors live on the device that was current at vvs_qcache_create, which has to be current at every call.
- * Calls on one cache share its workspace: issue them on one stream, or order them.  All calls can be captured into a graph. */
+ * Calls on one cache share its workspace: issue them on one stream, or order them.  All calls can be captured into a graph.
+ * One call appends, evicts down to, or reads about 2^31 / n_kv_heads slots per row at most (VVS_ESIZE beyond). */
 #define VVS_QCACHE_BLOCK 32
 typedef struct vvs_qcache vvs_qcache;  /* opaque host object; owns no device memory */
 
@@ -424,7 +425,7 @@ vvs_status vvs_rope_create(const vvs_rope_config* cfg, vvs_rope** out);   /* hos
 void vvs_rope_destroy(vvs_rope* r);
 const char* vvs_rope_last_error(const vvs_rope* r);                       /* r must not be NULL */
 
-/* Rotates queries and keys of n_tokens tokens in one launch; angles are taken in 64 bits, so that far positions are as exact as near ones.
+/* Rotates queries and keys of n_tokens tokens (up to 2^26 - 4) in one launch; angles are taken in 64 bits, so that far positions are as exact as near ones.
  *   d_pos      : int32 [n_tokens, n_axes], any sign
  *   d_q, d_q_out [n_tokens, n_heads, head_size]; d_k, d_k_out [n_tokens, n_kv_heads, head_size] (n_kv_heads 0: NULL); an output may be its input; strides as for
  *                the cache's tensors, 0: contiguous; pointers and strides multiples of 16 bytes

@@ -94,6 +94,9 @@ static int64_t stride_of(int64_t given, int64_t least, int dtype) {
   return s < least || s % per16 || s > ((int64_t)1 << 31) ? -1 : s;
 }
 
+// Units (waves, tokens) that a launch of four per workgroup of 256 threads holds: a grid has fewer than 2^32 threads along a dimension.  Asked in front of a call's first launch, so that none is left half done.
+constexpr int64_t kMostUnits = ((int64_t)1 << 26) - 4;
+
 }  // namespace vvs
 
 using namespace vvs;
@@ -150,6 +153,7 @@ vvs_status vvs_qcache_append(vvs_qcache* qc, int32_t layer, int32_t n_layers, co
   if (!d_len || !d_k || !d_v) return no(&c->err, VVS_EINVAL, "qcache append: NULL argument");
   if (n_tokens < 1 || src_tokens < 1 || n_tokens > (1 << 30) || src_tokens > (1 << 30)) return no(&c->err, VVS_EINVAL, "qcache append: numbers of tokens must be positive");
   if (!d_select && n_tokens > src_tokens) return no(&c->err, VVS_EINVAL, "qcache append: more tokens than d_k and d_v hold");
+  if (c->cfg.n_kv_heads * std::min<int64_t>(((int64_t)n_tokens + 2 * kQBlock - 2) / kQBlock, c->lay.blocks) > kMostUnits) return no(&c->err, VVS_ESIZE, "qcache append: too many tokens");
   const int64_t per = (int64_t)c->cfg.n_kv_heads * c->cfg.head_size, ks = stride_of(k_stride, per, c->cfg.dtype), vs = stride_of(v_stride, per, c->cfg.dtype);
   if (ks < 0 || vs < 0 || unaligned(d_k) || unaligned(d_v)) return no(&c->err, VVS_EINVAL, "qcache append: pointers and strides must be multiples of 16 bytes, strides cover a token");
   if ((st = check_device(c)) != VVS_OK) return st;
@@ -229,6 +233,7 @@ vvs_status vvs_qcache_evict(vvs_qcache* qc, int32_t layer, int32_t n_layers, con
   if (!d_pos != !d_pos_out) return no(&c->err, VVS_EINVAL, "qcache evict: d_pos and d_pos_out go together");
   if (keep < kQBlock || keep % kQBlock) return no(&c->err, VVS_EINVAL, "qcache evict: keep must be a positive multiple of VVS_QCACHE_BLOCK");
   if (recent < 0 || recent > keep) return no(&c->err, VVS_EINVAL, "qcache evict: recent must be in [0, keep]");
+  if (keep < c->cfg.capacity && (int64_t)c->cfg.n_kv_heads * (keep / kQBlock) > kMostUnits) return no(&c->err, VVS_ESIZE, "qcache evict: too many slots are kept");
   if (((uintptr_t)d_mass | (uintptr_t)d_mass_out | (uintptr_t)d_pos | (uintptr_t)d_pos_out) & 3) return no(&c->err, VVS_EINVAL, "qcache evict: unaligned weights or positions");
   if ((st = check_device(c)) != VVS_OK) return st;
   QEvict a{};
@@ -249,7 +254,7 @@ vvs_status vvs_qcache_read(vvs_qcache* qc, int32_t layer, int32_t n_layers, cons
   if (st != VVS_OK) return st;
   if (!d_len || !d_k || !d_v) return no(&c->err, VVS_EINVAL, "qcache read: NULL argument");
   if (n_slots < 1 || n_slots > (1 << 30)) return no(&c->err, VVS_EINVAL, "qcache read: n_slots must be positive");
-  if ((int64_t)c->cfg.n_kv_heads * (n_slots / kQBlock + 2) > INT32_MAX) return no(&c->err, VVS_ESIZE, "qcache read: too many slots");
+  if (c->cfg.n_kv_heads * (((int64_t)n_slots + 2 * kQBlock - 2) / kQBlock) > kMostUnits) return no(&c->err, VVS_ESIZE, "qcache read: too many slots");
   if (unaligned(d_k) || unaligned(d_v)) return no(&c->err, VVS_EINVAL, "qcache read: pointers must be multiples of 16 bytes");
   if ((st = check_device(c)) != VVS_OK) return st;
   QRead a{};
@@ -323,6 +328,7 @@ vvs_status vvs_rope_apply(vvs_rope* rope, int32_t n_tokens, const int32_t* d_pos
   if (!d_pos || !d_q || !d_q_out) return no(&r->err, VVS_EINVAL, "rope: NULL argument");
   if (n_tokens < 1 || n_heads < 1 || n_kv_heads < 0) return no(&r->err, VVS_EINVAL, "rope: n_tokens and n_heads must be positive, n_kv_heads not negative");
   if (n_heads > 4096 || n_kv_heads > 4096) return no(&r->err, VVS_ESIZE, "rope: at most 4096 heads");
+  if (n_tokens > kMostUnits) return no(&r->err, VVS_ESIZE, "rope: at most 2^26 - 4 tokens");
   if (n_kv_heads ? !d_k || !d_k_out : d_k || d_k_out) return no(&r->err, VVS_EINVAL, "rope: d_k, d_k_out and n_kv_heads go together");
   if (inverse != 0 && inverse != 1) return no(&r->err, VVS_EINVAL, "rope: inverse must be 0 or 1");
   const int64_t per = (int64_t)n_heads * g.head_size, kper = (int64_t)n_kv_heads * g.head_size;
