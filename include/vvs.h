@@ -378,7 +378,9 @@ vvs_status vvs_qcache_append(vvs_qcache* c, int32_t layer, int32_t n_layers, con
  *   n_counted  : the softmax weights of tokens 0 .. n_counted - 1 of every row, of all query heads of a key/value head, are added up per key:
  *   d_mass     : float [n_rows, n_kv_heads, capacity], cached slots: added to (NULL: left out)
  *   d_block_mass: float [n_rows, n_kv_heads, n_tokens], block tokens: set (NULL: left out)
- * Sums are in a fixed order: the same call gives the same bits. */
+ * Sums are in a fixed order: the same call gives the same bits.  They are taken in front of the division by the weights' sum, of up to 64 |v| per key: values of 2^121 over the number of
+ * keys and more may come out as infinities.  How a call is cut into pieces goes by n_tokens and the capacity, not by d_len, which a captured call finds changed: a large, nearly empty
+ * cache pays for joining pieces without slots. */
 vvs_status vvs_qcache_attention(vvs_qcache* c, int32_t layer, const int32_t* d_len, int32_t n_tokens, const int32_t* d_n_tokens, const int32_t* h_parent,
                                 const uint8_t* h_tree_mask, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v,
                                 int64_t v_stride, float scale, void* d_out, float* d_lse, int32_t n_counted, float* d_mass, float* d_block_mass, vvs_stream s);

@@ -61,6 +61,25 @@ __device__ __forceinline__ void store8(bf16_t* base, int row, int k0, int K, con
   *(uint4*)(base + pack_index(row, k0, K)) = o;
 }
 
+// 8 consecutive elements of a row as they lie in memory
+__device__ __forceinline__ void read8(const float* p, float (&v)[8]) {
+  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void read8(const bf16_t* p, float (&v)[8]) {
+  const uint4 a = *(const uint4*)p;
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void write8(float* p, const float (&v)[8]) {
+  ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void write8(bf16_t* p, const float (&v)[8]) {
+  *(uint4*)p = make_uint4(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7]));
+}
+
 // wave64 reductions, fixed order, the result in every lane.  Six steps of a dependent chain, each a plain VALU move: the halves and
 // the odd / even 16-lane rows are exchanged with gfx950's row swaps (given one value twice they return the pair to combine in
 // every lane), then inside a row the partner is 8 lanes on, mirrored inside 8 lanes, two lanes on, the neighbour.  A __shfl_xor

@@ -90,24 +90,6 @@ __device__ __forceinline__ uint4 transpose_halves(uint4 v, int lane) {
   return v;
 }
 
-__device__ __forceinline__ void read8(const float* p, float (&v)[8]) {
-  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void unpack8(uint4 a, float (&v)[8]) {
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-}
-__device__ __forceinline__ void read8(const bf16_t* p, float (&v)[8]) { unpack8(*(const uint4*)p, v); }
-__device__ __forceinline__ void write8(float* p, const float (&v)[8]) {
-  ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void write8(bf16_t* p, const float (&v)[8]) {
-  *(uint4*)p = make_uint4(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7]));
-}
-
 // slot of tile t's row that lane l % 16 = i supplies (keys), and the one whose dims it takes before the transpose (values)
 __device__ __forceinline__ int slot_of(int t, int i) { return 8 * (i >> 2) + 4 * t + (i & 3); }
 __device__ __forceinline__ int value_slot(int lane) { return 8 * (lane >> 4) + (lane & 7); }
@@ -541,7 +523,8 @@ __device__ __forceinline__ void store4(const QAttention& a, size_t at, int dim, 
   }
 }
 
-// log-sum-exp for the caller, and in units of log2 for the counted weights of many queries (its size takes some of the 24 bits: weights to 2^-20 of themselves)
+// log-sum-exp for the caller, and in units of log2 for the counted weights of many queries: as one number, so that its size takes some of the 24 bits, and weights are off by
+// 2^-24 of |norm| relative to themselves (2^-18 at scores 64 powers of two from 0), as they are by the rounding of the scores
 __device__ __forceinline__ void tell_norm(const QAttention& a, size_t at, float m, float l) {
   const bool none = l == 0.f;            // a query that sees nothing
   if (a.lse) a.lse[at] = none ? -INFINITY : (m + log2f(l)) * kLn2;
@@ -1099,14 +1082,14 @@ __global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, 
   if (dim == 0) tell_norm(a, at, m, l);
 }
 
-// Counted weights of many queries: the scores are made again, now with the normaliser known.  A wave holds the keys of STEPS steps of 32 in registers, the queries pass by, 64 at a
+// Counted weights of many queries: the scores are made again, now with the normaliser known.  A wave holds the keys of a step of 32 in registers, the queries pass by, 64 at a
 // time, through LDS, shared by the four waves; their order is fixed.  Nothing in the loop may wait for the queries that were requested last: with the norms looked at as soon as they were
 // requested, and keys on their way when the loop began, 4 rows of 512, 384, 256 and 128 tokens over 2048 slots each, 8 x 4 heads of 128, took 78 us, now 60.  Products and exponentials would be
 // some 18 us each: bound by the chain LDS - product - exponential of few waves, the longest row's workgroups last.
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
   using S = QShape<T, DH>;
-  constexpr int KD = S::KD, NS = S::NS, STEPS = 1;
+  constexpr int KD = S::KD, NS = S::NS;
   __shared__ uint4 s_q[2][4][KD * NS][64];
   __shared__ float s_norm[2][4][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
@@ -1117,38 +1100,33 @@ __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
   const T* q = (const T*)a.q + (size_t)r * a.T * a.q_stride + (size_t)hk * a.group * DH;
   const T* k = (const T*)a.k + (size_t)r * a.T * a.k_stride + (size_t)hk * DH;
   const size_t region = a.c.region(a.layer, r, hk) * a.c.blocks;
-  for (int step0 = first + blockIdx.x * 4 * STEPS; step0 < steps; step0 += gridDim.x * 4 * STEPS) {
-    bf16x8 kf[STEPS][2][KD][NS];
-    float sum[STEPS][8], c_exp[STEPS];
-    int valid[STEPS], tok0[STEPS], q_all[STEPS];  // keys there; first block token (cached: -1); first query from which on all see all keys
+  for (int step0 = first + blockIdx.x * 4; step0 < steps; step0 += gridDim.x * 4) {
+    bf16x8 kf[2][KD][NS];
+    float sum[8], c_exp = a.c_exp;
+    const int step = min(step0 + wave, steps - 1);
+    const bool there = step0 + wave < steps, cached = step < w.blocks;
+    const int tok0 = cached ? -1 : (step - w.blocks) * 32;                                         // first block token
+    const int q_all = cached ? 0 : a.causal ? (tok0 + 31) * a.group : INT_MAX;                      // first query from which on all see all keys
+    const int valid = !there ? 0 : cached ? min(w.len - step * kQBlock, 32) : min(seen - tok0, 32);  // keys there
 #pragma unroll
-    for (int n = 0; n < STEPS; ++n) {
-      const int step = min(step0 + wave * STEPS + n, steps - 1);
-      const bool there = step0 + wave * STEPS + n < steps, cached = step < w.blocks;
-      tok0[n] = cached ? -1 : (step - w.blocks) * 32;
-      q_all[n] = cached ? 0 : a.causal ? (tok0[n] + 31) * a.group : INT_MAX;
-      valid[n] = !there ? 0 : cached ? min(w.len - step * kQBlock, 32) : min(seen - tok0[n], 32);
-      c_exp[n] = a.c_exp;
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    if (cached) {
+      const uint8_t* data = a.c.data + (region + step) * a.c.block_bytes();
+      c_exp = fmaxf(a.c_exp * a.c.scale[region + step].x, FLT_MIN);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[n][i] = 0.f;
-      if (cached) {
-        const uint8_t* data = a.c.data + (region + step) * a.c.block_bytes();
-        c_exp[n] = fmaxf(a.c_exp * a.c.scale[region + step].x, FLT_MIN);
+      for (int kd = 0; kd < KD; ++kd) {
+        const uint4 b = *(const uint4*)(data + (kd * 64 + lane) * 16);
+        kf[0][kd][0] = e4m3_to_bf16(make_uint2(b.x, b.y), 1.f);
+        kf[1][kd][0] = e4m3_to_bf16(make_uint2(b.z, b.w), 1.f);
 #pragma unroll
-        for (int kd = 0; kd < KD; ++kd) {
-          const uint4 b = *(const uint4*)(data + (kd * 64 + lane) * 16);
-          kf[n][0][kd][0] = e4m3_to_bf16(make_uint2(b.x, b.y), 1.f);
-          kf[n][1][kd][0] = e4m3_to_bf16(make_uint2(b.z, b.w), 1.f);
-#pragma unroll
-          for (int p = 1; p < NS; ++p) kf[n][0][kd][p] = kf[n][1][kd][p] = as_bf16x8(make_uint4(0, 0, 0, 0));
-        }
-      } else {
-        keys_of_tokens<T, DH, NS>(k, a.k_stride, tok0[n], seen, lane, kf[n]);
+        for (int p = 1; p < NS; ++p) kf[0][kd][p] = kf[1][kd][p] = as_bf16x8(make_uint4(0, 0, 0, 0));
       }
+    } else {
+      keys_of_tokens<T, DH, NS>(k, a.k_stride, tok0, seen, lane, kf);
     }
-    // (of a chain only the queries from the workgroup's first block token on see anything of block tokens)
     // Keys that are still on their way here would have every pass of the loop wait for whatever was requested last
     __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0)
+    // (of a chain only the queries from the workgroup's first block token on see anything of block tokens)
     const int q_first = step0 >= w.blocks && a.causal ? (step0 - w.blocks) * 32 * a.group / 64 * 64 : 0;
     // a wave brings 16 of the 64 queries that pass by together: into registers while the ones before are at work, then to LDS; +inf as the norm of what is no query
     bf16x8 next[KD][NS];
@@ -1185,46 +1163,39 @@ __global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
 #pragma unroll
           for (int p = 0; p < NS; ++p) qf[kd][p] = as_bf16x8(s_q[buf][b][kd * NS + p][lane]);
         const float norm = s_norm[buf][b][col];
-        float sv[STEPS][8];
+        float sv[8];
+        step_scores<KD, NS, NS>(kf, qf, sv);
+        if (q0 + b * 16 >= q_all) {          // all queries see all keys that there are (the others' sums are left out below)
 #pragma unroll
-        for (int n = 0; n < STEPS; ++n) step_scores<KD, NS, NS>(kf[n], qf, sv[n]);
+          for (int i = 0; i < 8; ++i) sum[i] += __builtin_amdgcn_exp2f(fmaf(sv[i], c_exp, -norm));
+        } else {
+          const uint32_t vis = sees8(a, min(q0 + b * 16 + col, nq - 1) / a.group, tok0 + 8 * g, seen);
 #pragma unroll
-        for (int n = 0; n < STEPS; ++n) {
-          if (q0 + b * 16 >= q_all[n]) {       // all queries see all keys that there are (the others' sums are left out below)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[n][i] += __builtin_amdgcn_exp2f(fmaf(sv[n][i], c_exp[n], -norm));
-          } else {
-            const uint32_t vis = sees8(a, min(q0 + b * 16 + col, nq - 1) / a.group, tok0[n] + 8 * g, seen);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float p = __builtin_amdgcn_exp2f(fmaf(sv[n][i], c_exp[n], -norm));
-              sum[n][i] += (vis >> i) & 1 ? p : 0.f;
-            }
+          for (int i = 0; i < 8; ++i) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(sv[i], c_exp, -norm));
+            sum[i] += (vis >> i) & 1 ? p : 0.f;
           }
         }
       }
       __syncthreads();
     }
 #pragma unroll
-    for (int n = 0; n < STEPS; ++n) {
+    for (int i = 0; i < 8; ++i) {               // over the 16 queries of the lane's row
+      float x = sum[i];
+      x += dpp_move<0x128>(x);
+      x += dpp_move<0x141>(x);
+      x += dpp_move<0x4E>(x);
+      x += dpp_move<0xB1>(x);
+      sum[i] = x;
+    }
+    if (col < 8) {
+      float x = sum[0];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {               // over the 16 queries of the lane's row
-        float x = sum[n][i];
-        x += dpp_move<0x128>(x);
-        x += dpp_move<0x141>(x);
-        x += dpp_move<0x4E>(x);
-        x += dpp_move<0xB1>(x);
-        sum[n][i] = x;
-      }
-      if (col < 8) {
-        float x = sum[n][0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) x = col == i ? sum[n][i] : x;
-        const int at = 8 * g + col, step = step0 + wave * STEPS + n;
-        if (at < valid[n]) {
-          if (tok0[n] < 0) a.mass[((size_t)r * a.c.kv_heads + hk) * a.capacity + (size_t)step * kQBlock + at] += x;
-          else a.block_mass[((size_t)r * a.c.kv_heads + hk) * a.block_stride + tok0[n] + at] = x;
-        }
+      for (int i = 1; i < 8; ++i) x = col == i ? sum[i] : x;
+      const int at = 8 * g + col;
+      if (at < valid) {
+        if (cached) a.mass[((size_t)r * a.c.kv_heads + hk) * a.capacity + (size_t)step * kQBlock + at] += x;
+        else a.block_mass[((size_t)r * a.c.kv_heads + hk) * a.block_stride + tok0 + at] = x;
       }
     }
   }
@@ -1550,10 +1521,10 @@ __global__ __launch_bounds__(kQSelect) void k_qcache_select_long(QEvict a) {
   clear_behind(h, a.capacity, tid, kQSelect);
 }
 
-// Moves the elements: one wave per (layer, row, head, block below keep).  Of the keys a lane gathers 8 dims of its two slots, 8 bytes in a row.  Of the values it gathers its dims of 8 slots: the 16
-// lanes of a group read the 256 bytes in which a source's dims lie beside those of the 7 slots around it, and each picks its byte.  (Single bytes by the lane that holds the slot: every lane
-// touches a segment of its own, 370 us instead
-// of 276 for 36 x 16 x 20 rows of 696 slots cut to 256.)  Bound by HBM: a slot's values share their cache lines with 7 others, so that nearly all of them are read: about 1 GB with keys and stores, by arithmetic.
+// Moves the elements: one wave per (layer, row, head, block below keep).  Of the keys a lane gathers 8 dims of its two slots, 8 bytes in a row.  Of the values it gathers its dims of 8 slots: the
+// 16 lanes of a group read the 256 bytes in which a source's dims lie beside those of the 7 slots around it, and each picks its byte.  (Single bytes by the lane that holds the slot: every
+// lane touches a segment of its own, 370 us instead of 276 for 36 x 16 x 20 rows of 696 slots cut to 256.)  Bound by HBM: a slot's values share their cache lines with 7 others, so that
+// nearly all of them are read: about 1 GB with keys and stores, by arithmetic.
 template <int DH>
 __global__ __launch_bounds__(256) void k_qcache_move(QEvict a) {
   const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6), r = blockIdx.y, layer = blockIdx.z;

@@ -8,30 +8,12 @@ namespace vvs {
 // The angle is a product in 64 bits, counted in turns, so that taking whole turns off is exact: in 32 bits position 100000 would be off by 0.008 rad.
 constexpr int kRopeTokens = 4;
 
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void load8(const bf16_t* p, float (&v)[8]) {
-  const uint4 a = *(const uint4*)p;
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-}
-__device__ __forceinline__ void put8(float* p, const float (&v)[8]) {
-  ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void put8(bf16_t* p, const float (&v)[8]) {
-  *(uint4*)p = make_uint4(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]), pack2bf(v[4], v[5]), pack2bf(v[6], v[7]));
-}
-
 // 8 elements of a row of partial sums
-__device__ __forceinline__ void load8_sums(const RopeArgs& a, size_t at, float (&v)[8]) {
-  load8(a.sums + at, v);
+__device__ __forceinline__ void read8_sums(const RopeArgs& a, size_t at, float (&v)[8]) {
+  read8(a.sums + at, v);
   for (int s = 1; s < a.splits; ++s) {
     float x[8];
-    load8(a.sums + s * a.split_stride + at, x);
+    read8(a.sums + s * a.split_stride + at, x);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += x[j];
   }
@@ -58,7 +40,7 @@ __global__ __launch_bounds__(256) void k_rope_axes(RopeArgs a) {
       const bool is_v = hd >= a.heads + a.kv_heads;
       const size_t row = m0 + t, d = (size_t)a.heads * a.dh;
       float v[8];
-      load8_sums(a, row * (d + 2 * a.kv_heads * a.dh) + (size_t)hd * a.dh + e * 8, v);
+      read8_sums(a, row * (d + 2 * a.kv_heads * a.dh) + (size_t)hd * a.dh + e * 8, v);
       if (!is_v) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -69,7 +51,7 @@ __global__ __launch_bounds__(256) void k_rope_axes(RopeArgs a) {
         }
       }
       T* y = (T*)(is_v ? a.v_out : is_k ? a.k_out : a.q_out) + row * (is_k ? a.kv_heads : a.heads) * a.dh + (size_t)(is_v ? hd - a.heads - a.kv_heads : is_k ? hd - a.heads : hd) * a.dh;
-      put8(y + e * 8, v);
+      write8(y + e * 8, v);
       continue;
     }
     const size_t m = m0 + t, at = (size_t)(is_k ? hd - a.heads : hd) * a.dh;
@@ -78,22 +60,22 @@ __global__ __launch_bounds__(256) void k_rope_axes(RopeArgs a) {
     float v[8];
     if (e >= rot) {
       const int d = 2 * a.pairs + (e - rot) * 8;
-      load8(x + d, v);
-      put8(y + d, v);
+      read8(x + d, v);
+      write8(y + d, v);
     } else if (HALVES) {
       float b[8], p[8], q[8];
-      load8(x + e * 8, v);
-      load8(x + a.pairs + e * 8, b);
+      read8(x + e * 8, v);
+      read8(x + a.pairs + e * 8, b);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float2 c = turn[t][e * 8 + j];
         p[j] = v[j] * c.x - b[j] * c.y;
         q[j] = v[j] * c.y + b[j] * c.x;
       }
-      put8(y + e * 8, p);
-      put8(y + a.pairs + e * 8, q);
+      write8(y + e * 8, p);
+      write8(y + a.pairs + e * 8, q);
     } else {
-      load8(x + e * 8, v);
+      read8(x + e * 8, v);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2 c = turn[t][e * 4 + j];
@@ -101,7 +83,7 @@ __global__ __launch_bounds__(256) void k_rope_axes(RopeArgs a) {
         v[2 * j + 1] = v[2 * j] * c.y + v[2 * j + 1] * c.x;
         v[2 * j] = p;
       }
-      put8(y + e * 8, v);
+      write8(y + e * 8, v);
     }
   }
 }
