@@ -766,8 +766,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qc
 
 // Many queries: a workgroup takes 128 of them, 32 per wave, and all its waves go through the same keys, so that what is done once per key - load, conversion, turning - is
 // shared: the waves bring the operands of 64 keys to LDS while those before are at work, from registers that were loaded another 64 keys earlier.  bf16 calls; grid as above.
-// 8 rows x 32 query heads on 8 x 512 tokens over 4096 slots, head size 128: 434 us, 670 TFLOP/s (16 queries per wave 646: every operand read from LDS for half as many); 4 rows over 2048
-// slots 138 to 150 us.  Bound by vector instructions and the waits between them and the matrix cores, of two waves per SIMD.
+// 8 rows x 32 query heads on 8 x 512 tokens over 4096 slots, head size 128: 494 us, 591 TFLOP/s (444 with weights of a single product; with those, 16 queries per wave took half as
+// long again, every operand read from LDS for half as many); 4 rows over 2048 slots 151 us.  Matrix cores are busy 29 % of the busy CUs' time; of a wave's time vector instructions take
+// 33 %, waits for memory, LDS and barriers 32 %, waits to issue 24 %: bound by the chain product - exponential - split - product of two waves per SIMD.
 template <int DH>
 __global__ __launch_bounds__(256, 2) void k_qcache_attention_many(QAttention a, int q_tiles) {
   constexpr int KD = DH / 32, DT = DH / 16, NQB = 2, NQ = 64 * NQB;
