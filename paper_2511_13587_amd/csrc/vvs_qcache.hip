@@ -282,7 +282,7 @@ void launch_qcache_read(const QRead& a, int dtype, hipStream_t s) {
 // Scores S^T = K Q^T: e4m3 numbers are exact in bf16, the block's power of two is multiplied into the softmax's constant.  Values go into O^T += V^T P^T as bf16 too, times their
 // block's power of two (exact).  Weights are 2^(score c - M), M at most 2^6 below the largest exponent so far, so that the accumulators are rescaled only when a maximum grows by more
 // than that; beside bf16 values they go as sums of two bf16 values (to 2^-17 of themselves, as in the contexts' attention), in fp32 calls as three, as queries, block keys and block values do,
-// which hold all 24 bits.  The exponents of bf16 are those of fp32: a weight keeps its bits however far it lies below others, and a block's power of two has no say in M.  (Single fp16 weights,
+// which hold all 24 bits.  The exponents of bf16 are those of fp32: a weight keeps its bits down to 2^-117 of the largest, and a block's power of two has no say in M.  (Single fp16 weights,
 // times their block's power of two, took half of the products, but what lay 2^14 below the largest of them lost bits, and 2^25 below it vanished, beside a normaliser that had
 // it: whole outputs behind a first token without value, small values behind a block of zeros.)  The normaliser sums the fp32 weights per lane; lanes, waves and splits are joined at the end,
 // in a fixed order.

@@ -1,4 +1,4 @@
-"""Contexts with their cache in 8 bits: vvs_kv_evict keeps the slots of largest accumulated weight and the newest tokens, weights and positions kept by the 64-bit checker beside the context."""
+"""Contexts with their cache in 8 bits: vvs_kv_evict keeps the slots of largest accumulated weight and the newest tokens, weights and positions kept by the 64-bit oracle beside the context."""
 import numpy as np
 import pytest
 
@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 
 class Counted(Run):
-    """Run, with the weights that the checker's attention gives to every slot ([layer][heads, slots] per row) and the slots' positions in the sequence."""
+    """Run, with the weights that the oracle's attention gives to every slot ([layer][heads, slots] per row) and the slots' positions in the sequence."""
 
     def __init__(self, shape, monkeypatch):
         super().__init__(shape)
