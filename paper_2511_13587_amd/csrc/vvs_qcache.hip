@@ -1088,7 +1088,7 @@ __global__ __launch_bounds__(256) void k_qcache_join(QAttention a, int q_tiles, 
 // requested, and keys on their way when the loop began, 4 rows of 512, 384, 256 and 128 tokens over 2048 slots each, 8 x 4 heads of 128, took 78 us, now 60.  Products and exponentials would be
 // some 18 us each: bound by the chain LDS - product - exponential of few waves, the longest row's workgroups last.
 template <typename T, int DH>
-__global__ __launch_bounds__(256, 2) void k_qcache_mass(QAttention a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DH == 128 ? 1 : 2) void k_qcache_mass(QAttention a) {
   using S = QShape<T, DH>;
   constexpr int KD = S::KD, NS = S::NS;
   __shared__ uint4 s_q[2][4][KD * NS][64];
