@@ -193,17 +193,19 @@ def prepare(case, seed):
     out, gated = case["out"], path == "gate"
     weights = [mk.normal((width, out), torch.bfloat16, width ** -0.5).mul_(mk.spread(out, 0.4).to(torch.bfloat16)) for _ in range(2 if gated else 1)]
     x8, powers = _as_held(x)
+    held = [_as_held(w.t()) for w in weights]                     # [out, width]: a column's blocks lie along its row here
     if own:
         st["rows8"] = vb.QRows(rows, width)
         st["rows8"].values.copy_(x8)
         st["rows8"].powers.copy_(powers)
-        st["linear"] = vb.QLinear(width, out, rows, vb.VVS_BF16, gated=gated)
-        st["linear"].vvs_qlinear_load(*weights)
+        # what is loaded is rounded already: both sides have the same weights, also where ldexp of a tie is one rounding off a power of two
+        st["linear"] = vb.QLinear(width, out, rows, vb.VVS_FP32, gated=gated)
+        st["linear"].vvs_qlinear_load(*[_held_values(*w, width).t().contiguous() for w in held])
         if gated:
             st["out8"] = vb.QRows(rows, out)
     else:
         st["x8"], st["xe"] = x8, powers
-        st["w"] = [_as_held(w.t()) for w in weights]              # [out, width]: a column's blocks lie along its row here
+        st["w"] = held
     st["y"] = torch.empty((rows, out), dtype=torch.bfloat16 if gated else TYPES[case["dtype"]], device="cuda")
     return st
 
