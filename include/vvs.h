@@ -436,6 +436,73 @@ vvs_status vvs_rope_apply(vvs_rope* r, int32_t n_tokens, const int32_t* d_pos, i
                           int64_t q_out_stride, int32_t n_kv_heads, const void* d_k, int64_t k_stride, void* d_k_out, int64_t k_out_stride,
                           int32_t inverse, vvs_stream s);
 
+/* ---- Rows and weights in 8 bits: a layer's norms, projections and gated products -----------------------------------------
+ *
+ * What is held.  A row of `width` elements is cut into blocks of VVS_QROWS_BLOCK; a block has one power of two 2^E, and its elements are e4m3 numbers (4 exponent bits, 3 of mantissa,
+ * largest 448) times 2^E.  E is the smallest one, at least -110, with |x| <= 448 * 2^E for every finite x of the block.  Rounding is to nearest, ties to even; an element that is not finite
+ * is held as NaN.  Every column of a weight matrix [in, out] is held likewise, in blocks along `in`.
+ *
+ * Rows lie in two buffers (16-byte aligned): values, one byte per element, rows of `width` rounded up to VVS_QROWS_BLOCK, 0 behind the width; and powers, one byte E + 127 per
+ * block, rows of the number of blocks rounded up to 4, 0 behind the last block.  What is taken as rows in 8 bits has to lie so; what the calls below write does.
+ * Rows behind n_rows are neither read nor written.  Rows have at most 65536 elements.
+ *
+ * Tensors are [n_rows, width] in VVS_FP32 or VVS_BF16; a stride argument gives the elements from one row to the next where they lie further apart than `width` (0: they do not).  Any
+ * width, stride and element-aligned pointer is taken; 16-byte accesses are made where pointer and stride are multiples of 16 bytes (of 4 elements for outputs of
+ * vvs_qlinear_apply).  Outputs share no memory with inputs, except where stated.  All calls can be captured into a graph; those on rows go to the current device. */
+#define VVS_QROWS_BLOCK 128
+
+/* Sizes in bytes of the two buffers of n_rows rows. */
+vvs_status vvs_qrows_sizes(int32_t width, int32_t n_rows, size_t* value_bytes, size_t* power_bytes);
+const char* vvs_qrows_last_error(void);   /* of this thread's last failed vvs_qrows call */
+
+/* Rounds rows to 8 bits. */
+vvs_status vvs_qrows_round(int32_t n_rows, int32_t width, int32_t dtype, const void* d_x, int64_t x_stride, void* d_values, void* d_powers,
+                           vvs_stream s);
+
+/* Root-mean-square norm with the residual's addition: x' = x + delta, rounded to the type of x; y = x' * rsqrt(mean x'^2 + eps) * gain, which goes into 8 bits.  The sum of squares is in fp32:
+ * elements up to 2^63 / sqrt(width).
+ *   d_delta    : [n_rows, width] of its own type, or NULL: nothing is added
+ *   d_x_out    : x' in the type of x; may be d_x itself (with the same stride); NULL: not written
+ *   d_gain     : [width] of its own type
+ *   eps        : finite, not negative */
+vvs_status vvs_qrows_norm(int32_t n_rows, int32_t width, int32_t x_dtype, const void* d_x, int64_t x_stride, int32_t delta_dtype, const void* d_delta,
+                          int64_t delta_stride, void* d_x_out, int64_t x_out_stride, int32_t gain_dtype, const void* d_gain, float eps, void* d_values,
+                          void* d_powers, vvs_stream s);
+
+/* Rows in 8 bits as numbers (bf16 has all of them, but 2^128, what elements from 0.97 * 2^128 on are held as: it reads as an infinity). */
+vvs_status vvs_qrows_read(int32_t n_rows, int32_t width, const void* d_values, const void* d_powers, int32_t dtype, void* d_out, int64_t out_stride,
+                          vvs_stream s);
+
+typedef struct vvs_qlinear vvs_qlinear;   /* opaque host object; owns no device memory */
+
+typedef struct {
+  int32_t in, out;               /* elements of a row that goes in and of one that comes out */
+  int32_t max_rows;              /* largest n_rows of a call, at most 2^21 */
+  int32_t gated;                 /* 0: one matrix, for vvs_qlinear_apply; 1: gate and up, for vvs_qlinear_gate */
+  int32_t dtype;                 /* of the weights that vvs_qlinear_load takes and vvs_qlinear_read gives */
+} vvs_qlinear_config;
+
+/* Sizes in bytes of the two device buffers of a linear map: weights in 8 bits in the kernels' own order, workspace.  A workspace may serve several maps - it has to hold the largest one's
+ * bytes - if their calls are issued on one stream or ordered; captured graphs that share one must not run at the same time. */
+vvs_status vvs_qlinear_query_sizes(const vvs_qlinear_config* cfg, size_t* weight_bytes, size_t* workspace_bytes);
+/* Creates a map over caller-allocated device buffers (256-byte aligned) on the current device, which has to be current at every call.  Synchronous: clears the workspace. */
+vvs_status vvs_qlinear_create(const vvs_qlinear_config* cfg, void* d_weights, void* d_workspace, vvs_qlinear** out);
+void vvs_qlinear_destroy(vvs_qlinear* l);
+const char* vvs_qlinear_last_error(const vvs_qlinear* l);   /* l must not be NULL (a failed create or query: vvs_last_error(NULL)) */
+
+/* Rounds weights [in, out] (row-major, contiguous) to 8 bits; d_w_up: NULL, with a gate the up weights, likewise.  The tensors may be freed once the stream has passed this point. */
+vvs_status vvs_qlinear_load(vvs_qlinear* l, const void* d_w, const void* d_w_up, vvs_stream s);
+/* The weights that are held, as numbers in the type of the config; arguments as above. */
+vvs_status vvs_qlinear_read(vvs_qlinear* l, void* d_w, void* d_w_up, vvs_stream s);
+
+/* out = x W for rows in 8 bits of width `in`: out [n_rows, out] in out_dtype. */
+vvs_status vvs_qlinear_apply(vvs_qlinear* l, int32_t n_rows, const void* d_values, const void* d_powers, int32_t out_dtype, void* d_out, int64_t out_stride,
+                             vvs_stream s);
+
+/* silu(x W_gate) * (x W_up), silu(a) = a / (1 + e^-a), into rows in 8 bits of width `out`. */
+vvs_status vvs_qlinear_gate(vvs_qlinear* l, int32_t n_rows, const void* d_values, const void* d_powers, void* d_out_values, void* d_out_powers,
+                            vvs_stream s);
+
 /* 1 if a forward over n_tokens query tokens per row (a verify call with n_tokens - 1 draft nodes, or a
  * prefill chunk) takes the fused layer described at vvs_config.norm_mode, 0 if it runs the separate
  * normalisation kernels.  Host only; ctx must not be NULL. */

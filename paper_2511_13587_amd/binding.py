@@ -23,6 +23,7 @@ VVS_NORM_AUTO, VVS_NORM_SEPARATE = 0, 1
 VVS_CACHE_SAME, VVS_CACHE_E4M3 = 0, 1
 VVS_MAX_T = 64
 VVS_QCACHE_BLOCK = 32
+VVS_QROWS_BLOCK = 128
 VVS_ROPE_MAX_AXES = 4
 VVS_ROPE_OWN, VVS_ROPE_SHARED = 0, 1
 VVS_ROPE_ADJACENT, VVS_ROPE_HALVES = 0, 1
@@ -46,6 +47,10 @@ class VvsQCacheConfig(C.Structure):
 class VvsRopeConfig(C.Structure):
     _fields_ = [("head_size", C.c_int32), ("n_axes", C.c_int32), ("pairs", C.c_int32 * VVS_ROPE_MAX_AXES), ("series", C.c_int32),
                 ("pairing", C.c_int32), ("dtype", C.c_int32), ("base", C.c_float)]
+
+
+class VvsQLinearConfig(C.Structure):
+    _fields_ = [("in_", C.c_int32)] + [(n, C.c_int32) for n in ("out", "max_rows", "gated", "dtype")]
 
 
 class VvsError(RuntimeError):
@@ -105,6 +110,19 @@ def _load():
         "vvs_rope_destroy": (None, [vp]),
         "vvs_rope_last_error": (C.c_char_p, [vp]),
         "vvs_rope_apply": (i32, [vp, i32, vp, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp]),
+        "vvs_qrows_sizes": (i32, [i32, i32, C.POINTER(sz), C.POINTER(sz)]),
+        "vvs_qrows_last_error": (C.c_char_p, []),
+        "vvs_qrows_round": (i32, [i32, i32, i32, vp, i64, vp, vp, vp]),
+        "vvs_qrows_norm": (i32, [i32, i32, i32, vp, i64, i32, vp, i64, vp, i64, i32, vp, C.c_float, vp, vp, vp]),
+        "vvs_qrows_read": (i32, [i32, i32, vp, vp, i32, vp, i64, vp]),
+        "vvs_qlinear_query_sizes": (i32, [C.POINTER(VvsQLinearConfig), C.POINTER(sz), C.POINTER(sz)]),
+        "vvs_qlinear_create": (i32, [C.POINTER(VvsQLinearConfig), vp, vp, C.POINTER(vp)]),
+        "vvs_qlinear_destroy": (None, [vp]),
+        "vvs_qlinear_last_error": (C.c_char_p, [vp]),
+        "vvs_qlinear_load": (i32, [vp, vp, vp, vp]),
+        "vvs_qlinear_read": (i32, [vp, vp, vp, vp]),
+        "vvs_qlinear_apply": (i32, [vp, i32, vp, vp, i32, vp, i64, vp]),
+        "vvs_qlinear_gate": (i32, [vp, i32, vp, vp, vp, vp, vp]),
         "vvs_debug_wait_limit": (i32, [vp, i32]),
         "vvs_debug_fill_probe": (i32, [vp, vp, sz, sz, i32, i32, i32, i32, vp, vp]),
     }
@@ -624,3 +642,210 @@ class Rope:
                                     1 if inverse else 0, _raw_stream(device))
         if st != VVS_OK:
             raise VvsError(st, (lib.vvs_rope_last_error(self.h) or b"").decode())
+
+
+# ---- rows and weights in 8 bits
+_VVS_DTYPE = {torch.float32: VVS_FP32, torch.bfloat16: VVS_BF16}
+
+
+def vvs_qrows_sizes(width: int, n_rows: int):
+    values, powers = C.c_size_t(), C.c_size_t()
+    _rows_check(lib.vvs_qrows_sizes(width, n_rows, C.byref(values), C.byref(powers)))
+    return values.value, powers.value
+
+
+def _rows_check(st: int):
+    if st != VVS_OK:
+        raise VvsError(st, (lib.vvs_qrows_last_error() or b"").decode())
+
+
+class QRows:
+    """Rows of `width` elements in 8 bits: owns their two buffers.  values float8_e4m3fn [rows, width rounded up to VVS_QROWS_BLOCK], powers uint8 [rows, blocks rounded up to 4]: an element is
+    its value times 2 ** (power - 127).  first(n): the first n rows, in the same memory."""
+
+    def __init__(self, n_rows: int, width: int, device: str = "cuda:0"):
+        v, p = vvs_qrows_sizes(width, n_rows)
+        values = torch.empty((n_rows, v // n_rows), dtype=torch.float8_e4m3fn, device=device)
+        self._take(values, torch.empty((n_rows, p // n_rows), dtype=torch.uint8, device=values.device), width)
+
+    def _take(self, values: torch.Tensor, powers: torch.Tensor, width: int):
+        self.values, self.powers, self.width, self.n_rows, self.index = values, powers, width, values.shape[0], values.get_device()
+        self.pointers = (values.data_ptr(), powers.data_ptr())
+
+    def first(self, n_rows: int) -> "QRows":
+        if not 1 <= n_rows <= self.n_rows:
+            raise ValueError(f"first: {n_rows} of {self.n_rows} rows")
+        rows = object.__new__(QRows)
+        rows._take(self.values[:n_rows], self.powers[:n_rows], self.width)
+        return rows
+
+
+def _matrix(t: torch.Tensor, rows: int, width: int, device: int, what: str):
+    """(pointer, elements from row to row, vvs dtype) of a tensor [..., width] of `rows` rows that may be a part of a wider one."""
+    dtype, shape = _VVS_DTYPE.get(t.dtype), t.shape
+    if t.get_device() != device or dtype is None or not shape or shape[-1] != width or t.numel() != rows * width:
+        raise ValueError(f"{what}: wants float32 or bfloat16 [..., {width}], {rows} rows, on device {device}; got {t.dtype} {list(shape)} on device {t.get_device()}")
+    if t.is_contiguous():
+        return t.data_ptr(), width, dtype
+    strides = t.stride()
+    row, n, ok = None, 1, strides[-1] == 1 or width == 1
+    for d in range(len(shape) - 2, -1, -1):                 # n: rows below each dimension
+        if shape[d] > 1:
+            if row is None:
+                row = strides[d] // n
+            ok = ok and strides[d] == row * n
+        n *= shape[d]
+    row = width if row is None else row
+    if not ok or row < width:
+        raise ValueError(f"{what}: strides {strides} of {list(shape)} are not those of rows one after the other")
+    return t.data_ptr(), row, dtype
+
+
+def _span(p: int, rows: int, stride: int, width: int, size: int):
+    """Bytes that `rows` rows take."""
+    return p, p + ((rows - 1) * stride + width) * size
+
+
+def _held(rows: QRows):
+    v, p = rows.pointers
+    n = rows.n_rows
+    return (v, v + n * rows.values.shape[1]), (p, p + n * rows.powers.shape[1])
+
+
+def _no_overlap(outs, ins):
+    for a, b in outs:
+        for c, d in ins:
+            if a < d and c < b:
+                raise ValueError("an output shares memory with an input or another output")
+
+
+def vvs_qrows_round(x: torch.Tensor, rows: QRows):
+    """x [..., width] float32 or bfloat16, as many rows as `rows` holds."""
+    n, w, dev = rows.n_rows, rows.width, rows.index
+    xp, xs, xt = _matrix(x, n, w, dev, "x")
+    _no_overlap(_held(rows), (_span(xp, n, xs, w, x.dtype.itemsize),))
+    with _Current(dev):
+        _rows_check(lib.vvs_qrows_round(n, w, xt, xp, xs, *rows.pointers, _raw_stream(dev)))
+
+
+def vvs_qrows_norm(x: torch.Tensor, gain: torch.Tensor, eps: float, rows: QRows, delta: Optional[torch.Tensor] = None, x_out: Optional[torch.Tensor] = None):
+    """x, delta, x_out [..., width], as many rows as `rows` holds; gain [width].  x_out may be x itself; without it x + delta is not kept."""
+    n, w, dev = rows.n_rows, rows.width, rows.index
+    xp, xs, xt = _matrix(x, n, w, dev, "x")
+    gp, _, gt = _matrix(gain, 1, w, dev, "gain")
+    ins = [_span(xp, n, xs, w, x.dtype.itemsize), _span(gp, 1, w, w, gain.dtype.itemsize)]
+    outs = list(_held(rows))
+    dp, ds, dt = (None, 0, 0) if delta is None else _matrix(delta, n, w, dev, "delta")
+    if delta is not None:
+        ins.append(_span(dp, n, ds, w, delta.dtype.itemsize))
+    op, os_ = None, 0
+    if x_out is not None:
+        op, os_, ot = _matrix(x_out, n, w, dev, "x_out")
+        if ot != xt:
+            raise ValueError("x_out: wants the type of x")
+        span = _span(op, n, os_, w, x.dtype.itemsize)
+        if op == xp and os_ == xs:
+            _no_overlap((span,), ins[1:])
+        else:
+            _no_overlap((span,), ins)
+        _no_overlap(outs, (span,))
+    _no_overlap(outs, ins)
+    with _Current(dev):
+        _rows_check(lib.vvs_qrows_norm(n, w, xt, xp, xs, dt, dp, ds, op, os_, gt, gp, eps, *rows.pointers, _raw_stream(dev)))
+
+
+def vvs_qrows_read(rows: QRows, out: torch.Tensor):
+    """out [..., width] float32 or bfloat16."""
+    n, w, dev = rows.n_rows, rows.width, rows.index
+    op, os_, ot = _matrix(out, n, w, dev, "out")
+    _no_overlap((_span(op, n, os_, w, out.dtype.itemsize),), _held(rows))
+    with _Current(dev):
+        _rows_check(lib.vvs_qrows_read(n, w, *rows.pointers, ot, op, os_, _raw_stream(dev)))
+
+
+def vvs_qlinear_query_sizes(cfg: VvsQLinearConfig):
+    weights, ws = C.c_size_t(), C.c_size_t()
+    st = lib.vvs_qlinear_query_sizes(C.byref(cfg), C.byref(weights), C.byref(ws))
+    if st != VVS_OK:
+        raise VvsError(st, (lib.vvs_last_error(None) or b"").decode())
+    return weights.value, ws.value
+
+
+class QLinear:
+    """A linear map with its weights in 8 bits: owns its weights and, unless one is given, its workspace; methods mirror the C entry points (include/vvs.h).  in_width, out: elements of a row
+    that goes in and of one that comes out; dtype: of the tensors that are loaded; gated: gate and up weights, for vvs_qlinear_gate."""
+
+    def __init__(self, in_width: int, out: int, max_rows: int, dtype: int, gated: bool = False, device: str = "cuda:0", workspace: Optional[torch.Tensor] = None):
+        self.cfg = VvsQLinearConfig(in_width, out, max_rows, 1 if gated else 0, dtype)
+        self.weight_bytes, self.ws_bytes = vvs_qlinear_query_sizes(self.cfg)
+        if not torch.cuda.is_available():
+            raise RuntimeError("libvvs needs a HIP device; there is no CPU path")
+        self.device, self.dtype = torch.device(device), _TORCH_DTYPE[dtype]
+        self.index = torch.cuda.current_device() if self.device.index is None else self.device.index
+        if workspace is not None and (workspace.get_device() != self.index or not workspace.is_contiguous() or workspace.numel() * workspace.dtype.itemsize < self.ws_bytes):
+            raise ValueError(f"workspace: wants {self.ws_bytes} bytes on device {self.index}")
+        with torch.cuda.device(self.index):
+            self.weights = torch.empty(self.weight_bytes, dtype=torch.uint8, device=self.device)
+            self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device) if workspace is None else workspace
+            torch.cuda.synchronize()
+            h = C.c_void_p()
+            st = lib.vvs_qlinear_create(C.byref(self.cfg), self.weights.data_ptr(), self.ws.data_ptr(), C.byref(h))
+        if st != VVS_OK:
+            raise VvsError(st, (lib.vvs_last_error(None) or b"").decode())
+        self.h = h
+        self.sizes = (in_width, out, bool(gated))
+
+    def close(self):
+        if getattr(self, "h", None):
+            torch.cuda.synchronize(self.index)
+            lib.vvs_qlinear_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, st: int):
+        if st != VVS_OK:
+            raise VvsError(st, (lib.vvs_qlinear_last_error(self.h) or b"").decode())
+
+    def _weights(self, w, up):
+        shape = self.sizes[:2]
+        return _on(w, self.index, self.dtype, shape, "w"), _on(up, self.index, self.dtype, shape, "up")
+
+    def vvs_qlinear_load(self, w: torch.Tensor, up: Optional[torch.Tensor] = None):
+        """w (and, with a gate, up) [in_width, out], contiguous."""
+        wp, up_ = self._weights(w, up)
+        with _Current(self.index):
+            self._check(lib.vvs_qlinear_load(self.h, wp, up_, _raw_stream(self.index)))
+
+    def vvs_qlinear_read(self, w: torch.Tensor, up: Optional[torch.Tensor] = None):
+        """The held weights into w (and up) [in_width, out], contiguous."""
+        wp, up_ = self._weights(w, up)
+        with _Current(self.index):
+            self._check(lib.vvs_qlinear_read(self.h, wp, up_, _raw_stream(self.index)))
+
+    def _rows(self, rows: QRows, width: int, what: str):
+        if rows.width != width or rows.index != self.index:
+            raise ValueError(f"{what}: wants rows of {width} elements on device {self.index}, got {rows.width} on device {rows.index}")
+
+    def vvs_qlinear_apply(self, rows: QRows, out: torch.Tensor):
+        """out [..., out] float32 or bfloat16, as many rows as `rows` holds."""
+        n, (k, cols, gated) = rows.n_rows, self.sizes
+        self._rows(rows, k, "rows")
+        op, os_, ot = _matrix(out, n, cols, self.index, "out")
+        _no_overlap((_span(op, n, os_, cols, out.dtype.itemsize),), _held(rows))
+        with _Current(self.index):
+            self._check(lib.vvs_qlinear_apply(self.h, n, *rows.pointers, ot, op, os_, _raw_stream(self.index)))
+
+    def vvs_qlinear_gate(self, rows: QRows, out: QRows):
+        """out: rows of `out` elements, as many as `rows` holds."""
+        self._rows(rows, self.sizes[0], "rows")
+        self._rows(out, self.sizes[1], "out")
+        if out.n_rows != rows.n_rows:
+            raise ValueError(f"out: wants {rows.n_rows} rows, got {out.n_rows}")
+        _no_overlap(_held(out), _held(rows))
+        with _Current(self.index):
+            self._check(lib.vvs_qlinear_gate(self.h, rows.n_rows, *rows.pointers, *out.pointers, _raw_stream(self.index)))

@@ -5,7 +5,6 @@
 namespace vvs {
 
 constexpr int kQBlock = VVS_QCACHE_BLOCK;   // slots that share a power of two
-constexpr int kQLeast = -110;               // smallest exponent of a block
 constexpr int kQParts = 4096;               // partial results of a split attention call that the workspace has room for, of 16 queries each: 512 workgroups of 128 queries, two per
                                             // CU (us with room for 256 / 512 / 1024: 1 row x 32 heads x 512 tokens over 4096 slots 116 / 93 / 105, 4 rows x 256 over 2048 107 / 92 / 108)
 constexpr int kQKept = 8;                   // queries per row and key/value head whose scores are kept for the counted weights

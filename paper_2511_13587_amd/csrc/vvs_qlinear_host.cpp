@@ -1,0 +1,288 @@
+// Host side of the rows and weights in 8 bits: argument checks, buffer sizes, entry points.
+#include "vvs_qlinear.h"
+
+#include <math.h>
+#include <cmath>
+#include <new>
+
+namespace vvs {
+
+struct QLinear {
+  vvs_qlinear_config cfg;
+  QWeights w;
+  size_t weight_bytes, ws_bytes;
+  int dev, cus;
+  char* ws;
+  bool loaded;
+  std::string err;
+};
+
+// What vvs_last_error(NULL) tells of a failed create or query (vvs_host.cpp)
+vvs_status fail_without_context(vvs_status st, const char* msg);
+
+// The calls on rows have no object to keep a message in: one per thread
+static thread_local const char* t_rows_error = "";
+
+static vvs_status rows_no(vvs_status st, const char* msg) {
+  t_rows_error = msg;
+  return st;
+}
+
+static vvs_status rows_launched() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? VVS_OK : rows_no(VVS_EHIP, hipGetErrorString(e));
+}
+
+static vvs_status no(QLinear* l, vvs_status st, const char* msg) {
+  if (!l) return fail_without_context(st, msg);
+  l->err = msg;
+  return st;
+}
+
+static bool known(int dtype) { return dtype == VVS_FP32 || dtype == VVS_BF16; }
+static size_t size_of(int dtype) { return dtype == VVS_BF16 ? 2 : 4; }
+
+// Widths and strides of a tensor [n_rows, width]: elements from row to row, 0 where they follow each other; < 0: not allowed
+static int64_t stride_of(int64_t given, int width) {
+  const int64_t s = given ? given : width;
+  return s < width || s > ((int64_t)1 << 31) ? -1 : s;
+}
+// 16-byte accesses of 8 elements (by: 4, accesses of 4 elements)
+static int wide_rows(const void* p, int64_t stride, int dtype, int by = 8) {
+  const size_t bytes = by * size_of(dtype) < 16 ? by * size_of(dtype) : 16;
+  return ((uintptr_t)p | (uintptr_t)stride * size_of(dtype)) % bytes == 0;
+}
+static bool off_element(const void* p, int dtype) { return (uintptr_t)p % size_of(dtype) != 0; }
+static bool off16(const void* p) { return ((uintptr_t)p & 15) != 0; }
+
+constexpr int kWidest = 65536;                                 // of a row that a workgroup keeps in registers
+constexpr int64_t kMostThreads = ((int64_t)1 << 32) - 1024;    // of a launch along a dimension
+
+static vvs_status check_rows(int n_rows, int width, const void* values, const void* powers, int threads_per_row) {
+  if (n_rows < 1 || width < 1) return rows_no(VVS_EINVAL, "qrows: n_rows and width must be positive");
+  if (width > kWidest) return rows_no(VVS_ESIZE, "qrows: at most 65536 elements per row");
+  if (!values || !powers) return rows_no(VVS_EINVAL, "qrows: NULL argument");
+  if (off16(values) || off16(powers)) return rows_no(VVS_EINVAL, "qrows: values and powers must be 16-byte aligned");
+  if ((int64_t)n_rows * threads_per_row > kMostThreads) return rows_no(VVS_ESIZE, "qrows: more rows than a launch holds");
+  return VVS_OK;
+}
+
+static vvs_status plan_qlinear(const vvs_qlinear_config* cfg, QLinear* l) {
+  if (!cfg) return no(nullptr, VVS_EINVAL, "qlinear config is NULL");
+  const vvs_qlinear_config& g = *cfg;
+  if (g.in < 1 || g.out < 1 || g.max_rows < 1) return no(nullptr, VVS_EINVAL, "qlinear config: a dimension is not positive");
+  if (!known(g.dtype)) return no(nullptr, VVS_EINVAL, "qlinear config: unknown dtype");
+  if (g.gated != 0 && g.gated != 1) return no(nullptr, VVS_EINVAL, "qlinear config: gated must be 0 or 1");
+  if (g.in > kWidest || (g.gated && g.out > kWidest)) return no(nullptr, VVS_ESIZE, "qlinear config: at most 65536 elements per row");
+  if (g.out > (1 << 24) || g.max_rows > (1 << 21)) return no(nullptr, VVS_ESIZE, "qlinear config: at most 2^24 columns and 2^21 rows");
+  l->cfg = g;
+  QWeights& w = l->w;
+  w = QWeights{g.in, g.out, g.gated, qrows_blocks(g.in), 0, nullptr, nullptr};
+  w.groups = (g.out + w.unit() - 1) / w.unit();
+  if (g.gated) w.groups = (w.groups + 3) & ~3;                 // whole blocks of 128 hidden units
+  if ((int64_t)w.groups * w.blocks >= (1 << 24)) return no(nullptr, VVS_ESIZE, "qlinear config: more weights than a launch holds");
+  l->weight_bytes = align_up((size_t)w.groups * w.blocks * 8192, 256) + align_up((size_t)w.groups * ((w.blocks + 3) / 4) * 256, 256);
+  l->ws_bytes = g.gated ? align_up((size_t)g.max_rows * w.groups * 32 * sizeof(float), 256) : 256;
+  return VVS_OK;
+}
+
+static QLinear* of(vvs_qlinear* l) { return reinterpret_cast<QLinear*>(l); }
+
+static vvs_status check_device(QLinear* l) {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return no(l, VVS_EHIP, "qlinear: no current device");
+  if (dev != l->dev) return no(l, VVS_EINVAL, "qlinear: created on another device than the current one");
+  return VVS_OK;
+}
+
+static vvs_status launched(QLinear* l, const char* what) {
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return VVS_OK;
+  l->err = std::string(what) + ": " + hipGetErrorString(e);
+  return VVS_EHIP;
+}
+
+static vvs_status check_product(QLinear* l, int n_rows, const void* values, const void* powers) {
+  if (!l->loaded) return no(l, VVS_ESTATE, "qlinear: call vvs_qlinear_load first");
+  if (!values || !powers) return no(l, VVS_EINVAL, "qlinear: NULL argument");
+  if (n_rows < 1) return no(l, VVS_EINVAL, "qlinear: n_rows must be positive");
+  if (n_rows > l->cfg.max_rows) return no(l, VVS_ESIZE, "qlinear: n_rows exceeds max_rows");
+  if (off16(values) || off16(powers)) return no(l, VVS_EINVAL, "qlinear: values and powers must be 16-byte aligned");
+  return VVS_OK;
+}
+
+}  // namespace vvs
+
+using namespace vvs;
+
+extern "C" {
+
+const char* vvs_qrows_last_error(void) { return t_rows_error; }
+
+vvs_status vvs_qrows_sizes(int32_t width, int32_t n_rows, size_t* value_bytes, size_t* power_bytes) {
+  if (n_rows < 1 || width < 1) return rows_no(VVS_EINVAL, "qrows: n_rows and width must be positive");
+  if (width > kWidest) return rows_no(VVS_ESIZE, "qrows: at most 65536 elements per row");
+  if (value_bytes) *value_bytes = (size_t)n_rows * qrows_blocks(width) * kQRowBlock;
+  if (power_bytes) *power_bytes = (size_t)n_rows * qrows_powers(width);
+  return VVS_OK;
+}
+
+vvs_status vvs_qrows_round(int32_t n_rows, int32_t width, int32_t dtype, const void* d_x, int64_t x_stride, void* d_values, void* d_powers, vvs_stream s) {
+  const vvs_status st = check_rows(n_rows, width, d_values, d_powers, width > 0 && width <= kWidest ? 16 * qrows_powers(width) : 16);
+  if (st != VVS_OK) return st;
+  if (!d_x) return rows_no(VVS_EINVAL, "qrows round: NULL argument");
+  if (!known(dtype)) return rows_no(VVS_EINVAL, "qrows round: unknown dtype");
+  const int64_t xs = stride_of(x_stride, width);
+  if (xs < 0 || off_element(d_x, dtype)) return rows_no(VVS_EINVAL, "qrows round: the stride has to cover a row, the pointer to be aligned to an element");
+  QRound a{};
+  a.M = n_rows; a.width = width; a.dtype = dtype;
+  a.x = d_x; a.stride = (size_t)xs; a.wide = wide_rows(d_x, xs, dtype);
+  a.y = QRowsOut{(uint8_t*)d_values, (uint8_t*)d_powers};
+  launch_qrows_round(a, (hipStream_t)s);
+  return rows_launched();
+}
+
+vvs_status vvs_qrows_norm(int32_t n_rows, int32_t width, int32_t x_dtype, const void* d_x, int64_t x_stride, int32_t delta_dtype, const void* d_delta,
+                          int64_t delta_stride, void* d_x_out, int64_t x_out_stride, int32_t gain_dtype, const void* d_gain, float eps, void* d_values,
+                          void* d_powers, vvs_stream s) {
+  const vvs_status st = check_rows(n_rows, width, d_values, d_powers, 1024);
+  if (st != VVS_OK) return st;
+  if (!d_x || !d_gain) return rows_no(VVS_EINVAL, "qrows norm: NULL argument");
+  if (!known(x_dtype) || !known(gain_dtype) || (d_delta && !known(delta_dtype))) return rows_no(VVS_EINVAL, "qrows norm: unknown dtype");
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return rows_no(VVS_EINVAL, "qrows norm: eps must be finite and not negative");
+  const int64_t xs = stride_of(x_stride, width), ds = stride_of(delta_stride, width), os = stride_of(x_out_stride, width);
+  if (xs < 0 || (d_delta && ds < 0) || (d_x_out && os < 0) || off_element(d_x, x_dtype) || off_element(d_x_out, x_dtype) || off_element(d_gain, gain_dtype) ||
+      (d_delta && off_element(d_delta, delta_dtype)))
+    return rows_no(VVS_EINVAL, "qrows norm: strides have to cover a row, pointers to be aligned to an element");
+  if (d_x == d_x_out && xs != os) return rows_no(VVS_EINVAL, "qrows norm: in place, both strides are the same");
+  QNorm a{};
+  a.M = n_rows; a.width = width;
+  a.x = d_x; a.x_dtype = x_dtype; a.x_stride = (size_t)xs; a.x_wide = wide_rows(d_x, xs, x_dtype);
+  if (d_delta) { a.delta = d_delta; a.delta_dtype = delta_dtype; a.delta_stride = (size_t)ds; a.delta_wide = wide_rows(d_delta, ds, delta_dtype); }
+  if (d_x_out) { a.x_out = d_x_out; a.x_out_stride = (size_t)os; a.x_out_wide = wide_rows(d_x_out, os, x_dtype); }
+  a.gain = d_gain; a.gain_dtype = gain_dtype; a.gain_wide = wide_rows(d_gain, 0, gain_dtype);
+  a.eps = eps;
+  a.y = QRowsOut{(uint8_t*)d_values, (uint8_t*)d_powers};
+  launch_qrows_norm(a, (hipStream_t)s);
+  return rows_launched();
+}
+
+vvs_status vvs_qrows_read(int32_t n_rows, int32_t width, const void* d_values, const void* d_powers, int32_t dtype, void* d_out, int64_t out_stride, vvs_stream s) {
+  const vvs_status st = check_rows(n_rows, width, d_values, d_powers, width > 0 && width <= kWidest ? 16 * qrows_powers(width) : 16);
+  if (st != VVS_OK) return st;
+  if (!d_out) return rows_no(VVS_EINVAL, "qrows read: NULL argument");
+  if (!known(dtype)) return rows_no(VVS_EINVAL, "qrows read: unknown dtype");
+  const int64_t os = stride_of(out_stride, width);
+  if (os < 0 || off_element(d_out, dtype)) return rows_no(VVS_EINVAL, "qrows read: the stride has to cover a row, the pointer to be aligned to an element");
+  QRowsRead a{};
+  a.M = n_rows; a.width = width; a.dtype = dtype;
+  a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
+  a.y = d_out; a.stride = (size_t)os; a.wide = wide_rows(d_out, os, dtype);
+  launch_qrows_read(a, (hipStream_t)s);
+  return rows_launched();
+}
+
+vvs_status vvs_qlinear_query_sizes(const vvs_qlinear_config* cfg, size_t* weight_bytes, size_t* workspace_bytes) {
+  QLinear l{};
+  const vvs_status st = plan_qlinear(cfg, &l);
+  if (st != VVS_OK) return st;
+  if (weight_bytes) *weight_bytes = l.weight_bytes;
+  if (workspace_bytes) *workspace_bytes = l.ws_bytes;
+  return VVS_OK;
+}
+
+vvs_status vvs_qlinear_create(const vvs_qlinear_config* cfg, void* d_weights, void* d_workspace, vvs_qlinear** out) {
+  if (!out) return no(nullptr, VVS_EINVAL, "qlinear create: out is NULL");
+  *out = nullptr;
+  if (!d_weights || !d_workspace) return no(nullptr, VVS_EINVAL, "qlinear create: NULL device buffer");
+  if (((uintptr_t)d_weights | (uintptr_t)d_workspace) & 255) return no(nullptr, VVS_EINVAL, "qlinear create: device buffers must be 256-byte aligned");
+  QLinear plan{};
+  const vvs_status st = plan_qlinear(cfg, &plan);
+  if (st != VVS_OK) return st;
+  int ndev = 0;
+  if (hipGetDeviceCount(&ndev) != hipSuccess || ndev < 1) return no(nullptr, VVS_EHIP, "qlinear create: no HIP device (this library has no CPU path)");
+  hipError_t e = hipGetDevice(&plan.dev);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&plan.cus, hipDeviceAttributeMultiprocessorCount, plan.dev);
+  if (e != hipSuccess) return no(nullptr, VVS_EHIP, hipGetErrorString(e));
+  plan.ws = (char*)d_workspace;
+  plan.w.data = (uint8_t*)d_weights;
+  plan.w.powers = (uint8_t*)d_weights + align_up((size_t)plan.w.groups * plan.w.blocks * 8192, 256);
+  QLinear* l = new (std::nothrow) QLinear(plan);
+  if (!l) return no(nullptr, VVS_EHIP, "qlinear create: out of memory");
+  launch_fill_zero(d_workspace, l->ws_bytes, nullptr);
+  e = hipGetLastError();
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  if (e != hipSuccess) { delete l; return no(nullptr, VVS_EHIP, hipGetErrorString(e)); }
+  *out = reinterpret_cast<vvs_qlinear*>(l);
+  return VVS_OK;
+}
+
+void vvs_qlinear_destroy(vvs_qlinear* l) { delete of(l); }
+
+const char* vvs_qlinear_last_error(const vvs_qlinear* l) { return l ? reinterpret_cast<const QLinear*>(l)->err.c_str() : ""; }
+
+vvs_status vvs_qlinear_load(vvs_qlinear* ql, const void* d_w, const void* d_w_up, vvs_stream s) {
+  QLinear* l = of(ql);
+  if (!l) return VVS_EINVAL;
+  if (!d_w || !d_w_up != !l->cfg.gated) return no(l, VVS_EINVAL, "qlinear load: one weight tensor, with a gate two");
+  if (off_element(d_w, l->cfg.dtype) || off_element(d_w_up, l->cfg.dtype)) return no(l, VVS_EINVAL, "qlinear load: unaligned weights");
+  vvs_status st = check_device(l);
+  if (st != VVS_OK) return st;
+  launch_qlinear_load(QLoad{l->w, d_w, d_w_up, l->cfg.dtype}, (hipStream_t)s);
+  if ((st = launched(l, "qlinear load")) == VVS_OK) l->loaded = true;
+  return st;
+}
+
+vvs_status vvs_qlinear_read(vvs_qlinear* ql, void* d_w, void* d_w_up, vvs_stream s) {
+  QLinear* l = of(ql);
+  if (!l) return VVS_EINVAL;
+  if (!l->loaded) return no(l, VVS_ESTATE, "qlinear read: call vvs_qlinear_load first");
+  if (!d_w || !d_w_up != !l->cfg.gated) return no(l, VVS_EINVAL, "qlinear read: one weight tensor, with a gate two");
+  if (off_element(d_w, l->cfg.dtype) || off_element(d_w_up, l->cfg.dtype)) return no(l, VVS_EINVAL, "qlinear read: unaligned weights");
+  const vvs_status st = check_device(l);
+  if (st != VVS_OK) return st;
+  launch_qlinear_read(QWeightsRead{l->w, d_w, d_w_up, l->cfg.dtype}, (hipStream_t)s);
+  return launched(l, "qlinear read");
+}
+
+vvs_status vvs_qlinear_apply(vvs_qlinear* ql, int32_t n_rows, const void* d_values, const void* d_powers, int32_t out_dtype, void* d_out, int64_t out_stride, vvs_stream s) {
+  QLinear* l = of(ql);
+  if (!l) return VVS_EINVAL;
+  if (l->cfg.gated) return no(l, VVS_EINVAL, "qlinear apply: created with a gate (vvs_qlinear_gate)");
+  vvs_status st = check_product(l, n_rows, d_values, d_powers);
+  if (st != VVS_OK) return st;
+  if (!d_out) return no(l, VVS_EINVAL, "qlinear apply: NULL argument");
+  if (!known(out_dtype)) return no(l, VVS_EINVAL, "qlinear apply: unknown dtype");
+  const int64_t os = stride_of(out_stride, l->cfg.out);
+  if (os < 0 || off_element(d_out, out_dtype)) return no(l, VVS_EINVAL, "qlinear apply: the stride has to cover a row, the pointer to be aligned to an element");
+  if ((st = check_device(l)) != VVS_OK) return st;
+  QProduct a{};
+  a.w = l->w; a.M = n_rows;
+  a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
+  a.dtype = out_dtype; a.y = d_out; a.stride = (size_t)os; a.wide = wide_rows(d_out, os, out_dtype, 4);
+  a.cus = l->cus;
+  launch_qlinear_product(a, (hipStream_t)s);
+  return launched(l, "qlinear apply");
+}
+
+vvs_status vvs_qlinear_gate(vvs_qlinear* ql, int32_t n_rows, const void* d_values, const void* d_powers, void* d_out_values, void* d_out_powers, vvs_stream s) {
+  QLinear* l = of(ql);
+  if (!l) return VVS_EINVAL;
+  if (!l->cfg.gated) return no(l, VVS_EINVAL, "qlinear gate: created without a gate (vvs_qlinear_apply)");
+  vvs_status st = check_product(l, n_rows, d_values, d_powers);
+  if (st != VVS_OK) return st;
+  if (!d_out_values || !d_out_powers) return no(l, VVS_EINVAL, "qlinear gate: NULL argument");
+  if (off16(d_out_values) || off16(d_out_powers)) return no(l, VVS_EINVAL, "qlinear gate: values and powers must be 16-byte aligned");
+  if ((int64_t)n_rows * 16 * qrows_powers(l->cfg.out) > kMostThreads) return no(l, VVS_ESIZE, "qlinear gate: more rows than a launch holds");
+  if ((st = check_device(l)) != VVS_OK) return st;
+  QProduct a{};
+  a.w = l->w; a.M = n_rows;
+  a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
+  a.act = (float*)l->ws;
+  a.y8 = QRowsOut{(uint8_t*)d_out_values, (uint8_t*)d_out_powers};
+  a.cus = l->cus;
+  launch_qlinear_product(a, (hipStream_t)s);
+  return launched(l, "qlinear gate");
+}
+
+}  // extern "C"

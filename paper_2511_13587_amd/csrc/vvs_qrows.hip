@@ -1,0 +1,157 @@
+// Rows in 8 bits: rounding, norm with the residual's addition, reading back.
+#include "vvs_e4m3.h"
+#include "vvs_qlinear.h"
+
+namespace vvs {
+
+// 8 elements from `at` on of a row of n; those behind its end are 0
+template <typename T>
+__device__ __forceinline__ void read_row8(const T* row, int at, int n, bool wide, float (&v)[8]) {
+  if (wide && at + 8 <= n) {
+    read8(row + at, v);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = at + j < n ? ld(row + at + j) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void write_row8(T* row, int at, int n, bool wide, const float (&v)[8]) {
+  if (wide && at + 8 <= n) {
+    write8(row + at, v);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (at + j < n) st(row + at + j, v[j]);
+}
+
+// Largest over the 16 lanes of a row of the wave, left in all of them
+__device__ __forceinline__ float row16_max(float x) {
+  x = fmaxf(x, dpp_move<0x128>(x));         // row_ror:8
+  x = fmaxf(x, dpp_move<0x141>(x));         // row_half_mirror
+  x = fmaxf(x, dpp_move<0x4E>(x));          // quad_perm:[2,3,0,1]
+  return fmaxf(x, dpp_move<0xB1>(x));       // quad_perm:[1,0,3,2]
+}
+
+// Rounds a block of 128 elements, 8 in each of 16 lanes of a wave's row: their largest gives the power of two, the product with its inverse is exact (but for elements far below the
+// smallest e4m3 number), so that an element is rounded once.
+__device__ __forceinline__ void round_block(const float (&v)[8], uint8_t* values, uint8_t* power, bool held, bool first) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = fmaxf(top, finite(v[j]) ? fabsf(v[j]) : 0.f);
+  const int e = e4m3_exponent(row16_max(top));
+  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+  float w[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j] = v[j] * inv;
+  if (held) *(uint2*)values = to_e4m3x8(w);
+  if (first) *power = held ? (uint8_t)(e + 127) : 0;
+}
+
+// One unit of 16 lanes per block; blocks behind a row's last one (their number is rounded up to 4) are powers alone.  Bound by HBM.
+template <typename T>
+__global__ __launch_bounds__(256) void k_qrows_round(QRound a) {
+  const int powers = qrows_powers(a.width), blocks = qrows_blocks(a.width);
+  const uint32_t unit = blockIdx.x * 16u + (threadIdx.x >> 4);
+  const int m = unit / (uint32_t)powers, b = unit % (uint32_t)powers, sub = threadIdx.x & 15;
+  if (m >= a.M) return;
+  float v[8];
+  const int at = b * kQRowBlock + sub * 8;
+  read_row8((const T*)a.x + (size_t)m * a.stride, at, a.width, a.wide, v);
+  round_block(v, a.y.values + (size_t)m * blocks * kQRowBlock + at, a.y.powers + (size_t)m * powers + b, b < blocks, sub == 0);
+}
+
+void launch_qrows_round(const QRound& a, hipStream_t s) {
+  const size_t units = (size_t)a.M * qrows_powers(a.width);
+  const dim3 grid((unsigned)((units + 15) / 16));
+  if (a.dtype == VVS_BF16) hipLaunchKernelGGL(k_qrows_round<bf16_t>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_qrows_round<float>, grid, dim3(256), 0, s, a);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_qrows_read(QRowsRead a) {
+  const int powers = qrows_powers(a.width), blocks = qrows_blocks(a.width);
+  const uint32_t unit = blockIdx.x * 16u + (threadIdx.x >> 4);
+  const int m = unit / (uint32_t)blocks, b = unit % (uint32_t)blocks, at = b * kQRowBlock + (threadIdx.x & 15) * 8;
+  if (m >= a.M) return;
+  float v[8];
+  from_e4m3x8(*(const uint2*)(a.x.values + (size_t)m * blocks * kQRowBlock + at), v);
+  const float scale = __uint_as_float((uint32_t)a.x.powers[(size_t)m * powers + b] << 23);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] *= scale;
+  write_row8((T*)a.y + (size_t)m * a.stride, at, a.width, a.wide, v);
+}
+
+void launch_qrows_read(const QRowsRead& a, hipStream_t s) {
+  const size_t units = (size_t)a.M * qrows_blocks(a.width);
+  const dim3 grid((unsigned)((units + 15) / 16));
+  if (a.dtype == VVS_BF16) hipLaunchKernelGGL(k_qrows_read<bf16_t>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_qrows_read<float>, grid, dim3(256), 0, s, a);
+}
+
+__device__ __forceinline__ void read_any8(const void* row, int dtype, int at, int n, bool wide, float (&v)[8]) {
+  if (dtype == VVS_BF16) read_row8((const bf16_t*)row, at, n, wide, v);
+  else read_row8((const float*)row, at, n, wide, v);
+}
+
+// One workgroup of TH threads per row, which stays in registers: V times 8 elements per thread.  x + delta is rounded to the residual's type, and what is normalised is what is kept.
+template <int TH, int V>
+__global__ __launch_bounds__(TH) void k_qrows_norm(QNorm a) {
+  __shared__ float red[16];
+  const int m = blockIdx.x, blocks = qrows_blocks(a.width), powers = qrows_powers(a.width);
+  const size_t esz = a.x_dtype == VVS_BF16 ? 2 : 4, dsz = a.delta_dtype == VVS_BF16 ? 2 : 4;
+  float v[V][8];
+#pragma unroll
+  for (int j = 0; j < V; ++j) read_any8((const char*)a.x + (size_t)m * a.x_stride * esz, a.x_dtype, (j * TH + threadIdx.x) * 8, a.width, a.x_wide, v[j]);
+  if (a.delta) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float d[8];
+      read_any8((const char*)a.delta + (size_t)m * a.delta_stride * dsz, a.delta_dtype, (j * TH + threadIdx.x) * 8, a.width, a.delta_wide, d);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[j][i] += d[i];
+        if (a.x_dtype == VVS_BF16) v[j][i] = bf2f(f2bf(v[j][i]));
+      }
+    }
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss += v[j][i] * v[j][i];
+  }
+  if (a.x_out) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int at = (j * TH + threadIdx.x) * 8;
+      if (a.x_dtype == VVS_BF16) write_row8((bf16_t*)a.x_out + (size_t)m * a.x_out_stride, at, a.width, a.x_out_wide, v[j]);
+      else write_row8((float*)a.x_out + (size_t)m * a.x_out_stride, at, a.width, a.x_out_wide, v[j]);
+    }
+  }
+  ss = TH == 64 ? wave_sum(ss) : block_sum(ss, red);
+  const float r = 1.f / sqrtf(ss / (float)a.width + a.eps);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int at = (j * TH + threadIdx.x) * 8, b = at / kQRowBlock;
+    if (b >= powers) break;
+    float g[8], y[8];
+    read_any8(a.gain, a.gain_dtype, at, a.width, a.gain_wide, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = at + i < a.width ? v[j][i] * r * g[i] : 0.f;
+    round_block(y, a.y.values + (size_t)m * blocks * kQRowBlock + at, a.y.powers + (size_t)m * powers + b, b < blocks, (threadIdx.x & 15) == 0);
+  }
+}
+
+void launch_qrows_norm(const QNorm& a, hipStream_t s) {
+  const dim3 grid(a.M);
+  const int w = a.width;
+  if (w <= 512) hipLaunchKernelGGL((k_qrows_norm<64, 1>), grid, dim3(64), 0, s, a);
+  else if (w <= 2048) hipLaunchKernelGGL((k_qrows_norm<256, 1>), grid, dim3(256), 0, s, a);
+  else if (w <= 4096) hipLaunchKernelGGL((k_qrows_norm<256, 2>), grid, dim3(256), 0, s, a);
+  else if (w <= 8192) hipLaunchKernelGGL((k_qrows_norm<256, 4>), grid, dim3(256), 0, s, a);
+  else if (w <= 16384) hipLaunchKernelGGL((k_qrows_norm<1024, 2>), grid, dim3(1024), 0, s, a);
+  else hipLaunchKernelGGL((k_qrows_norm<1024, 8>), grid, dim3(1024), 0, s, a);
+}
+
+}  // namespace vvs

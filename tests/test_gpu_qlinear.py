@@ -1,0 +1,105 @@
+"""Products of rows and weights in 8 bits against plain statements in 64 bits."""
+import pytest
+import torch
+
+import qlinear_common as qc
+
+pytestmark = pytest.mark.gpu
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _vvs(vb, dtype):
+    return vb.VVS_FP32 if dtype == torch.float32 else vb.VVS_BF16
+
+
+def _normal(dims, seed, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(dims, generator=g) * torch.exp2(torch.randn(dims[-1:], generator=g) * spread)
+
+
+def _linear(vb, rows, width, out, dtype=torch.bfloat16, gated=False, seed=0):
+    """(linear, rows, held x, held weights in float64)"""
+    ws = [(_normal((width, out), seed + 1 + i) * width ** -0.5).to(dtype) for i in range(2 if gated else 1)]
+    lin = vb.QLinear(width, out, rows, _vvs(vb, dtype), gated=gated)
+    lin.vvs_qlinear_load(*[w.cuda() for w in ws])
+    r = vb.QRows(rows, width)
+    x = qc.put(r, _normal((rows, width), seed))
+    return lin, r, x, [qc.held(w.t())[0].t() for w in ws]
+
+
+def product_error(x, w):
+    """How far x @ w may be off (float64 x, w as held).  e4m3 numbers are exact in bf16, as are their products in fp32; 32 products go into an fp32 sum by a matrix instruction of at most 8 roundings in a row, partial
+    sums of eight waves are added: K / 4 + 16 roundings of at most the sum of magnitudes."""
+    return (x.shape[1] / 4 + 16) * 2.0 ** -24 * (x.abs() @ w.abs())
+
+
+def check_product(y, x, w, dtype):
+    want = x @ w
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24
+    err = product_error(x, w)
+    bound = err + half * (want.abs() + err)
+    worst = ((y.double().cpu() - want).abs() - bound).max().item()
+    assert worst <= 0, worst
+
+
+def check_gate(out, x, w):
+    g, u = x @ w[0], x @ w[1]
+    a = g * torch.sigmoid(g)
+    eg, eu = product_error(x, w[0]), product_error(x, w[1])
+    # |d silu| <= 1.1; exponential, sum, division, product: 8 roundings at most
+    err = 1.1 * eg * (u.abs() + eu) + (a.abs() + 1.1 * eg) * eu + 8 * 2.0 ** -24 * (a * u).abs()
+    qc.check_rounded(out, a * u, err)
+
+
+@pytest.mark.parametrize("width,out", [(1, 1), (128, 64), (129, 65), (344, 128), (1000, 77), (1280, 3840), (515, 300)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("gated", [False, True])
+def test_weights_are_held_by_column(width, out, dtype, gated):
+    from paper_2511_13587_amd import binding as vb
+    ws = [_normal((width, out), 5 + i, 3.0).to(TYPES[dtype]) for i in range(2 if gated else 1)]
+    lin = vb.QLinear(width, out, 1, _vvs(vb, TYPES[dtype]), gated=gated)
+    lin.vvs_qlinear_load(*[w.cuda() for w in ws])
+    got = [torch.full((width, out), 9.0, dtype=TYPES[dtype], device="cuda") for _ in ws]
+    lin.vvs_qlinear_read(*got)
+    for w, y in zip(ws, got):
+        assert torch.equal(y.cpu().double(), qc.held(w.t())[0].t())
+
+
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 31, 33, 64, 65, 100, 129, 257])
+@pytest.mark.parametrize("width,out", [(344, 128), (1000, 77), (128, 1), (1, 300)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_product_at_odd_sizes(rows, width, out, dtype):
+    from paper_2511_13587_amd import binding as vb
+    lin, r, x, (w,) = _linear(vb, rows, width, out, seed=rows)
+    y = torch.full((rows, out), 3.0, dtype=TYPES[dtype], device="cuda")
+    lin.vvs_qlinear_apply(r, y)
+    check_product(y, x, w, TYPES[dtype])
+
+
+@pytest.mark.parametrize("rows,width,out", [(8, 4096, 512), (28, 11008, 256), (48, 768, 2048), (200, 2048, 1280), (432, 1280, 3840), (1100, 512, 1024), (600, 640, 4160)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_product(rows, width, out, dtype):
+    from paper_2511_13587_amd import binding as vb
+    lin, r, x, (w,) = _linear(vb, rows, width, out, seed=rows)
+    y = torch.full((rows, out), 3.0, dtype=TYPES[dtype], device="cuda")
+    lin.vvs_qlinear_apply(r, y)
+    check_product(y, x, w, TYPES[dtype])
+
+
+@pytest.mark.parametrize("rows", [1, 14, 16, 17, 33, 65, 130, 300])
+@pytest.mark.parametrize("width,out", [(128, 32), (344, 129), (1000, 77), (100, 1)])
+def test_gate_at_odd_sizes(rows, width, out):
+    from paper_2511_13587_amd import binding as vb
+    lin, r, x, w = _linear(vb, rows, width, out, gated=True, seed=rows)
+    y = vb.QRows(rows, out)
+    lin.vvs_qlinear_gate(r, y)
+    check_gate(y, x, w)
+
+
+@pytest.mark.parametrize("rows,width,out", [(48, 768, 2048), (14, 4096, 1024), (432, 1280, 3456), (700, 512, 1100)])
+def test_gate(rows, width, out):
+    from paper_2511_13587_amd import binding as vb
+    lin, r, x, w = _linear(vb, rows, width, out, gated=True, seed=rows)
+    y = vb.QRows(rows, out)
+    lin.vvs_qlinear_gate(r, y)
+    check_gate(y, x, w)
