@@ -477,7 +477,7 @@ typedef struct vvs_qlinear vvs_qlinear;   /* opaque host object; owns no device 
 
 typedef struct {
   int32_t in, out;               /* elements of a row that goes in and of one that comes out */
-  int32_t max_rows;              /* largest n_rows of a call, at most 2^21 */
+  int32_t max_rows;              /* largest n_rows of a call, at most 2^20 */
   int32_t gated;                 /* 0: one matrix, for vvs_qlinear_apply; 1: gate and up, for vvs_qlinear_gate */
   int32_t dtype;                 /* of the weights that vvs_qlinear_load takes and vvs_qlinear_read gives */
 } vvs_qlinear_config;

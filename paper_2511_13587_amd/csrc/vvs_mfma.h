@@ -41,6 +41,23 @@ __device__ __forceinline__ void tile_of(int id, int MT, int NT, int* tile_m, int
   *tile_n = grp * 8 + rem % cols;
 }
 
+// 16 bytes per lane straight from global memory into LDS: lane l of a wave writes what it asked for to LDS address lds_byte_addr + 16 l.  The compiler knows nothing of these loads: waits are
+// written out by hand.  M0 is written here, so it is on the clobber list: the compiler must not keep a value of its own in it across
+// the statement (it names M0 "reserved" and warns about any clobber of it; that warning is silenced for this
+// one statement).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void lds_dma16(const void* g, uint32_t lds_byte_addr) {
+  const uint32_t a = __builtin_amdgcn_readfirstlane(lds_byte_addr);     // wave-uniform by construction
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(a), "v"(g) : "memory", "m0");
+}
+// the same from a wave-uniform address plus an offset of each lane's own
+__device__ __forceinline__ void lds_dma16(const void* base, uint32_t offset, uint32_t lds_byte_addr) {
+  const uint32_t a = __builtin_amdgcn_readfirstlane(lds_byte_addr);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(a), "v"(offset), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 // K and V of 32-key step STEP of the head whose caches start at kb and vb, into the operand registers of lane `lane`
 #define VVS_ATTN_LOAD(STEP, KF, VF)                                                                                   \
   {                                                                                                                   \

@@ -538,16 +538,6 @@ __global__ __launch_bounds__(NW * 64) void k_gemm_direct(const uint4* __restrict
 // slot stage s - 1 has left; multiply the first half of stage s on fragments read during the stage before, read and multiply
 // the second half; wait until this wave's part of stage s + 2 has landed - loads return in order, so "at most PER * (NS - 3)
 // younger loads outstanding" - and meet the other waves at the barrier.  The epilogue works on the accumulators.
-// M0 is written here, so it is on the clobber list: the compiler must not keep a value of its own in it across
-// the statement (it names M0 "reserved" and warns about any clobber of it; that warning is silenced for this
-// one statement).
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void lds_dma16(const void* g, uint32_t lds_byte_addr) {
-  const uint32_t a = __builtin_amdgcn_readfirstlane(lds_byte_addr);     // wave-uniform by construction
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(a), "v"(g) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 // L1 fill probe (vvs_debug_fill_probe): every workgroup reads the same region `reps` times; a wave takes 1 KiB blocks
 // round-robin, 8 in flight.  DMA: the blocks go straight to LDS (8 slots per wave), else into registers.
 template <bool DMA>

@@ -66,6 +66,15 @@ struct QWeightsRead {
   int dtype;
 };
 
+// Which kernel makes a product
+enum QTile { kTile128x256, kTile64x256, kTile64x128, kTile32x128, kTile32x256 };   // rows x packed columns of a workgroup
+struct QPlan {
+  bool few;                         // k_qlinear_few: rt tiles of 16 rows, ct of 16 columns, the contraction cut into splits; else k_qlinear_tile
+  int rt, ct, splits;
+  QTile tile;
+};
+QPlan plan_qlinear_product(const QWeights& w, int M);
+
 struct QProduct {
   QWeights w;
   int M;
@@ -74,9 +83,9 @@ struct QProduct {
   void* y;                          // !gated
   size_t stride;
   int wide;                         // stores of 4 elements at once
-  float* act;                       // gated: workspace [M][groups * 32]
+  float* act;                       // workspace: gated, [M][groups * 32]; else partial sums
+  uint32_t* counters;               // workspace: zero between calls
   QRowsOut y8;                      // gated
-  int cus;
 };
 
 void launch_qrows_round(const QRound& a, hipStream_t s);
@@ -84,6 +93,7 @@ void launch_qrows_norm(const QNorm& a, hipStream_t s);
 void launch_qrows_read(const QRowsRead& a, hipStream_t s);
 void launch_qlinear_load(const QLoad& a, hipStream_t s);
 void launch_qlinear_read(const QWeightsRead& a, hipStream_t s);
-void launch_qlinear_product(const QProduct& a, hipStream_t s);
+void launch_qlinear_product(const QProduct& a, const QPlan& p, hipStream_t s);
+void launch_qlinear_tile(const QProduct& a, QTile t, hipStream_t s);
 
 }  // namespace vvs

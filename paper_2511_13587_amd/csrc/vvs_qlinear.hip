@@ -2,7 +2,7 @@
 #include <algorithm>
 
 #include "vvs_e4m3.h"
-#include "vvs_qlinear.h"
+#include "vvs_qlinear_device.h"
 
 namespace vvs {
 
@@ -76,137 +76,202 @@ void launch_qlinear_read(const QWeightsRead& a, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------------------------------------ products
-// 32 bytes of a lane's operand: 32 contraction values of one row or column
-struct Held { uint4 h[2]; };
-// ... as the operands of four 16x16x32 MFMAs in bf16, times their power of two (exact)
-__device__ __forceinline__ bf16x8 part_of(const Held& x, int j, float scale) {
-  const uint4 q = x.h[j >> 1];
-  return e4m3_to_bf16(j & 1 ? make_uint2(q.z, q.w) : make_uint2(q.x, q.y), scale);
+// Agent scope: written through to the memory behind the XCDs' L2s, and read from there
+__device__ __forceinline__ void put4(float* p, const float (&v)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; j += 2)
+    __hip_atomic_store((uint64_t*)(p + j), (uint64_t)__float_as_uint(v[j]) | (uint64_t)__float_as_uint(v[j + 1]) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-
-template <typename T>
-__device__ __forceinline__ void store4(T* y, int n, bool wide, const float (&v)[4]) {
-  if (wide && n >= 4) {
-    if constexpr (sizeof(T) == 4) *(float4*)y = make_float4(v[0], v[1], v[2], v[3]);
-    else *(uint2*)y = make_uint2(pack2bf(v[0], v[1]), pack2bf(v[2], v[3]));
-    return;
+__device__ __forceinline__ void get4(const float* p, float* v) {
+#pragma unroll
+  for (int j = 0; j < 4; j += 2) {
+    const uint64_t u = __hip_atomic_load((const uint64_t*)(p + j), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    v[j] = __uint_as_float((uint32_t)u);
+    v[j + 1] = __uint_as_float((uint32_t)(u >> 32));
   }
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (j < n) st(y + j, v[j]);
 }
 
-__device__ __forceinline__ float silu(float x) { return x / (1.f + expf(-x)); }
-
-// Few rows.  A workgroup of 8 waves makes CT tiles of 16 columns for 16 RT rows; every wave takes each eighth block of the contraction, straight from memory into operand registers, and the
-// eight partial sums are added through LDS in the order of the waves.
-constexpr int kFewWaves = 8;
-template <int RT, int CT, bool GATED, typename T>
-__global__ __launch_bounds__(64 * kFewWaves) void k_qlinear_few(QProduct a) {
-  extern __shared__ float4 parts[];          // [wave][CT][RT][lane]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+// Few rows.  A workgroup of NW waves makes CT tiles of 16 columns for 16 RT rows; wave w takes blocks w, w + NW, ... of the contraction, straight from memory into operand registers, one block ahead,
+// and the partial sums are added through LDS in the order of the waves.  Powers of all blocks lie in LDS, four in a word.
+template <int NW, int RT, int CT, bool GATED, typename T>
+__global__ __launch_bounds__(64 * NW) void k_qlinear_few(QProduct a) {
+  extern __shared__ float4 parts[];          // [wave][CT][RT][lane]; until the products are made the powers: rows [16 RT][stride], columns [16 CT][stride]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
   const int group = blockIdx.x / (4 / CT), t0 = blockIdx.x % (4 / CT) * CT, m0 = blockIdx.y * 16 * RT;
-  const int blocks = a.w.blocks, powers = qrows_powers(a.w.in);
+  const int blocks = a.w.blocks, powers = qrows_powers(a.w.in), words = powers / 4, stride = words | 1;
   const size_t width = (size_t)blocks * kQRowBlock;
-  size_t row[RT];
+  const uint8_t* const rows = a.x.values + (size_t)m0 * width;
+  uint32_t row[RT];                          // rows behind the last one repeat it
 #pragma unroll
-  for (int r = 0; r < RT; ++r) row[r] = min(m0 + 16 * r + i, a.M - 1);     // rows behind the last one repeat it
+  for (int r = 0; r < RT; ++r) row[r] = (uint32_t)(min(16 * r + i, a.M - 1 - m0) * (int)width + g * 32);
   floatx4 acc[CT][RT];
 #pragma unroll
   for (int c = 0; c < CT; ++c)
 #pragma unroll
     for (int r = 0; r < RT; ++r) acc[c][r] = floatx4{0.f, 0.f, 0.f, 0.f};
-  for (int b = wave; b < blocks; b += kFewWaves) {
-    Held w[CT], x[RT];
-    float ws[CT], xs[RT];
+  u32x4 w[2][CT][2], x[2][RT][2];
+  auto request = [&](int b, u32x4 (&wb)[CT][2], u32x4 (&xb)[RT][2]) {
+    const uint8_t* p = a.w.data + a.w.tile_at(group, b, t0);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-      const uint4* p = (const uint4*)(a.w.data + a.w.tile_at(group, b, t0 + c));
-      w[c].h[0] = p[lane];
-      w[c].h[1] = p[64 + lane];
-      ws[c] = __uint_as_float((uint32_t)a.w.powers[a.w.power_at(group, b, t0 + c) + i * 4] << 23);
+      wb[c][0] = *(const u32x4*)(p + c * 2048 + lane * 16);
+      wb[c][1] = *(const u32x4*)(p + c * 2048 + 1024 + lane * 16);
     }
+    const uint8_t* q = rows + (size_t)b * kQRowBlock;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const uint4* p = (const uint4*)(a.x.values + row[r] * width + (size_t)b * kQRowBlock + g * 32);
-      x[r].h[0] = p[0];
-      x[r].h[1] = p[1];
-      xs[r] = __uint_as_float((uint32_t)a.x.powers[row[r] * powers + b] << 23);
+      xb[r][0] = *(const u32x4*)(q + row[r]);
+      xb[r][1] = *(const u32x4*)(q + row[r] + 16);
     }
+  };
+  int* const xpow = (int*)parts;
+  int* const wpow = xpow + 16 * RT * stride;
+  const int* const mine_xpow = xpow + i * stride;
+  const int* const mine_wpow = wpow + i * stride;
+  auto multiply = [&](int b, const u32x4 (&wb)[CT][2], const u32x4 (&xb)[RT][2]) {
+    const int at = b >> 2, sh = 8 * (b & 3);
+    int ws[CT], xs[RT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) ws[c] = mine_wpow[c * 16 * stride + at] >> sh & 0xFF;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) xs[r] = mine_xpow[r * 16 * stride + at] >> sh & 0xFF;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       bf16x8 wj[CT];
 #pragma unroll
-      for (int c = 0; c < CT; ++c) wj[c] = part_of(w[c], j, ws[c]);
+      for (int c = 0; c < CT; ++c) wj[c] = e4m3_to_bf16(make_uint2(wb[c][j >> 1][2 * (j & 1)], wb[c][j >> 1][2 * (j & 1) + 1]), __uint_as_float((uint32_t)ws[c] << 23));
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const bf16x8 xj = part_of(x[r], j, xs[r]);
+        const bf16x8 xj = e4m3_to_bf16(make_uint2(xb[r][j >> 1][2 * (j & 1)], xb[r][j >> 1][2 * (j & 1) + 1]), __uint_as_float((uint32_t)xs[r] << 23));
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wj[c], xj, acc[c][r], 0, 0, 0);
       }
     }
+  };
+  // this workgroup's blocks: b0 .. b1 - 1
+  const int b0 = (int)((int64_t)blocks * blockIdx.z / gridDim.z), b1 = (int)((int64_t)blocks * (blockIdx.z + 1) / gridDim.z);
+  if (b0 + wave < b1) request(b0 + wave, w[0], x[0]);
+  for (int u = tid; u < 16 * RT * words; u += 64 * NW) {
+    const int r = u / words, d = u % words;
+    xpow[r * stride + d] = *(const int*)(a.x.powers + (size_t)min(m0 + r, a.M - 1) * powers + d * 4);
   }
+  {
+    const int* p = (const int*)(a.w.powers + a.w.power_at(group, 0, t0));
+    for (int u = tid; u < 16 * CT * words; u += 64 * NW) wpow[u % (16 * CT) * stride + u / (16 * CT)] = p[u / (16 * CT) * 64 + u % (16 * CT)];
+  }
+  __syncthreads();
+  for (int b = b0 + wave; b < b1; b += 2 * NW) {
+    if (b + NW < b1) request(b + NW, w[1], x[1]);
+    multiply(b, w[0], x[0]);
+    if (b + 2 * NW < b1) request(b + 2 * NW, w[0], x[0]);
+    if (b + NW < b1) multiply(b + NW, w[1], x[1]);
+  }
+  __syncthreads();
 #pragma unroll
   for (int c = 0; c < CT; ++c)
 #pragma unroll
     for (int r = 0; r < RT; ++r) parts[((wave * CT + c) * RT + r) * 64 + lane] = make_float4(acc[c][r][0], acc[c][r][1], acc[c][r][2], acc[c][r][3]);
   __syncthreads();
+  const int busy = min(NW, b1 - b0);
   auto whole = [&](int c, int r, int l, float (&v)[4]) {
     float4 s = parts[(c * RT + r) * 64 + l];
-#pragma unroll
-    for (int u = 1; u < kFewWaves; ++u) {
+    for (int u = 1; u < busy; ++u) {
       const float4 p = parts[((u * CT + c) * RT + r) * 64 + l];
       s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
     }
     v[0] = s.x; v[1] = s.y; v[2] = s.z; v[3] = s.w;
   };
-  constexpr int kPairs = GATED ? CT / 2 : CT;
-  for (int u = threadIdx.x; u < kPairs * RT * 64; u += 64 * kFewWaves) {
-    const int l = u & 63, r = (u >> 6) % RT, c = (u >> 6) / RT, m = m0 + 16 * r + (l & 15);
-    if (m >= a.M) continue;
-    float v[4];
-    if constexpr (GATED) {
-      float up[4];
+  // Counts this workgroup in; the last of n goes on, for all.  What it reads was written through to memory before it was counted.
+  auto last_of = [&](uint32_t* counter, int n) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) {
+      const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)n - 1;
+      if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      *(int*)parts = last;
+    }
+    __syncthreads();
+    return *(const int*)parts != 0;
+  };
+  if constexpr (GATED) {
+    for (int u = tid; u < CT / 2 * RT * 64; u += 64 * NW) {
+      const int l = u & 63, r = (u >> 6) % RT, c = (u >> 6) / RT, m = m0 + 16 * r + (l & 15);
+      float v[4], up[4];
       whole(2 * c, r, l, v);
       whole(2 * c + 1, r, l, up);
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = silu(v[j]) * up[j];
-      *(float4*)(a.act + (size_t)m * a.w.groups * 32 + a.w.column(group, t0 + 2 * c, 4 * (l >> 4))) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
-      whole(c, r, l, v);
+      if (m < a.M) put4(a.act + (size_t)m * a.w.groups * 32 + a.w.column(group, t0 + 2 * c, 4 * (l >> 4)), v);
+    }
+    // a block of 128 hidden units is that of 16 / CT workgroups
+    if (!last_of(a.counters + blockIdx.y * (a.w.groups / 4) + group / 4, 16 / CT)) return;
+    const int out_blocks = qrows_blocks(a.w.out), out_powers = qrows_powers(a.w.out), block = group / 4, sub = tid & 15;
+    for (int r = tid >> 4; r < 16 * RT; r += 4 * NW) {
+      const int m = m0 + r;
+      if (m >= a.M || block >= out_blocks) break;
+      float v[8];
+      const float* p = a.act + (size_t)m * a.w.groups * 32 + block * kQRowBlock + sub * 8;
+      get4(p, v);
+      get4(p + 4, v + 4);
+      uint8_t* power = a.y8.powers + (size_t)m * out_powers;
+      round_block(v, a.y8.values + ((size_t)m * out_blocks + block) * kQRowBlock + sub * 8, power + block, true, sub == 0);
+      if (block == out_blocks - 1 && sub > 0 && block + sub < out_powers) power[block + sub] = 0;
+    }
+  } else {
+    const int splits = gridDim.z, unit = blockIdx.y * gridDim.x + blockIdx.x;
+    float* const mine = a.act + (size_t)unit * splits * (CT * RT * 256);      // [split][CT][RT][lane][4]
+    if (splits > 1) {
+      for (int u = tid; u < CT * RT * 64; u += 64 * NW) {
+        float v[4];
+        whole((u >> 6) / RT, (u >> 6) % RT, u & 63, v);
+        put4(mine + ((size_t)blockIdx.z * CT * RT * 64 + u) * 4, v);
+      }
+      if (!last_of(a.counters + unit, splits)) return;
+    }
+    for (int u = tid; u < CT * RT * 64; u += 64 * NW) {
+      const int l = u & 63, r = (u >> 6) % RT, c = (u >> 6) / RT, m = m0 + 16 * r + (l & 15);
+      if (m >= a.M) continue;
+      float v[4];
+      if (splits > 1) {
+        get4(mine + (size_t)u * 4, v);
+        for (int z = 1; z < splits; ++z) {
+          float p[4];
+          get4(mine + ((size_t)z * CT * RT * 64 + u) * 4, p);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] += p[j];
+        }
+      } else {
+        whole(c, r, l, v);
+      }
       const int col = a.w.column(group, t0 + c, 4 * (l >> 4));
       store4((T*)a.y + (size_t)m * a.stride + col, a.w.out - col, a.wide, v);
     }
   }
 }
 
-template <int RT, int CT, bool GATED, typename T>
-static void few_t(const QProduct& a, hipStream_t s) {
-  const size_t lds = (size_t)kFewWaves * CT * RT * 64 * sizeof(float4);
-  if (lds > 65536) allow_dynamic_lds((const void*)k_qlinear_few<RT, CT, GATED, T>, lds);
-  hipLaunchKernelGGL((k_qlinear_few<RT, CT, GATED, T>), dim3(a.w.groups * (4 / CT), (a.M + 16 * RT - 1) / (16 * RT)), dim3(64 * kFewWaves), lds, s, a);
+template <int NW, int RT, int CT, bool GATED, typename T>
+static void few_t(const QProduct& a, int splits, hipStream_t s) {
+  const size_t parts = (size_t)NW * CT * RT * 64 * sizeof(float4), powers = (size_t)16 * (RT + CT) * ((qrows_powers(a.w.in) / 4) | 1) * 4, lds = std::max(parts, powers);
+  auto kernel = k_qlinear_few<NW, RT, CT, GATED, T>;
+  if (lds > 65536) allow_dynamic_lds((const void*)kernel, kMostLds);
+  hipLaunchKernelGGL(kernel, dim3(a.w.groups * (4 / CT), (a.M + 16 * RT - 1) / (16 * RT), splits), dim3(64 * NW), lds, s, a);
 }
 
-template <bool GATED, typename T>
-static void few(const QProduct& a, hipStream_t s) {
-  if (a.M <= 16) few_t<1, 2, GATED, T>(a, s);
-  else if (a.M <= 32) few_t<2, 2, GATED, T>(a, s);
-  else few_t<4, 4, GATED, T>(a, s);
+template <typename T>
+static void few(const QProduct& a, const QPlan& p, hipStream_t s) {
+  if (p.rt == 1 && p.ct == 1) few_t<8, 1, 1, false, T>(a, p.splits, s);
+  else if (p.rt == 1) few_t<4, 1, 2, false, T>(a, p.splits, s);
+  else if (p.ct == 1) few_t<8, 2, 1, false, T>(a, p.splits, s);
+  else if (p.ct == 2) few_t<8, 2, 2, false, T>(a, p.splits, s);
+  else few_t<8, 2, 4, false, T>(a, p.splits, s);
 }
 
-void launch_qlinear_product(const QProduct& a, hipStream_t s) {
-  if (a.w.gated) {
-    few<true, float>(a, s);
-    QRound r{};
-    r.M = a.M; r.width = a.w.out; r.dtype = VVS_FP32;
-    r.x = a.act; r.stride = (size_t)a.w.groups * 32; r.wide = 1;
-    r.y = a.y8;
-    launch_qrows_round(r, s);
-  } else if (a.dtype == VVS_BF16) {
-    few<false, bf16_t>(a, s);
-  } else {
-    few<false, float>(a, s);
-  }
+void launch_qlinear_product(const QProduct& a, const QPlan& p, hipStream_t s) {
+  if (!p.few) launch_qlinear_tile(a, p.tile, s);
+  else if (a.w.gated && p.rt == 1) few_t<4, 1, 2, true, float>(a, 1, s);
+  else if (a.w.gated) few_t<4, 2, 2, true, float>(a, 1, s);
+  else if (a.dtype == VVS_BF16) few<bf16_t>(a, p, s);
+  else few<float>(a, p, s);
 }
 
 }  // namespace vvs

@@ -1,7 +1,7 @@
 // Host side of the rows and weights in 8 bits: argument checks, buffer sizes, entry points.
 #include "vvs_qlinear.h"
 
-#include <math.h>
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -10,8 +10,8 @@ namespace vvs {
 struct QLinear {
   vvs_qlinear_config cfg;
   QWeights w;
-  size_t weight_bytes, ws_bytes;
-  int dev, cus;
+  size_t weight_bytes, ws_bytes, counter_bytes;
+  int dev;
   char* ws;
   bool loaded;
   std::string err;
@@ -67,6 +67,40 @@ static vvs_status check_rows(int n_rows, int width, const void* values, const vo
   return VVS_OK;
 }
 
+// Few rows are bound by the weights' bytes, which every wave streams for itself; more rows share them, and themselves pass through LDS.  us per call in a graph, weights rotating through 400 MB.
+//   16 rows: columns a tile each while there are no more tiles than CUs (8 rows, 11008 -> 4096: 1 tile 11.9, 2 tiles 14.5; 1280 -> 3840 4.39 / 4.68), else two (4096 -> 12288 14.1 / 12.9)
+//   up to 64 rows: 32 rows x 2 tiles (60 rows: 4096 -> 12288 21.0, 11008 -> 4096 19.6, 1280 -> 3840 5.6; tiles of 32 x 128 22.9, 54, 7.4), up to 32 rows again 1 tile where few (28 rows, 4096 -> 4096 7.9 / 8.3),
+//     but a long contraction in two halves (28 rows, 11008 -> 4096: 1 tile 17.2, 2 tiles 19.9, 2 tiles in halves 15.3)
+//   beyond: the largest tiles of which there are enough.  128 x 256 from two per CU on (8192 rows, 4096 -> 12288: 362, 64 x 256 418); 64 x 256 from 224 (1000 rows, 1280 -> 3840, 240 tiles: 12.1, 64 x 128
+//     12.6, 128 x 256 15.3); 64 x 128 from 176 (432 rows, 1280 -> 3840, 210: 9.3, 64 x 256 11.1; 128 rows, 4096 -> 12288, 192: 26.3, 32 x 128 28.6); 32 x 128 from 130 (432 rows, 1280 -> 1280, 140: 7.5,
+//     few 8.6); fewer leave CUs idle and latency bare: k_qlinear_few, 32 rows x 4 tiles (128 rows: 11008 -> 4096 25.3 / 32 x 128 53.9, 1280 -> 3840 6.8 / 7.5)
+//   with a gate: up to 32 rows 2 tiles (28 rows, 4096 -> 11008: 26.2, 32 x 256 30.4), up to 64 tiles of 32 x 256 (60 rows: 30.5, few 38.5), 64 x 256 (128 rows 34.7, 128 x 256 45.6; 432 rows, 1280 ->
+//     3456 11.9 / 16.2), 128 x 256 from 384 tiles on
+QPlan plan_qlinear_product(const QWeights& w, int M) {
+  QPlan p{true, M <= 16 ? 1 : 2, 2, 1, kTile32x128};
+  const int columns = 4 * w.groups;
+  auto tiles = [&](int rows, int groups) { return (int64_t)((M + rows - 1) / rows) * ((w.groups + groups - 1) / groups); };
+  if (w.gated) {
+    p.few = M <= 32;
+    p.tile = M <= 64 ? kTile32x256 : tiles(128, 4) >= 384 ? kTile128x256 : kTile64x256;
+    return p;
+  }
+  if (M <= 64) {
+    if (M <= 32 && columns <= 256) {
+      if (M > 16 && w.blocks >= 64) p.splits = 2;
+      else p.ct = 1;
+    }
+    return p;
+  }
+  if (tiles(32, 2) < 130) {
+    p.ct = 4;
+    return p;
+  }
+  p.few = false;
+  p.tile = tiles(128, 4) >= 512 ? kTile128x256 : tiles(64, 4) >= 224 ? kTile64x256 : tiles(64, 2) >= 176 ? kTile64x128 : kTile32x128;
+  return p;
+}
+
 static vvs_status plan_qlinear(const vvs_qlinear_config* cfg, QLinear* l) {
   if (!cfg) return no(nullptr, VVS_EINVAL, "qlinear config is NULL");
   const vvs_qlinear_config& g = *cfg;
@@ -74,15 +108,19 @@ static vvs_status plan_qlinear(const vvs_qlinear_config* cfg, QLinear* l) {
   if (!known(g.dtype)) return no(nullptr, VVS_EINVAL, "qlinear config: unknown dtype");
   if (g.gated != 0 && g.gated != 1) return no(nullptr, VVS_EINVAL, "qlinear config: gated must be 0 or 1");
   if (g.in > kWidest || (g.gated && g.out > kWidest)) return no(nullptr, VVS_ESIZE, "qlinear config: at most 65536 elements per row");
-  if (g.out > (1 << 24) || g.max_rows > (1 << 21)) return no(nullptr, VVS_ESIZE, "qlinear config: at most 2^24 columns and 2^21 rows");
+  if (g.out > (1 << 24) || g.max_rows > (1 << 20)) return no(nullptr, VVS_ESIZE, "qlinear config: at most 2^24 columns and 2^20 rows");
   l->cfg = g;
   QWeights& w = l->w;
   w = QWeights{g.in, g.out, g.gated, qrows_blocks(g.in), 0, nullptr, nullptr};
   w.groups = (g.out + w.unit() - 1) / w.unit();
   if (g.gated) w.groups = (w.groups + 3) & ~3;                 // whole blocks of 128 hidden units
+  // (a launch of the smallest tiles, a wave per 64 columns and 32 rows)
+  if ((int64_t)w.groups * ((g.max_rows + 31) / 32 + 1) * 64 > kMostThreads) return no(nullptr, VVS_ESIZE, "qlinear config: more outputs than a launch holds");
   if ((int64_t)w.groups * w.blocks >= (1 << 24)) return no(nullptr, VVS_ESIZE, "qlinear config: more weights than a launch holds");
   l->weight_bytes = align_up((size_t)w.groups * w.blocks * 8192, 256) + align_up((size_t)w.groups * ((w.blocks + 3) / 4) * 256, 256);
-  l->ws_bytes = g.gated ? align_up((size_t)g.max_rows * w.groups * 32 * sizeof(float), 256) : 256;
+  // counters, then: activations of up to 32 rows; two partial sums of tiles of 32 rows
+  l->counter_bytes = align_up((size_t)w.groups * 4 * sizeof(uint32_t), 256);
+  l->ws_bytes = l->counter_bytes + align_up(g.gated ? (size_t)std::min(g.max_rows, 32) * w.groups * 32 * sizeof(float) : (size_t)2 * 32 * w.groups * 64 * sizeof(float), 256);
   return VVS_OK;
 }
 
@@ -202,7 +240,6 @@ vvs_status vvs_qlinear_create(const vvs_qlinear_config* cfg, void* d_weights, vo
   int ndev = 0;
   if (hipGetDeviceCount(&ndev) != hipSuccess || ndev < 1) return no(nullptr, VVS_EHIP, "qlinear create: no HIP device (this library has no CPU path)");
   hipError_t e = hipGetDevice(&plan.dev);
-  if (e == hipSuccess) e = hipDeviceGetAttribute(&plan.cus, hipDeviceAttributeMultiprocessorCount, plan.dev);
   if (e != hipSuccess) return no(nullptr, VVS_EHIP, hipGetErrorString(e));
   plan.ws = (char*)d_workspace;
   plan.w.data = (uint8_t*)d_weights;
@@ -260,8 +297,8 @@ vvs_status vvs_qlinear_apply(vvs_qlinear* ql, int32_t n_rows, const void* d_valu
   a.w = l->w; a.M = n_rows;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
   a.dtype = out_dtype; a.y = d_out; a.stride = (size_t)os; a.wide = wide_rows(d_out, os, out_dtype, 4);
-  a.cus = l->cus;
-  launch_qlinear_product(a, (hipStream_t)s);
+  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + l->counter_bytes);
+  launch_qlinear_product(a, plan_qlinear_product(l->w, n_rows), (hipStream_t)s);
   return launched(l, "qlinear apply");
 }
 
@@ -278,10 +315,9 @@ vvs_status vvs_qlinear_gate(vvs_qlinear* ql, int32_t n_rows, const void* d_value
   QProduct a{};
   a.w = l->w; a.M = n_rows;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
-  a.act = (float*)l->ws;
+  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + l->counter_bytes);
   a.y8 = QRowsOut{(uint8_t*)d_out_values, (uint8_t*)d_out_powers};
-  a.cus = l->cus;
-  launch_qlinear_product(a, (hipStream_t)s);
+  launch_qlinear_product(a, plan_qlinear_product(l->w, n_rows), (hipStream_t)s);
   return launched(l, "qlinear gate");
 }
 

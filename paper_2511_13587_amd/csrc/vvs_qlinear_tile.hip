@@ -1,0 +1,263 @@
+// Products of many rows in 8 bits: tiles whose rows pass through LDS.
+#include <algorithm>
+#include <type_traits>
+
+#include "vvs_e4m3.h"
+#include "vvs_qlinear_device.h"
+
+namespace vvs {
+
+// Order of the tiles.  Workgroups are dealt to the 8 XCDs round-robin; each takes a run of consecutive tiles of an order that goes through bands of 8 row tiles column by column, so that what an
+// XCD's 32 CUs work on at a time - 8 row tiles times 4 column tiles - shares its rows and weights in the XCD's L2.
+__device__ __forceinline__ void qtile_of(int id, int MT, int NT, int* tile_m, int* tile_n) {
+  const int all = MT * NT, x = id & 7, q = all >> 3, p = x * q + min(x, all & 7) + (id >> 3);
+  const int band = p / (8 * NT), rem = p % (8 * NT), h = min(8, MT - 8 * band);
+  *tile_n = rem / h;
+  *tile_m = band * 8 + rem % h;
+}
+
+// A workgroup of WM x WN waves makes 16 RT WM rows by WN groups of 64 columns; a wave 16 RT rows of one group, whose weights come straight into its operand registers, one block of 128 contraction
+// values ahead.  The rows' bytes of a block pass through LDS, two stages: while one is multiplied the next is on its way (lds_dma16).  16 bytes c of row r lie at place c ^ (r & 7) of the row,
+// so that the 8 lanes that LDS serves at a time read 8 different places.
+// FAST: the e4m3 numbers go into the matrix cores as they are, with both powers of two as scales (16x16x128, twice the rate of bf16 and fewer instructions).  These products lose what lies 2^13
+// below the largest of a few neighbours: 1.3e-5 in the 2-norm, 200 times below the rounding of bf16 outputs and 3000 times below that of 8 bits.  Outputs in fp32 take !FAST: bf16 operands.
+constexpr int kPowerBlocks = 64, kPowerStride = kPowerBlocks / 4 + 1;   // (an odd number of words: 16 rows on 16 banks)
+
+// Place of 16 bytes c of row r in LDS: c ^ swizzle(r).  LDS serves a wave's 16-byte reads 16 lanes at a time - lanes 0-3, 12-15, 20-23, 24-27; 4-7, 8-11, 16-19, 28-31; and the same 32 on - from 64
+// banks, two rows of 128 bytes: rows 4 to 11 of a tile go by with the other half of the contraction than the rest.  (r & 7: two lanes on every bank, by SQ_LDS_BANK_CONFLICT; so none.)
+__device__ __forceinline__ int swizzle(int r) { return ((r >> 1) & 7) ^ (((r + 4) >> 3 & 1) << 1); }
+
+template <int WM, int WN, int RT, bool FAST, bool GATED, typename T, int NB>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(QProduct a, int MT, int NT) {
+  constexpr int BM = 16 * RT * WM, NW = WM * WN, NQ = BM / 8 / NW, kStages = NB == 2 ? 3 : NB;
+  static_assert(BM <= 64 * NW && BM % (8 * NW) == 0 && (!GATED || WN == 4), "");
+  extern __shared__ uint4 lds[];                     // rows [kStages][BM][128 bytes], then powers of kPowerBlocks blocks: [BM][17], [64 WN][17], four in a word
+  int* const xpow = (int*)((char*)lds + kStages * BM * kQRowBlock);
+  int* const wpow = xpow + BM * kPowerStride;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+  const int wm = wave / WN, wn = wave % WN;
+  int tile_m, tile_n;
+  qtile_of(blockIdx.x, MT, NT, &tile_m, &tile_n);
+  const int m0 = tile_m * BM, blocks = a.w.blocks, powers = qrows_powers(a.w.in);
+  const int own_group = tile_n * WN + wn, group = min(own_group, a.w.groups - 1);
+  const size_t width = (size_t)blocks * kQRowBlock;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+
+  // rows behind the last one repeat it
+  const uint8_t* const tile_rows = a.x.values + (size_t)m0 * width;
+  uint32_t src[NQ];
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    const int r = (wave * NQ + q) * 8 + (lane >> 3);
+    src[q] = (uint32_t)(min(r, a.M - 1 - m0) * (int)width + ((lane & 7) ^ swizzle(r)) * 16);
+  }
+  auto request = [&](int kb, int stage, int q) { lds_dma16(tile_rows + (size_t)kb * kQRowBlock, src[q], lds0 + stage * BM * kQRowBlock + (wave * NQ + q) * 1024); };
+  const uint8_t* const wsrc = a.w.data + a.w.tile_at(group, 0, 0);
+  auto weights = [&](int kb, u32x4 (&w)[4][2], int c, int h) { w[c][h] = *(const u32x4*)(wsrc + (size_t)kb * 8192 + c * 2048 + h * 1024 + lane * 16); };
+  // powers of blocks k0 .. k0 + kPowerBlocks - 1 into LDS: bytes from memory at every block were a tenth of the time of a large product (384 us without, 353 us)
+  auto fetch_powers = [&](int k0) {
+    const int words = min(kPowerBlocks, powers - k0) / 4;
+    for (int u = tid; u < BM * words; u += 64 * NW) {
+      const int r = u / words, d = u % words;
+      xpow[r * kPowerStride + d] = *(const int*)(a.x.powers + (size_t)min(m0 + r, a.M - 1) * powers + k0 + d * 4);
+    }
+    const int* p = (const int*)(a.w.powers + a.w.power_at(group, k0, 0));
+    for (int d = 0; d < words; ++d) wpow[(wn * 64 + lane) * kPowerStride + d] = p[d * 64 + lane];
+  };
+
+  floatx4 acc[4][RT];
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[c][r] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  u32x4 w[NB][4][2];
+  int ws[4];
+  // ahead: blocks 0 and 1 of the rows, 0 of the weights; NB = 4: 0 to 2 of both
+#pragma unroll
+  for (int k = 0; k < (NB == 2 ? 2 : 3); ++k) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) request(min(k, blocks - 1), k, q);
+    if (k == 0 || NB == 4) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) weights(min(k, blocks - 1), w[k], c >> 1, c & 1);
+    }
+  }
+  fetch_powers(0);
+
+  const char* const mine = (const char*)lds + (wm * RT * 16 + i) * kQRowBlock;
+  const int* const mine_xpow = xpow + (wm * RT * 16 + i) * kPowerStride;
+  const int* const mine_wpow = wpow + (wn * 64 + i) * kPowerStride;
+  const int sw = swizzle(i);
+  int st_next = 0;                                   // stage of the next step
+  auto step = [&](auto uc, int k4) {                 // block k4 + U, k4 a multiple of 4
+    constexpr int U = decltype(uc)::value, B = U & (NB - 1);
+    const int st = NB == 2 ? st_next : U;
+    const int kb = k4 + U, pw = (k4 & (kPowerBlocks - 1)) >> 2;
+    // this block's rows and weights have landed - what may be under way is the next block's rows - and the stage before is free
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NB == 2 ? NQ : 2 * (NQ + 8)) : "memory");
+#pragma unroll
+    for (int c = 0; c < 4; ++c) asm volatile("" : "+v"(w[B][c][0]), "+v"(w[B][c][1]));
+    const int wnext = min(kb + NB - 1, blocks - 1), xnext = min(kb + (NB == 2 ? 2 : 3), blocks - 1);        // (the last block is requested again)
+    const int free = NB == 2 ? (st == 0 ? 2 : st - 1) : (U + 3) & 3;
+    constexpr int BF = (B + NB - 1) & (NB - 1);
+    if constexpr (U == 0) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) ws[c] = mine_wpow[c * 16 * kPowerStride + pw];
+    }
+    const char* const stage = mine + st * BM * kQRowBlock;
+    // requests go out between the products; what the next step waits for first: NB = 2, its weights
+    auto later = [&](int r) {
+      constexpr int H = RT / 2, PW = (8 + H - 1) / H, PQ = (NQ + H - 1) / H;
+      const int h = r < H ? r : r - H;
+      if ((r < H) == (NB == 2)) {
+#pragma unroll
+        for (int p = h * PW; p < min((h + 1) * PW, 8); ++p) weights(wnext, w[BF], p >> 1, p & 1);
+      } else {
+#pragma unroll
+        for (int q = h * PQ; q < min((h + 1) * PQ, NQ); ++q) request(xnext, free, q);
+      }
+    };
+    if constexpr (FAST) {
+      // row tile r + 1 is read from LDS while r is multiplied, and no further ones: left to itself the compiler reads them all first and spills
+      constexpr int NX = RT > 8 ? 3 : 2;
+      struct Rows { u32x4 h[2]; } x[NX];
+      int xs[NX];
+      auto rows = [&](int r) {
+        x[r % NX].h[0] = *(const u32x4*)(stage + r * 16 * kQRowBlock + ((2 * g) ^ sw) * 16);
+        x[r % NX].h[1] = *(const u32x4*)(stage + r * 16 * kQRowBlock + ((2 * g + 1) ^ sw) * 16);
+        xs[r % NX] = mine_xpow[r * 16 * kPowerStride + pw];
+      };
+#pragma unroll
+      for (int r = 0; r < NX - 1; ++r) rows(r);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        if (r + NX - 1 < RT) rows(r + NX - 1);
+        later(r);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          acc[c][r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(intx8, w[B][c]), __builtin_bit_cast(intx8, x[r % NX]), acc[c][r], 0, 0, U, ws[c], U, xs[r % NX]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      float wsc[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) wsc[c] = __uint_as_float(((uint32_t)ws[c] >> (8 * U) & 0xFF) << 23);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x8 wj[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) wj[c] = e4m3_to_bf16(make_uint2(w[B][c][j >> 1][2 * (j & 1)], w[B][c][j >> 1][2 * (j & 1) + 1]), wsc[c]);
+        uint2 x[2];
+        int xs[2];
+        auto rows = [&](int r) {
+          x[r & 1] = *(const uint2*)(stage + r * 16 * kQRowBlock + ((2 * g + (j >> 1)) ^ sw) * 16 + (j & 1) * 8);
+          xs[r & 1] = mine_xpow[r * 16 * kPowerStride + pw];
+        };
+        rows(0);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          if (r + 1 < RT) rows(r + 1);
+          if (j == 0) later(r);
+          const bf16x8 xj = e4m3_to_bf16(x[r & 1], __uint_as_float(((uint32_t)xs[r & 1] >> (8 * U) & 0xFF) << 23));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wj[c], xj, acc[c][r], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    if (NB == 2) st_next = st == 2 ? 0 : st + 1;
+  };
+  for (int k4 = 0; k4 < blocks; k4 += 4) {
+    if (k4 && (k4 & (kPowerBlocks - 1)) == 0) {
+      asm volatile("s_barrier" ::: "memory");       // all have read the last ones: their products were waited for
+      fetch_powers(k4);
+    }
+    step(std::integral_constant<int, 0>{}, k4);
+    if (k4 + 1 < blocks) step(std::integral_constant<int, 1>{}, k4);
+    if (k4 + 2 < blocks) step(std::integral_constant<int, 2>{}, k4);
+    if (k4 + 3 < blocks) step(std::integral_constant<int, 3>{}, k4);
+  }
+  // no request may be under way when LDS is used again or given back
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+  if constexpr (GATED) {
+    // a wave's 32 hidden units, 8 in a row per lane; the largest of a block of 128 is that of four waves
+    float* const top = (float*)lds;                  // [4][BM]
+    float v[RT][8];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      float t = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[r][j] = silu(acc[2 * (j >> 2)][r][j & 3]) * acc[2 * (j >> 2) + 1][r][j & 3];
+        t = fmaxf(t, finite(v[r][j]) ? fabsf(v[r][j]) : 0.f);
+      }
+      t = rows_max(t);
+      if (g == 0) top[wn * BM + (wm * RT + r) * 16 + i] = t;
+    }
+    __syncthreads();
+    const int out_blocks = qrows_blocks(a.w.out), out_powers = qrows_powers(a.w.out);
+    if (tile_n < out_blocks) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const int lm = (wm * RT + r) * 16 + i, m = m0 + lm;
+        const int e = e4m3_exponent(fmaxf(fmaxf(top[lm], top[BM + lm]), fmaxf(top[2 * BM + lm], top[3 * BM + lm])));
+        const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[r][j] *= inv;
+        if (m < a.M) {
+          *(uint2*)(a.y8.values + ((size_t)m * out_blocks + tile_n) * kQRowBlock + wn * 32 + g * 8) = to_e4m3x8(v[r]);
+          if (lane < 16 && wn == 0) {
+            uint8_t* p = a.y8.powers + (size_t)m * out_powers;
+            p[tile_n] = (uint8_t)(e + 127);
+            if (tile_n == out_blocks - 1)
+              for (int b = out_blocks; b < out_powers; ++b) p[b] = 0;
+          }
+        }
+      }
+    }
+  } else {
+    const int col0 = a.w.column(own_group, 0, 4 * g), left = a.w.out - col0;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int m = m0 + (wm * RT + r) * 16 + i;
+      if (m >= a.M || own_group >= a.w.groups) continue;
+      T* y = (T*)a.y + (size_t)m * a.stride + col0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float v[4] = {acc[c][r][0], acc[c][r][1], acc[c][r][2], acc[c][r][3]};
+        store4(y + 4 * c, left - 4 * c, a.wide, v);
+      }
+    }
+  }
+}
+
+template <int WM, int WN, int RT, bool FAST, bool GATED, typename T, int NB>
+static void tile_t(const QProduct& a, hipStream_t s) {
+  constexpr int BM = 16 * RT * WM;
+  constexpr size_t lds = (NB == 2 ? 3 : NB) * BM * kQRowBlock + (BM + 64 * WN) * kPowerStride * 4;
+  const int MT = (a.M + BM - 1) / BM, NT = (a.w.groups + WN - 1) / WN;
+  auto kernel = k_qlinear_tile<WM, WN, RT, FAST, GATED, T, NB>;
+  if (lds > 65536) allow_dynamic_lds((const void*)kernel, lds);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((size_t)MT * NT)), dim3(64 * WM * WN), lds, s, a, MT, NT);
+}
+
+template <bool FAST, bool GATED, typename T>
+static void tile_by(const QProduct& a, QTile t, hipStream_t s) {
+  switch (t) {
+    case kTile128x256: tile_t<1, 4, 8, FAST, GATED, T, 2>(a, s); break;
+    case kTile64x256: tile_t<1, 4, 4, FAST, GATED, T, 4>(a, s); break;
+    case kTile64x128: if constexpr (!GATED) tile_t<1, 2, 4, FAST, GATED, T, 4>(a, s); break;
+    default: if constexpr (!GATED) tile_t<1, 2, 2, FAST, GATED, T, 4>(a, s);
+  }
+}
+
+void launch_qlinear_tile(const QProduct& a, QTile t, hipStream_t s) {
+  if (a.w.gated && t == kTile32x256) tile_t<1, 4, 2, false, true, float, 4>(a, s);
+  else if (a.w.gated) tile_by<true, true, float>(a, t, s);
+  else if (a.dtype == VVS_BF16) tile_by<true, false, bf16_t>(a, t, s);
+  else tile_by<false, false, float>(a, t, s);
+}
+
+}  // namespace vvs
