@@ -683,13 +683,13 @@ class QRows:
 def _matrix(t: torch.Tensor, rows: int, width: int, device: int, what: str):
     """(pointer, elements from row to row, vvs dtype) of a tensor [..., width] of `rows` rows that may be a part of a wider one."""
     dtype, shape = _VVS_DTYPE.get(t.dtype), t.shape
-    if t.get_device() != device or dtype is None or not shape or shape[-1] != width or t.numel() != rows * width:
+    if t.get_device() != device or dtype is None or (shape != (rows, width) and (not shape or shape[-1] != width or t.numel() != rows * width)):
         raise ValueError(f"{what}: wants float32 or bfloat16 [..., {width}], {rows} rows, on device {device}; got {t.dtype} {list(shape)} on device {t.get_device()}")
     if t.is_contiguous():
         return t.data_ptr(), width, dtype
-    strides = t.stride()
+    dims, strides = len(shape), t.stride()
     row, n, ok = None, 1, strides[-1] == 1 or width == 1
-    for d in range(len(shape) - 2, -1, -1):                 # n: rows below each dimension
+    for d in range(dims - 2, -1, -1):                       # n: rows below each dimension
         if shape[d] > 1:
             if row is None:
                 row = strides[d] // n
@@ -701,31 +701,22 @@ def _matrix(t: torch.Tensor, rows: int, width: int, device: int, what: str):
     return t.data_ptr(), row, dtype
 
 
-def _span(p: int, rows: int, stride: int, width: int, size: int):
-    """Bytes that `rows` rows take."""
-    return p, p + ((rows - 1) * stride + width) * size
+_current_device = torch._C._cuda_getDevice               # (as for _raw_stream: the function around it is 0.3 us)
 
 
-def _held(rows: QRows):
-    v, p = rows.pointers
-    n = rows.n_rows
-    return (v, v + n * rows.values.shape[1]), (p, p + n * rows.powers.shape[1])
-
-
-def _no_overlap(outs, ins):
-    for a, b in outs:
-        for c, d in ins:
-            if a < d and c < b:
-                raise ValueError("an output shares memory with an input or another output")
+def _on_device(device: int, fn, *args):
+    """fn(*args, current stream of the device) with the device current."""
+    if _current_device() == device:
+        return fn(*args, _raw_stream(device))
+    with _Current(device):
+        return fn(*args, _raw_stream(device))
 
 
 def vvs_qrows_round(x: torch.Tensor, rows: QRows):
     """x [..., width] float32 or bfloat16, as many rows as `rows` holds."""
     n, w, dev = rows.n_rows, rows.width, rows.index
     xp, xs, xt = _matrix(x, n, w, dev, "x")
-    _no_overlap(_held(rows), (_span(xp, n, xs, w, x.dtype.itemsize),))
-    with _Current(dev):
-        _rows_check(lib.vvs_qrows_round(n, w, xt, xp, xs, *rows.pointers, _raw_stream(dev)))
+    _rows_check(_on_device(dev, lib.vvs_qrows_round, n, w, xt, xp, xs, *rows.pointers))
 
 
 def vvs_qrows_norm(x: torch.Tensor, gain: torch.Tensor, eps: float, rows: QRows, delta: Optional[torch.Tensor] = None, x_out: Optional[torch.Tensor] = None):
@@ -733,34 +724,18 @@ def vvs_qrows_norm(x: torch.Tensor, gain: torch.Tensor, eps: float, rows: QRows,
     n, w, dev = rows.n_rows, rows.width, rows.index
     xp, xs, xt = _matrix(x, n, w, dev, "x")
     gp, _, gt = _matrix(gain, 1, w, dev, "gain")
-    ins = [_span(xp, n, xs, w, x.dtype.itemsize), _span(gp, 1, w, w, gain.dtype.itemsize)]
-    outs = list(_held(rows))
     dp, ds, dt = (None, 0, 0) if delta is None else _matrix(delta, n, w, dev, "delta")
-    if delta is not None:
-        ins.append(_span(dp, n, ds, w, delta.dtype.itemsize))
-    op, os_ = None, 0
-    if x_out is not None:
-        op, os_, ot = _matrix(x_out, n, w, dev, "x_out")
-        if ot != xt:
-            raise ValueError("x_out: wants the type of x")
-        span = _span(op, n, os_, w, x.dtype.itemsize)
-        if op == xp and os_ == xs:
-            _no_overlap((span,), ins[1:])
-        else:
-            _no_overlap((span,), ins)
-        _no_overlap(outs, (span,))
-    _no_overlap(outs, ins)
-    with _Current(dev):
-        _rows_check(lib.vvs_qrows_norm(n, w, xt, xp, xs, dt, dp, ds, op, os_, gt, gp, eps, *rows.pointers, _raw_stream(dev)))
+    op, os_, ot = (None, 0, xt) if x_out is None else _matrix(x_out, n, w, dev, "x_out")
+    if ot != xt:
+        raise ValueError("x_out: wants the type of x")
+    _rows_check(_on_device(dev, lib.vvs_qrows_norm, n, w, xt, xp, xs, dt, dp, ds, op, os_, gt, gp, eps, *rows.pointers))
 
 
 def vvs_qrows_read(rows: QRows, out: torch.Tensor):
     """out [..., width] float32 or bfloat16."""
     n, w, dev = rows.n_rows, rows.width, rows.index
     op, os_, ot = _matrix(out, n, w, dev, "out")
-    _no_overlap((_span(op, n, os_, w, out.dtype.itemsize),), _held(rows))
-    with _Current(dev):
-        _rows_check(lib.vvs_qrows_read(n, w, *rows.pointers, ot, op, os_, _raw_stream(dev)))
+    _rows_check(_on_device(dev, lib.vvs_qrows_read, n, w, *rows.pointers, ot, op, os_))
 
 
 def vvs_qlinear_query_sizes(cfg: VvsQLinearConfig):
@@ -836,9 +811,7 @@ class QLinear:
         n, (k, cols, gated) = rows.n_rows, self.sizes
         self._rows(rows, k, "rows")
         op, os_, ot = _matrix(out, n, cols, self.index, "out")
-        _no_overlap((_span(op, n, os_, cols, out.dtype.itemsize),), _held(rows))
-        with _Current(self.index):
-            self._check(lib.vvs_qlinear_apply(self.h, n, *rows.pointers, ot, op, os_, _raw_stream(self.index)))
+        self._check(_on_device(self.index, lib.vvs_qlinear_apply, self.h, n, *rows.pointers, ot, op, os_))
 
     def vvs_qlinear_gate(self, rows: QRows, out: QRows):
         """out: rows of `out` elements, as many as `rows` holds."""
@@ -846,6 +819,4 @@ class QLinear:
         self._rows(out, self.sizes[1], "out")
         if out.n_rows != rows.n_rows:
             raise ValueError(f"out: wants {rows.n_rows} rows, got {out.n_rows}")
-        _no_overlap(_held(out), _held(rows))
-        with _Current(self.index):
-            self._check(lib.vvs_qlinear_gate(self.h, rows.n_rows, *rows.pointers, *out.pointers, _raw_stream(self.index)))
+        self._check(_on_device(self.index, lib.vvs_qlinear_gate, self.h, rows.n_rows, *rows.pointers, *out.pointers))

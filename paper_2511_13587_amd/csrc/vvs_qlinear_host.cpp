@@ -55,6 +55,29 @@ static int wide_rows(const void* p, int64_t stride, int dtype, int by = 8) {
 static bool off_element(const void* p, int dtype) { return (uintptr_t)p % size_of(dtype) != 0; }
 static bool off16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
+// Rows of `width` bytes, `stride` bytes apart.  Two such tensors share memory unless one lies behind the other or, with the same stride, each row beside the other's
+struct Span { uintptr_t at; uint64_t width, stride; int64_t rows; };
+static Span span_of(const void* p, int64_t rows, int64_t width, int64_t stride, size_t size) { return Span{(uintptr_t)p, (uint64_t)width * size, (uint64_t)stride * size, rows}; }
+static bool share(const Span& a, const Span& b) {
+  if (!a.at || !b.at) return false;
+  if (a.at + (uint64_t)(a.rows - 1) * a.stride + a.width <= b.at || b.at + (uint64_t)(b.rows - 1) * b.stride + b.width <= a.at) return false;
+  if (a.stride != b.stride) return true;
+  const uint64_t d = b.at >= a.at ? (b.at - a.at) % a.stride : (a.stride - (a.at - b.at) % a.stride) % a.stride;
+  return d < a.width || d + b.width > a.stride;
+}
+static Span values_span(const void* p, int64_t rows, int width) { const int64_t w = (int64_t)qrows_blocks(width) * kQRowBlock; return span_of(p, rows, w, w, 1); }
+static Span powers_span(const void* p, int64_t rows, int width) { const int64_t w = qrows_powers(width); return span_of(p, rows, w, w, 1); }
+template <size_t N, size_t K>
+static bool share_any(const Span (&outs)[N], const Span (&ins)[K]) {
+  for (size_t i = 0; i < N; ++i) {
+    for (size_t j = i + 1; j < N; ++j)
+      if (share(outs[i], outs[j])) return true;
+    for (const Span& b : ins)
+      if (share(outs[i], b)) return true;
+  }
+  return false;
+}
+
 constexpr int kWidest = 65536;                                 // of a row that a workgroup keeps in registers
 constexpr int64_t kMostThreads = ((int64_t)1 << 32) - 1024;    // of a launch along a dimension
 
@@ -172,6 +195,8 @@ vvs_status vvs_qrows_round(int32_t n_rows, int32_t width, int32_t dtype, const v
   if (!known(dtype)) return rows_no(VVS_EINVAL, "qrows round: unknown dtype");
   const int64_t xs = stride_of(x_stride, width);
   if (xs < 0 || off_element(d_x, dtype)) return rows_no(VVS_EINVAL, "qrows round: the stride has to cover a row, the pointer to be aligned to an element");
+  const Span outs[] = {values_span(d_values, n_rows, width), powers_span(d_powers, n_rows, width)}, ins[] = {span_of(d_x, n_rows, width, xs, size_of(dtype))};
+  if (share_any(outs, ins)) return rows_no(VVS_EINVAL, "qrows round: an output shares memory with the input or with the other");
   QRound a{};
   a.M = n_rows; a.width = width; a.dtype = dtype;
   a.x = d_x; a.stride = (size_t)xs; a.wide = wide_rows(d_x, xs, dtype);
@@ -193,6 +218,11 @@ vvs_status vvs_qrows_norm(int32_t n_rows, int32_t width, int32_t x_dtype, const 
       (d_delta && off_element(d_delta, delta_dtype)))
     return rows_no(VVS_EINVAL, "qrows norm: strides have to cover a row, pointers to be aligned to an element");
   if (d_x == d_x_out && xs != os) return rows_no(VVS_EINVAL, "qrows norm: in place, both strides are the same");
+  Span x = span_of(d_x, n_rows, width, xs, size_of(x_dtype));
+  const Span out = span_of(d_x_out, n_rows, width, os, size_of(x_dtype)), outs[] = {values_span(d_values, n_rows, width), powers_span(d_powers, n_rows, width), out};
+  if (d_x == d_x_out) x.at = 0;                                // (in place; as an output it is compared with the others)
+  const Span ins[] = {x, span_of(d_delta, n_rows, width, ds, d_delta ? size_of(delta_dtype) : 4), span_of(d_gain, 1, width, width, size_of(gain_dtype))};
+  if (share_any(outs, ins)) return rows_no(VVS_EINVAL, "qrows norm: an output shares memory with an input or with another output");
   QNorm a{};
   a.M = n_rows; a.width = width;
   a.x = d_x; a.x_dtype = x_dtype; a.x_stride = (size_t)xs; a.x_wide = wide_rows(d_x, xs, x_dtype);
@@ -212,6 +242,8 @@ vvs_status vvs_qrows_read(int32_t n_rows, int32_t width, const void* d_values, c
   if (!known(dtype)) return rows_no(VVS_EINVAL, "qrows read: unknown dtype");
   const int64_t os = stride_of(out_stride, width);
   if (os < 0 || off_element(d_out, dtype)) return rows_no(VVS_EINVAL, "qrows read: the stride has to cover a row, the pointer to be aligned to an element");
+  const Span outs[] = {span_of(d_out, n_rows, width, os, size_of(dtype))}, ins[] = {values_span(d_values, n_rows, width), powers_span(d_powers, n_rows, width)};
+  if (share_any(outs, ins)) return rows_no(VVS_EINVAL, "qrows read: the output shares memory with the rows");
   QRowsRead a{};
   a.M = n_rows; a.width = width; a.dtype = dtype;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
@@ -292,6 +324,8 @@ vvs_status vvs_qlinear_apply(vvs_qlinear* ql, int32_t n_rows, const void* d_valu
   if (!known(out_dtype)) return no(l, VVS_EINVAL, "qlinear apply: unknown dtype");
   const int64_t os = stride_of(out_stride, l->cfg.out);
   if (os < 0 || off_element(d_out, out_dtype)) return no(l, VVS_EINVAL, "qlinear apply: the stride has to cover a row, the pointer to be aligned to an element");
+  const Span outs[] = {span_of(d_out, n_rows, l->cfg.out, os, size_of(out_dtype))}, ins[] = {values_span(d_values, n_rows, l->cfg.in), powers_span(d_powers, n_rows, l->cfg.in)};
+  if (share_any(outs, ins)) return no(l, VVS_EINVAL, "qlinear apply: the output shares memory with the rows");
   if ((st = check_device(l)) != VVS_OK) return st;
   QProduct a{};
   a.w = l->w; a.M = n_rows;
@@ -311,6 +345,8 @@ vvs_status vvs_qlinear_gate(vvs_qlinear* ql, int32_t n_rows, const void* d_value
   if (!d_out_values || !d_out_powers) return no(l, VVS_EINVAL, "qlinear gate: NULL argument");
   if (off16(d_out_values) || off16(d_out_powers)) return no(l, VVS_EINVAL, "qlinear gate: values and powers must be 16-byte aligned");
   if ((int64_t)n_rows * 16 * qrows_powers(l->cfg.out) > kMostThreads) return no(l, VVS_ESIZE, "qlinear gate: more rows than a launch holds");
+  const Span outs[] = {values_span(d_out_values, n_rows, l->cfg.out), powers_span(d_out_powers, n_rows, l->cfg.out)}, ins[] = {values_span(d_values, n_rows, l->cfg.in), powers_span(d_powers, n_rows, l->cfg.in)};
+  if (share_any(outs, ins)) return no(l, VVS_EINVAL, "qlinear gate: an output shares memory with the rows or with the other");
   if ((st = check_device(l)) != VVS_OK) return st;
   QProduct a{};
   a.w = l->w; a.M = n_rows;

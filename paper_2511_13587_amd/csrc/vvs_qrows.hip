@@ -70,26 +70,33 @@ __device__ __forceinline__ void read_any8(const void* row, int dtype, int at, in
   else read_row8((const float*)row, at, n, wide, v);
 }
 
-// One workgroup of TH threads per row, which stays in registers: V times 8 elements per thread.  x + delta is rounded to the residual's type, and what is normalised is what is kept.
-template <int TH, int V>
-__global__ __launch_bounds__(TH) void k_qrows_norm(QNorm a) {
+// One workgroup per row, which stays in registers: V times 8 elements per thread.  x + delta is rounded to the residual's type, and what is normalised is what is kept.
+template <int V, int MOST>
+__global__ __launch_bounds__(MOST) void k_qrows_norm(QNorm a) {
   __shared__ float red[16];
   const int m = blockIdx.x, blocks = qrows_blocks(a.width), powers = qrows_powers(a.width);
   const size_t esz = a.x_dtype == VVS_BF16 ? 2 : 4, dsz = a.delta_dtype == VVS_BF16 ? 2 : 4;
   float v[V][8];
 #pragma unroll
-  for (int j = 0; j < V; ++j) read_any8((const char*)a.x + (size_t)m * a.x_stride * esz, a.x_dtype, (j * TH + threadIdx.x) * 8, a.width, a.x_wide, v[j]);
+  for (int j = 0; j < V; ++j) read_any8((const char*)a.x + (size_t)m * a.x_stride * esz, a.x_dtype, (j * blockDim.x + threadIdx.x) * 8, a.width, a.x_wide, v[j]);
   if (a.delta) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       float d[8];
-      read_any8((const char*)a.delta + (size_t)m * a.delta_stride * dsz, a.delta_dtype, (j * TH + threadIdx.x) * 8, a.width, a.delta_wide, d);
+      read_any8((const char*)a.delta + (size_t)m * a.delta_stride * dsz, a.delta_dtype, (j * blockDim.x + threadIdx.x) * 8, a.width, a.delta_wide, d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         v[j][i] += d[i];
         if (a.x_dtype == VVS_BF16) v[j][i] = bf2f(f2bf(v[j][i]));
       }
     }
+  }
+  // the gain is on its way while the sum is taken (but for the widest rows, which fill the registers)
+  constexpr bool kAhead = V <= 4;
+  float g[kAhead ? V : 1][8];
+  if constexpr (kAhead) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) read_any8(a.gain, a.gain_dtype, (j * blockDim.x + threadIdx.x) * 8, a.width, a.gain_wide, g[j]);
   }
   float ss = 0.f;
 #pragma unroll
@@ -100,34 +107,35 @@ __global__ __launch_bounds__(TH) void k_qrows_norm(QNorm a) {
   if (a.x_out) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int at = (j * TH + threadIdx.x) * 8;
+      const int at = (j * blockDim.x + threadIdx.x) * 8;
       if (a.x_dtype == VVS_BF16) write_row8((bf16_t*)a.x_out + (size_t)m * a.x_out_stride, at, a.width, a.x_out_wide, v[j]);
       else write_row8((float*)a.x_out + (size_t)m * a.x_out_stride, at, a.width, a.x_out_wide, v[j]);
     }
   }
-  ss = TH == 64 ? wave_sum(ss) : block_sum(ss, red);
+  ss = blockDim.x == 64 ? wave_sum(ss) : block_sum(ss, red);
   const float r = 1.f / sqrtf(ss / (float)a.width + a.eps);
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int at = (j * TH + threadIdx.x) * 8, b = at / kQRowBlock;
+    const int at = (j * blockDim.x + threadIdx.x) * 8, b = at / kQRowBlock;
     if (b >= powers) break;
-    float g[8], y[8];
-    read_any8(a.gain, a.gain_dtype, at, a.width, a.gain_wide, g);
+    if constexpr (!kAhead) read_any8(a.gain, a.gain_dtype, at, a.width, a.gain_wide, g[0]);
+    float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = at + i < a.width ? v[j][i] * r * g[i] : 0.f;
+    for (int i = 0; i < 8; ++i) y[i] = at + i < a.width ? v[j][i] * r * g[kAhead ? j : 0][i] : 0.f;
     round_block(y, a.y.values + (size_t)m * blocks * kQRowBlock + at, a.y.powers + (size_t)m * powers + b, b < blocks, (threadIdx.x & 15) == 0);
   }
 }
 
 void launch_qrows_norm(const QNorm& a, hipStream_t s) {
-  const dim3 grid(a.M);
-  const int w = a.width;
-  if (w <= 512) hipLaunchKernelGGL((k_qrows_norm<64, 1>), grid, dim3(64), 0, s, a);
-  else if (w <= 2048) hipLaunchKernelGGL((k_qrows_norm<256, 1>), grid, dim3(256), 0, s, a);
-  else if (w <= 4096) hipLaunchKernelGGL((k_qrows_norm<256, 2>), grid, dim3(256), 0, s, a);
-  else if (w <= 8192) hipLaunchKernelGGL((k_qrows_norm<256, 4>), grid, dim3(256), 0, s, a);
-  else if (w <= 16384) hipLaunchKernelGGL((k_qrows_norm<1024, 2>), grid, dim3(1024), 0, s, a);
-  else hipLaunchKernelGGL((k_qrows_norm<1024, 8>), grid, dim3(1024), 0, s, a);
+  // 8 elements per thread as long as the row fits (4096 wide: 28 rows 3.5 us, 432 rows 6.8, 8192 rows in bf16 49.0; 16 elements per thread 4.2, 7.5, 50.6; a wave per row 8.0, 11.3, 64.3).  Powers are in
+  // fours, so that whole waves cover them.
+  const int units = qrows_powers(a.width) * 16;
+  auto go = [&](auto kernel, int v) { hipLaunchKernelGGL(kernel, dim3(a.M), dim3(((units + v - 1) / v + 63) & ~63), 0, s, a); };
+  if (units <= 512) go(k_qrows_norm<1, 512>, 1);
+  else if (units <= 1024) go(k_qrows_norm<1, 1024>, 1);
+  else if (units <= 2048) go(k_qrows_norm<2, 1024>, 2);   // (4096 rows of 11008 in bf16 79.9 us, 32 elements per thread 88.6)
+  else if (units <= 4096) go(k_qrows_norm<4, 1024>, 4);
+  else go(k_qrows_norm<8, 1024>, 8);
 }
 
 }  // namespace vvs
