@@ -103,9 +103,15 @@ typedef struct {
                                       a call are taken as they are (a verify call: of all its nodes; a prefill: of a chunk of up to 512 tokens, fp32
                                       64), and rounded when they are cached (see vvs_set_state for roll-backs).  Layers run as separate launches (no drafter contexts; head size 32,
                                       64 or 128, as the dtype allows), so that calls of few rows take longer than with VVS_CACHE_SAME */
+  int32_t weight_kind;           /* VVS_WEIGHTS_SAME: weights have the context's dtype;
+                                    VVS_WEIGHTS_E4M3: a layer's seven matrices are held in 8 bits, and what they are multiplied by - the norms' outputs, the
+                                      attention's (rounded to the dtype first), the activations - is rounded to 8 bits as well (see vvs_qrows below); products, residual stream
+                                      and all else are as ever.  For contexts whose steps are bound by the weights' bytes.  Embeddings, gains and the output head
+                                      keep the dtype.  Layers run as separate launches (no drafter contexts; d_model a multiple of 64, d_ff at most 65536) */
 } vvs_config;
 enum { VVS_NORM_AUTO = 0, VVS_NORM_SEPARATE = 1 };
 enum { VVS_CACHE_SAME = 0, VVS_CACHE_E4M3 = 1 };
+enum { VVS_WEIGHTS_SAME = 0, VVS_WEIGHTS_E4M3 = 1 };
 #define VVS_MAX_FEATURE_SLOTS 8
 
 /* Sizes in bytes of the three device buffers a context needs.  VVS_ESIZE if the shape is not

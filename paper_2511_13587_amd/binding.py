@@ -21,6 +21,7 @@ VVS_FP32, VVS_BF16 = 0, 1
 VVS_STRICT, VVS_RELAXED = 0, 1
 VVS_NORM_AUTO, VVS_NORM_SEPARATE = 0, 1
 VVS_CACHE_SAME, VVS_CACHE_E4M3 = 0, 1
+VVS_WEIGHTS_SAME, VVS_WEIGHTS_E4M3 = 0, 1
 VVS_MAX_T = 64
 VVS_QCACHE_BLOCK = 32
 VVS_QROWS_BLOCK = 128
@@ -37,7 +38,7 @@ class VvsConfig(C.Structure):
                [("cfg_scale", C.c_float), ("rms_eps", C.c_float), ("rope_base", C.c_float),
                 ("relax_k", C.c_int32), ("relax_delta", C.c_float),
                 ("feature_slots", C.c_int32), ("feature_pre_norm", C.c_int32), ("draft_input", C.c_int32),
-                ("norm_mode", C.c_int32), ("cache_kind", C.c_int32)]
+                ("norm_mode", C.c_int32), ("cache_kind", C.c_int32), ("weight_kind", C.c_int32)]
 
 
 class VvsQCacheConfig(C.Structure):
@@ -136,13 +137,13 @@ lib, EXPORTS = _load()
 
 
 def make_config(shape, max_nodes: Optional[int] = None, feature_slots: int = 5, feature_pre_norm: int = 0,
-                draft_input: int = 0, norm_mode: int = 0, cache_kind: int = 0) -> VvsConfig:
+                draft_input: int = 0, norm_mode: int = 0, cache_kind: int = 0, weight_kind: int = 0) -> VvsConfig:
     """vvs_config from a synth.Shape-like object."""
     return VvsConfig(shape.n_layers, shape.d_model, shape.n_heads, shape.d_ff, shape.vocab, shape.logit_lo,
                      shape.logit_hi, shape.grid_h, shape.grid_w, shape.prefix_len, shape.prefix_kind,
                      shape.n_classes, shape.n_prompts, shape.n_nodes if max_nodes is None else max_nodes,
                      shape.dtype, shape.cfg_scale, shape.rms_eps, shape.rope_base, shape.relax_k, shape.relax_delta,
-                     feature_slots, feature_pre_norm, draft_input, norm_mode, cache_kind)
+                     feature_slots, feature_pre_norm, draft_input, norm_mode, cache_kind, weight_kind)
 
 
 def vvs_query_sizes(cfg: VvsConfig):

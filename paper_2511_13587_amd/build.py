@@ -9,7 +9,7 @@ LIB = os.path.join(HERE, "libvvs.so")
 SOURCES = ["vvs_host.cpp", "vvs_kernels.hip", "vvs_accept.hip", "vvs_mfma.hip", "vvs_few.hip", "vvs_schedule.hip", "vvs_draft.hip",
            "vvs_qcache_host.cpp", "vvs_qcache.hip", "vvs_qcache_ctx.hip",
            "vvs_rope.hip", "vvs_qlinear_host.cpp", "vvs_qrows.hip", "vvs_qlinear.hip",
-           "vvs_qlinear_tile.hip"]
+           "vvs_qlinear_tile.hip", "vvs_qlinear_ctx.hip"]
 
 
 def build(verbose: bool = True) -> str:

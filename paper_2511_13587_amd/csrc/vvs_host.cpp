@@ -2,6 +2,7 @@
 // points.  Everything here runs before any launch, so bad input never reaches a kernel.
 #include "vvs_internal.h"
 #include "vvs_qcache.h"
+#include "vvs_qlinear.h"
 
 #include <math.h>
 #include <stdio.h>
@@ -180,7 +181,7 @@ GemmPlan plan_resid(const Ctx* c, int M) {
 // the layer is (measured without any kernel: 2 x the noise floor of a correct bf16 evaluation at d = 1280,
 // 3 x at d = 4096).
 bool plan_fused(const Ctx* c, int M) {
-  if (c->cfg.cache_kind) return false;      // the fused layer writes a cache of the context's dtype
+  if (c->cfg.cache_kind || c->cfg.weight_kind) return false;      // the fused layer writes a cache, and reads weights, of the context's dtype
   (void)M;
   if (c->cfg.dtype != VVS_BF16 || c->cfg.norm_mode == VVS_NORM_SEPARATE) return false;
   const size_t layer_weight_bytes = c->esz * ((size_t)4 * c->d * c->d + (size_t)3 * c->d * c->F);
@@ -223,7 +224,7 @@ int few_rows(const Ctx* c) {
 //     (13440) 356 / 398, 768 (6144) 570 / 543, (7680) 589 / 634, 896 (8960) 541 / 570, 1024 (8192) 1.14, (10240) 484 / 494, 1280 (10240) 1.02 (O and down share
 //     their operands through LDS where d is a multiple of 128)
 int few_wide_rows(const Ctx* c) {
-  if (plan_fused(c, c->R) || c->cfg.dtype != VVS_BF16 || c->cfg.draft_input || c->d > 4096 || c->cfg.cache_kind) return 0;
+  if (plan_fused(c, c->R) || c->cfg.dtype != VVS_BF16 || c->cfg.draft_input || c->d > 4096 || c->cfg.cache_kind || c->cfg.weight_kind) return 0;
   const size_t layer_weight_bytes = c->esz * ((size_t)4 * c->d * c->d + (size_t)3 * c->d * c->F);
   const int d = c->d, F = c->F;
   if (layer_weight_bytes > (size_t)440 << 20 || (d >= 3584 && F > 12288)) return 0;
@@ -266,6 +267,9 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   if (g.norm_mode != VVS_NORM_AUTO && g.norm_mode != VVS_NORM_SEPARATE) return fail(err, VVS_EINVAL, "config: unknown norm_mode");
   if (g.cache_kind != VVS_CACHE_SAME && g.cache_kind != VVS_CACHE_E4M3) return fail(err, VVS_EINVAL, "config: unknown cache_kind");
   if (g.cache_kind && g.draft_input) return fail(err, VVS_EINVAL, "config: a drafter context keeps no cache (cache_kind must be VVS_CACHE_SAME)");
+  if (g.weight_kind != VVS_WEIGHTS_SAME && g.weight_kind != VVS_WEIGHTS_E4M3) return fail(err, VVS_EINVAL, "config: unknown weight_kind");
+  if (g.weight_kind && g.draft_input) return fail(err, VVS_EINVAL, "config: a drafter context keeps its weights (weight_kind must be VVS_WEIGHTS_SAME)");
+  if (g.weight_kind && (g.d_model % 64 || g.d_ff > 65536)) return fail(err, VVS_ESIZE, "config: VVS_WEIGHTS_E4M3 needs d_model to be a multiple of 64, and d_ff of at most 65536");
   int dh = g.d_model / g.n_heads;
   if (g.cache_kind && dh != 32 && dh != 64 && dh != 128) return fail(err, VVS_ESIZE, "config: VVS_CACHE_E4M3 needs head size 32, 64 or 128");
   if (dh % 4) return fail(err, VVS_ESIZE, "config: head size must be a multiple of 4 (2D rotary pairs)");
@@ -334,6 +338,7 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
     sums(d, F);                              // down
     if (g.draft_input) sums(d, 2 * d);       // a drafter's input map
   }
+  if (g.weight_kind) go = std::max(go, (size_t)c->Mmax * 3 * d);           // whole products
   // workspace carve-up
   Workspace& w = c->w;
   size_t off = 0;
@@ -350,6 +355,12 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   const int wide = few_wide_rows(c), few = std::max(few_rows(c), wide);
   go = std::max(go, (size_t)kFewWideShares * wide * d);
   w.few_sync = take(few ? sizeof(uint32_t) * kFewLine * (kFewHead + (size_t)few_layer_counters(c->H, few / 32) * c->L + 8) : 0);   // zeroed with the state
+  size_t map_counters = 0, map_parts = 0;
+  for (QMap m : {kMapQkv, kMapO, kMapGate, kMapDown}) {
+    map_counters = std::max(map_counters, qlinear_counter_bytes(context_map(c, m)));
+    map_parts = std::max(map_parts, qlinear_part_bytes(context_map(c, m)));
+  }
+  w.map_counters = take(g.weight_kind ? map_counters : 0);      // zeroed with the state
   w.x = take(sizeof(float) * (size_t)c->Mmax * d);
   w.h = take(c->esz * (size_t)c->Mmax * d);
   // (a call whose layers are one launch has no partial sums: what its phases hand on lies in their place)
@@ -375,6 +386,13 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   w.q_norm = take(sizeof(float) * heads * widest);
   w.q_origin = take(sizeof(int32_t) * heads * c->S_cap * c->L);
   w.q_scores = take(sizeof(float) * heads * qcache_score_steps(c->S_cap / kQBlock, widest) * kQKept * kQBlock);
+  // weights in 8 bits: rows in 8 bits of the residual's width and of the hidden units, workspace of the maps
+  const size_t rows8 = g.weight_kind ? c->Mmax : 0;
+  w.h8 = take(rows8 * qrows_blocks(d) * kQRowBlock);
+  w.h8_powers = take(rows8 * qrows_powers(d));
+  w.act8 = take(rows8 * qrows_blocks(F) * kQRowBlock);
+  w.act8_powers = take(rows8 * qrows_powers(F));
+  w.map_parts = take(g.weight_kind ? map_parts : 0);
   w.total = off;
   // packed weights
   PackedLayout& p = c->p;
@@ -387,11 +405,12 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   p.layer0 = off;
   size_t base = off;
   p.g1 = take(sizeof(float) * d) - base;
-  p.wqkv = take(e * (size_t)3 * d * d) - base;
-  p.wo = take(e * (size_t)d * d) - base;
+  auto map = [&](QMap m, size_t same) { const QWeights q = context_map(c, m); return take(g.weight_kind ? qweights_bytes(q.groups, q.blocks) : same); };
+  p.wqkv = map(kMapQkv, e * (size_t)3 * d * d) - base;
+  p.wo = map(kMapO, e * (size_t)d * d) - base;
   p.g2 = take(sizeof(float) * d) - base;
-  p.wgu = take(e * (size_t)2 * F * d) - base;
-  p.wd = take(e * (size_t)d * F) - base;
+  p.wgu = map(kMapGate, e * (size_t)2 * F * d) - base;
+  p.wd = map(kMapDown, e * (size_t)d * F) - base;
   p.layer_stride = off - base;
   off = p.layer0 + p.layer_stride * c->L;
   p.fc = take(g.draft_input ? e * (size_t)2 * d * d : 0);

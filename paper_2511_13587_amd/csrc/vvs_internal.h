@@ -40,7 +40,7 @@ struct GemmPlan { int bm, bn, splits; bool row_owner = false, shared = false; };
 // Byte offsets into the caller's workspace.
 struct Workspace {
   size_t state, outcome, node_result, tokens, rope_tab, x, h, gemm_out, q, attn, act, hf, logits, probs, q_stage, q_pos, q_parts, q_norm, q_origin, q_scores,
-      pq_work, ss, ss2, ring, ring_state, din, few_sync, few_buf, few_gave_up, walk_sync, total;
+      h8, h8_powers, act8, act8_powers, map_counters, map_parts, pq_work, ss, ss2, ring, ring_state, din, few_sync, few_buf, few_gave_up, walk_sync, total;
 };
 
 struct PackedLayout {

@@ -4,6 +4,7 @@
 // vvs_accept.hip.
 #include "vvs_device.h"
 #include "vvs_qcache.h"
+#include "vvs_qlinear.h"
 
 #include <stdlib.h>
 #include <algorithm>
@@ -130,6 +131,11 @@ static void pack_weights_t(Ctx* c, const void* const* t, hipStream_t s) {
     const void* const* w = t + 2 + 9 * l;
     size_t base = c->p.layer0 + c->p.layer_stride * l;
     gain(w[0], base + c->p.g1);
+    if (c->cfg.weight_kind == VVS_WEIGHTS_E4M3) {
+      gain(w[5], base + c->p.g2);
+      launch_context_load(c, l, w, s);
+      continue;
+    }
     char* qkv = c->pw + base + c->p.wqkv;
     for (int i = 0; i < 3; ++i) transpose_into<T>(w[1 + i], qkv + (size_t)i * d * d * sizeof(T), d, d, d, 0, s);
     transpose_into<T>(w[4], c->pw + base + c->p.wo, d, d, d, 0, s);
@@ -826,7 +832,8 @@ static void forward_t(Ctx* c, const TreeDesc& tree, const PosDesc& pos, int Tq, 
   // d 1024, d_ff 4096, 128 rows 1014 / 824; beyond each, 256 rows (d 1024, d_ff 2752) 1405 / 1222, d 1280 (128 rows) 1205 / 1008, d_ff 5504
   // (128 rows) 1297 / 1029; well inside, d 128 with 10 rows 138 / 91.
   const bool held8 = c->cfg.cache_kind == VVS_CACHE_E4M3;
-  if (sizeof(T) == 4 && M <= 128 && d <= 1024 && F <= 4096 && !held8) {
+  const bool weights8 = c->cfg.weight_kind == VVS_WEIGHTS_E4M3;
+  if (sizeof(T) == 4 && M <= 128 && d <= 1024 && F <= 4096 && !held8 && !weights8) {
     forward_small(c, tree, pos, Tq, d_tokens_bt, pc, pu, chunk_start, forced, n_forced, logits_mode, s, from_din);
     return;
   }
@@ -863,22 +870,28 @@ static void forward_t(Ctx* c, const TreeDesc& tree, const PosDesc& pos, int Tq, 
     T* kc = (T*)c->kv + c->kv_layer_stride * l;
     T* vc = (T*)c->kv + c->kv_v_off + c->kv_layer_stride * l;
     { Timed timed(c, VVS_K_ELEMENTWISE, s);
-    launch_add_rmsnorm<T>(M, x, go, splits, sstride, d, (const float*)(lw + c->p.g1), c->cfg.rms_eps, h, 1, 0, s);
+    if (weights8) launch_context_norm(c, M, (const float*)(lw + c->p.g1), splits ? go : nullptr, s);
+    else launch_add_rmsnorm<T>(M, x, go, splits, sstride, d, (const float*)(lw + c->p.g1), c->cfg.rms_eps, h, 1, 0, s);
     }
     int sp;
+    auto project = [&](QMap m) {
+      Timed timed(c, VVS_K_GEMM, s);
+      launch_context_product(c, l, m, M, go, s);
+      return 1;
+    };
     GemmPlan pq = plan_qkv(c, M);
     // with 160+ tiles an unsplit projection streams its weights as fast as a split one, and its epilogue
     // does the rotary embedding and the cache write: one kernel less
     if (pq.splits > 1 && ((M + pq.bm - 1) / pq.bm) * (3 * d / pq.bn) >= 160) pq.splits = 1;
     if (held8) {
-      sp = run_gemm(c, h, lw + c->p.wqkv, go, M, 3 * d, d, plan_partial(c, M, 3 * d, d), s);
+      sp = weights8 ? project(kMapQkv) : run_gemm(c, h, lw + c->p.wqkv, go, M, 3 * d, d, plan_partial(c, M, 3 * d, d), s);
       Timed timed(c, VVS_K_ELEMENTWISE, s);
       launch_context_rope(c, l, M, go, sp, s);
-    } else if (c->cfg.dtype == VVS_BF16 && pq.splits == 1) {
+    } else if (c->cfg.dtype == VVS_BF16 && pq.splits == 1 && !weights8) {
       Timed timed(c, VVS_K_GEMM, s);           // projection + rotary + cache write in one kernel
       mfma_gemm_qkv(c, l, (const bf16_t*)h, (const bf16_t*)(lw + c->p.wqkv), nullptr, tree, pos, Tq, pq, s);
     } else {
-      sp = run_gemm(c, h, lw + c->p.wqkv, go, M, 3 * d, d, pq, s);
+      sp = weights8 ? project(kMapQkv) : run_gemm(c, h, lw + c->p.wqkv, go, M, 3 * d, d, pq, s);
       Timed timed(c, VVS_K_ELEMENTWISE, s);
       hipLaunchKernelGGL(k_rope_kv<T>, dim3(M, ((d >> 1) + 255) / 256), dim3(256), 0, s, go, sp, (size_t)M * 3 * d, q, kc, vc, rope, tree, pos, Tq, d, c->dh,
                          c->kv_row_stride, c->kv_head_stride, c->S_cap, c->rope_pos);
@@ -894,6 +907,15 @@ static void forward_t(Ctx* c, const TreeDesc& tree, const PosDesc& pos, int Tq, 
       size_t lds = sizeof(float) * (c->S_cap + 16);
       hipLaunchKernelGGL(k_attn_simple, dim3(Tq, c->H, c->R), dim3(256), lds, s, q, kc, vc, attn, tree, pos, Tq, d, c->dh,
                          c->kv_row_stride, c->kv_head_stride, c->S_cap);
+    }
+    if (weights8) {
+      { Timed timed(c, VVS_K_ELEMENTWISE, s); launch_context_round(c, M, s); }
+      project(kMapO);
+      { Timed timed(c, VVS_K_ELEMENTWISE, s); launch_context_norm(c, M, (const float*)(lw + c->p.g2), go, s); }
+      project(kMapGate);
+      splits = project(kMapDown);
+      sstride = (size_t)M * d;
+      continue;
     }
     sp = run_gemm(c, attn, lw + c->p.wo, go, M, d, d, plan_partial(c, M, d, d), s);
     { Timed timed(c, VVS_K_ELEMENTWISE, s);

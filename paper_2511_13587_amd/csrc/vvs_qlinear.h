@@ -18,6 +18,7 @@ struct QRound {
   const void* x;
   size_t stride;
   int wide;                         // 16-byte loads: pointer and stride allow them
+  int packed;                       // contexts: x lies in the operand order of the projections (bf16, pack_index)
   QRowsOut y;
 };
 
@@ -54,6 +55,19 @@ struct QWeights {
   __host__ __device__ size_t power_at(int group, int block, int t) const { return (((size_t)group * ((blocks + 3) / 4) + block / 4) * 4 + t) * 64 + block % 4; }
 };
 
+constexpr size_t qweights_data_bytes(size_t groups, int blocks) { return groups * blocks * 8192; }
+constexpr size_t qweights_bytes(size_t groups, int blocks) { return qweights_data_bytes(groups, blocks) + groups * ((blocks + 3) / 4) * 256; }   // powers behind the data
+inline QWeights qweights(int in, int out, int gated, void* base = nullptr) {
+  QWeights w{in, out, gated, qrows_blocks(in), 0, (uint8_t*)base, nullptr};
+  w.groups = (out + w.unit() - 1) / w.unit();
+  if (gated) w.groups = (w.groups + 3) & ~3;                   // whole blocks of 128 hidden units
+  w.powers = w.data ? w.data + qweights_data_bytes(w.groups, w.blocks) : nullptr;
+  return w;
+}
+// Workspace of a product: counters, then activations of up to 32 rows (gated) or two partial sums of tiles of 32 rows
+inline size_t qlinear_counter_bytes(const QWeights& w) { return align_up((size_t)w.groups * 4 * sizeof(uint32_t), 256); }
+inline size_t qlinear_part_bytes(const QWeights& w) { return align_up((size_t)32 * w.groups * (w.gated ? 32 : 2 * 64) * sizeof(float), 256); }
+
 struct QLoad {
   QWeights w;
   const void *a, *b;                // [in][out]; b: up weights
@@ -80,6 +94,7 @@ struct QProduct {
   int M;
   QRowsIn x;
   int dtype;                        // of y
+  int fast;                         // e4m3 products for an fp32 y as well (k_qlinear_tile)
   void* y;                          // !gated
   size_t stride;
   int wide;                         // stores of 4 elements at once
@@ -95,5 +110,15 @@ void launch_qlinear_load(const QLoad& a, hipStream_t s);
 void launch_qlinear_read(const QWeightsRead& a, hipStream_t s);
 void launch_qlinear_product(const QProduct& a, const QPlan& p, hipStream_t s);
 void launch_qlinear_tile(const QProduct& a, QTile t, hipStream_t s);
+
+// Contexts with VVS_WEIGHTS_E4M3 (vvs_qlinear_ctx.hip): a layer's maps, in the order of its projections
+enum QMap { kMapQkv, kMapO, kMapGate, kMapDown };
+inline QWeights context_map(const Ctx* c, QMap m, void* base = nullptr) {
+  return m == kMapQkv ? qweights(c->d, 3 * c->d, 0, base) : m == kMapO ? qweights(c->d, c->d, 0, base) : m == kMapGate ? qweights(c->d, c->F, 1, base) : qweights(c->F, c->d, 0, base);
+}
+void launch_context_load(Ctx* c, int layer, const void* const* tensors, hipStream_t s);          // the layer's tensors in canonical order
+void launch_context_norm(Ctx* c, int M, const float* gain, const float* delta, hipStream_t s);   // x (+ delta) -> rows in 8 bits
+void launch_context_round(Ctx* c, int M, hipStream_t s);                                         // the attention's output -> rows in 8 bits
+void launch_context_product(Ctx* c, int layer, QMap m, int M, float* out, hipStream_t s);        // kMapGate: into the rows of hidden units
 
 }  // namespace vvs

@@ -76,21 +76,6 @@ void launch_qlinear_read(const QWeightsRead& a, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------------------------------------ products
-// Agent scope: written through to the memory behind the XCDs' L2s, and read from there
-__device__ __forceinline__ void put4(float* p, const float (&v)[4]) {
-#pragma unroll
-  for (int j = 0; j < 4; j += 2)
-    __hip_atomic_store((uint64_t*)(p + j), (uint64_t)__float_as_uint(v[j]) | (uint64_t)__float_as_uint(v[j + 1]) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ void get4(const float* p, float* v) {
-#pragma unroll
-  for (int j = 0; j < 4; j += 2) {
-    const uint64_t u = __hip_atomic_load((const uint64_t*)(p + j), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    v[j] = __uint_as_float((uint32_t)u);
-    v[j + 1] = __uint_as_float((uint32_t)(u >> 32));
-  }
-}
-
 // Few rows.  A workgroup of NW waves makes CT tiles of 16 columns for 16 RT rows; wave w takes blocks w, w + NW, ... of the contraction, straight from memory into operand registers, one block ahead,
 // and the partial sums are added through LDS in the order of the waves.  Powers of all blocks lie in LDS, four in a word.
 template <int NW, int RT, int CT, bool GATED, typename T>
@@ -181,18 +166,7 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_few(QProduct a) {
     }
     v[0] = s.x; v[1] = s.y; v[2] = s.z; v[3] = s.w;
   };
-  // Counts this workgroup in; the last of n goes on, for all.  What it reads was written through to memory before it was counted.
-  auto last_of = [&](uint32_t* counter, int n) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-      const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)n - 1;
-      if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      *(int*)parts = last;
-    }
-    __syncthreads();
-    return *(const int*)parts != 0;
-  };
+  auto last_of = [&](uint32_t* counter, int n) { return last_workgroup(counter, n, (int*)parts); };
   if constexpr (GATED) {
     for (int u = tid; u < CT / 2 * RT * 64; u += 64 * NW) {
       const int l = u & 63, r = (u >> 6) % RT, c = (u >> 6) / RT, m = m0 + 16 * r + (l & 15);

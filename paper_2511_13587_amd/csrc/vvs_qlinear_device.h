@@ -47,4 +47,33 @@ __device__ __forceinline__ void round_block(const float (&v)[8], uint8_t* values
   if (first) *power = held ? (uint8_t)(e + 127) : 0;
 }
 
+// Agent scope: written through to the memory behind the XCDs' L2s, and read from there
+__device__ __forceinline__ void put4(float* p, const float (&v)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; j += 2)
+    __hip_atomic_store((uint64_t*)(p + j), (uint64_t)__float_as_uint(v[j]) | (uint64_t)__float_as_uint(v[j + 1]) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void get4(const float* p, float* v) {
+#pragma unroll
+  for (int j = 0; j < 4; j += 2) {
+    const uint64_t u = __hip_atomic_load((const uint64_t*)(p + j), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    v[j] = __uint_as_float((uint32_t)u);
+    v[j + 1] = __uint_as_float((uint32_t)(u >> 32));
+  }
+}
+
+// Counts a workgroup in; the last of n goes on, for all.  What it reads was written through to memory before it was counted.  Leaves the counter at zero.  flag: a word of LDS that nobody reads any more
+// once all threads are here.
+__device__ __forceinline__ bool last_workgroup(uint32_t* counter, int n, int* flag) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const bool last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)n - 1;
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last;
+  }
+  __syncthreads();
+  return *flag != 0;
+}
+
 }  // namespace vvs

@@ -10,7 +10,7 @@ namespace vvs {
 struct QLinear {
   vvs_qlinear_config cfg;
   QWeights w;
-  size_t weight_bytes, ws_bytes, counter_bytes;
+  size_t weight_bytes, ws_bytes;
   int dev;
   char* ws;
   bool loaded;
@@ -96,7 +96,8 @@ static vvs_status check_rows(int n_rows, int width, const void* values, const vo
 //     but a long contraction in two halves (28 rows, 11008 -> 4096: 1 tile 17.2, 2 tiles 19.9, 2 tiles in halves 15.3)
 //   beyond: the largest tiles of which there are enough.  128 x 256 from two per CU on (8192 rows, 4096 -> 12288: 362, 64 x 256 418); 64 x 256 from 224 (1000 rows, 1280 -> 3840, 240 tiles: 12.1, 64 x 128
 //     12.6, 128 x 256 15.3); 64 x 128 from 176 (432 rows, 1280 -> 3840, 210: 9.3, 64 x 256 11.1; 128 rows, 4096 -> 12288, 192: 26.3, 32 x 128 28.6); 32 x 128 from 130 (432 rows, 1280 -> 1280, 140: 7.5,
-//     few 8.6); fewer leave CUs idle and latency bare: k_qlinear_few, 32 rows x 4 tiles (128 rows: 11008 -> 4096 25.3 / 32 x 128 53.9, 1280 -> 3840 6.8 / 7.5)
+//     few 8.6); fewer leave CUs idle and latency bare: k_qlinear_few, 32 rows x 4 tiles (128 rows: 11008 -> 4096 25.3 / 32 x 128 53.9, 1280 -> 3840 6.8 / 7.5), with a long contraction up to 229
+//     (224 rows, 11008 -> 4096, 224: 43.3 / 53.8; 300 rows, 320: 61.1 / 59.8).  Not built: tiles of 64 x 128 in 2 to 4 shares, joined by the last (224 rows 36.4, 300 rows 43.1, but 432 rows, 3456 -> 1280 15.6 / 14.9)
 //   with a gate: up to 32 rows 2 tiles (28 rows, 4096 -> 11008: 26.2, 32 x 256 30.4), up to 64 tiles of 32 x 256 (60 rows: 30.5, few 38.5), 64 x 256 (128 rows 34.7, 128 x 256 45.6; 432 rows, 1280 ->
 //     3456 11.9 / 16.2), 128 x 256 from 384 tiles on
 QPlan plan_qlinear_product(const QWeights& w, int M) {
@@ -115,7 +116,7 @@ QPlan plan_qlinear_product(const QWeights& w, int M) {
     }
     return p;
   }
-  if (tiles(32, 2) < 130) {
+  if (tiles(32, 2) < (w.blocks >= 64 ? 230 : 130)) {
     p.ct = 4;
     return p;
   }
@@ -134,16 +135,12 @@ static vvs_status plan_qlinear(const vvs_qlinear_config* cfg, QLinear* l) {
   if (g.out > (1 << 24) || g.max_rows > (1 << 20)) return no(nullptr, VVS_ESIZE, "qlinear config: at most 2^24 columns and 2^20 rows");
   l->cfg = g;
   QWeights& w = l->w;
-  w = QWeights{g.in, g.out, g.gated, qrows_blocks(g.in), 0, nullptr, nullptr};
-  w.groups = (g.out + w.unit() - 1) / w.unit();
-  if (g.gated) w.groups = (w.groups + 3) & ~3;                 // whole blocks of 128 hidden units
+  w = qweights(g.in, g.out, g.gated);
   // (a launch of the smallest tiles, a wave per 64 columns and 32 rows)
   if ((int64_t)w.groups * ((g.max_rows + 31) / 32 + 1) * 64 > kMostThreads) return no(nullptr, VVS_ESIZE, "qlinear config: more outputs than a launch holds");
   if ((int64_t)w.groups * w.blocks >= (1 << 24)) return no(nullptr, VVS_ESIZE, "qlinear config: more weights than a launch holds");
-  l->weight_bytes = align_up((size_t)w.groups * w.blocks * 8192, 256) + align_up((size_t)w.groups * ((w.blocks + 3) / 4) * 256, 256);
-  // counters, then: activations of up to 32 rows; two partial sums of tiles of 32 rows
-  l->counter_bytes = align_up((size_t)w.groups * 4 * sizeof(uint32_t), 256);
-  l->ws_bytes = l->counter_bytes + align_up(g.gated ? (size_t)std::min(g.max_rows, 32) * w.groups * 32 * sizeof(float) : (size_t)2 * 32 * w.groups * 64 * sizeof(float), 256);
+  l->weight_bytes = align_up(qweights_bytes(w.groups, w.blocks), 256);
+  l->ws_bytes = qlinear_counter_bytes(w) + qlinear_part_bytes(w);
   return VVS_OK;
 }
 
@@ -274,8 +271,7 @@ vvs_status vvs_qlinear_create(const vvs_qlinear_config* cfg, void* d_weights, vo
   hipError_t e = hipGetDevice(&plan.dev);
   if (e != hipSuccess) return no(nullptr, VVS_EHIP, hipGetErrorString(e));
   plan.ws = (char*)d_workspace;
-  plan.w.data = (uint8_t*)d_weights;
-  plan.w.powers = (uint8_t*)d_weights + align_up((size_t)plan.w.groups * plan.w.blocks * 8192, 256);
+  plan.w = qweights(plan.cfg.in, plan.cfg.out, plan.cfg.gated, d_weights);
   QLinear* l = new (std::nothrow) QLinear(plan);
   if (!l) return no(nullptr, VVS_EHIP, "qlinear create: out of memory");
   launch_fill_zero(d_workspace, l->ws_bytes, nullptr);
@@ -331,7 +327,7 @@ vvs_status vvs_qlinear_apply(vvs_qlinear* ql, int32_t n_rows, const void* d_valu
   a.w = l->w; a.M = n_rows;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
   a.dtype = out_dtype; a.y = d_out; a.stride = (size_t)os; a.wide = wide_rows(d_out, os, out_dtype, 4);
-  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + l->counter_bytes);
+  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + qlinear_counter_bytes(l->w));
   launch_qlinear_product(a, plan_qlinear_product(l->w, n_rows), (hipStream_t)s);
   return launched(l, "qlinear apply");
 }
@@ -351,7 +347,7 @@ vvs_status vvs_qlinear_gate(vvs_qlinear* ql, int32_t n_rows, const void* d_value
   QProduct a{};
   a.w = l->w; a.M = n_rows;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
-  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + l->counter_bytes);
+  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + qlinear_counter_bytes(l->w));
   a.y8 = QRowsOut{(uint8_t*)d_out_values, (uint8_t*)d_out_powers};
   launch_qlinear_product(a, plan_qlinear_product(l->w, n_rows), (hipStream_t)s);
   return launched(l, "qlinear gate");

@@ -33,7 +33,13 @@ __global__ __launch_bounds__(256) void k_qrows_round(QRound a) {
   if (m >= a.M) return;
   float v[8];
   const int at = b * kQRowBlock + sub * 8;
-  read_row8((const T*)a.x + (size_t)m * a.stride, at, a.width, a.wide, v);
+  if constexpr (sizeof(T) == 2) {
+    if (a.packed && at < a.width) read8((const T*)a.x + pack_index(m, at, a.width), v);      // (a multiple of 64 elements wide)
+    else if (a.packed) read_row8((const T*)a.x, at, a.width, 1, v);
+    else read_row8((const T*)a.x + (size_t)m * a.stride, at, a.width, a.wide, v);
+  } else {
+    read_row8((const T*)a.x + (size_t)m * a.stride, at, a.width, a.wide, v);
+  }
   round_block(v, a.y.values + (size_t)m * blocks * kQRowBlock + at, a.y.powers + (size_t)m * powers + b, b < blocks, sub == 0);
 }
 

@@ -245,6 +245,8 @@ int main() {
   { QPlan p = plan(1280, 3840, 0, 1000); CHECK(!p.few && p.tile == kTile64x256); }
   { QPlan p = plan(4096, 12288, 0, 8192); CHECK(!p.few && p.tile == kTile128x256); }
   { QPlan p = plan(1280, 3840, 0, 128); CHECK(p.few && p.ct == 4); }
+  { QPlan p = plan(11008, 4096, 0, 224); CHECK(p.few && p.ct == 4); }
+  { QPlan p = plan(11008, 4096, 0, 300); CHECK(!p.few && p.tile == kTile32x128); }
   { QPlan p = plan(4096, 11008, 1, 14); CHECK(p.few && p.rt == 1); }
   { QPlan p = plan(4096, 11008, 1, 60); CHECK(!p.few && p.tile == kTile32x256); }
   { QPlan p = plan(4096, 11008, 1, 128); CHECK(!p.few && p.tile == kTile64x256); }

@@ -45,6 +45,25 @@ def test_sizes():
     assert 2 * 4096 * 11008 <= weights <= 2 * 4096 * 11008 * 1.01 and ws < 2 << 20      # half of bf16
 
 
+def test_contexts_with_weights_in_8_bits():
+    """Half of the layers' bytes; refused where it does not go."""
+    from paper_2511_13587_amd import binding as vb
+    from paper_2511_13587_amd import synth
+    _, _, same = vb.vvs_query_sizes(vb.make_config(synth.SEVEN_B))
+    _, _, held8 = vb.vvs_query_sizes(vb.make_config(synth.SEVEN_B, weight_kind=vb.VVS_WEIGHTS_E4M3))
+    layers = 32 * (4 * 4096 ** 2 + 3 * 4096 * 11008)
+    assert layers * 0.98 <= same - held8 <= layers
+    for shape, kw, status in ((synth.XL_TREE, dict(weight_kind=2), vb.VVS_EINVAL), (synth.XL_TREE, dict(weight_kind=-1), vb.VVS_EINVAL), (synth.XL_TREE, dict(weight_kind=1, draft_input=1), vb.VVS_EINVAL),
+                              (synth.TINY.replace(d_model=72, n_heads=2), dict(weight_kind=1), vb.VVS_ESIZE), (synth.TINY.replace(d_model=72, n_heads=2), dict(), vb.VVS_OK),
+                              (synth.TINY.replace(d_ff=65544), dict(weight_kind=1), vb.VVS_ESIZE), (synth.TINY, dict(weight_kind=1, cache_kind=1), vb.VVS_OK)):
+        try:
+            vb.vvs_query_sizes(vb.make_config(shape, **kw))
+            got = vb.VVS_OK
+        except vb.VvsError as e:
+            got = e.status
+        assert got == status, (shape.name, kw)
+
+
 def test_rows_of_matrices():
     """What the binding takes as rows of a matrix: parts of wider ones, any leading dimensions; not what lies otherwise."""
     import torch
