@@ -105,8 +105,8 @@ typedef struct {
                                       64 or 128, as the dtype allows), so that calls of few rows take longer than with VVS_CACHE_SAME */
   int32_t weight_kind;           /* VVS_WEIGHTS_SAME: weights have the context's dtype;
                                     VVS_WEIGHTS_E4M3: a layer's seven matrices are held in 8 bits, and what they are multiplied by - the norms' outputs, the
-                                      attention's (rounded to the dtype first), the activations - is rounded to 8 bits as well (see vvs_qrows below); products, residual stream
-                                      and all else are as ever.  For contexts whose steps are bound by the weights' bytes.  Embeddings, gains and the output head
+                                      attention's (rounded to the dtype first), the activations - is rounded to 8 bits as well (see vvs_qrows below); residual stream
+                                      and all else are as ever, products too, but in bf16 contexts from 65 rows on (as those of vvs_qlinear_apply for bf16).  For contexts whose steps are bound by the weights' bytes.  Embeddings, gains and the output head
                                       keep the dtype.  Layers run as separate launches (no drafter contexts; d_model a multiple of 64, d_ff at most 65536) */
 } vvs_config;
 enum { VVS_NORM_AUTO = 0, VVS_NORM_SEPARATE = 1 };
@@ -470,7 +470,7 @@ vvs_status vvs_qrows_round(int32_t n_rows, int32_t width, int32_t dtype, const v
  *   d_delta    : [n_rows, width] of its own type, or NULL: nothing is added
  *   d_x_out    : x' in the type of x; may be d_x itself (with the same stride); NULL: not written
  *   d_gain     : [width] of its own type
- *   eps        : finite, not negative */
+ *   eps        : finite, not negative (0: a row of zeros becomes NaN) */
 vvs_status vvs_qrows_norm(int32_t n_rows, int32_t width, int32_t x_dtype, const void* d_x, int64_t x_stride, int32_t delta_dtype, const void* d_delta,
                           int64_t delta_stride, void* d_x_out, int64_t x_out_stride, int32_t gain_dtype, const void* d_gain, float eps, void* d_values,
                           void* d_powers, vvs_stream s);
@@ -488,10 +488,11 @@ typedef struct {
   int32_t dtype;                 /* of the weights that vvs_qlinear_load takes and vvs_qlinear_read gives */
 } vvs_qlinear_config;
 
-/* Sizes in bytes of the two device buffers of a linear map: weights in 8 bits in the kernels' own order, workspace.  A workspace may serve several maps - it has to hold the largest one's
- * bytes - if their calls are issued on one stream or ordered; captured graphs that share one must not run at the same time. */
+/* Sizes in bytes of the two device buffers of a linear map: weights in 8 bits in the kernels' own order, workspace.  Calls on a map, vvs_qlinear_load among them, are issued on one stream or ordered by
+ * the caller.  A workspace may serve several maps - it has to hold the largest one's bytes - if the calls of all of them are; captured graphs that share one must not run at the same time. */
 vvs_status vvs_qlinear_query_sizes(const vvs_qlinear_config* cfg, size_t* weight_bytes, size_t* workspace_bytes);
-/* Creates a map over caller-allocated device buffers (256-byte aligned) on the current device, which has to be current at every call.  Synchronous: clears the workspace. */
+/* Creates a map over caller-allocated device buffers (256-byte aligned) on the current device, which has to be current at every call.  Synchronous: clears the workspace,
+ * which no other call may be using. */
 vvs_status vvs_qlinear_create(const vvs_qlinear_config* cfg, void* d_weights, void* d_workspace, vvs_qlinear** out);
 void vvs_qlinear_destroy(vvs_qlinear* l);
 const char* vvs_qlinear_last_error(const vvs_qlinear* l);   /* l must not be NULL (a failed create or query: vvs_last_error(NULL)) */
@@ -501,7 +502,10 @@ vvs_status vvs_qlinear_load(vvs_qlinear* l, const void* d_w, const void* d_w_up,
 /* The weights that are held, as numbers in the type of the config; arguments as above. */
 vvs_status vvs_qlinear_read(vvs_qlinear* l, void* d_w, void* d_w_up, vvs_stream s);
 
-/* out = x W for rows in 8 bits of width `in`: out [n_rows, out] in out_dtype. */
+/* out = x W for rows in 8 bits of width `in`: out [n_rows, out] in out_dtype.
+ * Sums are in fp32 and in a fixed order: the same call gives the same bits.  With up to 64 rows, and wherever out_dtype is VVS_FP32, products of e4m3 numbers enter them whole.  Calls of more rows with
+ * outputs in bf16, and such calls of vvs_qlinear_gate, may take the matrix instructions for e4m3, twice as fast, which cut off what lies 2^13 below the largest of 8 neighbouring products: 1.3e-5 of the
+ * result in the 2-norm, where the rounding of the output is 1.7e-3 in bf16 and 2.6e-2 in 8 bits.  The bits of a row may so depend on how many rows a call has. */
 vvs_status vvs_qlinear_apply(vvs_qlinear* l, int32_t n_rows, const void* d_values, const void* d_powers, int32_t out_dtype, void* d_out, int64_t out_stride,
                              vvs_stream s);
 

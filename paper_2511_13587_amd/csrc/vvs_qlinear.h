@@ -30,6 +30,7 @@ struct QNorm {
   const void* gain; int gain_dtype;
   int x_wide, delta_wide, x_out_wide, gain_wide;             // 16-byte accesses
   float eps;
+  double per_element;               // 1 / width
   QRowsOut y;
 };
 

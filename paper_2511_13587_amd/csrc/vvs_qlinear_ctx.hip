@@ -33,7 +33,7 @@ void launch_context_norm(Ctx* c, int M, const float* gain, const float* delta, h
   a.delta = delta; a.delta_dtype = VVS_FP32; a.delta_stride = c->d; a.delta_wide = 1;
   if (delta) { a.x_out = c->ws + c->w.x; a.x_out_stride = c->d; a.x_out_wide = 1; }
   a.gain = gain; a.gain_dtype = VVS_FP32; a.gain_wide = 1;
-  a.eps = c->cfg.rms_eps;
+  a.eps = c->cfg.rms_eps; a.per_element = 1.0 / c->d;
   a.y = rows_of(c);
   launch_qrows_norm(a, s);
 }

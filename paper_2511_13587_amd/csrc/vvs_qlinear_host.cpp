@@ -205,7 +205,7 @@ vvs_status vvs_qrows_round(int32_t n_rows, int32_t width, int32_t dtype, const v
 vvs_status vvs_qrows_norm(int32_t n_rows, int32_t width, int32_t x_dtype, const void* d_x, int64_t x_stride, int32_t delta_dtype, const void* d_delta,
                           int64_t delta_stride, void* d_x_out, int64_t x_out_stride, int32_t gain_dtype, const void* d_gain, float eps, void* d_values,
                           void* d_powers, vvs_stream s) {
-  const vvs_status st = check_rows(n_rows, width, d_values, d_powers, 1024);
+  const vvs_status st = check_rows(n_rows, width, d_values, d_powers, width > 0 ? std::min(1024, 16 * qrows_powers(std::min(width, kWidest))) : 1024);
   if (st != VVS_OK) return st;
   if (!d_x || !d_gain) return rows_no(VVS_EINVAL, "qrows norm: NULL argument");
   if (!known(x_dtype) || !known(gain_dtype) || (d_delta && !known(delta_dtype))) return rows_no(VVS_EINVAL, "qrows norm: unknown dtype");
@@ -226,7 +226,7 @@ vvs_status vvs_qrows_norm(int32_t n_rows, int32_t width, int32_t x_dtype, const 
   if (d_delta) { a.delta = d_delta; a.delta_dtype = delta_dtype; a.delta_stride = (size_t)ds; a.delta_wide = wide_rows(d_delta, ds, delta_dtype); }
   if (d_x_out) { a.x_out = d_x_out; a.x_out_stride = (size_t)os; a.x_out_wide = wide_rows(d_x_out, os, x_dtype); }
   a.gain = d_gain; a.gain_dtype = gain_dtype; a.gain_wide = wide_rows(d_gain, 0, gain_dtype);
-  a.eps = eps;
+  a.eps = eps; a.per_element = 1.0 / width;
   a.y = QRowsOut{(uint8_t*)d_values, (uint8_t*)d_powers};
   launch_qrows_norm(a, (hipStream_t)s);
   return rows_launched();
@@ -340,7 +340,6 @@ vvs_status vvs_qlinear_gate(vvs_qlinear* ql, int32_t n_rows, const void* d_value
   if (st != VVS_OK) return st;
   if (!d_out_values || !d_out_powers) return no(l, VVS_EINVAL, "qlinear gate: NULL argument");
   if (off16(d_out_values) || off16(d_out_powers)) return no(l, VVS_EINVAL, "qlinear gate: values and powers must be 16-byte aligned");
-  if ((int64_t)n_rows * 16 * qrows_powers(l->cfg.out) > kMostThreads) return no(l, VVS_ESIZE, "qlinear gate: more rows than a launch holds");
   const Span outs[] = {values_span(d_out_values, n_rows, l->cfg.out), powers_span(d_out_powers, n_rows, l->cfg.out)}, ins[] = {values_span(d_values, n_rows, l->cfg.in), powers_span(d_powers, n_rows, l->cfg.in)};
   if (share_any(outs, ins)) return no(l, VVS_EINVAL, "qlinear gate: an output shares memory with the rows or with the other");
   if ((st = check_device(l)) != VVS_OK) return st;

@@ -119,8 +119,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(QProduct a, in
       }
     };
     if constexpr (FAST) {
-      // row tile r + 1 is read from LDS while r is multiplied, and no further ones: left to itself the compiler reads them all first and spills
-      constexpr int NX = RT > 8 ? 3 : 2;
+      // two row tiles are on their way from LDS while one is multiplied (one: 356 us for 354), and no more: left to itself the compiler moves the reads to where they spill (382)
+      constexpr int NX = RT > 2 ? 3 : 2;
       struct Rows { u32x4 h[2]; } x[NX];
       int xs[NX];
       auto rows = [&](int r) {

@@ -118,8 +118,21 @@ __global__ __launch_bounds__(MOST) void k_qrows_norm(QNorm a) {
       else write_row8((float*)a.x_out + (size_t)m * a.x_out_stride, at, a.width, a.x_out_wide, v[j]);
     }
   }
-  ss = blockDim.x == 64 ? wave_sum(ss) : block_sum(ss, red);
-  const float r = 1.f / sqrtf(ss / (float)a.width + a.eps);
+  // The waves' sums are added, and the factor is taken, in 64 bits, so that it is off by one rounding, not by several that a whole row would share: values end next to a border of e4m3 now and then.
+  // (8192 rows of 4096 in bf16: 49.2 us, 49.5 all in fp32; an element's two products exact as well 52.6, in 64 bits 53.4)
+  ss = wave_sum(ss);
+  double all = ss;
+  if (blockDim.x > 64) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
+    __syncthreads();
+    all = 0.0;
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) all += red[w];
+  }
+  // (fp32's reciprocal root and one step of Newton's method)
+  const double mean = all * a.per_element + (double)a.eps;
+  double factor = rsqrtf((float)mean);
+  factor = factor > 0.0 && factor < INFINITY ? factor * (1.5 - 0.5 * mean * factor * factor) : 1.0 / sqrt(mean);
+  const float r = (float)factor;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const int at = (j * blockDim.x + threadIdx.x) * 8, b = at / kQRowBlock;
