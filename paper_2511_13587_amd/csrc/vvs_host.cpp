@@ -355,12 +355,9 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   const int wide = few_wide_rows(c), few = std::max(few_rows(c), wide);
   go = std::max(go, (size_t)kFewWideShares * wide * d);
   w.few_sync = take(few ? sizeof(uint32_t) * kFewLine * (kFewHead + (size_t)few_layer_counters(c->H, few / 32) * c->L + 8) : 0);   // zeroed with the state
-  size_t map_counters = 0, map_parts = 0;
-  for (QMap m : {kMapQkv, kMapO, kMapGate, kMapDown}) {
-    map_counters = std::max(map_counters, qlinear_counter_bytes(context_map(c, m)));
-    map_parts = std::max(map_parts, qlinear_part_bytes(context_map(c, m)));
-  }
-  w.map_counters = take(g.weight_kind ? map_counters : 0);      // zeroed with the state
+  size_t map_parts = 0;
+  for (QMap m : {kMapQkv, kMapO, kMapGate, kMapDown}) map_parts = std::max(map_parts, qlinear_part_bytes(context_map(c, m)));
+  w.map_counters = take(g.weight_kind ? kQlinearCounters : 0);      // zeroed with the state
   w.x = take(sizeof(float) * (size_t)c->Mmax * d);
   w.h = take(c->esz * (size_t)c->Mmax * d);
   // (a call whose layers are one launch has no partial sums: what its phases hand on lies in their place)

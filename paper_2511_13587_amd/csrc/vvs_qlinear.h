@@ -65,9 +65,15 @@ inline QWeights qweights(int in, int out, int gated, void* base = nullptr) {
   w.powers = w.data ? w.data + qweights_data_bytes(w.groups, w.blocks) : nullptr;
   return w;
 }
-// Workspace of a product: counters, then activations of up to 32 rows (gated) or two partial sums of tiles of 32 rows
-inline size_t qlinear_counter_bytes(const QWeights& w) { return align_up((size_t)w.groups * 4 * sizeof(uint32_t), 256); }
-inline size_t qlinear_part_bytes(const QWeights& w) { return align_up((size_t)32 * w.groups * (w.gated ? 32 : 2 * 64) * sizeof(float), 256); }
+// Workspace of a product that k_qlinear_few makes: counters, in a place of one size, so that maps can share a workspace, then for a contraction in halves two partial sums of 32 rows, with a gate the
+// activations in fp32 of up to 32 rows, or of as many as have no more workgroups than kGateWorkgroups (of 32 rows x 32 packed columns).
+constexpr int kGateWorkgroups = 704;
+constexpr size_t kQlinearCounters = 4096;                      // bytes: a counter per 32 rows x 32 columns of up to 64 groups, or per row tile and block of 128 hidden units of up to 2048 groups
+inline bool qlinear_in_halves(const QWeights& w) { return !w.gated && w.blocks >= 40 && w.groups > 32 && w.groups <= 64; }
+inline size_t qlinear_part_bytes(const QWeights& w) {
+  const size_t gate = (size_t)(w.groups > kGateWorkgroups / 2 ? w.groups : kGateWorkgroups / 2) * 32 * 32, halves = qlinear_in_halves(w) ? (size_t)w.groups * 64 * 32 * 2 : 0;
+  return align_up((w.gated ? gate : halves) * sizeof(float), 256);
+}
 
 struct QLoad {
   QWeights w;
@@ -95,7 +101,7 @@ struct QProduct {
   int M;
   QRowsIn x;
   int dtype;                        // of y
-  int fast;                         // e4m3 products for an fp32 y as well (k_qlinear_tile)
+  int fast;                         // e4m3 products (k_qlinear_tile; gated: by the tile)
   void* y;                          // !gated
   size_t stride;
   int wide;                         // stores of 4 elements at once

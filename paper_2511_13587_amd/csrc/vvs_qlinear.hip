@@ -235,7 +235,6 @@ template <typename T>
 static void few(const QProduct& a, const QPlan& p, hipStream_t s) {
   if (p.rt == 1 && p.ct == 1) few_t<8, 1, 1, false, T>(a, p.splits, s);
   else if (p.rt == 1) few_t<4, 1, 2, false, T>(a, p.splits, s);
-  else if (p.ct == 1) few_t<8, 2, 1, false, T>(a, p.splits, s);
   else if (p.ct == 2) few_t<8, 2, 2, false, T>(a, p.splits, s);
   else few_t<8, 2, 4, false, T>(a, p.splits, s);
 }

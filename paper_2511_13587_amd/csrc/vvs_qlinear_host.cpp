@@ -90,39 +90,48 @@ static vvs_status check_rows(int n_rows, int width, const void* values, const vo
   return VVS_OK;
 }
 
-// Few rows are bound by the weights' bytes, which every wave streams for itself; more rows share them, and themselves pass through LDS.  us per call in a graph, weights rotating through 400 MB.
-//   16 rows: columns a tile each while there are no more tiles than CUs (8 rows, 11008 -> 4096: 1 tile 11.9, 2 tiles 14.5; 1280 -> 3840 4.39 / 4.68), else two (4096 -> 12288 14.1 / 12.9)
-//   up to 64 rows: 32 rows x 2 tiles (60 rows: 4096 -> 12288 21.0, 11008 -> 4096 19.6, 1280 -> 3840 5.6; tiles of 32 x 128 22.9, 54, 7.4), up to 32 rows again 1 tile where few (28 rows, 4096 -> 4096 7.9 / 8.3),
-//     but a long contraction in two halves (28 rows, 11008 -> 4096: 1 tile 17.2, 2 tiles 19.9, 2 tiles in halves 15.3)
-//   beyond: the largest tiles of which there are enough.  128 x 256 from two per CU on (8192 rows, 4096 -> 12288: 362, 64 x 256 418); 64 x 256 from 224 (1000 rows, 1280 -> 3840, 240 tiles: 12.1, 64 x 128
-//     12.6, 128 x 256 15.3); 64 x 128 from 176 (432 rows, 1280 -> 3840, 210: 9.3, 64 x 256 11.1; 128 rows, 4096 -> 12288, 192: 26.3, 32 x 128 28.6); 32 x 128 from 130 (432 rows, 1280 -> 1280, 140: 7.5,
-//     few 8.6); fewer leave CUs idle and latency bare: k_qlinear_few, 32 rows x 4 tiles (128 rows: 11008 -> 4096 25.3 / 32 x 128 53.9, 1280 -> 3840 6.8 / 7.5), with a long contraction up to 229
-//     (224 rows, 11008 -> 4096, 224: 43.3 / 53.8; 300 rows, 320: 61.1 / 59.8).  Not built: tiles of 64 x 128 in 2 to 4 shares, joined by the last (224 rows 36.4, 300 rows 43.1, but 432 rows, 3456 -> 1280 15.6 / 14.9)
-//   with a gate: up to 32 rows 2 tiles (28 rows, 4096 -> 11008: 26.2, 32 x 256 30.4), up to 64 tiles of 32 x 256 (60 rows: 30.5, few 38.5), 64 x 256 (128 rows 34.7, 128 x 256 45.6; 432 rows, 1280 ->
-//     3456 11.9 / 16.2), 128 x 256 from 384 tiles on
+// Few rows are bound by the weights' bytes, which every wave streams for itself, and by how many waves there are to do so; more rows share the weights, and themselves pass through LDS.  The rule goes by
+// the number of workgroups: the smallest tiles that fit the 256 CUs one each, then larger ones.  us per call in a graph, weights rotating through 400 MB, bf16 outputs (the rule is within 1 % of the
+// best of all variants in the mean over 500 sizes, 8 to 1200 rows, and at most 17 % behind it at one).
+//   k_qlinear_few, rows x columns of a workgroup:
+//   16 x 16 up to 256 workgroups (28 rows: 1280 -> 1280 3.7, 32 x 16 4.4; 4096 -> 2048 6.0, 32 x 16 7.7, 16 x 32 7.0)
+//   16 x 32 for up to 16 rows (8 rows, 4096 -> 12288 13.3, 16 x 16 13.6); up to 256 workgroups (64 rows: 1280 -> 1280 4.2, 16 x 16 4.5; 4096 -> 2048 7.2, 32 x 32 8.6); up to 640 where the contraction is short (128
+//     rows, 1280 -> 1280 5.0, 32 x 32 5.3; 256 rows 5.8, 32 x 64 6.4)
+//   32 x 32 with the contraction in halves for one row tile and a long one (28 rows, 11008 -> 4096: 15.0, 16 x 32 17.5, 32 x 16 16.3, whole 19.5)
+//   32 x 32 up to 256 workgroups (128 rows, 4096 -> 2048 8.6, 32 x 64 10.0; 64 rows, 4096 -> 4096 8.8, 16 x 32 9.4) and up to 64 rows (4096 -> 12288 21.3, 32 x 64 23.0) of which there are up
+//     to 256 tiles of 32 x 128 (48 rows, fp32 outputs: 4096 -> 16384, 256, 27.0, tiles 28.4; 4096 -> 32768, 512, 47.7, tiles 37.0)
+//   32 x 64 up to 256 workgroups (128 rows, 4096 -> 4096 10.3, 32 x 32 13.1, tiles of 32 x 128 14.4; 28 rows, 4096 -> 12288 14.6, 32 x 32 15.4); up to 512 with a long contraction (256 rows, 11008 -> 4096
+//     43.4, tiles of 32 x 128 53.8)
+//   k_qlinear_tile: 64 x 128 where all of its workgroups are on the card at once, three per CU (432 rows, 4096 -> 12288, 672: 38.3, 64 x 256 40.9, 128 x 256 40.2); 128 x 256 from 208 on (600 rows, 4096 -> 16384,
+//     320: 54.3, 64 x 256 66.5; 8192 rows, 4096 -> 12288 354, 64 x 256 418); 64 x 256 from 192 (256 rows, 4096 -> 12288 31.5, 64 x 128 33.7); 64 x 128 from 176 (432 rows, 1280 -> 3840 9.4, 32 x 128 9.5,
+//     64 x 256 11.2); 32 x 128 (256 rows, 4096 -> 4096 14.7, 64 x 128 17.6).  Not built: tiles of 64 x 128 in 2 to 4 shares, joined by the last (224 rows, 11008 -> 4096 36.4, 300 rows 43.1, but 432 rows, 3456 ->
+//     1280 15.6 / 14.9)
+// With a gate, columns counted twice: 16 x 32 up to 16 rows and up to 768 workgroups (48 rows: 768 -> 2048 8.0, 32 x 32 8.5, tiles 9.1; 2048 -> 1024 8.3, 32 x 32 9.9, tiles 14.6), 32 x 32 up to 32 rows (4096 ->
+//   11008 26.0, 16 x 32 32.1) and up to 704 (64 rows, 2048 -> 5632 15.5, tiles 20.1), of more than 64 rows with a longer contraction (128 rows: 4096 -> 2048 16.7, tiles 21.6; 1280 -> 3456 16.7 / 11.9); tiles of
+//   32 x 256 up to 64 rows (4096 -> 11008 35.2, 32 x 32 41.9) and where the contraction is one or two blocks (128 rows, 128 -> 344 5.2, 16 x 32 6.0, 64 x 256 6.2); 128 x 256 from 208 on (432 rows, 4096 -> 11008,
+//   344: 55.5, 64 x 256 64.9); 64 x 256 (128 rows, 4096 -> 11008 34.7, 128 x 256 45.7)
 QPlan plan_qlinear_product(const QWeights& w, int M) {
-  QPlan p{true, M <= 16 ? 1 : 2, 2, 1, kTile32x128};
-  const int columns = 4 * w.groups;
+  auto few = [&](int rt, int ct) { return (int64_t)((M + 16 * rt - 1) / (16 * rt)) * w.groups * (4 / ct); };
   auto tiles = [&](int rows, int groups) { return (int64_t)((M + rows - 1) / rows) * ((w.groups + groups - 1) / groups); };
+  auto small = [](int rt, int ct, int splits = 1) { return QPlan{true, rt, ct, splits, kTile32x128}; };
+  auto large = [](QTile t) { return QPlan{false, 2, 2, 1, t}; };
   if (w.gated) {
-    p.few = M <= 32;
-    p.tile = M <= 64 ? kTile32x256 : tiles(128, 4) >= 384 ? kTile128x256 : kTile64x256;
-    return p;
+    if (M > 32 && w.blocks <= 2 && tiles(32, 4) <= 256) return large(kTile32x256);
+    if (M <= 16 || few(1, 2) <= 768) return small(1, 2);
+    if (M <= 32 || (few(2, 2) <= kGateWorkgroups && (M <= 64 || w.blocks >= 16))) return small(2, 2);
+    return large(M <= 64 ? kTile32x256 : tiles(128, 4) >= 208 ? kTile128x256 : kTile64x256);
   }
-  if (M <= 64) {
-    if (M <= 32 && columns <= 256) {
-      if (M > 16 && w.blocks >= 64) p.splits = 2;
-      else p.ct = 1;
-    }
-    return p;
-  }
-  if (tiles(32, 2) < (w.blocks >= 64 ? 230 : 130)) {
-    p.ct = 4;
-    return p;
-  }
-  p.few = false;
-  p.tile = tiles(128, 4) >= 512 ? kTile128x256 : tiles(64, 4) >= 224 ? kTile64x256 : tiles(64, 2) >= 176 ? kTile64x128 : kTile32x128;
-  return p;
+  const bool lengthy = w.blocks >= 40;
+  if (few(1, 1) <= 256) return small(1, 1);
+  if (M <= 16) return small(1, 2);
+  if (few(1, 2) <= 256) return M <= 32 && qlinear_in_halves(w) ? small(2, 2, 2) : small(1, 2);
+  if (few(1, 2) <= 640 && w.blocks <= 16) return small(1, 2);
+  if (few(2, 2) <= 256) return small(2, 2);
+  if (few(2, 4) <= 256) return small(2, 4);
+  if (M <= 64) return tiles(32, 2) <= 256 ? small(2, 2) : large(kTile32x128);
+  if (lengthy && M <= 256 && few(2, 4) <= 512) return small(2, 4);
+  if (tiles(64, 2) > 512 && tiles(64, 2) <= 768) return large(kTile64x128);
+  return large(tiles(128, 4) >= 208 ? kTile128x256 : tiles(64, 4) >= 192 ? kTile64x256 : tiles(64, 2) >= 176 ? kTile64x128 : kTile32x128);
 }
 
 static vvs_status plan_qlinear(const vvs_qlinear_config* cfg, QLinear* l) {
@@ -140,7 +149,7 @@ static vvs_status plan_qlinear(const vvs_qlinear_config* cfg, QLinear* l) {
   if ((int64_t)w.groups * ((g.max_rows + 31) / 32 + 1) * 64 > kMostThreads) return no(nullptr, VVS_ESIZE, "qlinear config: more outputs than a launch holds");
   if ((int64_t)w.groups * w.blocks >= (1 << 24)) return no(nullptr, VVS_ESIZE, "qlinear config: more weights than a launch holds");
   l->weight_bytes = align_up(qweights_bytes(w.groups, w.blocks), 256);
-  l->ws_bytes = qlinear_counter_bytes(w) + qlinear_part_bytes(w);
+  l->ws_bytes = kQlinearCounters + qlinear_part_bytes(w);
   return VVS_OK;
 }
 
@@ -326,8 +335,9 @@ vvs_status vvs_qlinear_apply(vvs_qlinear* ql, int32_t n_rows, const void* d_valu
   QProduct a{};
   a.w = l->w; a.M = n_rows;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
-  a.dtype = out_dtype; a.y = d_out; a.stride = (size_t)os; a.wide = wide_rows(d_out, os, out_dtype, 4);
-  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + qlinear_counter_bytes(l->w));
+  a.dtype = out_dtype; a.fast = out_dtype == VVS_BF16 && n_rows > 64;
+  a.y = d_out; a.stride = (size_t)os; a.wide = wide_rows(d_out, os, out_dtype, 4);
+  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + kQlinearCounters);
   launch_qlinear_product(a, plan_qlinear_product(l->w, n_rows), (hipStream_t)s);
   return launched(l, "qlinear apply");
 }
@@ -346,7 +356,7 @@ vvs_status vvs_qlinear_gate(vvs_qlinear* ql, int32_t n_rows, const void* d_value
   QProduct a{};
   a.w = l->w; a.M = n_rows;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
-  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + qlinear_counter_bytes(l->w));
+  a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + kQlinearCounters);
   a.y8 = QRowsOut{(uint8_t*)d_out_values, (uint8_t*)d_out_powers};
   launch_qlinear_product(a, plan_qlinear_product(l->w, n_rows), (hipStream_t)s);
   return launched(l, "qlinear gate");

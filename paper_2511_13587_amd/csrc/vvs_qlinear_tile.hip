@@ -256,6 +256,7 @@ static void tile_by(const QProduct& a, QTile t, hipStream_t s) {
 void launch_qlinear_tile(const QProduct& a, QTile t, hipStream_t s) {
   if (a.w.gated && t == kTile32x256) tile_t<1, 4, 2, false, true, float, 4>(a, s);
   else if (a.w.gated) tile_by<true, true, float>(a, t, s);
+  else if (a.dtype == VVS_BF16 && !a.fast) tile_t<1, 2, 2, false, false, bf16_t, 4>(a, s);      // (up to 64 rows: kTile32x128)
   else if (a.dtype == VVS_BF16) tile_by<true, false, bf16_t>(a, t, s);
   else if (a.fast) tile_by<true, false, float>(a, t, s);
   else tile_by<false, false, float>(a, t, s);

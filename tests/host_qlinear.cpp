@@ -60,15 +60,17 @@ void launch_qlinear_product(const QProduct& a, const QPlan& p, hipStream_t) {
   if (a.M < 1 || a.w.blocks != qrows_blocks(a.w.in)) abort();
   if (a.w.gated) fill(a.y8, a.M, a.w.out);
   else if (a.stride < (size_t)a.w.out) abort();
+  // maps that share a workspace: no map's sums lie where another's counters do
+  if ((char*)a.act - (char*)a.counters != (ptrdiff_t)kQlinearCounters) abort();
   if (p.few) {
     const int rows = (a.M + 16 * p.rt - 1) / (16 * p.rt), columns = a.w.groups * (4 / p.ct);
     if (rows > 65535 || (p.rt != 1 && p.rt != 2) || (p.ct != 1 && p.ct != 2 && p.ct != 4) || p.splits < 1) abort();
     if (a.w.gated) {
-      if (rows != 1 || p.ct != 2 || p.splits != 1 || a.w.groups % 4) abort();
-      memset(a.counters, 0, sizeof(uint32_t) * a.w.groups / 4);
+      if (p.ct != 2 || p.splits != 1 || a.w.groups % 4) abort();
+      if (sizeof(uint32_t) * rows * a.w.groups / 4 > kQlinearCounters) abort();
       memset(a.act, 0, sizeof(float) * a.M * a.w.groups * 32);
     } else if (p.splits > 1) {
-      memset(a.counters, 0, sizeof(uint32_t) * rows * columns);
+      if (sizeof(uint32_t) * rows * columns > kQlinearCounters) abort();
       memset(a.act, 0, sizeof(float) * (size_t)rows * columns * p.splits * p.rt * p.ct * 256);
     }
   } else if (a.w.gated && a.w.groups % 4) {
@@ -234,6 +236,10 @@ int main() {
     map(8192, 4096, 33, gated);
     map(65536, 40, 65, gated);
     map(130, 5000, 4200, gated);
+    map(5000, 2100, 40, gated);
+    map(2100, 2100, 300, gated);
+    map(2100, 5600, 70, gated);
+    map(300, 65536, 130, gated);
   }
   // which kernel
   auto plan = [](int in, int out, int gated, int M) { QWeights w{in, out, gated, qrows_blocks(in), 0, nullptr, nullptr}; w.groups = (out + w.unit() - 1) / w.unit(); if (gated) w.groups = (w.groups + 3) & ~3; return plan_qlinear_product(w, M); };
@@ -251,6 +257,20 @@ int main() {
   { QPlan p = plan(4096, 11008, 1, 60); CHECK(!p.few && p.tile == kTile32x256); }
   { QPlan p = plan(4096, 11008, 1, 128); CHECK(!p.few && p.tile == kTile64x256); }
   { QPlan p = plan(4096, 11008, 1, 4093); CHECK(!p.few && p.tile == kTile128x256); }
+  { QPlan p = plan(1280, 1280, 0, 28); CHECK(p.few && p.rt == 1 && p.ct == 1); }
+  { QPlan p = plan(4096, 2048, 0, 60); CHECK(p.few && p.rt == 1 && p.ct == 2); }
+  { QPlan p = plan(1280, 1280, 0, 256); CHECK(p.few && p.rt == 1 && p.ct == 2); }
+  { QPlan p = plan(4096, 2048, 0, 128); CHECK(p.few && p.rt == 2 && p.ct == 2 && p.splits == 1); }
+  { QPlan p = plan(4096, 12288, 0, 28); CHECK(p.few && p.rt == 2 && p.ct == 4); }
+  { QPlan p = plan(4096, 16384, 0, 48); CHECK(p.few && p.rt == 2 && p.ct == 2); }
+  { QPlan p = plan(4096, 32768, 0, 48); CHECK(!p.few && p.tile == kTile32x128); }
+  { QPlan p = plan(4096, 12288, 0, 432); CHECK(!p.few && p.tile == kTile64x128); }
+  { QPlan p = plan(4096, 16384, 0, 600); CHECK(!p.few && p.tile == kTile128x256); }
+  { QPlan p = plan(768, 2048, 1, 48); CHECK(p.few && p.rt == 1); }
+  { QPlan p = plan(4096, 11008, 1, 28); CHECK(p.few && p.rt == 2); }
+  { QPlan p = plan(4096, 2048, 1, 128); CHECK(p.few && p.rt == 2); }
+  { QPlan p = plan(1280, 3456, 1, 128); CHECK(!p.few && p.tile == kTile64x256); }
+  { QPlan p = plan(128, 344, 1, 128); CHECK(!p.few && p.tile == kTile32x256); }
 
   // configs
   vvs_qlinear_config g{256, 128, 40, 0, VVS_FP32};

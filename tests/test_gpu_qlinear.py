@@ -107,6 +107,27 @@ def test_gate_at_odd_sizes(rows, width, out):
     check_gate(y, x, w, fast=rows > 64)
 
 
+# further rows, columns and lengths at which another kernel takes over: tiles of 16 x 16 and 16 x 32 for more than one row tile, 32 x 32 whole and in halves, 32 x 64, tiles for few rows of many columns
+@pytest.mark.parametrize("rows,width,out", [(17, 500, 300), (64, 700, 400), (60, 2100, 2050), (100, 1000, 1290), (28, 5200, 2100), (17, 5121, 4096), (100, 4200, 2000), (60, 4100, 4090), (30, 4096, 9000), (100, 2200, 4100),
+                                            (200, 5200, 4100), (33, 300, 33000), (64, 1030, 40001), (300, 400, 16390), (600, 390, 16400)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_product_where_another_kernel_takes_over(rows, width, out, dtype):
+    from paper_2511_13587_amd import binding as vb
+    lin, r, x, (w,) = _linear(vb, rows, width, out, seed=rows)
+    y = torch.full((rows, out), 3.0, dtype=TYPES[dtype], device="cuda")
+    lin.vvs_qlinear_apply(r, y)
+    check_product(y, x, w, TYPES[dtype], fast=rows > 64 and dtype == "bf16")
+
+
+@pytest.mark.parametrize("rows,width,out", [(17, 900, 900), (48, 1100, 1030), (33, 640, 2100), (60, 2100, 5600), (100, 2100, 2050), (130, 2049, 1000), (40, 200, 100), (300, 256, 300), (280, 2100, 600), (440, 400, 11000)])
+def test_gate_where_another_kernel_takes_over(rows, width, out):
+    from paper_2511_13587_amd import binding as vb
+    lin, r, x, w = _linear(vb, rows, width, out, gated=True, seed=rows)
+    y = vb.QRows(rows, out)
+    lin.vvs_qlinear_gate(r, y)
+    check_gate(y, x, w, fast=rows > 64)
+
+
 @pytest.mark.parametrize("rows,width,out", [(14, 4096, 1024), (16, 8300, 150), (28, 1280, 3456), (32, 8449, 129), (48, 768, 2048), (64, 8400, 1000), (432, 1280, 3456), (300, 9000, 500), (700, 512, 1100),
                                             (4100, 640, 1500), (4099, 8321, 1600)])
 def test_gate(rows, width, out):

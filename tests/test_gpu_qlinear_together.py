@@ -164,6 +164,35 @@ def test_maps_share_a_workspace_on_a_stream():
         vb.QLinear(1280, 700, 30, vb.VVS_BF16, gated=True, workspace=ws[:1000])
 
 
+def test_maps_of_different_sizes_share_a_workspace():
+    """The sums of one map (a contraction in halves, 64 rows of hidden units) do not lie where the counters of a much wider one are."""
+    from paper_2511_13587_amd import binding as vb
+    calls = [(28, 5200, 2100, False), (14, 300, 20000, True), (20, 5200, 4000, False), (48, 300, 900, True), (32, 300, 20000, True)]
+    ws = torch.empty(max(vb.vvs_qlinear_query_sizes(vb.VvsQLinearConfig(k, n, m, int(g), vb.VVS_BF16))[1] for m, k, n, g in calls), dtype=torch.uint8, device="cuda")
+    maps = []
+    for i, (m, k, n, g) in enumerate(calls):
+        w = [(_normal((k, n), 70 + i + j) * k ** -0.5).bfloat16().cuda() for j in range(2 if g else 1)]
+        r = vb.QRows(m, k)
+        qc.put(r, _normal((m, k), 80 + i))
+        both = [vb.QLinear(k, n, m, vb.VVS_BF16, gated=g), vb.QLinear(k, n, m, vb.VVS_BF16, gated=g, workspace=ws)]
+        outs = []
+        for lin in both:
+            lin.vvs_qlinear_load(*w)
+            outs.append(vb.QRows(m, n) if g else torch.empty((m, n), device="cuda"))
+        maps.append((r, both, outs, g))
+    for _ in range(3):
+        for r, both, outs, g in maps:
+            for lin, y in zip(both, outs):
+                for t in (y.values, y.powers) if g else (y,):
+                    t.view(torch.uint8).fill_(255)
+                lin.vvs_qlinear_gate(r, y) if g else lin.vvs_qlinear_apply(r, y)
+        for _, _, (a, b), g in maps:
+            if g:
+                assert torch.equal(a.values.view(torch.uint8), b.values.view(torch.uint8)) and torch.equal(a.powers, b.powers)
+            else:
+                assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
 def test_two_maps_with_workspaces_of_their_own_run_at_once():
     """On two streams, again and again: the same bits."""
     from paper_2511_13587_amd import binding as vb
