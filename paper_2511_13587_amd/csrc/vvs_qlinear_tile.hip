@@ -16,15 +16,21 @@ __device__ __forceinline__ void qtile_of(int id, int MT, int NT, int* tile_m, in
   *tile_m = band * 8 + rem % h;
 }
 
-// A workgroup of WM x WN waves makes 16 RT WM rows by WN groups of 64 columns; a wave 16 RT rows of one group, whose weights come straight into its operand registers, one block of 128 contraction
-// values ahead.  The rows' bytes of a block pass through LDS, two stages: while one is multiplied the next is on its way (lds_dma16).  16 bytes c of row r lie at place c ^ (r & 7) of the row,
-// so that the 8 lanes that LDS serves at a time read 8 different places.
+// Y^T = W^T X^T.  A workgroup of WM x WN waves makes 16 RT WM rows by WN groups of 64 columns; a wave 16 RT rows of one group, whose weights nobody else in the workgroup needs: they come straight into its operand
+// registers, NB - 1 blocks of 128 contraction values ahead.  The rows' bytes of a block are every wave's, and pass through LDS (lds_dma16, no registers), two or three blocks ahead.  Bound by the matrix cores: 8192 rows,
+// 4096 -> 12288, 825 GFLOP in 337 to 354 us, 2.3 to 2.4 PFLOP/s (an 8192^3 product in e4m3 by the library 2.7), the matrix cores busy 62 % of the time; a tile of 128 x 256 reads 48 KB a block for 8.4 MFLOP, and
+// 85 % of its requests to the L2 are hits.  Few blocks of 64 rows wait for loads instead: NB = 4 (432 rows, 1280 -> 3840 8.7 us).
+// Parts of that large product left out, in turn, of 385 us (all of the following: 223): powers of two from memory at every block 353, the requests for rows 350, for weights 321, reads of LDS 379.  Hence powers in
+// LDS (362), and two row tiles on their way from there (354).  Requests at the start of a block instead of between products 420.  Tried and slower: 256 x 256 by 8 waves 448, 4 waves that have a SIMD each 405, a
+// higher priority for waves at their products 403, bands of 4 or 16 row tiles 397 and 404.
 // FAST: the e4m3 numbers go into the matrix cores as they are, with both powers of two as scales (16x16x128, twice the rate of bf16 and fewer instructions).  These products lose what lies 2^13
-// below the largest of a few neighbours: 1.3e-5 in the 2-norm, 200 times below the rounding of bf16 outputs and 3000 times below that of 8 bits.  Outputs in fp32 take !FAST: bf16 operands.
+// below the largest of a few neighbours: 1.3e-5 in the 2-norm, 200 times below the rounding of bf16 outputs and 3000 times below that of 8 bits.  Outputs in fp32, and up to 64 rows of any, take !FAST: bf16
+// operands, exact.
 constexpr int kPowerBlocks = 64, kPowerStride = kPowerBlocks / 4 + 1;   // (an odd number of words: 16 rows on 16 banks)
 
-// Place of 16 bytes c of row r in LDS: c ^ swizzle(r).  LDS serves a wave's 16-byte reads 16 lanes at a time - lanes 0-3, 12-15, 20-23, 24-27; 4-7, 8-11, 16-19, 28-31; and the same 32 on - from 64
-// banks, two rows of 128 bytes: rows 4 to 11 of a tile go by with the other half of the contraction than the rest.  (r & 7: two lanes on every bank, by SQ_LDS_BANK_CONFLICT; so none.)
+// Place of 16 bytes c of row r in LDS: c ^ swizzle(r), so that the lanes that LDS serves at a time read different banks.  It serves a wave's 16-byte reads 16 lanes at a time - lanes 0-3, 12-15, 20-23, 24-27;
+// 4-7, 8-11, 16-19, 28-31; and the same 32 on - from 64 banks, two rows of 128 bytes: rows 4 to 11 of a tile go by with the other half of the contraction than the rest.  (r & 7: two lanes on every bank, by
+// SQ_LDS_BANK_CONFLICT; so none.)
 __device__ __forceinline__ int swizzle(int r) { return ((r >> 1) & 7) ^ (((r + 4) >> 3 & 1) << 1); }
 
 template <int WM, int WN, int RT, bool FAST, bool GATED, typename T, int NB>

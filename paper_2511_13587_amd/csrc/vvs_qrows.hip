@@ -1,4 +1,5 @@
-// Rows in 8 bits: rounding, norm with the residual's addition, reading back.
+// Rows in 8 bits: rounding, norm with the residual's addition, reading back.  All three are bound by HBM once there are some hundreds of rows and by the launch before; elements go through once, 8 to a thread,
+// so that 16 neighbouring lanes hold a block and its largest value is found by four exchanges inside a row of 16 lanes (round_block), without LDS.
 #include "vvs_qlinear_device.h"
 
 namespace vvs {
@@ -24,7 +25,8 @@ __device__ __forceinline__ void write_row8(T* row, int at, int n, bool wide, con
     if (at + j < n) st(row + at + j, v[j]);
 }
 
-// One unit of 16 lanes per block; blocks behind a row's last one (their number is rounded up to 4) are powers alone.  Bound by HBM.
+// y = e4m3(x / 2^E), E the least power that brings a block's largest value to 448 or less.  One unit of 16 lanes per block; blocks behind a row's last one (their number is rounded up to 4) are powers
+// alone.  8191 rows of 4096 in bf16: 101 MB in 18.5 us, 5.5 TB/s (a copy of 4 GiB 4.7; part of these rows is still in the last-level cache); 432 rows of 1280 3.1 us.
 template <typename T>
 __global__ __launch_bounds__(256) void k_qrows_round(QRound a) {
   const int powers = qrows_powers(a.width), blocks = qrows_blocks(a.width);
@@ -50,6 +52,7 @@ void launch_qrows_round(const QRound& a, hipStream_t s) {
   else hipLaunchKernelGGL(k_qrows_round<float>, grid, dim3(256), 0, s, a);
 }
 
+// x = y 2^E, the same units.  8191 rows of 4096 to bf16: 101 MB in 16.6 us, 6.1 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void k_qrows_read(QRowsRead a) {
   const int powers = qrows_powers(a.width), blocks = qrows_blocks(a.width);
@@ -76,7 +79,9 @@ __device__ __forceinline__ void read_any8(const void* row, int dtype, int at, in
   else read_row8((const float*)row, at, n, wide, v);
 }
 
-// One workgroup per row, which stays in registers: V times 8 elements per thread.  x + delta is rounded to the residual's type, and what is normalised is what is kept.
+// x' = x + delta, y = x' g / sqrt(mean(x'^2) + eps), in 8 bits.  One workgroup per row, which stays in registers, V times 8 elements per thread, so that x and delta are read once and nothing is read back; a
+// barrier for the sum is the only meeting of the waves.  x' is rounded to the residual's type, and what is normalised is what is kept.
+// 8192 rows of 4096, x, delta and x' in bf16: 235 MB in 47.8 us, 4.9 TB/s, where a copy of 4 GiB has 4.7; few rows wait for one chain of load, sum, barrier, rounding: 10 rows of 128 3.8 us, 432 rows of 1280 4.5.
 template <int V, int MOST>
 __global__ __launch_bounds__(MOST) void k_qrows_norm(QNorm a) {
   __shared__ float red[16];
