@@ -106,8 +106,9 @@ typedef struct {
   int32_t weight_kind;           /* VVS_WEIGHTS_SAME: weights have the context's dtype;
                                     VVS_WEIGHTS_E4M3: a layer's seven matrices are held in 8 bits, and what they are multiplied by - the norms' outputs, the
                                       attention's (rounded to the dtype first), the activations - is rounded to 8 bits as well (see vvs_qrows below); residual stream
-                                      and all else are as ever, products too, but in bf16 contexts from 65 rows on (as those of vvs_qlinear_apply for bf16).  For contexts whose steps are bound by the weights' bytes.  Embeddings, gains and the output head
-                                      keep the dtype.  Layers run as separate launches (no drafter contexts; d_model a multiple of 64, d_ff at most 65536) */
+                                      and all else are as ever.  Products of e4m3 numbers enter their sums whole, but from 65 rows on, in bf16 contexts and in front of
+                                      the activations, as at vvs_qlinear_apply and vvs_qlinear_gate.  For contexts whose steps are bound by the weights' bytes.
+                                      Embeddings, gains and the output head keep the dtype.  Layers run as separate launches (no drafter contexts; d_model a multiple of 64, d_ff at most 65536) */
 } vvs_config;
 enum { VVS_NORM_AUTO = 0, VVS_NORM_SEPARATE = 1 };
 enum { VVS_CACHE_SAME = 0, VVS_CACHE_E4M3 = 1 };

@@ -96,6 +96,9 @@ struct QPlan {
 };
 QPlan plan_qlinear_product(const QWeights& w, int M);
 
+// Whether a product may take the matrix instructions for e4m3 (outputs of type `dtype`, or of a context of it)
+inline int qlinear_fast(int dtype, int M) { return dtype == VVS_BF16 && M > 64; }
+
 struct QProduct {
   QWeights w;
   int M;

@@ -55,7 +55,7 @@ void launch_context_product(Ctx* c, int layer, QMap m, int M, float* out, hipStr
   QProduct a{};
   a.w = map_of(c, layer, m); a.M = M;
   a.x = m == kMapDown ? QRowsIn{act.values, act.powers} : QRowsIn{h.values, h.powers};
-  a.dtype = VVS_FP32; a.fast = c->cfg.dtype == VVS_BF16;         // (the sums go on in fp32, but what they are of was rounded to 2^-4, and in bf16 contexts what comes of them is to 2^-9)
+  a.dtype = VVS_FP32; a.fast = qlinear_fast(c->cfg.dtype, M);         // (the sums go on in fp32, but what they are of was rounded to 2^-4, and in bf16 contexts what comes of them is to 2^-9)
   a.y = out; a.stride = a.w.out; a.wide = 1;
   a.y8 = act;
   a.counters = (uint32_t*)(c->ws + c->w.map_counters); a.act = (float*)(c->ws + c->w.map_parts);

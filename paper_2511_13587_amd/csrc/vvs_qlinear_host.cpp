@@ -335,7 +335,7 @@ vvs_status vvs_qlinear_apply(vvs_qlinear* ql, int32_t n_rows, const void* d_valu
   QProduct a{};
   a.w = l->w; a.M = n_rows;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
-  a.dtype = out_dtype; a.fast = out_dtype == VVS_BF16 && n_rows > 64;
+  a.dtype = out_dtype; a.fast = qlinear_fast(out_dtype, n_rows);
   a.y = d_out; a.stride = (size_t)os; a.wide = wide_rows(d_out, os, out_dtype, 4);
   a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + kQlinearCounters);
   launch_qlinear_product(a, plan_qlinear_product(l->w, n_rows), (hipStream_t)s);

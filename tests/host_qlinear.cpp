@@ -217,6 +217,8 @@ static void map(int in, int out, int max_rows, int gated) {
     if (n <= max_rows) {
       WANT(call(n), VVS_OK);
       CHECK(g_product.M == n && g_product.w.in == in && g_product.w.out == out);
+      if (!gated) CHECK(g_product.fast == (n > 64));             // (outputs in bf16)
+      if (n <= 64) CHECK(g_plan.few || g_plan.tile == (gated ? kTile32x256 : kTile32x128));    // the tiles that multiply whole
     }
   WANT(call(max_rows + 1), VVS_ESIZE);
   WANT(call(0), VVS_EINVAL);
