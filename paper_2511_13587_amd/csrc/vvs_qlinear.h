@@ -90,11 +90,14 @@ struct QWeightsRead {
 // Which kernel makes a product
 enum QTile { kTile128x256, kTile64x256, kTile64x128, kTile32x128, kTile32x256 };   // rows x packed columns of a workgroup
 struct QPlan {
-  bool few;                         // k_qlinear_few: rt tiles of 16 rows, ct of 16 columns, the contraction cut into splits; else k_qlinear_tile
+  bool few;                         // k_qlinear_few: rt tiles of 16 rows, ct of 16 columns, the contraction cut into splits; else k_qlinear_tile, whose workgroups cut it into splits
   int rt, ct, splits;
   QTile tile;
 };
-QPlan plan_qlinear_product(const QWeights& w, int M);
+QPlan plan_qlinear_product(const QWeights& w, int M, bool fast);   // fast: see QProduct (gated: no matter)
+
+// Shares of the contraction that a workgroup of k_qlinear_tile has waves for: 1, 2 or 4, and each at least a block
+inline int qlinear_shares(const QWeights& w, int wanted) { return wanted >= 4 && w.blocks >= 4 ? 4 : wanted >= 2 && w.blocks >= 2 ? 2 : 1; }
 
 // Whether a product may take the matrix instructions for e4m3 (outputs of type `dtype`, or of a context of it)
 inline int qlinear_fast(int dtype, int M) { return dtype == VVS_BF16 && M > 64; }
@@ -119,7 +122,7 @@ void launch_qrows_read(const QRowsRead& a, hipStream_t s);
 void launch_qlinear_load(const QLoad& a, hipStream_t s);
 void launch_qlinear_read(const QWeightsRead& a, hipStream_t s);
 void launch_qlinear_product(const QProduct& a, const QPlan& p, hipStream_t s);
-void launch_qlinear_tile(const QProduct& a, QTile t, hipStream_t s);
+void launch_qlinear_tile(const QProduct& a, QTile t, int shares, hipStream_t s);
 
 // Contexts with VVS_WEIGHTS_E4M3 (vvs_qlinear_ctx.hip): a layer's maps, in the order of its projections
 enum QMap { kMapQkv, kMapO, kMapGate, kMapDown };

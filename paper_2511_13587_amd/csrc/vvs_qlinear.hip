@@ -246,7 +246,7 @@ static void few(const QProduct& a, const QPlan& p, hipStream_t s) {
 }
 
 void launch_qlinear_product(const QProduct& a, const QPlan& p, hipStream_t s) {
-  if (!p.few) launch_qlinear_tile(a, p.tile, s);
+  if (!p.few) launch_qlinear_tile(a, p.tile, p.splits, s);
   else if (a.w.gated && p.rt == 1) few_t<4, 1, 2, true, float>(a, 1, s);
   else if (a.w.gated) few_t<4, 2, 2, true, float>(a, 1, s);
   else if (a.dtype == VVS_BF16) few<bf16_t>(a, p, s);

@@ -59,7 +59,7 @@ void launch_context_product(Ctx* c, int layer, QMap m, int M, float* out, hipStr
   a.y = out; a.stride = a.w.out; a.wide = 1;
   a.y8 = act;
   a.counters = (uint32_t*)(c->ws + c->w.map_counters); a.act = (float*)(c->ws + c->w.map_parts);
-  launch_qlinear_product(a, plan_qlinear_product(a.w, M), s);
+  launch_qlinear_product(a, plan_qlinear_product(a.w, M, a.fast), s);
 }
 
 }  // namespace vvs

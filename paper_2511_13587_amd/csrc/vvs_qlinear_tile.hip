@@ -19,38 +19,48 @@ __device__ __forceinline__ void qtile_of(int id, int MT, int NT, int* tile_m, in
 // Y^T = W^T X^T.  A workgroup of WM x WN waves makes 16 RT WM rows by WN groups of 64 columns; a wave 16 RT rows of one group, whose weights nobody else in the workgroup needs: they come straight into its operand
 // registers, NB - 1 blocks of 128 contraction values ahead.  The rows' bytes of a block are every wave's, and pass through LDS (lds_dma16, no registers), two or three blocks ahead.  Bound by the matrix cores: 8192 rows,
 // 4096 -> 12288, 825 GFLOP in 337 to 354 us, 2.3 to 2.4 PFLOP/s (an 8192^3 product in e4m3 by the library 2.7), the matrix cores busy 62 % of the time; a tile of 128 x 256 reads 48 KB a block for 8.4 MFLOP, and
-// 85 % of its requests to the L2 are hits.  Few blocks of 64 rows wait for loads instead: NB = 4 (432 rows, 1280 -> 3840 8.7 us).
+// 85 % of its requests to the L2 are hits.  Few tiles wait for loads
+// instead, 0.6 us per block with three on their way: NB = 4, and KS shares of the contraction with waves, stages and powers of their own, whose sums the first adds up through LDS in their order (432 rows: 1280 ->
+// 3840 in one share 8.0 us; 3456 -> 1280 in four 10.8, one 12.2; 11008 -> 4096 in four 39.5, one 54.8).  Powers of the first blocks are asked for in front of everything else: 432 rows, 1280 -> 3840 9.3 -> 8.3.
 // Parts of that large product left out, in turn, of 385 us (all of the following: 223): powers of two from memory at every block 353, the requests for rows 350, for weights 321, reads of LDS 379.  Hence powers in
 // LDS (362), and two row tiles on their way from there (354).  Requests at the start of a block instead of between products 420.  Tried and slower: 256 x 256 by 8 waves 448, 4 waves that have a SIMD each 405, a
 // higher priority for waves at their products 403, bands of 4 or 16 row tiles 397 and 404.
 // FAST: the e4m3 numbers go into the matrix cores as they are, with both powers of two as scales (16x16x128, twice the rate of bf16 and fewer instructions).  These products lose what lies 2^13
 // below the largest of a few neighbours: 1.3e-5 in the 2-norm, 200 times below the rounding of bf16 outputs and 3000 times below that of 8 bits.  Outputs in fp32, and up to 64 rows of any, take !FAST: bf16
 // operands, exact.
-constexpr int kPowerBlocks = 64, kPowerStride = kPowerBlocks / 4 + 1;   // (an odd number of words: 16 rows on 16 banks)
+constexpr int power_blocks(int shares) { return shares > 1 ? 32 : 64; }                  // whose powers lie in LDS at a time
+constexpr int power_stride(int shares) { return power_blocks(shares) / 4 + 1; }          // (an odd number of words: 16 rows on 16 banks)
+// LDS of a share: rows [stages][BM][128 bytes], then powers of its next blocks: [BM][stride], [64 WN][stride], four in a word
+constexpr int tile_stages(int NB) { return NB == 2 ? 3 : NB; }
+constexpr int share_lds(int BM, int WN, int NB, int shares) { return tile_stages(NB) * BM * kQRowBlock + (BM + 64 * WN) * power_stride(shares) * 4; }
 
 // Place of 16 bytes c of row r in LDS: c ^ swizzle(r), so that the lanes that LDS serves at a time read different banks.  It serves a wave's 16-byte reads 16 lanes at a time - lanes 0-3, 12-15, 20-23, 24-27;
 // 4-7, 8-11, 16-19, 28-31; and the same 32 on - from 64 banks, two rows of 128 bytes: rows 4 to 11 of a tile go by with the other half of the contraction than the rest.  (r & 7: two lanes on every bank, by
 // SQ_LDS_BANK_CONFLICT; so none.)
 __device__ __forceinline__ int swizzle(int r) { return ((r >> 1) & 7) ^ (((r + 4) >> 3 & 1) << 1); }
 
-template <int WM, int WN, int RT, bool FAST, bool GATED, typename T, int NB>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(QProduct a, int MT, int NT) {
-  constexpr int BM = 16 * RT * WM, NW = WM * WN, NQ = BM / 8 / NW, kStages = NB == 2 ? 3 : NB;
-  static_assert(BM <= 64 * NW && BM % (8 * NW) == 0 && (!GATED || WN == 4), "");
-  extern __shared__ uint4 lds[];                     // rows [kStages][BM][128 bytes], then powers of kPowerBlocks blocks: [BM][17], [64 WN][17], four in a word
-  int* const xpow = (int*)((char*)lds + kStages * BM * kQRowBlock);
+template <int WM, int WN, int RT, bool FAST, bool GATED, typename T, int NB, int KS>
+__global__ __launch_bounds__(64 * WM * WN * KS, 2) void k_qlinear_tile(QProduct a, int MT, int NT) {
+  constexpr int BM = 16 * RT * WM, NW = WM * WN, NQ = BM / 8 / NW, kStages = tile_stages(NB), kPowerBlocks = power_blocks(KS), kPowerStride = power_stride(KS);
+  static_assert(BM <= 64 * NW && BM % (8 * NW) == 0 && (!GATED || WN == 4) && (NW & (NW - 1)) == 0, "");
+  extern __shared__ uint4 lds[];
+  const int all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = KS == 1 ? 0 : all_waves / NW, wave = KS == 1 ? all_waves : all_waves % NW;
+  const int tid = KS == 1 ? threadIdx.x : threadIdx.x & (64 * NW - 1), lane = tid & 63, i = lane & 15, g = lane >> 4;
+  char* const my_lds = (char*)lds + share * share_lds(BM, WN, NB, KS);
+  int* const xpow = (int*)(my_lds + kStages * BM * kQRowBlock);
   int* const wpow = xpow + BM * kPowerStride;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
   const int wm = wave / WN, wn = wave % WN;
   int tile_m, tile_n;
   qtile_of(blockIdx.x, MT, NT, &tile_m, &tile_n);
-  const int m0 = tile_m * BM, blocks = a.w.blocks, powers = qrows_powers(a.w.in);
+  // this share's blocks: first .. first + blocks - 1, of `most` at most
+  const int m0 = tile_m * BM, powers = qrows_powers(a.w.in), first = KS == 1 ? 0 : share * a.w.blocks / KS, blocks = KS == 1 ? a.w.blocks : (share + 1) * a.w.blocks / KS - first;
+  const int most = KS == 1 ? blocks : (a.w.blocks + KS - 1) / KS;
   const int own_group = tile_n * WN + wn, group = min(own_group, a.w.groups - 1);
-  const size_t width = (size_t)blocks * kQRowBlock;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  const size_t width = (size_t)a.w.blocks * kQRowBlock;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)my_lds;
 
   // rows behind the last one repeat it
-  const uint8_t* const tile_rows = a.x.values + (size_t)m0 * width;
+  const uint8_t* const tile_rows = a.x.values + (size_t)m0 * width + first * kQRowBlock;
   uint32_t src[NQ];
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
@@ -58,17 +68,41 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(QProduct a, in
     src[q] = (uint32_t)(min(r, a.M - 1 - m0) * (int)width + ((lane & 7) ^ swizzle(r)) * 16);
   }
   auto request = [&](int kb, int stage, int q) { lds_dma16(tile_rows + (size_t)kb * kQRowBlock, src[q], lds0 + stage * BM * kQRowBlock + (wave * NQ + q) * 1024); };
-  const uint8_t* const wsrc = a.w.data + a.w.tile_at(group, 0, 0);
+  const uint8_t* const wsrc = a.w.data + a.w.tile_at(group, first, 0);
   auto weights = [&](int kb, u32x4 (&w)[4][2], int c, int h) { w[c][h] = *(const u32x4*)(wsrc + (size_t)kb * 8192 + c * 2048 + h * 1024 + lane * 16); };
-  // powers of blocks k0 .. k0 + kPowerBlocks - 1 into LDS: bytes from memory at every block were a tenth of the time of a large product (384 us without, 353 us)
-  auto fetch_powers = [&](int k0) {
-    const int words = min(kPowerBlocks, powers - k0) / 4;
-    for (int u = tid; u < BM * words; u += 64 * NW) {
-      const int r = u / words, d = u % words;
-      xpow[r * kPowerStride + d] = *(const int*)(a.x.powers + (size_t)min(m0 + r, a.M - 1) * powers + k0 + d * 4);
+  // powers of blocks k0 .. k0 + kPowerBlocks - 1 of the share into LDS: bytes from memory at every block were a tenth of the time of a large product (384 us without, 353 us).  A share that begins inside a word of
+  // four moves the bytes to where they are in its own count.
+  constexpr int kLanes = 64 * NW / BM;                           // threads that a row's words are dealt to
+  struct Powers { int x[4], w[8]; };
+  auto load_powers = [&](int k0, int d0) {                       // words d0 .. d0 + 7 of the columns', d0 / 2 * kLanes and on of the rows'
+    const int words = (min(kPowerBlocks, blocks - k0) + 3) / 4, at = (first + k0) / 4, last = powers / 4 - 1, sh = 8 * (first & 3);
+    auto word = [&](const int* p, int d, int step) {
+      if constexpr (KS == 1) return p[(size_t)(at + d) * step];
+      else return (int)(((uint64_t)(uint32_t)p[(size_t)min(at + d + 1, last) * step] << 32 | (uint32_t)p[(size_t)(at + d) * step]) >> sh);
+    };
+    Powers v;
+    const int* const px = (const int*)(a.x.powers + (size_t)min(m0 + tid % BM, a.M - 1) * powers);
+    const int* const pw = (const int*)(a.w.powers + a.w.power_at(group, 0, 0)) + lane;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.x[j] = word(px, min(d0 / 2 * kLanes + tid / BM + j * kLanes, words - 1), 1);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v.w[j] = word(pw, min(d0 + j, words - 1), 64);
+    return v;
+  };
+  auto store_powers = [&](const Powers& v, int k0, int d0) {
+    const int words = (min(kPowerBlocks, blocks - k0) + 3) / 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = d0 / 2 * kLanes + tid / BM + j * kLanes;
+      if (d < words) xpow[tid % BM * kPowerStride + d] = v.x[j];
     }
-    const int* p = (const int*)(a.w.powers + a.w.power_at(group, k0, 0));
-    for (int d = 0; d < words; ++d) wpow[(wn * 64 + lane) * kPowerStride + d] = p[d * 64 + lane];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (d0 + j < words) wpow[(wn * 64 + lane) * kPowerStride + d0 + j] = v.w[j];
+  };
+  static_assert(kLanes >= 2, "");
+  auto fetch_powers = [&](int k0, int from) {
+    for (int d0 = from; d0 * 4 < min(kPowerBlocks, blocks - k0); d0 += 8) store_powers(load_powers(k0, d0), k0, d0);
   };
 
   floatx4 acc[4][RT];
@@ -79,6 +113,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(QProduct a, in
 
   u32x4 w[NB][4][2];
   int ws[4];
+  const Powers ahead = load_powers(0, 0);              // (the loads that follow do not wait for these to be in LDS)
   // ahead: blocks 0 and 1 of the rows, 0 of the weights; NB = 4: 0 to 2 of both
 #pragma unroll
   for (int k = 0; k < (NB == 2 ? 2 : 3); ++k) {
@@ -89,9 +124,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(QProduct a, in
       for (int c = 0; c < 8; ++c) weights(min(k, blocks - 1), w[k], c >> 1, c & 1);
     }
   }
-  fetch_powers(0);
+  store_powers(ahead, 0, 0);
+  fetch_powers(0, 8);
 
-  const char* const mine = (const char*)lds + (wm * RT * 16 + i) * kQRowBlock;
+  const char* const mine = my_lds + (wm * RT * 16 + i) * kQRowBlock;
   const int* const mine_xpow = xpow + (wm * RT * 16 + i) * kPowerStride;
   const int* const mine_wpow = wpow + (wn * 64 + i) * kPowerStride;
   const int sw = swizzle(i);
@@ -174,22 +210,52 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(QProduct a, in
     }
     if (NB == 2) st_next = st == 2 ? 0 : st + 1;
   };
-  for (int k4 = 0; k4 < blocks; k4 += 4) {
+  auto step_or_wait = [&](auto uc, int k4) {
+    const int k = k4 + decltype(uc)::value;
+    if (k < blocks) step(uc, k4);
+    else if (KS > 1 && k < most) asm volatile("s_barrier" ::: "memory");        // (another share has one more)
+  };
+  for (int k4 = 0; k4 < most; k4 += 4) {
     if (k4 && (k4 & (kPowerBlocks - 1)) == 0) {
       asm volatile("s_barrier" ::: "memory");       // all have read the last ones: their products were waited for
-      fetch_powers(k4);
+      if (k4 < blocks) fetch_powers(k4, 0);
     }
-    step(std::integral_constant<int, 0>{}, k4);
-    if (k4 + 1 < blocks) step(std::integral_constant<int, 1>{}, k4);
-    if (k4 + 2 < blocks) step(std::integral_constant<int, 2>{}, k4);
-    if (k4 + 3 < blocks) step(std::integral_constant<int, 3>{}, k4);
+    step_or_wait(std::integral_constant<int, 0>{}, k4);
+    step_or_wait(std::integral_constant<int, 1>{}, k4);
+    step_or_wait(std::integral_constant<int, 2>{}, k4);
+    step_or_wait(std::integral_constant<int, 3>{}, k4);
   }
   // no request may be under way when LDS is used again or given back
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
+  // the shares' sums, added in their order by the first
+  constexpr int kJoin = (KS - 1) * NW * 4 * RT * 1024;           // bytes
+  if constexpr (KS > 1) {
+    float4* const join = (float4*)lds + wave * 4 * RT * 64 + lane;
+    if (share) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) join[((share - 1) * NW * 4 * RT + c * RT + r) * 64] = make_float4(acc[c][r][0], acc[c][r][1], acc[c][r][2], acc[c][r][3]);
+    }
+    __syncthreads();
+    if (share) {
+      if constexpr (!GATED) return;
+    } else {
+      for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            const float4 p = join[(k * NW * 4 * RT + c * RT + r) * 64];
+            acc[c][r] += floatx4{p.x, p.y, p.z, p.w};
+          }
+    }
+  }
+
   if constexpr (GATED) {
     // a wave's 32 hidden units, 8 in a row per lane; the largest of a block of 128 is that of four waves
-    float* const top = (float*)lds;                  // [4][BM]
+    float* const top = (float*)((char*)lds + kJoin);   // [4][BM]
     float v[RT][8];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -200,11 +266,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(QProduct a, in
         t = fmaxf(t, finite(v[r][j]) ? fabsf(v[r][j]) : 0.f);
       }
       t = rows_max(t);
-      if (g == 0) top[wn * BM + (wm * RT + r) * 16 + i] = t;
+      if (g == 0 && share == 0) top[wn * BM + (wm * RT + r) * 16 + i] = t;
     }
     __syncthreads();
     const int out_blocks = qrows_blocks(a.w.out), out_powers = qrows_powers(a.w.out);
-    if (tile_n < out_blocks) {
+    if (tile_n < out_blocks && share == 0) {
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const int lm = (wm * RT + r) * 16 + i, m = m0 + lm;
@@ -239,33 +305,48 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_qlinear_tile(QProduct a, in
   }
 }
 
-template <int WM, int WN, int RT, bool FAST, bool GATED, typename T, int NB>
+template <int WM, int WN, int RT, bool FAST, bool GATED, typename T, int NB, int KS>
 static void tile_t(const QProduct& a, hipStream_t s) {
   constexpr int BM = 16 * RT * WM;
-  constexpr size_t lds = (NB == 2 ? 3 : NB) * BM * kQRowBlock + (BM + 64 * WN) * kPowerStride * 4;
+  constexpr size_t lds = KS * share_lds(BM, WN, NB, KS);
+  static_assert(lds >= (KS - 1) * WM * WN * 4 * RT * 1024 + (GATED ? 16 * BM : 0) && lds <= kMostLds, "");
   const int MT = (a.M + BM - 1) / BM, NT = (a.w.groups + WN - 1) / WN;
-  auto kernel = k_qlinear_tile<WM, WN, RT, FAST, GATED, T, NB>;
+  auto kernel = k_qlinear_tile<WM, WN, RT, FAST, GATED, T, NB, KS>;
   if (lds > 65536) allow_dynamic_lds((const void*)kernel, lds);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((size_t)MT * NT)), dim3(64 * WM * WN), lds, s, a, MT, NT);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((size_t)MT * NT)), dim3(64 * WM * WN * KS), lds, s, a, MT, NT);
 }
 
-template <bool FAST, bool GATED, typename T>
-static void tile_by(const QProduct& a, QTile t, hipStream_t s) {
+template <bool FAST, typename T>
+static void tile_least(const QProduct& a, int shares, hipStream_t s) {
+  if (shares == 4) tile_t<1, 2, 2, FAST, false, T, 4, 4>(a, s);
+  else if (shares == 2) tile_t<1, 2, 2, FAST, false, T, 4, 2>(a, s);
+  else tile_t<1, 2, 2, FAST, false, T, 4, 1>(a, s);
+}
+
+template <bool FAST, typename T>
+static void tile_by(const QProduct& a, QTile t, int shares, hipStream_t s) {
   switch (t) {
-    case kTile128x256: tile_t<1, 4, 8, FAST, GATED, T, 2>(a, s); break;
-    case kTile64x256: tile_t<1, 4, 4, FAST, GATED, T, 4>(a, s); break;
-    case kTile64x128: if constexpr (!GATED) tile_t<1, 2, 4, FAST, GATED, T, 4>(a, s); break;
-    default: if constexpr (!GATED) tile_t<1, 2, 2, FAST, GATED, T, 4>(a, s);
+    case kTile128x256: return tile_t<1, 4, 8, FAST, false, T, 2, 1>(a, s);
+    case kTile64x256: return tile_t<1, 4, 4, FAST, false, T, 4, 1>(a, s);
+    case kTile64x128:
+      if constexpr (FAST) {
+        if (shares == 4) return tile_t<1, 2, 4, FAST, false, T, 4, 4>(a, s);
+      }
+      if (shares == 2) return tile_t<1, 2, 4, FAST, false, T, 4, 2>(a, s);
+      return tile_t<1, 2, 4, FAST, false, T, 4, 1>(a, s);
+    default: tile_least<FAST, T>(a, shares, s);
   }
 }
 
-void launch_qlinear_tile(const QProduct& a, QTile t, hipStream_t s) {
-  if (a.w.gated && t == kTile32x256) tile_t<1, 4, 2, false, true, float, 4>(a, s);
-  else if (a.w.gated) tile_by<true, true, float>(a, t, s);
-  else if (a.dtype == VVS_BF16 && !a.fast) tile_t<1, 2, 2, false, false, bf16_t, 4>(a, s);      // (up to 64 rows: kTile32x128)
-  else if (a.dtype == VVS_BF16) tile_by<true, false, bf16_t>(a, t, s);
-  else if (a.fast) tile_by<true, false, float>(a, t, s);
-  else tile_by<false, false, float>(a, t, s);
+void launch_qlinear_tile(const QProduct& a, QTile t, int shares, hipStream_t s) {
+  shares = qlinear_shares(a.w, shares);                // (a share without a block would ask for one in front of the first)
+  if (a.w.gated && t == kTile32x256) tile_t<1, 4, 2, false, true, float, 4, 1>(a, s);
+  else if (a.w.gated && t == kTile64x256) tile_t<1, 4, 4, true, true, float, 4, 1>(a, s);
+  else if (a.w.gated) tile_t<1, 4, 8, true, true, float, 2, 1>(a, s);
+  else if (a.dtype == VVS_BF16 && !a.fast) tile_least<false, bf16_t>(a, shares, s);      // (33 to 64 rows)
+  else if (a.dtype == VVS_BF16) tile_by<true, bf16_t>(a, t, shares, s);
+  else if (a.fast) tile_by<true, float>(a, t, shares, s);
+  else tile_by<false, float>(a, t, shares, s);
 }
 
 }  // namespace vvs

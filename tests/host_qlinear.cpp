@@ -3,6 +3,8 @@
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
+
+#include <algorithm>
 #include <cmath>
 #include <thread>
 #include <vector>
@@ -73,8 +75,11 @@ void launch_qlinear_product(const QProduct& a, const QPlan& p, hipStream_t) {
       if (sizeof(uint32_t) * rows * columns > kQlinearCounters) abort();
       memset(a.act, 0, sizeof(float) * (size_t)rows * columns * p.splits * p.rt * p.ct * 256);
     }
-  } else if (a.w.gated && a.w.groups % 4) {
-    abort();
+  } else {
+    if (a.w.gated && a.w.groups % 4) abort();
+    // every share of the contraction has a block, and the tiles are there in so many shares
+    if ((p.splits != 1 && p.splits != 2 && p.splits != 4) || p.splits > a.w.blocks || (p.splits > 1 && (a.w.gated || p.tile == kTile128x256 || p.tile == kTile64x256))) abort();
+    if (p.splits == 4 && p.tile == kTile64x128 && !a.fast) abort();
   }
   g_product = a;
   g_plan = p;
@@ -244,7 +249,7 @@ int main() {
     map(300, 65536, 130, gated);
   }
   // which kernel
-  auto plan = [](int in, int out, int gated, int M) { QWeights w{in, out, gated, qrows_blocks(in), 0, nullptr, nullptr}; w.groups = (out + w.unit() - 1) / w.unit(); if (gated) w.groups = (w.groups + 3) & ~3; return plan_qlinear_product(w, M); };
+  auto plan = [](int in, int out, int gated, int M) { QWeights w{in, out, gated, qrows_blocks(in), 0, nullptr, nullptr}; w.groups = (out + w.unit() - 1) / w.unit(); if (gated) w.groups = (w.groups + 3) & ~3; return plan_qlinear_product(w, M, !gated && M > 64); };
   { QPlan p = plan(11008, 4096, 0, 28); CHECK(p.few && p.splits == 2 && p.rt == 2 && p.ct == 2); }
   { QPlan p = plan(11008, 4096, 0, 8); CHECK(p.few && p.splits == 1 && p.rt == 1 && p.ct == 1); }
   { QPlan p = plan(4096, 12288, 0, 8); CHECK(p.few && p.rt == 1 && p.ct == 2); }
@@ -253,8 +258,15 @@ int main() {
   { QPlan p = plan(1280, 3840, 0, 1000); CHECK(!p.few && p.tile == kTile64x256); }
   { QPlan p = plan(4096, 12288, 0, 8192); CHECK(!p.few && p.tile == kTile128x256); }
   { QPlan p = plan(1280, 3840, 0, 128); CHECK(p.few && p.ct == 4); }
-  { QPlan p = plan(11008, 4096, 0, 224); CHECK(p.few && p.ct == 4); }
-  { QPlan p = plan(11008, 4096, 0, 300); CHECK(!p.few && p.tile == kTile32x128); }
+  { QPlan p = plan(11008, 4096, 0, 224); CHECK(!p.few && p.tile == kTile32x128 && p.splits == 4); }
+  { QPlan p = plan(11008, 4096, 0, 300); CHECK(!p.few && p.tile == kTile64x128 && p.splits == 4); }
+  { QPlan p = plan(4096, 4096, 0, 432); CHECK(!p.few && p.tile == kTile64x128 && p.splits == 2); }
+  { QPlan p = plan(3456, 1280, 0, 432); CHECK(!p.few && p.tile == kTile32x128 && p.splits == 4); }
+  { QPlan p = plan(2048, 2048, 0, 432); CHECK(!p.few && p.tile == kTile32x128 && p.splits == 2); }
+  for (int blocks = 1; blocks < 8; ++blocks) {
+    const QWeights w{blocks * 128, 64, 0, blocks, 1, nullptr, nullptr};
+    for (int wanted : {0, 1, 2, 3, 4, 8}) CHECK(qlinear_shares(w, wanted) >= 1 && qlinear_shares(w, wanted) <= std::min(4, blocks) && qlinear_shares(w, wanted) != 3);
+  }
   { QPlan p = plan(4096, 11008, 1, 14); CHECK(p.few && p.rt == 1); }
   { QPlan p = plan(4096, 11008, 1, 60); CHECK(!p.few && p.tile == kTile32x256); }
   { QPlan p = plan(4096, 11008, 1, 128); CHECK(!p.few && p.tile == kTile64x256); }
@@ -264,8 +276,8 @@ int main() {
   { QPlan p = plan(1280, 1280, 0, 256); CHECK(p.few && p.rt == 1 && p.ct == 2); }
   { QPlan p = plan(4096, 2048, 0, 128); CHECK(p.few && p.rt == 2 && p.ct == 2 && p.splits == 1); }
   { QPlan p = plan(4096, 12288, 0, 28); CHECK(p.few && p.rt == 2 && p.ct == 4); }
-  { QPlan p = plan(4096, 16384, 0, 48); CHECK(p.few && p.rt == 2 && p.ct == 2); }
-  { QPlan p = plan(4096, 32768, 0, 48); CHECK(!p.few && p.tile == kTile32x128); }
+  { QPlan p = plan(4096, 16384, 0, 48); CHECK(!p.few && p.tile == kTile32x128 && p.splits == 4); }
+  { QPlan p = plan(4096, 32768, 0, 48); CHECK(!p.few && p.tile == kTile32x128 && p.splits == 2); }
   { QPlan p = plan(4096, 12288, 0, 432); CHECK(!p.few && p.tile == kTile64x128); }
   { QPlan p = plan(4096, 16384, 0, 600); CHECK(!p.few && p.tile == kTile128x256); }
   { QPlan p = plan(768, 2048, 1, 48); CHECK(p.few && p.rt == 1); }

@@ -119,6 +119,18 @@ def test_product_where_another_kernel_takes_over(rows, width, out, dtype):
     check_product(y, x, w, TYPES[dtype], fast=rows > 64 and dtype == "bf16")
 
 
+# tiles whose workgroups cut the contraction into shares: two and four, shares that begin inside a word of four powers, with one block more than another, with more blocks than their powers lie in LDS at a time
+@pytest.mark.parametrize("rows,width,out", [(200, 5200, 4100), (130, 3201, 3000), (432, 2100, 2048), (300, 5200, 4200), (432, 2100, 4200), (200, 1100, 4200), (432, 4200, 8200), (40, 3200, 16390), (61, 3330, 16300), (64, 900, 16300),
+                                            (300, 17000, 2100), (600, 8500, 5000), (1000, 1030, 2300), (900, 1153, 1290)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_product_in_shares(rows, width, out, dtype):
+    from paper_2511_13587_amd import binding as vb
+    lin, r, x, (w,) = _linear(vb, rows, width, out, seed=rows)
+    y = torch.full((rows, out), 3.0, dtype=TYPES[dtype], device="cuda")
+    lin.vvs_qlinear_apply(r, y)
+    check_product(y, x, w, TYPES[dtype], fast=rows > 64 and dtype == "bf16")
+
+
 @pytest.mark.parametrize("rows,width,out", [(17, 900, 900), (48, 1100, 1030), (33, 640, 2100), (60, 2100, 5600), (100, 2100, 2050), (130, 2049, 1000), (40, 200, 100), (300, 256, 300), (280, 2100, 600), (440, 400, 11000)])
 def test_gate_where_another_kernel_takes_over(rows, width, out):
     from paper_2511_13587_amd import binding as vb
