@@ -18,7 +18,7 @@ __device__ __forceinline__ void qtile_of(int id, int MT, int NT, int* tile_m, in
 
 // Y^T = W^T X^T.  A workgroup of WM x WN waves makes 16 RT WM rows by WN groups of 64 columns; a wave 16 RT rows of one group, whose weights nobody else in the workgroup needs: they come straight into its operand
 // registers, NB - 1 blocks of 128 contraction values ahead.  The rows' bytes of a block are every wave's, and pass through LDS (lds_dma16, no registers), two or three blocks ahead.  Bound by the matrix cores: 8192 rows,
-// 4096 -> 12288, 825 GFLOP in 337 to 354 us, 2.3 to 2.4 PFLOP/s (an 8192^3 product in e4m3 by the library 2.7), the matrix cores busy 62 % of the time; a tile of 128 x 256 reads 48 KB a block for 8.4 MFLOP, and
+// 4096 -> 12288, 825 GFLOP in 321 to 331 us, 2.5 to 2.6 PFLOP/s (an 8192^3 product in e4m3 by the library 2.7), the matrix cores busy 62 % of the time; a tile of 128 x 256 reads 48 KB a block for 8.4 MFLOP, and
 // 85 % of its requests to the L2 are hits.  Few tiles wait for loads
 // instead, 0.6 us per block with three on their way: NB = 4, and KS shares of the contraction with waves, stages and powers of their own, whose sums the first adds up through LDS in their order (432 rows: 1280 ->
 // 3840 in one share 8.0 us; 3456 -> 1280 in four 10.8, one 12.2; 11008 -> 4096 in four 39.5, one 54.8).  Powers of the first blocks are asked for in front of everything else: 432 rows, 1280 -> 3840 9.3 -> 8.3.
@@ -39,10 +39,12 @@ constexpr int share_lds(int BM, int WN, int NB, int shares) { return tile_stages
 // SQ_LDS_BANK_CONFLICT; so none.)
 __device__ __forceinline__ int swizzle(int r) { return ((r >> 1) & 7) ^ (((r + 4) >> 3 & 1) << 1); }
 
+struct __attribute__((aligned(8))) Bytes16 { uint32_t x, y, z, w; };     // (rows of bf16 may lie at multiples of 8 bytes)
+
 template <int WM, int WN, int RT, bool FAST, bool GATED, typename T, int NB, int KS>
 __global__ __launch_bounds__(64 * WM * WN * KS, 2) void k_qlinear_tile(QProduct a, int MT, int NT) {
   constexpr int BM = 16 * RT * WM, NW = WM * WN, NQ = BM / 8 / NW, kStages = tile_stages(NB), kPowerBlocks = power_blocks(KS), kPowerStride = power_stride(KS);
-  static_assert(BM <= 64 * NW && BM % (8 * NW) == 0 && (!GATED || WN == 4) && (NW & (NW - 1)) == 0, "");
+  static_assert(BM <= 64 * NW && BM % (8 * NW) == 0 && (!GATED || (WM == 1 && WN == 4 && KS == 1)) && (NW & (NW - 1)) == 0, "");
   extern __shared__ uint4 lds[];
   const int all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = KS == 1 ? 0 : all_waves / NW, wave = KS == 1 ? all_waves : all_waves % NW;
   const int tid = KS == 1 ? threadIdx.x : threadIdx.x & (64 * NW - 1), lane = tid & 63, i = lane & 15, g = lane >> 4;
@@ -239,23 +241,21 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void k_qlinear_tile(QProduct 
         for (int r = 0; r < RT; ++r) join[((share - 1) * NW * 4 * RT + c * RT + r) * 64] = make_float4(acc[c][r][0], acc[c][r][1], acc[c][r][2], acc[c][r][3]);
     }
     __syncthreads();
-    if (share) {
-      if constexpr (!GATED) return;
-    } else {
-      for (int k = 0; k < KS - 1; ++k)
+    if (share) return;
+    for (int k = 0; k < KS - 1; ++k)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int r = 0; r < RT; ++r) {
-            const float4 p = join[(k * NW * 4 * RT + c * RT + r) * 64];
-            acc[c][r] += floatx4{p.x, p.y, p.z, p.w};
-          }
-    }
+        for (int r = 0; r < RT; ++r) {
+          const float4 p = join[(k * NW * 4 * RT + c * RT + r) * 64];
+          acc[c][r] += floatx4{p.x, p.y, p.z, p.w};
+        }
   }
 
   if constexpr (GATED) {
     // a wave's 32 hidden units, 8 in a row per lane; the largest of a block of 128 is that of four waves
-    float* const top = (float*)((char*)lds + kJoin);   // [4][BM]
+    float* const top = (float*)lds;                  // [4][BM], then the bytes of the block: [BM][128], 16 bytes c of row r at place c ^ (r & 7)
+    char* const bytes = (char*)lds + 16 * BM;
     float v[RT][8];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -266,35 +266,66 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void k_qlinear_tile(QProduct 
         t = fmaxf(t, finite(v[r][j]) ? fabsf(v[r][j]) : 0.f);
       }
       t = rows_max(t);
-      if (g == 0 && share == 0) top[wn * BM + (wm * RT + r) * 16 + i] = t;
+      if (g == 0) top[wn * BM + r * 16 + i] = t;
     }
     __syncthreads();
     const int out_blocks = qrows_blocks(a.w.out), out_powers = qrows_powers(a.w.out);
-    if (tile_n < out_blocks && share == 0) {
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        const int lm = (wm * RT + r) * 16 + i, m = m0 + lm;
-        const int e = e4m3_exponent(fmaxf(fmaxf(top[lm], top[BM + lm]), fmaxf(top[2 * BM + lm], top[3 * BM + lm])));
-        const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    for (int r = 0; r < RT; ++r) {
+      const int lm = r * 16 + i, m = m0 + lm;
+      const int e = e4m3_exponent(fmaxf(fmaxf(top[lm], top[BM + lm]), fmaxf(top[2 * BM + lm], top[3 * BM + lm])));
+      const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[r][j] *= inv;
-        if (m < a.M) {
-          *(uint2*)(a.y8.values + ((size_t)m * out_blocks + tile_n) * kQRowBlock + wn * 32 + g * 8) = to_e4m3x8(v[r]);
-          if (lane < 16 && wn == 0) {
-            uint8_t* p = a.y8.powers + (size_t)m * out_powers;
-            p[tile_n] = (uint8_t)(e + 127);
-            if (tile_n == out_blocks - 1)
-              for (int b = out_blocks; b < out_powers; ++b) p[b] = 0;
-          }
-        }
+      for (int j = 0; j < 8; ++j) v[r][j] *= inv;
+      *(uint2*)(bytes + lm * kQRowBlock + (((2 * wn + (g >> 1)) ^ (lm & 7)) * 16) + (g & 1) * 8) = to_e4m3x8(v[r]);
+      if (m < a.M && lane < 16 && wn == 0) {
+        uint8_t* p = a.y8.powers + (size_t)m * out_powers;
+        p[tile_n] = (uint8_t)(e + 127);
+        if (tile_n == out_blocks - 1)
+          for (int b = out_blocks; b < out_powers; ++b) p[b] = 0;
       }
     }
+    __syncthreads();
+    // (a row's 128 bytes by neighbouring lanes; pieces of 8 bytes from where the products are would be 32 in a row: 4093 rows, 4096 -> 11008 with reading back 330 us, so 322)
+#pragma unroll
+    for (int k = 0; k < BM / 32; ++k) {
+      const int lm = k * 32 + (tid >> 3), c = tid & 7;
+      if (m0 + lm < a.M) *(uint4*)(a.y8.values + ((size_t)(m0 + lm) * out_blocks + tile_n) * kQRowBlock + c * 16) = *(const uint4*)(bytes + lm * kQRowBlock + (c ^ (lm & 7)) * 16);
+    }
   } else {
+    if (own_group >= a.w.groups) return;
+    // A lane has 16 columns of a row; 64 whole ones go through LDS, so that a store writes all of a row's, not pieces of 8 or 16 bytes that lie apart (16 bytes c of row i at place c ^ i).
+    // 8192 rows, 4096 -> 12288 in bf16 350 -> 331 us, 432 rows, 1280 -> 3840 8.5 -> 8.2, fp32 12.1 -> 9.2
+    if (a.wide && a.w.out - own_group * 64 >= 64) {
+      constexpr int kChunks = 4 * sizeof(T), kRows = 64 / kChunks;                          // of 16 bytes in a row; rows of a store
+      char* const buf = (char*)lds + kJoin + wave * 16 * kChunks * 16;
+      const int chunk = lane % kChunks, sub = lane / kChunks;
+      T* const y = (T*)a.y + own_group * 64 + chunk * (16 / sizeof(T));
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+#pragma unroll
+        for (int h = 0; h < kChunks / 4; ++h) {
+          Bytes16 v;
+          if constexpr (sizeof(T) == 4) v = __builtin_bit_cast(Bytes16, acc[h][r]);
+          else v = Bytes16{pack2bf(acc[2 * h][r][0], acc[2 * h][r][1]), pack2bf(acc[2 * h][r][2], acc[2 * h][r][3]), pack2bf(acc[2 * h + 1][r][0], acc[2 * h + 1][r][1]), pack2bf(acc[2 * h + 1][r][2], acc[2 * h + 1][r][3])};
+          *(Bytes16*)(buf + (i * kChunks + ((kChunks / 4 * g + h) ^ (i & (kChunks - 1)))) * 16) = v;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int k = 0; k < 16 / kRows; ++k) {
+          const int row = k * kRows + sub, m = m0 + (wm * RT + r) * 16 + row;
+          const Bytes16 v = *(const Bytes16*)(buf + (row * kChunks + (chunk ^ (row & (kChunks - 1)))) * 16);
+          if (m < a.M) *(Bytes16*)(y + (size_t)m * a.stride) = v;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+      return;
+    }
     const int col0 = a.w.column(own_group, 0, 4 * g), left = a.w.out - col0;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const int m = m0 + (wm * RT + r) * 16 + i;
-      if (m >= a.M || own_group >= a.w.groups) continue;
+      if (m >= a.M) continue;
       T* y = (T*)a.y + (size_t)m * a.stride + col0;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -309,7 +340,7 @@ template <int WM, int WN, int RT, bool FAST, bool GATED, typename T, int NB, int
 static void tile_t(const QProduct& a, hipStream_t s) {
   constexpr int BM = 16 * RT * WM;
   constexpr size_t lds = KS * share_lds(BM, WN, NB, KS);
-  static_assert(lds >= (KS - 1) * WM * WN * 4 * RT * 1024 + (GATED ? 16 * BM : 0) && lds <= kMostLds, "");
+  static_assert(lds >= (KS - 1) * WM * WN * 4 * RT * 1024 + (GATED ? (16 + kQRowBlock) * BM : 4096 * WM * WN) && lds <= kMostLds, "");
   const int MT = (a.M + BM - 1) / BM, NT = (a.w.groups + WN - 1) / WN;
   auto kernel = k_qlinear_tile<WM, WN, RT, FAST, GATED, T, NB, KS>;
   if (lds > 65536) allow_dynamic_lds((const void*)kernel, lds);
