@@ -1,7 +1,7 @@
 // Weights in 8 bits inside a context: what the forward of a VVS_WEIGHTS_E4M3 context launches.  The operators are those of vvs_qrows.hip and vvs_qlinear.hip; here they get the context's buffers.
 // A layer is nine launches: norm into 8 bits, q|k|v, rotary positions and cache, attention, rounding, O, norm, gate|up, down.  Bound by the weights' bytes where they are large (7B shape, 14 rows, us per layer: gate|up 26.0, q|k|v
 // 14.6, down 15.0, O 9.2, attention 13.2, two norms 8.0, positions and cache 5.1, rounding 3.9), else by the launches: narrower shapes, whose layers run in few launches with weights in bf16, take longer in
-// 8 bits (us per step, bf16 / 8 bits: 7B shape 1 token 3116 / 2598, 2 x 7 tokens 3308 / 3183; 1280 wide, 8 x 27 tokens 2288 / 3605; 768 wide, 4 x 6 tokens 286 / 515).
+// 8 bits (us per step, bf16 / 8 bits: 7B shape 1 token 3104 / 2592, 2 x 7 tokens 3304 / 3171, 16 x 7 6740 / 6211; 1280 wide, 8 x 27 tokens 2279 / 3073, 32 x 61 9187 / 8973; 768 wide, 4 x 6 tokens 286 / 509).
 #include "vvs_device.h"
 #include "vvs_qlinear.h"
 

@@ -17,14 +17,15 @@ __device__ __forceinline__ void qtile_of(int id, int MT, int NT, int* tile_m, in
 }
 
 // Y^T = W^T X^T.  A workgroup of WM x WN waves makes 16 RT WM rows by WN groups of 64 columns; a wave 16 RT rows of one group, whose weights nobody else in the workgroup needs: they come straight into its operand
-// registers, NB - 1 blocks of 128 contraction values ahead.  The rows' bytes of a block are every wave's, and pass through LDS (lds_dma16, no registers), two or three blocks ahead.  Bound by the matrix cores: 8192 rows,
-// 4096 -> 12288, 825 GFLOP in 321 to 331 us, 2.5 to 2.6 PFLOP/s (an 8192^3 product in e4m3 by the library 2.7), the matrix cores busy 62 % of the time; a tile of 128 x 256 reads 48 KB a block for 8.4 MFLOP, and
-// 85 % of its requests to the L2 are hits.  Few tiles wait for loads
-// instead, 0.6 us per block with three on their way: NB = 4, and KS shares of the contraction with waves, stages and powers of their own, whose sums the first adds up through LDS in their order (432 rows: 1280 ->
-// 3840 in one share 8.0 us; 3456 -> 1280 in four 10.8, one 12.2; 11008 -> 4096 in four 39.5, one 54.8).  Powers of the first blocks are asked for in front of everything else: 432 rows, 1280 -> 3840 9.3 -> 8.3.
-// Parts of that large product left out, in turn, of 385 us (all of the following: 223): powers of two from memory at every block 353, the requests for rows 350, for weights 321, reads of LDS 379.  Hence powers in
-// LDS (362), and two row tiles on their way from there (354).  Requests at the start of a block instead of between products 420.  Tried and slower: 256 x 256 by 8 waves 448, 4 waves that have a SIMD each 405, a
-// higher priority for waves at their products 403, bands of 4 or 16 row tiles 397 and 404.
+// registers, NB - 1 blocks of 128 contraction values ahead.  The rows' bytes of a block are every wave's, and pass through LDS (lds_dma16, no registers), two or three blocks ahead.
+// Bound by the matrix cores: 8192 rows, 4096 -> 12288, 825 GFLOP in 321 us, 2.6 PFLOP/s (an 8192^3 product in e4m3 by the library 2.7), the matrix cores busy 75 % of the time; a tile of 128 x 256 reads 48 KB a
+// block for 8.4 MFLOP, and 82 % of the requests to the L2 are hits.
+// Few tiles wait for loads instead, 0.6 us per block with three on their way: NB = 4, and KS shares of the contraction with waves, stages and powers of their own, whose sums the first adds up through LDS in their
+// order (432 rows: 1280 -> 3840 in one share 7.7 us; 3456 -> 1280 in four 10.9, one 12.3; 11008 -> 4096 in four 39.5, one 54.8).  Powers of the first blocks are asked for in front of everything else (432 rows, 1280 ->
+// 3840 9.3 -> 8.3).
+// Parts of the large product left out in turn, when it took 385 us (all of the following: 223): powers of two from memory at every block 353, the requests for rows 350, for weights 321, reads of LDS 379.  Hence powers
+// in LDS (362), two row tiles on their way from there (354), and outputs through LDS (331).  Requests at the start of a block instead of between products 420.  Tried and slower, of 385 to 400: 256 x 256 by 8 waves 448,
+// 4 waves that have a SIMD each 405, a higher priority for waves at their products 403, bands of 4 or 16 row tiles 397 and 404.
 // FAST: the e4m3 numbers go into the matrix cores as they are, with both powers of two as scales (16x16x128, twice the rate of bf16 and fewer instructions).  These products lose what lies 2^13
 // below the largest of a few neighbours: 1.3e-5 in the 2-norm, 200 times below the rounding of bf16 outputs and 3000 times below that of 8 bits.  Outputs in fp32, and up to 64 rows of any, take !FAST: bf16
 // operands, exact.
