@@ -240,6 +240,22 @@ def test_rows_behind_the_last_one_stay(rows, most):
                 assert (flat[~mine] == 5.0).all()
 
 
+# outputs that are part of a wider tensor, at multiples of 16 bytes, of 4 elements, of one: the same bits as beside each other, and nothing written around them
+@pytest.mark.parametrize("rows,width,out", [(9, 700, 300), (50, 3300, 17000), (70, 1000, 700), (200, 3300, 1000), (300, 2100, 4160), (330, 5300, 4200), (700, 300, 2300), (1100, 640, 3900)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_outputs_inside_a_wider_tensor(rows, width, out, dtype):
+    from paper_2511_13587_amd import binding as vb
+    lin, r, _, _ = _linear(vb, rows, width, out, seed=rows)
+    want = torch.full((rows, out), 3.0, dtype=dtype, device="cuda")
+    lin.vvs_qlinear_apply(r, want)
+    for at, wider in ((0, 64), (8, 72 + -out % 8), (4, 12 + -out % 4), (1, 3), (3, 5 - out % 2)):
+        whole = torch.full((rows + 3, out + at + wider), 3.0, dtype=dtype, device="cuda")
+        lin.vvs_qlinear_apply(r, whole[1:rows + 1, at:at + out])
+        assert torch.equal(whole[1:rows + 1, at:at + out], want)
+        whole[1:rows + 1, at:at + out] = 3.0
+        assert (whole == 3.0).all()
+
+
 @pytest.mark.parametrize("rows", [5, 40, 100, 500])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_what_is_not_finite_stays_in_its_row_and_column(rows, dtype):
