@@ -65,14 +65,15 @@ inline QWeights qweights(int in, int out, int gated, void* base = nullptr) {
   w.powers = w.data ? w.data + qweights_data_bytes(w.groups, w.blocks) : nullptr;
   return w;
 }
-// Workspace of a product that k_qlinear_few makes: counters, in a place of one size, so that maps can share a workspace, then for a contraction in halves two partial sums of 32 rows, with a gate the
+// Workspace of a product that k_qlinear_few makes: counters, in a place of one size, so that maps can share a workspace, then for a contraction in parts their partial sums of 32 rows, with a gate the
 // activations in fp32 of up to 32 rows, or of as many as have no more workgroups than kGateWorkgroups (of 32 rows x 32 packed columns).
 constexpr int kGateWorkgroups = 704;
-constexpr size_t kQlinearCounters = 4096;                      // bytes: a counter per 32 rows x 32 columns of up to 64 groups, or per row tile and block of 128 hidden units of up to 2048 groups
-inline bool qlinear_in_halves(const QWeights& w) { return !w.gated && w.blocks >= 40 && w.groups > 32 && w.groups <= 64; }
+constexpr size_t kQlinearCounters = 4096;                      // bytes: a counter per 32 rows x 32 columns of up to 85 groups, or per row tile and block of 128 hidden units of up to 2048 groups
+// Parts of the contraction of up to 32 rows x 32 columns: as many as give one or two workgroups to every CU
+inline int qlinear_parts(const QWeights& w) { return w.gated ? 1 : w.blocks >= 40 && w.groups > 32 && w.groups <= 64 ? 2 : w.blocks >= 80 && w.groups > 74 && w.groups <= 85 ? 3 : 1; }
 inline size_t qlinear_part_bytes(const QWeights& w) {
-  const size_t gate = (size_t)(w.groups > kGateWorkgroups / 2 ? w.groups : kGateWorkgroups / 2) * 32 * 32, halves = qlinear_in_halves(w) ? (size_t)w.groups * 64 * 32 * 2 : 0;
-  return align_up((w.gated ? gate : halves) * sizeof(float), 256);
+  const size_t gate = (size_t)(w.groups > kGateWorkgroups / 2 ? w.groups : kGateWorkgroups / 2) * 32 * 32, parts = qlinear_parts(w) > 1 ? (size_t)w.groups * 64 * 32 * qlinear_parts(w) : 0;
+  return align_up((w.gated ? gate : parts) * sizeof(float), 256);
 }
 
 struct QLoad {

@@ -97,7 +97,8 @@ static vvs_status check_rows(int n_rows, int width, const void* values, const vo
 //   16 x 16 up to 256 workgroups (28 rows: 1280 -> 1280 3.7, 32 x 16 4.4; 4096 -> 2048 6.0, 32 x 16 7.7, 16 x 32 7.0)
 //   16 x 32 for up to 16 rows (8 rows, 4096 -> 12288 13.3, 16 x 16 13.6); up to 256 workgroups (64 rows: 1280 -> 1280 4.2, 16 x 16 4.5; 4096 -> 2048 7.2, 32 x 32 8.6); up to 768 where the contraction is short (128
 //     rows, 1280 -> 1280 5.0, 32 x 32 5.3; 256 rows 5.8, 32 x 64 6.4), 1152 where the tiles are those of exact products (128 rows, 1536 -> 4608, fp32: 9.4, tiles 10.6)
-//   32 x 32 with the contraction in halves for one row tile and a long one (28 rows, 11008 -> 4096: 15.0, 16 x 32 17.5, 32 x 16 16.3, whole 19.5)
+//   32 x 32 with a long contraction in two parts for one row tile where those fit the CUs (28 rows, 11008 -> 4096: 15.0, 16 x 32 17.5, 32 x 16 16.3, whole 19.5, three parts 16.8), in three where they give two workgroups to
+//     nearly every CU (28 rows, 11008 -> 5000 18.0, whole 20.5, two 21.6, four 21.9; 13824 -> 5120 20.4, whole 24.5; 8 rows 18.6, 16 x 32 24.2; 6144 -> 5120 13.4, 16 x 32 13.4)
 //   32 x 32 up to 256 workgroups (128 rows, 4096 -> 2048 8.6, 32 x 64 10.0; 64 rows, 4096 -> 4096 8.8, 16 x 32 9.4) and up to 32 rows, or 512 of up to 64 rows where
 //     the contraction is short (40 rows, 2560 -> 6912 8.8, 32 x 64 10.3)
 //   32 x 64 up to 256 workgroups (128 rows, 4096 -> 4096 10.3, 32 x 32 13.1, tiles of 32 x 128 in four shares 11.5; 28 rows, 4096 -> 12288 14.6, 32 x 32 15.4), but tiles for more than 64 rows and less than 10 blocks
@@ -126,8 +127,9 @@ QPlan plan_qlinear_product(const QWeights& w, int M, bool fast) {
     return large(M <= 64 ? kTile32x256 : tiles(128, 4) >= 208 ? kTile128x256 : kTile64x256);
   }
   if (few(1, 1) <= 256) return small(1, 1);
-  if (M <= 16) return small(1, 2);
-  if (few(1, 2) <= 256) return M <= 32 && qlinear_in_halves(w) ? small(2, 2, 2) : small(1, 2);
+  const int parts = M <= 32 ? qlinear_parts(w) : 1;
+  if (parts == 3 || (parts == 2 && M > 16)) return small(2, 2, parts);
+  if (M <= 16 || few(1, 2) <= 256) return small(1, 2);
   if (w.blocks <= 16 && few(1, 2) <= (M <= 64 ? 640 : 768)) return small(1, 2);
   if (w.blocks <= 12 && few(1, 2) <= 1152 && M > 64 && !fast) return small(1, 2);
   if (few(2, 2) <= 256) return small(2, 2);

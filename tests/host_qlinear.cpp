@@ -244,6 +244,8 @@ int main() {
     map(65536, 40, 65, gated);
     map(130, 5000, 4200, gated);
     map(5000, 2100, 40, gated);
+    map(10300, 5000, 40, gated);
+    map(10300, 5440, 33, gated);
     map(2100, 2100, 300, gated);
     map(2100, 5600, 70, gated);
     map(300, 65536, 130, gated);
@@ -252,6 +254,8 @@ int main() {
   auto plan = [](int in, int out, int gated, int M) { QWeights w{in, out, gated, qrows_blocks(in), 0, nullptr, nullptr}; w.groups = (out + w.unit() - 1) / w.unit(); if (gated) w.groups = (w.groups + 3) & ~3; return plan_qlinear_product(w, M, !gated && M > 64); };
   { QPlan p = plan(11008, 4096, 0, 28); CHECK(p.few && p.splits == 2 && p.rt == 2 && p.ct == 2); }
   { QPlan p = plan(11008, 4096, 0, 8); CHECK(p.few && p.splits == 1 && p.rt == 1 && p.ct == 1); }
+  for (int M : {8, 28}) { QPlan p = plan(11008, 5000, 0, M); CHECK(p.few && p.splits == 3 && p.rt == 2 && p.ct == 2); }
+  { QPlan p = plan(11008, 5000, 0, 33); CHECK(p.splits == 1); }
   { QPlan p = plan(4096, 12288, 0, 8); CHECK(p.few && p.rt == 1 && p.ct == 2); }
   { QPlan p = plan(1280, 3840, 0, 432); CHECK(!p.few && p.tile == kTile64x128); }
   { QPlan p = plan(1280, 1280, 0, 432); CHECK(!p.few && p.tile == kTile32x128); }

@@ -107,8 +107,8 @@ def test_gate_at_odd_sizes(rows, width, out):
     check_gate(y, x, w, fast=rows > 64)
 
 
-# further rows, columns and lengths at which another kernel takes over: tiles of 16 x 16 and 16 x 32 for more than one row tile, 32 x 32 whole and in halves, 32 x 64, tiles for few rows of many columns
-@pytest.mark.parametrize("rows,width,out", [(17, 500, 300), (64, 700, 400), (60, 2100, 2050), (100, 1000, 1290), (28, 5200, 2100), (17, 5121, 4096), (100, 4200, 2000), (60, 4100, 4090), (30, 4096, 9000), (100, 2200, 4100),
+# further rows, columns and lengths at which another kernel takes over: tiles of 16 x 16 and 16 x 32 for more than one row tile, 32 x 32 whole and in two and three parts, 32 x 64, tiles for few rows of many columns
+@pytest.mark.parametrize("rows,width,out", [(17, 500, 300), (64, 700, 400), (60, 2100, 2050), (100, 1000, 1290), (28, 5200, 2100), (17, 5121, 4096), (28, 10300, 5000), (5, 10241, 4801), (100, 4200, 2000), (60, 4100, 4090), (30, 4096, 9000), (100, 2200, 4100),
                                             (200, 5200, 4100), (33, 300, 33000), (64, 1030, 40001), (300, 400, 16390), (600, 390, 16400)])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_product_where_another_kernel_takes_over(rows, width, out, dtype):
