@@ -256,6 +256,55 @@ def test_outputs_inside_a_wider_tensor(rows, width, out, dtype):
         assert (whole == 3.0).all()
 
 
+@pytest.mark.parametrize("rows,width,out", [(5, 300, 200), (70, 300, 200), (70, 300, 40000)])
+def test_rows_further_apart_than_four_billion_elements(rows, width, out):
+    """Offsets behind 2^32 elements, of what is rounded, normalised and written."""
+    from paper_2511_13587_amd import binding as vb
+    stride = 2 ** 32 // (rows - 1) // 8 * 8 + 8 * 4096
+    lin, r, x, _ = _linear(vb, rows, width, out, seed=rows)
+    want = torch.empty((rows, out), dtype=torch.bfloat16, device="cuda")
+    lin.vvs_qlinear_apply(r, want)
+    far = torch.empty((rows - 1) * stride + max(out, width), dtype=torch.bfloat16, device="cuda")
+    y = far.as_strided((rows, out), (stride, 1))
+    lin.vvs_qlinear_apply(r, y)
+    assert torch.equal(y, want)
+    near, at_far = vb.QRows(rows, width), vb.QRows(rows, width)
+    x = _normal((rows, width), 5).bfloat16().cuda()
+    far_x = far.as_strided((rows, width), (stride, 1))
+    far_x.copy_(x)
+    vb.vvs_qrows_round(x, near)
+    vb.vvs_qrows_round(far_x, at_far)
+    assert torch.equal(near.values.view(torch.uint8), at_far.values.view(torch.uint8)) and torch.equal(near.powers, at_far.powers)
+    gain = torch.ones(width, device="cuda")
+    x2 = torch.empty_like(x)
+    vb.vvs_qrows_norm(x, gain, 1e-5, near, delta=x, x_out=x2)
+    vb.vvs_qrows_norm(far_x, gain, 1e-5, at_far, delta=x, x_out=far_x)
+    assert torch.equal(near.values.view(torch.uint8), at_far.values.view(torch.uint8)) and torch.equal(far_x, x2)
+    vb.vvs_qrows_read(near, x2)
+    vb.vvs_qrows_read(at_far, far_x)
+    assert torch.equal(far_x, x2)
+
+
+@pytest.mark.parametrize("rows", [5, 100])
+def test_weights_of_more_than_four_billion_bytes(rows):
+    """65536 x 70000 in 8 bits: 4.6 GB.  The first and last columns beside their products in 64 bits; sums of 65536 products of e4m3 numbers in fp32, of at most 512 blocks in turn behind sums of 32 in the matrix cores:
+    an error of 2^-24 sqrt(65536 / 32) = 2.7e-6 in the 2-norm at most where roundings are independent."""
+    from paper_2511_13587_amd import binding as vb
+    width, out, part = 65536, 70000, 96
+    w = torch.empty((width, out), dtype=torch.bfloat16, device="cuda").normal_(0.0, width ** -0.5, generator=torch.Generator("cuda").manual_seed(1))
+    lin = vb.QLinear(width, out, rows, vb.VVS_BF16)
+    lin.vvs_qlinear_load(w)
+    lin.vvs_qlinear_read(w)
+    r, x = vb.QRows(rows, width), torch.empty((rows, width), device="cuda")
+    vb.vvs_qrows_round(_normal((rows, width), 2, 0).cuda(), r)
+    vb.vvs_qrows_read(r, x)
+    y = torch.empty((rows, out), device="cuda")
+    lin.vvs_qlinear_apply(r, y)
+    for cut in (slice(0, part), slice(out - part, out)):
+        want = x.cpu().double() @ w[:, cut].cpu().double()
+        assert ((y[:, cut].cpu().double() - want).norm() / want.norm()).item() < 2.7e-6
+
+
 @pytest.mark.parametrize("rows", [5, 40, 100, 500])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_what_is_not_finite_stays_in_its_row_and_column(rows, dtype):
