@@ -107,12 +107,13 @@ typedef struct {
                                     VVS_WEIGHTS_E4M3: a layer's seven matrices are held in 8 bits, and what they are multiplied by - the norms' outputs, the
                                       attention's (rounded to the dtype first), the activations - is rounded to 8 bits as well (see vvs_qrows below); residual stream
                                       and all else are as ever.  Products of e4m3 numbers enter their sums whole, but from 65 rows on, in bf16 contexts and in front of
-                                      the activations, as at vvs_qlinear_apply and vvs_qlinear_gate.  For contexts whose steps are bound by the weights' bytes.
-                                      Embeddings, gains and the output head keep the dtype.  Layers run as separate launches (no drafter contexts; d_model a multiple of 64, d_ff at most 65536) */
+                                      the activations, where they are made as VVS_PRODUCTS_E4M3 says.  For contexts whose steps are bound by the weights' bytes.
+                                      Embeddings, gains and the output head keep the dtype.  Layers run as separate launches (no drafter contexts; d_model a multiple of 64, d_ff at most 65536);
+                                    VVS_WEIGHTS_E4M3_WHOLE: the same, with VVS_PRODUCTS_WHOLE: calls of more than 64 rows take longer */
 } vvs_config;
 enum { VVS_NORM_AUTO = 0, VVS_NORM_SEPARATE = 1 };
 enum { VVS_CACHE_SAME = 0, VVS_CACHE_E4M3 = 1 };
-enum { VVS_WEIGHTS_SAME = 0, VVS_WEIGHTS_E4M3 = 1 };
+enum { VVS_WEIGHTS_SAME = 0, VVS_WEIGHTS_E4M3 = 1, VVS_WEIGHTS_E4M3_WHOLE = 3 };
 #define VVS_MAX_FEATURE_SLOTS 8
 
 /* Sizes in bytes of the three device buffers a context needs.  VVS_ESIZE if the shape is not
@@ -487,7 +488,14 @@ typedef struct {
   int32_t max_rows;              /* largest n_rows of a call, at most 2^20 */
   int32_t gated;                 /* 0: one matrix, for vvs_qlinear_apply; 1: gate and up, for vvs_qlinear_gate */
   int32_t dtype;                 /* of the weights that vvs_qlinear_load takes and vvs_qlinear_read gives */
+  int32_t products;              /* how products of e4m3 numbers are summed:
+                                    VVS_PRODUCTS_WHOLE: they enter sums in fp32 whole, in every call;
+                                    VVS_PRODUCTS_E4M3: calls of more than 64 rows may take the matrix instructions for e4m3, twice as fast, which cut off what lies 2^13 below the largest of 8
+                                      neighbouring products.  A sum is so off by up to 7 * 2^-13 of the sum of its products' magnitudes - a hundredth of what rounding both sides to e4m3 may have cost it,
+                                      but more than fp32's rounding, which shows in sums that cancel and in small elements beside far larger ones;
+                                    VVS_PRODUCTS_AUTO: as VVS_PRODUCTS_E4M3 where the result is rounded to bf16 or 8 bits, as VVS_PRODUCTS_WHOLE for outputs in VVS_FP32 */
 } vvs_qlinear_config;
+enum { VVS_PRODUCTS_AUTO = 0, VVS_PRODUCTS_WHOLE = 1, VVS_PRODUCTS_E4M3 = 2 };
 
 /* Sizes in bytes of the two device buffers of a linear map: weights in 8 bits in the kernels' own order, workspace.  Calls on a map, vvs_qlinear_load among them, are issued on one stream or ordered by
  * the caller.  A workspace may serve several maps - it has to hold the largest one's bytes - if the calls of all of them are; captured graphs that share one must not run at the same time. */
@@ -504,9 +512,9 @@ vvs_status vvs_qlinear_load(vvs_qlinear* l, const void* d_w, const void* d_w_up,
 vvs_status vvs_qlinear_read(vvs_qlinear* l, void* d_w, void* d_w_up, vvs_stream s);
 
 /* out = x W for rows in 8 bits of width `in`: out [n_rows, out] in out_dtype.
- * Sums are in fp32 and in a fixed order: the same call gives the same bits.  With up to 64 rows, and wherever out_dtype is VVS_FP32, products of e4m3 numbers enter them whole.  Calls of more rows with
- * outputs in bf16, and such calls of vvs_qlinear_gate, may take the matrix instructions for e4m3, twice as fast, which cut off what lies 2^13 below the largest of 8 neighbouring products: 1.3e-5 of the
- * result in the 2-norm, where the rounding of the output is 1.7e-3 in bf16 and 2.6e-2 in 8 bits.  The bits of a row may so depend on how many rows a call has. */
+ * Sums are in fp32 and in a fixed order: the same call gives the same bits.  With up to 64 rows products of e4m3 numbers enter them whole, with more rows as vvs_qlinear_config.products says; what the matrix
+ * instructions for e4m3 cut off was 1.3e-5 of the result in the 2-norm for normally distributed operands, where the rounding of the output is 1.7e-3 in bf16 and 2.6e-2 in 8 bits.  The order of a sum, and so the
+ * last bits of a row, may depend on how many rows a call has. */
 vvs_status vvs_qlinear_apply(vvs_qlinear* l, int32_t n_rows, const void* d_values, const void* d_powers, int32_t out_dtype, void* d_out, int64_t out_stride,
                              vvs_stream s);
 

@@ -21,7 +21,8 @@ VVS_FP32, VVS_BF16 = 0, 1
 VVS_STRICT, VVS_RELAXED = 0, 1
 VVS_NORM_AUTO, VVS_NORM_SEPARATE = 0, 1
 VVS_CACHE_SAME, VVS_CACHE_E4M3 = 0, 1
-VVS_WEIGHTS_SAME, VVS_WEIGHTS_E4M3 = 0, 1
+VVS_WEIGHTS_SAME, VVS_WEIGHTS_E4M3, VVS_WEIGHTS_E4M3_WHOLE = 0, 1, 3
+VVS_PRODUCTS_AUTO, VVS_PRODUCTS_WHOLE, VVS_PRODUCTS_E4M3 = 0, 1, 2
 VVS_MAX_T = 64
 VVS_QCACHE_BLOCK = 32
 VVS_QROWS_BLOCK = 128
@@ -51,7 +52,7 @@ class VvsRopeConfig(C.Structure):
 
 
 class VvsQLinearConfig(C.Structure):
-    _fields_ = [("in_", C.c_int32)] + [(n, C.c_int32) for n in ("out", "max_rows", "gated", "dtype")]
+    _fields_ = [("in_", C.c_int32)] + [(n, C.c_int32) for n in ("out", "max_rows", "gated", "dtype", "products")]
 
 
 class VvsError(RuntimeError):
@@ -749,10 +750,10 @@ def vvs_qlinear_query_sizes(cfg: VvsQLinearConfig):
 
 class QLinear:
     """A linear map with its weights in 8 bits: owns its weights and, unless one is given, its workspace; methods mirror the C entry points (include/vvs.h).  in_width, out: elements of a row
-    that goes in and of one that comes out; dtype: of the tensors that are loaded; gated: gate and up weights, for vvs_qlinear_gate."""
+    that goes in and of one that comes out; dtype: of the tensors that are loaded; gated: gate and up weights, for vvs_qlinear_gate; products: how they are summed, VVS_PRODUCTS_*."""
 
-    def __init__(self, in_width: int, out: int, max_rows: int, dtype: int, gated: bool = False, device: str = "cuda:0", workspace: Optional[torch.Tensor] = None):
-        self.cfg = VvsQLinearConfig(in_width, out, max_rows, 1 if gated else 0, dtype)
+    def __init__(self, in_width: int, out: int, max_rows: int, dtype: int, gated: bool = False, device: str = "cuda:0", workspace: Optional[torch.Tensor] = None, products: int = VVS_PRODUCTS_AUTO):
+        self.cfg = VvsQLinearConfig(in_width, out, max_rows, 1 if gated else 0, dtype, products)
         self.weight_bytes, self.ws_bytes = vvs_qlinear_query_sizes(self.cfg)
         if not torch.cuda.is_available():
             raise RuntimeError("libvvs needs a HIP device; there is no CPU path")

@@ -267,9 +267,9 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   if (g.norm_mode != VVS_NORM_AUTO && g.norm_mode != VVS_NORM_SEPARATE) return fail(err, VVS_EINVAL, "config: unknown norm_mode");
   if (g.cache_kind != VVS_CACHE_SAME && g.cache_kind != VVS_CACHE_E4M3) return fail(err, VVS_EINVAL, "config: unknown cache_kind");
   if (g.cache_kind && g.draft_input) return fail(err, VVS_EINVAL, "config: a drafter context keeps no cache (cache_kind must be VVS_CACHE_SAME)");
-  if (g.weight_kind != VVS_WEIGHTS_SAME && g.weight_kind != VVS_WEIGHTS_E4M3) return fail(err, VVS_EINVAL, "config: unknown weight_kind");
+  if (g.weight_kind != VVS_WEIGHTS_SAME && g.weight_kind != VVS_WEIGHTS_E4M3 && g.weight_kind != VVS_WEIGHTS_E4M3_WHOLE) return fail(err, VVS_EINVAL, "config: unknown weight_kind");
   if (g.weight_kind && g.draft_input) return fail(err, VVS_EINVAL, "config: a drafter context keeps its weights (weight_kind must be VVS_WEIGHTS_SAME)");
-  if (g.weight_kind && (g.d_model % 64 || g.d_ff > 65536)) return fail(err, VVS_ESIZE, "config: VVS_WEIGHTS_E4M3 needs d_model to be a multiple of 64, and d_ff of at most 65536");
+  if (g.weight_kind && (g.d_model % 64 || g.d_ff > 65536)) return fail(err, VVS_ESIZE, "config: weights in 8 bits need d_model to be a multiple of 64, and d_ff of at most 65536");
   int dh = g.d_model / g.n_heads;
   if (g.cache_kind && dh != 32 && dh != 64 && dh != 128) return fail(err, VVS_ESIZE, "config: VVS_CACHE_E4M3 needs head size 32, 64 or 128");
   if (dh % 4) return fail(err, VVS_ESIZE, "config: head size must be a multiple of 4 (2D rotary pairs)");

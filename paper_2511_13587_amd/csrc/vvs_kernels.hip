@@ -131,7 +131,7 @@ static void pack_weights_t(Ctx* c, const void* const* t, hipStream_t s) {
     const void* const* w = t + 2 + 9 * l;
     size_t base = c->p.layer0 + c->p.layer_stride * l;
     gain(w[0], base + c->p.g1);
-    if (c->cfg.weight_kind == VVS_WEIGHTS_E4M3) {
+    if (c->cfg.weight_kind != VVS_WEIGHTS_SAME) {
       gain(w[5], base + c->p.g2);
       launch_context_load(c, l, w, s);
       continue;
@@ -832,7 +832,7 @@ static void forward_t(Ctx* c, const TreeDesc& tree, const PosDesc& pos, int Tq, 
   // d 1024, d_ff 4096, 128 rows 1014 / 824; beyond each, 256 rows (d 1024, d_ff 2752) 1405 / 1222, d 1280 (128 rows) 1205 / 1008, d_ff 5504
   // (128 rows) 1297 / 1029; well inside, d 128 with 10 rows 138 / 91.
   const bool held8 = c->cfg.cache_kind == VVS_CACHE_E4M3;
-  const bool weights8 = c->cfg.weight_kind == VVS_WEIGHTS_E4M3;
+  const bool weights8 = c->cfg.weight_kind != VVS_WEIGHTS_SAME;
   if (sizeof(T) == 4 && M <= 128 && d <= 1024 && F <= 4096 && !held8 && !weights8) {
     forward_small(c, tree, pos, Tq, d_tokens_bt, pc, pu, chunk_start, forced, n_forced, logits_mode, s, from_din);
     return;

@@ -95,20 +95,20 @@ struct QPlan {
   int rt, ct, splits;
   QTile tile;
 };
-QPlan plan_qlinear_product(const QWeights& w, int M, bool fast);   // fast: see QProduct (gated: no matter)
+QPlan plan_qlinear_product(const QWeights& w, int M, bool fast);   // fast: see QProduct (gated: the same choice for both)
 
 // Shares of the contraction that a workgroup of k_qlinear_tile has waves for: 1, 2 or 4, and each at least a block
 inline int qlinear_shares(const QWeights& w, int wanted) { return wanted >= 4 && w.blocks >= 4 ? 4 : wanted >= 2 && w.blocks >= 2 ? 2 : 1; }
 
-// Whether a product may take the matrix instructions for e4m3 (outputs of type `dtype`, or of a context of it)
-inline int qlinear_fast(int dtype, int M) { return dtype == VVS_BF16 && M > 64; }
+// Whether a product may take the matrix instructions for e4m3 (outputs of type `dtype`, or of a context of it; in 8 bits: as VVS_BF16)
+inline int qlinear_fast(int products, int dtype, int M) { return M > 64 && (products == VVS_PRODUCTS_E4M3 || (products == VVS_PRODUCTS_AUTO && dtype == VVS_BF16)); }
 
 struct QProduct {
   QWeights w;
   int M;
   QRowsIn x;
   int dtype;                        // of y
-  int fast;                         // e4m3 products (k_qlinear_tile; gated: by the tile)
+  int fast;                         // e4m3 products (k_qlinear_tile; gated tiles of 32 rows: exact ones all the same)
   void* y;                          // !gated
   size_t stride;
   int wide;                         // stores of 4 elements at once
@@ -125,7 +125,7 @@ void launch_qlinear_read(const QWeightsRead& a, hipStream_t s);
 void launch_qlinear_product(const QProduct& a, const QPlan& p, hipStream_t s);
 void launch_qlinear_tile(const QProduct& a, QTile t, int shares, hipStream_t s);
 
-// Contexts with VVS_WEIGHTS_E4M3 (vvs_qlinear_ctx.hip): a layer's maps, in the order of its projections
+// Contexts with their weights in 8 bits (vvs_qlinear_ctx.hip): a layer's maps, in the order of its projections
 enum QMap { kMapQkv, kMapO, kMapGate, kMapDown };
 inline QWeights context_map(const Ctx* c, QMap m, void* base = nullptr) {
   return m == kMapQkv ? qweights(c->d, 3 * c->d, 0, base) : m == kMapO ? qweights(c->d, c->d, 0, base) : m == kMapGate ? qweights(c->d, c->F, 1, base) : qweights(c->F, c->d, 0, base);

@@ -1,4 +1,4 @@
-// Weights in 8 bits inside a context: what the forward of a VVS_WEIGHTS_E4M3 context launches.  The operators are those of vvs_qrows.hip and vvs_qlinear.hip; here they get the context's buffers.
+// Weights in 8 bits inside a context: what the forward of a VVS_WEIGHTS_E4M3 or VVS_WEIGHTS_E4M3_WHOLE context launches.  The operators are those of vvs_qrows.hip and vvs_qlinear.hip; here they get the context's buffers.
 // A layer is nine launches: norm into 8 bits, q|k|v, rotary positions and cache, attention, rounding, O, norm, gate|up, down.  Bound by the weights' bytes where they are large (7B shape, 14 rows, us per layer: gate|up 26.0, q|k|v
 // 14.6, down 15.0, O 9.2, attention 13.2, two norms 8.0, positions and cache 5.1, rounding 3.9), else by the launches: narrower shapes, whose layers run in few launches with weights in bf16, take longer in
 // 8 bits (us per step, bf16 / 8 bits: 7B shape 1 token 3104 / 2592, 2 x 7 tokens 3304 / 3171, 16 x 7 6740 / 6211; 1280 wide, 8 x 27 tokens 2279 / 3073, 32 x 61 9187 / 8973; 768 wide, 4 x 6 tokens 286 / 509).
@@ -55,7 +55,8 @@ void launch_context_product(Ctx* c, int layer, QMap m, int M, float* out, hipStr
   QProduct a{};
   a.w = map_of(c, layer, m); a.M = M;
   a.x = m == kMapDown ? QRowsIn{act.values, act.powers} : QRowsIn{h.values, h.powers};
-  a.dtype = VVS_FP32; a.fast = qlinear_fast(c->cfg.dtype, M);         // (the sums go on in fp32, but what they are of was rounded to 2^-4, and in bf16 contexts what comes of them is to 2^-9)
+  // (the sums go on in fp32, but what they are of was rounded to 2^-4, and in bf16 contexts what comes of them is to 2^-9)
+  a.dtype = VVS_FP32; a.fast = qlinear_fast(c->cfg.weight_kind == VVS_WEIGHTS_E4M3_WHOLE ? VVS_PRODUCTS_WHOLE : VVS_PRODUCTS_AUTO, m == kMapGate ? VVS_BF16 : c->cfg.dtype, M);
   a.y = out; a.stride = a.w.out; a.wide = 1;
   a.y8 = act;
   a.counters = (uint32_t*)(c->ws + c->w.map_counters); a.act = (float*)(c->ws + c->w.map_parts);

@@ -156,6 +156,7 @@ static vvs_status plan_qlinear(const vvs_qlinear_config* cfg, QLinear* l) {
   const vvs_qlinear_config& g = *cfg;
   if (g.in < 1 || g.out < 1 || g.max_rows < 1) return no(nullptr, VVS_EINVAL, "qlinear config: a dimension is not positive");
   if (!known(g.dtype)) return no(nullptr, VVS_EINVAL, "qlinear config: unknown dtype");
+  if (g.products != VVS_PRODUCTS_AUTO && g.products != VVS_PRODUCTS_WHOLE && g.products != VVS_PRODUCTS_E4M3) return no(nullptr, VVS_EINVAL, "qlinear config: unknown products");
   if (g.gated != 0 && g.gated != 1) return no(nullptr, VVS_EINVAL, "qlinear config: gated must be 0 or 1");
   if (g.in > kWidest || (g.gated && g.out > kWidest)) return no(nullptr, VVS_ESIZE, "qlinear config: at most 65536 elements per row");
   if (g.out > (1 << 24) || g.max_rows > (1 << 20)) return no(nullptr, VVS_ESIZE, "qlinear config: at most 2^24 columns and 2^20 rows");
@@ -352,7 +353,7 @@ vvs_status vvs_qlinear_apply(vvs_qlinear* ql, int32_t n_rows, const void* d_valu
   QProduct a{};
   a.w = l->w; a.M = n_rows;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
-  a.dtype = out_dtype; a.fast = qlinear_fast(out_dtype, n_rows);
+  a.dtype = out_dtype; a.fast = qlinear_fast(l->cfg.products, out_dtype, n_rows);
   a.y = d_out; a.stride = (size_t)os; a.wide = wide_rows(d_out, os, out_dtype, 4);
   a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + kQlinearCounters);
   launch_qlinear_product(a, plan_qlinear_product(l->w, n_rows, a.fast), (hipStream_t)s);
@@ -373,6 +374,7 @@ vvs_status vvs_qlinear_gate(vvs_qlinear* ql, int32_t n_rows, const void* d_value
   QProduct a{};
   a.w = l->w; a.M = n_rows;
   a.x = QRowsIn{(const uint8_t*)d_values, (const uint8_t*)d_powers};
+  a.fast = qlinear_fast(l->cfg.products, VVS_BF16, n_rows);
   a.counters = (uint32_t*)l->ws; a.act = (float*)(l->ws + kQlinearCounters);
   a.y8 = QRowsOut{(uint8_t*)d_out_values, (uint8_t*)d_out_powers};
   launch_qlinear_product(a, plan_qlinear_product(l->w, n_rows, false), (hipStream_t)s);

@@ -27,8 +27,8 @@ __device__ __forceinline__ void qtile_of(int id, int MT, int NT, int* tile_m, in
 // in LDS (362), two row tiles on their way from there (354), and outputs through LDS (331).  Requests at the start of a block instead of between products 420.  Tried and slower, of 385 to 400: 256 x 256 by 8 waves 448,
 // 4 waves that have a SIMD each 405, a higher priority for waves at their products 403, bands of 4 or 16 row tiles 397 and 404.
 // FAST: the e4m3 numbers go into the matrix cores as they are, with both powers of two as scales (16x16x128, twice the rate of bf16 and fewer instructions).  These products lose what lies 2^13
-// below the largest of a few neighbours: 1.3e-5 in the 2-norm, 200 times below the rounding of bf16 outputs and 3000 times below that of 8 bits.  Outputs in fp32, and up to 64 rows of any, take !FAST: bf16
-// operands, exact.
+// below the largest of a few neighbours: 1.3e-5 of the result in the 2-norm for normally distributed operands, 130 times below the rounding of bf16 outputs and 2000 times below that of 8 bits; more of sums that
+// cancel.  !FAST: bf16 operands, exact; what up to 64 rows take, and more where the caller wants it (vvs_qlinear_config.products) or outputs are in fp32, but for the sums of bf16 contexts.
 constexpr int power_blocks(int shares) { return shares > 1 ? 32 : 64; }                  // whose powers lie in LDS at a time
 constexpr int power_stride(int shares) { return power_blocks(shares) / 4 + 1; }          // (an odd number of words: 16 rows on 16 banks)
 // LDS of a share: rows [stages][BM][128 bytes], then powers of its next blocks: [BM][stride], [64 WN][stride], four in a word
@@ -373,9 +373,9 @@ static void tile_by(const QProduct& a, QTile t, int shares, hipStream_t s) {
 void launch_qlinear_tile(const QProduct& a, QTile t, int shares, hipStream_t s) {
   shares = qlinear_shares(a.w, shares);                // (a share without a block would ask for one in front of the first)
   if (a.w.gated && t == kTile32x256) tile_t<1, 4, 2, false, true, float, 4, 1>(a, s);
-  else if (a.w.gated && t == kTile64x256) tile_t<1, 4, 4, true, true, float, 4, 1>(a, s);
-  else if (a.w.gated) tile_t<1, 4, 8, true, true, float, 2, 1>(a, s);
-  else if (a.dtype == VVS_BF16 && !a.fast) tile_least<false, bf16_t>(a, shares, s);      // (33 to 64 rows)
+  else if (a.w.gated && t == kTile64x256) a.fast ? tile_t<1, 4, 4, true, true, float, 4, 1>(a, s) : tile_t<1, 4, 4, false, true, float, 4, 1>(a, s);
+  else if (a.w.gated) a.fast ? tile_t<1, 4, 8, true, true, float, 2, 1>(a, s) : tile_t<1, 4, 8, false, true, float, 2, 1>(a, s);
+  else if (a.dtype == VVS_BF16 && !a.fast) tile_by<false, bf16_t>(a, t, shares, s);
   else if (a.dtype == VVS_BF16) tile_by<true, bf16_t>(a, t, shares, s);
   else if (a.fast) tile_by<true, float>(a, t, shares, s);
   else tile_by<false, float>(a, t, shares, s);
