@@ -193,6 +193,10 @@ __global__ __launch_bounds__(64 * NW) void k_qlinear_few(QProduct a) {
       const float* p = a.act + (size_t)m * a.w.groups * 32 + block * kQRowBlock + sub * 8;
       get4(p, v);
       get4(p + 4, v + 4);
+      // units behind the last one are held as 0, also in a row whose other units are NaN (a product with weights of 0 is not always 0)
+      const int left = a.w.out - block * kQRowBlock - sub * 8;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = j < left ? v[j] : 0.f;
       uint8_t* power = a.y8.powers + (size_t)m * out_powers;
       round_block(v, a.y8.values + ((size_t)m * out_blocks + block) * kQRowBlock + sub * 8, power + block, true, sub == 0);
       if (block == out_blocks - 1 && sub > 0 && block + sub < out_powers) power[block + sub] = 0;

@@ -288,10 +288,16 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void k_qlinear_tile(QProduct 
     }
     __syncthreads();
     // (a row's 128 bytes by neighbouring lanes; pieces of 8 bytes from where the products are would be 32 in a row: 4093 rows, 4096 -> 11008 with reading back 330 us, so 322)
+    // Bytes of units behind the last one are 0, also in a row whose other units are NaN: a product with weights of 0 is NaN there (and has no part in the largest).
+    const int c = tid & 7, left = a.w.out - tile_n * kQRowBlock - c * 16;
+    auto keep = [&](int at) { return left >= at + 4 ? ~0u : left <= at ? 0u : ~0u >> (8 * (at + 4 - left)); };
+    const uint4 mask = make_uint4(keep(0), keep(4), keep(8), keep(12));
 #pragma unroll
     for (int k = 0; k < BM / 32; ++k) {
-      const int lm = k * 32 + (tid >> 3), c = tid & 7;
-      if (m0 + lm < a.M) *(uint4*)(a.y8.values + ((size_t)(m0 + lm) * out_blocks + tile_n) * kQRowBlock + c * 16) = *(const uint4*)(bytes + lm * kQRowBlock + (c ^ (lm & 7)) * 16);
+      const int lm = k * 32 + (tid >> 3);
+      uint4 q = *(const uint4*)(bytes + lm * kQRowBlock + (c ^ (lm & 7)) * 16);
+      q.x &= mask.x; q.y &= mask.y; q.z &= mask.z; q.w &= mask.w;
+      if (m0 + lm < a.M) *(uint4*)(a.y8.values + ((size_t)(m0 + lm) * out_blocks + tile_n) * kQRowBlock + c * 16) = q;
     }
   } else {
     if (own_group >= a.w.groups) return;
