@@ -125,16 +125,50 @@ __global__ __launch_bounds__(MOST) void k_qrows_norm(QNorm a) {
   }
   // The waves' sums are added, and the factor is taken, in 64 bits, so that it is off by one rounding, not by several that a whole row would share: values end next to a border of e4m3 now and then.
   // (8192 rows of 4096 in bf16: 49.2 us, 49.5 all in fp32; an element's two products exact as well 52.6, in 64 bits 53.4)
-  ss = wave_sum(ss);
-  double all = ss;
-  if (blockDim.x > 64) {
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
-    __syncthreads();
-    all = 0.0;
-    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) all += red[w];
+  auto sum_of_waves = [&](float mine) {
+    mine = wave_sum(mine);
+    double all = mine;
+    if (blockDim.x > 64) {
+      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = mine;
+      __syncthreads();
+      all = 0.0;
+      for (int w = 0; w < (int)(blockDim.x >> 6); ++w) all += red[w];
+    }
+    return all;
+  };
+  double all = sum_of_waves(ss), eps = a.eps;
+  // Squares below 2^-126 lose bits and those below 2^-149 vanish (65536 of them are 2^-30 of a sum of 2^-80; an eps from 2^-50 on hides them all), and a sum may overflow.  Then the row is brought to
+  // 1 .. 2 by a power of two, exactly, and eps by its square, and summed again: the same quotient.  All threads have the same sum, and go the same way.
+  if (!(all < INFINITY) || (all < 0x1p-80 && a.eps < 0x1p-50f)) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, finite(v[j][i]) ? fabsf(v[j][i]) : 0.f);
+    }
+    top = wave_max(top);
+    if (blockDim.x > 64) {
+      __syncthreads();                                  // (the sums have been read)
+      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+      __syncthreads();
+      for (int w = 0; w < (int)(blockDim.x >> 6); ++w) top = fmaxf(top, red[w]);
+      __syncthreads();
+    }
+    const int shift = top > 0.f ? -ilogbf(top) : 0;
+    ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[j][i] = ldexpf(v[j][i], shift);
+        ss += v[j][i] * v[j][i];
+      }
+    }
+    all = sum_of_waves(ss);
+    eps = ldexp(eps, 2 * shift);
   }
   // (fp32's reciprocal root and one step of Newton's method)
-  const double mean = all * a.per_element + (double)a.eps;
+  const double mean = all * a.per_element + eps;
   double factor = rsqrtf((float)mean);
   factor = factor > 0.0 && factor < INFINITY ? factor * (1.5 - 0.5 * mean * factor * factor) : 1.0 / sqrt(mean);
   const float r = (float)factor;
