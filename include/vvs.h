@@ -456,7 +456,7 @@ vvs_status vvs_rope_apply(vvs_rope* r, int32_t n_tokens, const int32_t* d_pos, i
  *
  * Tensors are [n_rows, width] in VVS_FP32 or VVS_BF16; a stride argument gives the elements from one row to the next where they lie further apart than `width` (0: they do not).  Any
  * width, stride and element-aligned pointer is taken; 16-byte accesses are made where pointer and stride are multiples of 16 bytes (of 4 elements for outputs of
- * vvs_qlinear_apply).  Outputs share no memory with inputs, except where stated.  All calls can be captured into a graph; those on rows go to the current device. */
+ * vvs_qlinear_apply).  Outputs share no memory with inputs, with each other or with a map's buffers, except where stated: such calls are refused (VVS_EINVAL).  All calls can be captured into a graph; those on rows go to the current device. */
 #define VVS_QROWS_BLOCK 128
 
 /* Sizes in bytes of the two buffers of n_rows rows. */

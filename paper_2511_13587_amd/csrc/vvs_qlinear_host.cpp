@@ -187,12 +187,20 @@ static vvs_status launched(QLinear* l, const char* what) {
   return VVS_EHIP;
 }
 
+// A map's own buffers, and a weight tensor of its config
+static Span bytes_span(const void* p, size_t bytes) { return Span{(uintptr_t)p, bytes, bytes, 1}; }
+static Span held_span(const QLinear* l) { return bytes_span(l->w.data, l->weight_bytes); }
+static Span workspace_span(const QLinear* l) { return bytes_span(l->ws, l->ws_bytes); }
+static Span tensor_span(const QLinear* l, const void* p) { return bytes_span(p, (size_t)l->cfg.in * l->cfg.out * size_of(l->cfg.dtype)); }
+
 static vvs_status check_product(QLinear* l, int n_rows, const void* values, const void* powers) {
   if (!l->loaded) return no(l, VVS_ESTATE, "qlinear: call vvs_qlinear_load first");
   if (!values || !powers) return no(l, VVS_EINVAL, "qlinear: NULL argument");
   if (n_rows < 1) return no(l, VVS_EINVAL, "qlinear: n_rows must be positive");
   if (n_rows > l->cfg.max_rows) return no(l, VVS_ESIZE, "qlinear: n_rows exceeds max_rows");
   if (off16(values) || off16(powers)) return no(l, VVS_EINVAL, "qlinear: values and powers must be 16-byte aligned");
+  const Span ws[] = {workspace_span(l)}, rows[] = {values_span(values, n_rows, l->cfg.in), powers_span(powers, n_rows, l->cfg.in)};
+  if (share_any(ws, rows)) return no(l, VVS_EINVAL, "qlinear: the workspace shares memory with the rows");
   return VVS_OK;
 }
 
@@ -293,6 +301,7 @@ vvs_status vvs_qlinear_create(const vvs_qlinear_config* cfg, void* d_weights, vo
   QLinear plan{};
   const vvs_status st = plan_qlinear(cfg, &plan);
   if (st != VVS_OK) return st;
+  if (share(bytes_span(d_weights, plan.weight_bytes), bytes_span(d_workspace, plan.ws_bytes))) return no(nullptr, VVS_EINVAL, "qlinear create: the workspace shares memory with the weights");
   int ndev = 0;
   if (hipGetDeviceCount(&ndev) != hipSuccess || ndev < 1) return no(nullptr, VVS_EHIP, "qlinear create: no HIP device (this library has no CPU path)");
   hipError_t e = hipGetDevice(&plan.dev);
@@ -318,6 +327,7 @@ vvs_status vvs_qlinear_load(vvs_qlinear* ql, const void* d_w, const void* d_w_up
   if (!l) return VVS_EINVAL;
   if (!d_w || !d_w_up != !l->cfg.gated) return no(l, VVS_EINVAL, "qlinear load: one weight tensor, with a gate two");
   if (off_element(d_w, l->cfg.dtype) || off_element(d_w_up, l->cfg.dtype)) return no(l, VVS_EINVAL, "qlinear load: unaligned weights");
+  if (share(held_span(l), tensor_span(l, d_w)) || share(held_span(l), tensor_span(l, d_w_up))) return no(l, VVS_EINVAL, "qlinear load: a weight tensor shares memory with the map's buffer");
   vvs_status st = check_device(l);
   if (st != VVS_OK) return st;
   launch_qlinear_load(QLoad{l->w, d_w, d_w_up, l->cfg.dtype}, (hipStream_t)s);
@@ -331,6 +341,8 @@ vvs_status vvs_qlinear_read(vvs_qlinear* ql, void* d_w, void* d_w_up, vvs_stream
   if (!l->loaded) return no(l, VVS_ESTATE, "qlinear read: call vvs_qlinear_load first");
   if (!d_w || !d_w_up != !l->cfg.gated) return no(l, VVS_EINVAL, "qlinear read: one weight tensor, with a gate two");
   if (off_element(d_w, l->cfg.dtype) || off_element(d_w_up, l->cfg.dtype)) return no(l, VVS_EINVAL, "qlinear read: unaligned weights");
+  const Span outs[] = {tensor_span(l, d_w), tensor_span(l, d_w_up)}, own[] = {held_span(l), workspace_span(l)};
+  if (share_any(outs, own)) return no(l, VVS_EINVAL, "qlinear read: a weight tensor shares memory with the map's buffers or with the other");
   const vvs_status st = check_device(l);
   if (st != VVS_OK) return st;
   launch_qlinear_read(QWeightsRead{l->w, d_w, d_w_up, l->cfg.dtype}, (hipStream_t)s);
@@ -347,8 +359,9 @@ vvs_status vvs_qlinear_apply(vvs_qlinear* ql, int32_t n_rows, const void* d_valu
   if (!known(out_dtype)) return no(l, VVS_EINVAL, "qlinear apply: unknown dtype");
   const int64_t os = stride_of(out_stride, l->cfg.out);
   if (os < 0 || off_element(d_out, out_dtype)) return no(l, VVS_EINVAL, "qlinear apply: the stride has to cover a row, the pointer to be aligned to an element");
-  const Span outs[] = {span_of(d_out, n_rows, l->cfg.out, os, size_of(out_dtype))}, ins[] = {values_span(d_values, n_rows, l->cfg.in), powers_span(d_powers, n_rows, l->cfg.in)};
-  if (share_any(outs, ins)) return no(l, VVS_EINVAL, "qlinear apply: the output shares memory with the rows");
+  const Span outs[] = {span_of(d_out, n_rows, l->cfg.out, os, size_of(out_dtype))},
+             ins[] = {values_span(d_values, n_rows, l->cfg.in), powers_span(d_powers, n_rows, l->cfg.in), held_span(l), workspace_span(l)};
+  if (share_any(outs, ins)) return no(l, VVS_EINVAL, "qlinear apply: the output shares memory with the rows or the map's buffers");
   if ((st = check_device(l)) != VVS_OK) return st;
   QProduct a{};
   a.w = l->w; a.M = n_rows;
@@ -368,8 +381,9 @@ vvs_status vvs_qlinear_gate(vvs_qlinear* ql, int32_t n_rows, const void* d_value
   if (st != VVS_OK) return st;
   if (!d_out_values || !d_out_powers) return no(l, VVS_EINVAL, "qlinear gate: NULL argument");
   if (off16(d_out_values) || off16(d_out_powers)) return no(l, VVS_EINVAL, "qlinear gate: values and powers must be 16-byte aligned");
-  const Span outs[] = {values_span(d_out_values, n_rows, l->cfg.out), powers_span(d_out_powers, n_rows, l->cfg.out)}, ins[] = {values_span(d_values, n_rows, l->cfg.in), powers_span(d_powers, n_rows, l->cfg.in)};
-  if (share_any(outs, ins)) return no(l, VVS_EINVAL, "qlinear gate: an output shares memory with the rows or with the other");
+  const Span outs[] = {values_span(d_out_values, n_rows, l->cfg.out), powers_span(d_out_powers, n_rows, l->cfg.out)},
+             ins[] = {values_span(d_values, n_rows, l->cfg.in), powers_span(d_powers, n_rows, l->cfg.in), held_span(l), workspace_span(l)};
+  if (share_any(outs, ins)) return no(l, VVS_EINVAL, "qlinear gate: an output shares memory with the rows, the map's buffers or the other output");
   if ((st = check_device(l)) != VVS_OK) return st;
   QProduct a{};
   a.w = l->w; a.M = n_rows;
