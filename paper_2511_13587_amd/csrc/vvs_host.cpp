@@ -359,13 +359,13 @@ vvs_status plan_sizes(const vvs_config* cfg, Ctx* c, std::string* err) {
   for (QMap m : {kMapQkv, kMapO, kMapGate, kMapDown}) map_parts = std::max(map_parts, qlinear_part_bytes(context_map(c, m)));
   w.map_counters = take(g.weight_kind ? kQlinearCounters : 0);      // zeroed with the state
   w.x = take(sizeof(float) * (size_t)c->Mmax * d);
-  w.h = take(c->esz * (size_t)c->Mmax * d);
+  w.h = take(g.weight_kind ? 0 : c->esz * (size_t)c->Mmax * d);       // (weights in 8 bits: h8 and act8 instead of h and act)
   // (a call whose layers are one launch has no partial sums: what its phases hand on lies in their place)
   w.gemm_out = w.few_buf = take(std::max(sizeof(float) * go, wide ? 0 : few_buf_bytes(few, d, F) * c->L));
   if (wide) w.few_buf = take(few_buf_bytes(few, d, F) * c->L);
   w.q = take(c->esz * (size_t)c->Mmax * d);
   w.attn = take(c->esz * (size_t)c->Mmax * d);
-  w.act = take(c->esz * (size_t)c->Mmax * F);
+  w.act = take(g.weight_kind ? 0 : c->esz * (size_t)c->Mmax * F);
   w.hf = take(c->esz * (size_t)c->Mlog * d);
   w.logits = take(sizeof(float) * (size_t)c->Mlog * veff);
   w.probs = take(sizeof(float) * (size_t)c->B * c->Tmax * veff);
