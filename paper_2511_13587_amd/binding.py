@@ -464,6 +464,14 @@ def _apart(out: int, n_out: int, tensors, tokens: int, width: int):
 _raw_stream = torch._C._cuda_getCurrentRawStream     # (current_stream() makes a stream object each time: 1.5 us of a 5 us call)
 
 
+def _gpu(device) -> torch.device:
+    """A device whose memory kernels can read: buffers on another one would fault the GPU at the first call."""
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"device: wants a GPU, got {device}")
+    return device
+
+
 class _Current:
     """Makes a device current for a call, where it is not already (torch.cuda.device does it always: 2 us)."""
 
@@ -491,11 +499,12 @@ class QCache:
 
     def __init__(self, n_layers: int, n_rows: int, n_heads: int, n_kv_heads: int, head_size: int, capacity: int, max_tokens: int, dtype: int,
                  device: str = "cuda:0"):
+        self.device = _gpu(device)
         self.cfg = VvsQCacheConfig(n_layers, n_rows, n_heads, n_kv_heads, head_size, capacity, max_tokens, dtype)
         self.cache_bytes, self.ws_bytes = vvs_qcache_query_sizes(self.cfg)
         if not torch.cuda.is_available():
             raise RuntimeError("libvvs needs a HIP device; there is no CPU path")
-        self.device, self.dtype = torch.device(device), _TORCH_DTYPE[dtype]
+        self.dtype = _TORCH_DTYPE[dtype]
         self.width = self.dtype.itemsize
         self.index = torch.cuda.current_device() if self.device.index is None else self.device.index
         with torch.cuda.device(self.index):
@@ -707,7 +716,9 @@ _current_device = torch._C._cuda_getDevice               # (as for _raw_stream: 
 
 
 def _on_device(device: int, fn, *args):
-    """fn(*args, current stream of the device) with the device current."""
+    """fn(*args, current stream of the device) with the device current.  Not for the host's memory (-1), which a kernel must not be given."""
+    if device < 0:
+        raise ValueError("rows: on the host; wants them on a GPU")
     if _current_device() == device:
         return fn(*args, _raw_stream(device))
     with _Current(device):
@@ -753,11 +764,12 @@ class QLinear:
     that goes in and of one that comes out; dtype: of the tensors that are loaded; gated: gate and up weights, for vvs_qlinear_gate; products: how they are summed, VVS_PRODUCTS_*."""
 
     def __init__(self, in_width: int, out: int, max_rows: int, dtype: int, gated: bool = False, device: str = "cuda:0", workspace: Optional[torch.Tensor] = None, products: int = VVS_PRODUCTS_AUTO):
+        self.device = _gpu(device)
         self.cfg = VvsQLinearConfig(in_width, out, max_rows, 1 if gated else 0, dtype, products)
         self.weight_bytes, self.ws_bytes = vvs_qlinear_query_sizes(self.cfg)
         if not torch.cuda.is_available():
             raise RuntimeError("libvvs needs a HIP device; there is no CPU path")
-        self.device, self.dtype = torch.device(device), _TORCH_DTYPE[dtype]
+        self.dtype = _TORCH_DTYPE[dtype]
         self.index = torch.cuda.current_device() if self.device.index is None else self.device.index
         if workspace is not None and (workspace.get_device() != self.index or not workspace.is_contiguous() or workspace.numel() * workspace.dtype.itemsize < self.ws_bytes):
             raise ValueError(f"workspace: wants {self.ws_bytes} bytes on device {self.index}")
