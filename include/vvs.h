@@ -467,7 +467,7 @@ const char* vvs_qrows_last_error(void);   /* of this thread's last failed vvs_qr
 vvs_status vvs_qrows_round(int32_t n_rows, int32_t width, int32_t dtype, const void* d_x, int64_t x_stride, void* d_values, void* d_powers,
                            vvs_stream s);
 
-/* Root-mean-square norm with the residual's addition: x' = x + delta, rounded to the type of x; y = x' * rsqrt(mean x'^2 + eps) * gain, which goes into 8 bits.  The sum of squares is in
+/* Root-mean-square norm with the residual's addition: x' = x + delta in fp32, rounded to the type of x; y = x' * rsqrt(mean x'^2 + eps) * gain, which goes into 8 bits.  The sum of squares is in
  * fp32; rows whose squares fp32 does not hold are scaled by a power of two for it, so that elements may be of any size.
  *   d_delta    : [n_rows, width] of its own type, or NULL: nothing is added
  *   d_x_out    : x' in the type of x; may be d_x itself (with the same stride); NULL: not written

@@ -78,12 +78,14 @@ void launch_qlinear_read(const QWeightsRead& a, hipStream_t s) {
 
 // ------------------------------------------------------------------------------------------------ products
 // Few rows: Y^T = W^T X^T in tiles of 16 columns x 16 rows.  A workgroup of NW waves makes CT tiles of 16 columns for 16 RT rows; wave w takes blocks w, w + NW, ... of the contraction, straight from
-// memory into operand registers, one block ahead, and the partial sums are added through LDS in the order of the waves.  Powers of all blocks lie in LDS, four in a word.
-// Bound by the weights' bytes where they are many, by the latency of a first load, of the exchange through LDS and of the launch where not: 14 rows, gated, 4096 -> 11008, 91 MB in 18.8 us, 4.8 TB/s; 28 rows,
-// 11008 -> 4096, 45 MB in 13.7 us, 3.3 TB/s; 10 rows, 344 -> 128 3.3 us.  Every wave has its part of the contraction, not of the columns: a wave alone with 11008 values would go through 86 blocks one after another.
+// memory into operand registers, and the partial sums are added through LDS in the order of the waves.  Powers of all blocks lie in LDS, four in a word.  A block is asked for in front of the products of the one before,
+// under a condition; where the paths join the compiler waits for the youngest loads, so that of every two blocks one is on its way during products and the other is waited for at once.  The powers are asked for behind the
+// first blocks, a word per thread at a time, rows' first: each round is a memory latency (4096 values: two; 11008: four).
+// Bound by the weights' bytes where they are many (14 rows, gated, 4096 -> 11008, 91 MB in 18.8 us, 4.8 TB/s), by the latencies of powers, first blocks, every other block, the exchange through LDS and the launch
+// where not: 28 rows, 11008 -> 4096, 45 MB in 13.7 us, 3.3 TB/s; 10 rows, 344 -> 128 3.3 us.  Every wave has its part of the contraction, not of the columns: a wave alone with 11008 values would go through 86 blocks one after another.
 // Weights pass LDS by: nobody shares them.  Products are those of bf16 operands: an e4m3 number times its power of two is one exactly (8 bits of exponent, 3 of mantissa), so that what is summed in fp32
 // are the true products; turning eight of a lane's numbers takes four instructions, and the matrix cores wait for memory anyway (busy 8 % of the time in the gated case above, waves waiting for loads 56 %).
-// Two and three blocks ahead instead of one: 28 rows, 4096 -> 12288 17.1, 18.6, 20.2 us, gated 14 rows 23.9, 22.8, 23.3, 28 rows 27.7, 27.4, 30.3 (weights from HBM).
+// (Two and three blocks ahead, under the same kind of condition: 28 rows, 4096 -> 12288 18.6, 20.2 us for 17.1.)
 template <int NW, int RT, int CT, bool GATED, typename T>
 __global__ __launch_bounds__(64 * NW) void k_qlinear_few(QProduct a) {
   extern __shared__ float4 parts[];          // [wave][CT][RT][lane]; until the products are made the powers: rows [16 RT][stride], columns [16 CT][stride]

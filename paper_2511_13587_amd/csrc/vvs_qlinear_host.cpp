@@ -90,31 +90,38 @@ static vvs_status check_rows(int n_rows, int width, const void* values, const vo
   return VVS_OK;
 }
 
-// Few rows are bound by the weights' bytes, which every wave streams for itself, and by how many waves there are to do so; more rows share the weights, and themselves pass through LDS.  The rule goes by
-// the number of workgroups: the smallest tiles that fit the 256 CUs one each, then larger ones; where tiles are few and the contraction long, a workgroup has waves for 2 or 4 shares of it.  us per call in a
-// graph, weights rotating through 400 MB, bf16 outputs unless said otherwise (the rule is 0.5 % behind the best of all variants in the mean over some 900 sizes, 8 to 4000 rows, and 15 % at one).
-//   k_qlinear_few, rows x columns of a workgroup:
-//   16 x 16 up to 256 workgroups (28 rows: 1280 -> 1280 3.7, 32 x 16 4.4; 4096 -> 2048 6.0, 32 x 16 7.7, 16 x 32 7.0)
-//   16 x 32 for up to 16 rows (8 rows, 4096 -> 12288 13.3, 16 x 16 13.6); up to 256 workgroups (64 rows: 1280 -> 1280 4.2, 16 x 16 4.5; 4096 -> 2048 7.2, 32 x 32 8.6); up to 768 where the contraction is short (128
-//     rows, 1280 -> 1280 5.0, 32 x 32 5.3; 256 rows 5.8, 32 x 64 6.4), 1152 where the tiles are those of exact products (128 rows, 1536 -> 4608, fp32: 9.4, tiles 10.6)
-//   32 x 32 with a long contraction in two parts for one row tile where those fit the CUs (28 rows, 11008 -> 4096: 15.0, 16 x 32 17.5, 32 x 16 16.3, whole 19.5, three parts 16.8), in three where they give two workgroups to
-//     nearly every CU (28 rows, 11008 -> 5000 18.0, whole 20.5, two 21.6, four 21.9; 13824 -> 5120 20.4, whole 24.5; 8 rows 18.6, 16 x 32 24.2; 6144 -> 5120 13.4, 16 x 32 13.4)
-//   32 x 32 up to 256 workgroups (128 rows, 4096 -> 2048 8.6, 32 x 64 10.0; 64 rows, 4096 -> 4096 8.8, 16 x 32 9.4) and up to 32 rows, or 512 of up to 64 rows where
-//     the contraction is short (40 rows, 2560 -> 6912 8.8, 32 x 64 10.3)
-//   32 x 64 up to 256 workgroups (128 rows, 4096 -> 4096 10.3, 32 x 32 13.1, tiles of 32 x 128 in four shares 11.5; 28 rows, 4096 -> 12288 14.6, 32 x 32 15.4), but tiles for more than 64 rows and less than 10 blocks
-//     (160 rows, 768 -> 2304 5.5 / 4.9)
-//   k_qlinear_tile with e4m3 products: 64 x 128 where all of its workgroups are on the card at once, three per CU (432 rows, 4096 -> 12288, 672: 38.3, 64 x 256 40.9, 128 x 256 40.2); 128 x 256 from 208 on (600
-//     rows, 4096 -> 16384, 320: 54.3, 64 x 256 66.5; 8192 rows, 4096 -> 12288 331, before stores of whole rows 350, 64 x 256 418); 32 x 128 up to 256 (432 rows: 1280 -> 1280 6.5, 64 x 128 7.6), in four shares
-//     from 24 blocks (3456 -> 1280 10.9, whole 12.3; 256 rows of 11008 -> 4096 33.4, whole 48.9), in two from 16 (2048 -> 2048 8.4, whole 9.0); 64 x 128 up to 256 in four shares from 40 blocks (432 rows, 11008 -> 4096
-//     39.5, two 44.3, whole 54.8); 64 x 256 from 150 up to 32 blocks (600 rows: 1536 -> 4608, 180, 10.7, 64 x 128 11.4; 4096 -> 4096, 160, 21.3, 64 x 128 22.8, in two shares 21.3), else 64 x 128 in two shares (11008 ->
-//     4096 56.3, 64 x 256 68.6; 432 rows, 4096 -> 4096 15.8, whole 17.7, 32 x 128 18.0); of a short contraction 64 x 128 from 144 (432 rows, 1280 -> 3840 8.2, 32 x 128 8.1; 512 rows, 768 -> 2304 6.4 / 6.9)
-//   k_qlinear_tile with exact products (twice the instructions, more for smaller tiles to hide): 32 x 128 up to 1024 workgroups (600 rows, 1280 -> 3840 18.3, 64 x 256 21.7, 64 x 128 23.9), up to 256 in four shares
-//     from 24 blocks (432 rows, 3456 -> 1280 15.1, two 16.4, whole 20.8) or two from 8 (432 rows, 1280 -> 1280 9.8, whole 11.0), up to 512 in two (432 rows, 4096 -> 4096 26.0, whole 35.6, 64 x 128 in two 27.6), but
-//     64 x 128 in two from 32 blocks beyond (432 rows, 8192 -> 8192 66.9, 32 x 128 77.5)
-// With a gate, columns counted twice: 16 x 32 up to 16 rows and up to 768 workgroups (48 rows: 768 -> 2048 8.0, 32 x 32 8.5, tiles 9.1; 2048 -> 1024 8.3, 32 x 32 9.9, tiles 14.6), 32 x 32 up to 32 rows (4096 ->
-//   11008 26.0, 16 x 32 32.1) and up to 704 (64 rows, 2048 -> 5632 15.5, tiles 18.6), of more than 64 rows with a longer contraction (128 rows: 4096 -> 2048 16.7, tiles 21.6; 1280 -> 3456 16.7 / 11.2); tiles of
-//   32 x 256 up to 64 rows (4096 -> 11008 35.2, 32 x 32 41.9) and where the contraction is one or two blocks, of more rows up to four (128 rows: 128 -> 344 5.2, 16 x 32 6.0, 64 x 256 6.2; 512 -> 1408 7.5, 16 x 32 8.3); 128 x 256 from 208 on (432 rows, 4096 -> 11008,
-//   344: 55.5, 64 x 256 64.9); 64 x 256 (128 rows, 4096 -> 11008 34.6, 128 x 256 45.7).  (In shares: 48 rows, 4096 -> 11008 33.5 / 34.4, 128 rows 33.6 / 34.6, 432 rows, 1280 -> 3456 12.9 / 11.2: not built.)
+// Which kernel makes a product.  Few rows are bound by the weights' bytes, which every wave streams for itself, and by how many waves there are to do so; more rows share the weights, and themselves pass
+// through LDS.  The rule goes by the number of workgroups - the smallest tiles that fit the 256 CUs once, twice or three times, then larger ones - and by the length of the contraction in blocks of 128: where
+// tiles are few and it is long, several workgroups (parts) or a workgroup's waves (shares) divide it.  It is 0.5 % behind the best of all variants in the mean over some 900 sizes, 8 to 4000 rows, and 15 %
+// at one.  Each border was taken where the kernels, as they are, cross; us per call in a graph, weights rotating through 400 MB, outputs in bf16: as chosen / the next variant.
+//   k_qlinear_few
+//     16 x 16   up to 256 workgroups                                  28 rows, 4096 -> 2048 6.0 / 32 x 16 7.7
+//     16 x 32   up to 16 rows; up to 256 workgroups                   8 rows, 4096 -> 12288 13.3 / 16 x 16 13.6; 64 rows, 4096 -> 2048 7.2 / 32 x 32 8.6
+//               up to 768 (640 for 64 rows) and 16 blocks             256 rows, 1280 -> 1280 5.8 / 32 x 64 6.4
+//               up to 1152 and 12 blocks, whole products              128 rows, 1536 -> 4608 in fp32 9.4 / tiles 10.6
+//     32 x 32   one row tile in two or three parts (qlinear_parts)    28 rows, 11008 -> 4096 15.0 / whole 19.5, 11008 -> 5000 18.0 / whole 20.5
+//               up to 256 workgroups; up to 32 rows                   128 rows, 4096 -> 2048 8.6 / 32 x 64 10.0
+//               up to 64 rows, 512 workgroups, 23 blocks              40 rows, 2560 -> 6912 8.8 / 32 x 64 10.3
+//     32 x 64   up to 256, from 24 blocks, over 64 rows from 10       128 rows, 4096 -> 4096 10.3 / tiles in four shares 11.5
+//   k_qlinear_tile, e4m3 products
+//     64 x 128  all workgroups on the card at once, three per CU      432 rows, 4096 -> 12288 38.3 / 128 x 256 40.2
+//     128 x 256 from 208 workgroups on                                600 rows, 4096 -> 16384 54.3 / 64 x 256 66.5
+//     32 x 128  up to 256; in four shares from 24 blocks, two from 16 432 rows, 1280 -> 1280 6.5 / 64 x 128 7.6; 3456 -> 1280 10.9 / one share 12.3; 2048 -> 2048 8.4 / 9.0
+//     64 x 128  up to 256, four shares from 40 blocks                 432 rows, 11008 -> 4096 39.5 / two shares 44.3
+//     64 x 256  from 150, up to 32 blocks                             600 rows, 1536 -> 4608 10.7 / 64 x 128 11.4
+//     64 x 128  up to 512, two shares from 16 blocks; whole from 144  432 rows, 4096 -> 4096 15.8 / one share 17.7; 512 rows, 768 -> 2304 6.4 / 32 x 128 6.9
+//   k_qlinear_tile, whole products (twice the instructions, more for smaller tiles to hide)
+//     32 x 128  up to 1024 workgroups                                 600 rows, 1280 -> 3840 18.3 / 64 x 256 21.7
+//               up to 256: four shares from 24 blocks, two from 8     432 rows, 3456 -> 1280 15.1 / two shares 16.4; 1280 -> 1280 9.8 / one share 11.0
+//               up to 512 in two shares                               432 rows, 4096 -> 4096 26.0 / one share 35.6
+//     64 x 128  beyond, two shares from 32 blocks                     432 rows, 8192 -> 8192 66.9 / 32 x 128 77.5
+//   with a gate (columns counted twice; not in shares: 48 rows, 4096 -> 11008 33.5 / 34.4)
+//     16 x 32   up to 16 rows; up to 768 workgroups                   48 rows, 768 -> 2048 8.0 / 32 x 32 8.5
+//     32 x 32   up to 32 rows                                         28 rows, 4096 -> 11008 26.0 / 16 x 32 32.1
+//               up to 704: up to 64 rows, or from 16 blocks           64 rows, 2048 -> 5632 15.5 / tiles 18.6; 128 rows, 4096 -> 2048 16.7 / tiles 21.6
+//     32 x 256  up to 64 rows                                         64 rows, 4096 -> 11008 35.2 / 32 x 32 41.9
+//               one or two blocks, over 64 rows up to four            128 rows, 512 -> 1408 7.5 / 16 x 32 8.3
+//     128 x 256 from 208 on, else 64 x 256                            432 rows, 4096 -> 11008 55.5 / 64 x 256 64.9; 128 rows 34.6 / 128 x 256 45.7
 QPlan plan_qlinear_product(const QWeights& w, int M, bool fast) {
   auto few = [&](int rt, int ct) { return (int64_t)((M + 16 * rt - 1) / (16 * rt)) * w.groups * (4 / ct); };
   auto tiles = [&](int rows, int groups) { return (int64_t)((M + rows - 1) / rows) * ((w.groups + groups - 1) / groups); };

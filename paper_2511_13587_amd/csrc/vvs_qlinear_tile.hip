@@ -18,14 +18,14 @@ __device__ __forceinline__ void qtile_of(int id, int MT, int NT, int* tile_m, in
 
 // Y^T = W^T X^T.  A workgroup of WM x WN waves makes 16 RT WM rows by WN groups of 64 columns; a wave 16 RT rows of one group, whose weights nobody else in the workgroup needs: they come straight into its operand
 // registers, NB - 1 blocks of 128 contraction values ahead.  The rows' bytes of a block are every wave's, and pass through LDS (lds_dma16, no registers), two or three blocks ahead.
-// Bound by the matrix cores: 8192 rows, 4096 -> 12288, 825 GFLOP in 321 us, 2.6 PFLOP/s (an 8192^3 product in e4m3 by the library 2.7), the matrix cores busy 75 % of the time; a tile of 128 x 256 reads 48 KB a
-// block for 8.4 MFLOP, and 82 % of the requests to the L2 are hits.
-// Few tiles wait for loads instead, 0.6 us per block with three on their way: NB = 4, and KS shares of the contraction with waves, stages and powers of their own, whose sums the first adds up through LDS in their
+// Bound by the matrix cores: 8192 rows, 4096 -> 12288, 825 GFLOP in 321 us, 2.6 PFLOP/s (an 8192^3 product in e4m3 by the library 2.7), the matrix cores busy 75 % of the time, waves waiting 24 % of theirs; a
+// tile of 128 x 256 reads 48 KB a block for 8.4 MFLOP, and 82 % of the requests to the L2 are hits.
+// What is under way: the waits written out let the requests of one block (NB = 2) or two (NB = 4) be.  The compiler adds waits for the weights' loads, which it knows, and cannot count the rows', which it does not: in
+// front of the products of every step (NB = 2, where the rows are asked for last), of two steps in four (NB = 4; with shares of three, and in part of the fourth), it waits until all has landed.  What was asked for half a
+// step before is then waited for.  Too strict, never too lax: the results do not depend on it.
+// Few tiles wait for loads, some 0.6 us per block: NB = 4, and KS shares of the contraction with waves, stages and powers of their own, whose sums the first adds up through LDS in their
 // order (432 rows: 1280 -> 3840 in one share 7.7 us; 3456 -> 1280 in four 10.9, one 12.3; 11008 -> 4096 in four 39.5, one 54.8).  Powers of the first blocks are asked for in front of everything else (432 rows, 1280 ->
 // 3840 9.3 -> 8.3).
-// Parts of the large product left out in turn, when it took 385 us (all of the following: 223): powers of two from memory at every block 353, the requests for rows 350, for weights 321, reads of LDS 379.  Hence powers
-// in LDS (362), two row tiles on their way from there (354), and outputs through LDS (331).  Requests at the start of a block instead of between products 420.  Tried and slower, of 385 to 400: 256 x 256 by 8 waves 448,
-// 4 waves that have a SIMD each 405, a higher priority for waves at their products 403, bands of 4 or 16 row tiles 397 and 404.
 // FAST: the e4m3 numbers go into the matrix cores as they are, with both powers of two as scales (16x16x128, twice the rate of bf16 and fewer instructions).  These products lose what lies 2^13
 // below the largest of a few neighbours: 1.3e-5 of the result in the 2-norm for normally distributed operands, 130 times below the rounding of bf16 outputs and 2000 times below that of 8 bits; more of sums that
 // cancel.  !FAST: bf16 operands, exact; what up to 64 rows take, and more where the caller wants it (vvs_qlinear_config.products) or outputs are in fp32, but for the sums of bf16 contexts.
@@ -73,8 +73,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void k_qlinear_tile(QProduct 
   auto request = [&](int kb, int stage, int q) { lds_dma16(tile_rows + (size_t)kb * kQRowBlock, src[q], lds0 + stage * BM * kQRowBlock + (wave * NQ + q) * 1024); };
   const uint8_t* const wsrc = a.w.data + a.w.tile_at(group, first, 0);
   auto weights = [&](int kb, u32x4 (&w)[4][2], int c, int h) { w[c][h] = *(const u32x4*)(wsrc + (size_t)kb * 8192 + c * 2048 + h * 1024 + lane * 16); };
-  // powers of blocks k0 .. k0 + kPowerBlocks - 1 of the share into LDS: bytes from memory at every block were a tenth of the time of a large product (384 us without, 353 us).  A share that begins inside a word of
-  // four moves the bytes to where they are in its own count.
+  // powers of blocks k0 .. k0 + kPowerBlocks - 1 of the share into LDS (bytes from memory at every block cost a large product 6 %).  A share that begins inside a word of four moves the bytes to where they are
+  // in its own count.
   constexpr int kLanes = 64 * NW / BM;                           // threads that a row's words are dealt to
   struct Powers { int x[4], w[8]; };
   auto load_powers = [&](int k0, int d0) {                       // words d0 .. d0 + 7 of the columns', d0 / 2 * kLanes and on of the rows'
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void k_qlinear_tile(QProduct 
     constexpr int U = decltype(uc)::value, B = U & (NB - 1);
     const int st = NB == 2 ? st_next : U;
     const int kb = k4 + U, pw = (k4 & (kPowerBlocks - 1)) >> 2;
-    // this block's rows and weights have landed - what may be under way is the next block's rows - and the stage before is free
+    // this block's rows and weights have landed - what may be under way is what later blocks asked for, but see above - and the stage before is free
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NB == 2 ? NQ : 2 * (NQ + 8)) : "memory");
 #pragma unroll
     for (int c = 0; c < 4; ++c) asm volatile("" : "+v"(w[B][c][0]), "+v"(w[B][c][1]));
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void k_qlinear_tile(QProduct 
       }
     };
     if constexpr (FAST) {
-      // two row tiles are on their way from LDS while one is multiplied (one: 356 us for 354), and no more: left to itself the compiler moves the reads to where they spill (382)
+      // two row tiles are on their way from LDS while one is multiplied, and no more: left to itself the compiler moves the reads to where they spill (8 % of a large product)
       constexpr int NX = RT > 2 ? 3 : 2;
       struct Rows { u32x4 h[2]; } x[NX];
       int xs[NX];

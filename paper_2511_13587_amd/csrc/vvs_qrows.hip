@@ -80,8 +80,10 @@ __device__ __forceinline__ void read_any8(const void* row, int dtype, int at, in
 }
 
 // x' = x + delta, y = x' g / sqrt(mean(x'^2) + eps), in 8 bits.  One workgroup per row, which stays in registers, V times 8 elements per thread, so that x and delta are read once and nothing is read back; a
-// barrier for the sum is the only meeting of the waves.  x' is rounded to the residual's type, and what is normalised is what is kept.
-// 8192 rows of 4096, x, delta and x' in bf16: 235 MB in 47.8 us, 4.9 TB/s, where a copy of 4 GiB has 4.7; few rows wait for one chain of load, sum, barrier, rounding: 10 rows of 128 3.8 us, 432 rows of 1280 4.5.
+// barrier for the sum is the only meeting of the waves (but in rows whose squares fp32 does not hold).  x' is rounded to the residual's type, and what is normalised is what is kept.
+// 8192 rows of 4096, x, delta and x' in bf16: 235 MB in 48.1 us, 4.9 TB/s, where a copy of 4 GiB has 4.7; few rows wait for a
+// chain of loads, sum, barrier, rounding: 10 rows of 128 3.9 us, 432 rows of 1280 4.6.  Loads of bf16 are turned to fp32 where they are made: each of x, delta and gain that is in bf16 is waited for before the next is asked
+// for, and off 16 bytes each element of it.
 template <int V, int MOST>
 __global__ __launch_bounds__(MOST) void k_qrows_norm(QNorm a) {
   __shared__ float red[16];
